@@ -44,7 +44,10 @@
  *     available from pk_last_error() (thread-local).  Arguments are checked
  *     before anything is launched.  Nothing throws or aborts: every entry
  *     point catches host exceptions (PK_ENOMEM when host memory runs out).
- *   - dtype: PK_BF16 (MFMA path) or PK_F32 (plain-FMA debug path).
+ *   - dtype: PK_BF16 (MFMA path) or PK_F32 (plain-FMA debug path).  The calls
+ *     of the second half of this file (norm, rotation, paged cache, drafted
+ *     tokens) need no plan; their lengths and tables are device arrays, which
+ *     the kernels bound by the sizes given on the host.
  *     out_dtype: PK_BF16 or PK_F32 for the attention outputs.
  */
 #ifndef PACKINFER_H
@@ -58,7 +61,7 @@ extern "C" {
 #endif
 
 enum { PK_OK = 0, PK_EINVAL = -1, PK_ENOMEM = -2, PK_EUNSUPPORTED = -3, PK_EHIP = -4 };
-enum { PK_BF16 = 0, PK_F32 = 1 };
+enum { PK_BF16 = 0, PK_F32 = 1, PK_F8 = 2 };   /* PK_F8: of a pk_cache only */
 
 /* Layout constants of the group-contiguous buffer. */
 #define PK_GROUP_ALIGN 32      /* group bases are multiples of this many tokens */
@@ -458,6 +461,158 @@ int64_t pk_plan_stat(const pk_plan* plan, int what);
 #define PK_TUNE_DECODE_SPLIT 0
 #define PK_TUNE_PREFILL_PIPELINE 1
 int pk_plan_tune(pk_plan* plan, int knob, int64_t value);
+
+/* ========================================================================
+ * One step of a (speculative) decode loop on a paged cache: the projections
+ * of the new tokens are normed and rotated, quantised into the cache as they
+ * are written, attended to, and the drafted tokens that were accepted stay.
+ *
+ *   pk_qk_norm_rope    norm and rotation of queries and keys
+ *   pk_kv_cache_write  rows of K and V into the cache
+ *   pk_qkv_cache_write the two in one launch
+ *   pk_kv_cache_read   the cache back as rows, as pk_packed_prefill_attn takes
+ *                      the context of a chunk
+ *   pk_tree_attn       drafted tokens of every request over its cache; with one
+ *                      token a request a plain decode step
+ *   pk_kv_cache_keep   accepted tokens move up behind the context
+ *
+ * Nothing here allocates, and nothing depends on host copies of lengths: a
+ * step can be captured in a graph and replayed while the lengths grow.
+ * ======================================================================== */
+
+/* Rows [token][head][d] in device memory; strides in elements, the d columns of
+ * a row contiguous.  dtype PK_BF16 or PK_F32.  data and both strides are whole
+ * multiples of 16 bytes (PK_EINVAL otherwise); strides are not negative, those
+ * of outputs keep rows apart.  An output may be its own input (same data and
+ * strides), and otherwise does not overlap any input. */
+typedef struct pk_rows {
+    void* data;
+    int64_t token_stride, head_stride;
+    int32_t dtype;
+} pk_rows;
+
+/* Rotary positions.  Pair p of a row is rotated by the angle whose cosine and
+ * sine stand in row positions[axis(p)][token] of the table:
+ *   (a, b) -> (a cos - b sin, b cos + a sin)
+ *   table      device float [max_pos][2][rot_dim / 2]: cosines, then sines
+ *   positions  device int32, axis x at positions + x * axis_stride, [tokens]
+ *              each; clamped into [0, max_pos)
+ *   rot_dim    a multiple of 16, at most d; columns from rot_dim on stay
+ *   pair_axis  host [rot_dim / 2]: axis of every pair (several axes: time,
+ *              height and width of images and video); NULL: axis 0
+ *   interleaved  0: pair p is columns (p, p + rot_dim / 2); 1: (2p, 2p + 1) */
+typedef struct pk_rope {
+    const float* table;
+    const int32_t* positions;
+    int64_t axis_stride;
+    const uint8_t* pair_axis;
+    int32_t max_pos, rot_dim, n_axes, interleaved;
+} pk_rope;
+
+/* Paged cache of keys and values.
+ *   k       device [num_blocks][Hkv][page_size][d]
+ *   v       device [num_blocks][Hkv][page_size / 4][d][4]: four tokens
+ *           interleaved, so that the four keys that a lane of an MFMA takes of a
+ *           column lie side by side
+ *   scales  device [num_blocks][Hkv][2][page_size] (of K, of V); PK_F8 only
+ * page_size is a multiple of 16, d 64 or 128 (PK_EUNSUPPORTED otherwise).
+ * dtype PK_BF16: k and v are bf16 and scales is not read.  dtype PK_F8: k and v
+ * are E4M3 codes (4 exponent bits, 3 fraction bits, no infinities), scales are
+ * exponent bytes: b stands for 2^(b - 127), 1 <= b <= 254.  A row's byte is the
+ * smallest whose scale s keeps its largest finite magnitude within 448 s, and
+ * the code of x is x / s rounded to nearest even: dividing is exact, and what a
+ * code stands for, code * s, is a bf16 number.  NaN and infinities become NaN.
+ * Slot number s of the cache is token s % page_size of block s / page_size. */
+typedef struct pk_cache {
+    void* k;
+    void* v;
+    void* scales;
+    int64_t num_blocks;
+    int32_t page_size, Hkv, d, dtype;
+} pk_cache;
+
+/* pk_qk_norm_rope -- for every row x of q and k:  y = x * rsqrt(mean(x^2) + eps)
+ * * weight, then the rotation; one pass, in fp32, rounded once to the type of
+ * the output (any of the two, for any type of the input).
+ *   q [tokens][Hq][d], k [tokens][Hkv][d], both of one dtype; q_out, k_out too
+ *   q_weight, k_weight  device [d] in the dtype of q and k; NULL: no norm of q
+ *                       (of k)
+ *   rope                NULL: no rotation
+ * d is a multiple of 8 and at most 256 (PK_EUNSUPPORTED otherwise).
+ * Errors: PK_EINVAL; PK_EUNSUPPORTED. */
+int pk_qk_norm_rope(const pk_rows* q, const pk_rows* k, const pk_rows* q_out, const pk_rows* k_out,
+                    const void* q_weight, const void* k_weight, float eps, const pk_rope* rope,
+                    int64_t tokens, int Hq, int Hkv, int d, void* stream);
+
+/* pk_kv_cache_write -- rows of K and V [tokens][Hkv][d] (one dtype) into the
+ * slots of the cache.
+ *   slots  device int64 [tokens]; a token whose slot is outside of the cache
+ *          (-1: padding) is not written.  Two tokens must not have one slot.
+ * Errors: PK_EINVAL; PK_EUNSUPPORTED (page size, d). */
+int pk_kv_cache_write(const pk_cache* cache, const pk_rows* k, const pk_rows* v, const int64_t* slots,
+                      int64_t tokens, void* stream);
+
+/* pk_qkv_cache_write -- pk_qk_norm_rope and pk_kv_cache_write in one launch: q
+ * goes to q_out, k is normed, rotated and written to the cache from fp32
+ * without a rounding in between, v is written.  q, k and v of one dtype. */
+int pk_qkv_cache_write(const pk_cache* cache, const pk_rows* q, const pk_rows* k, const pk_rows* v,
+                       const int64_t* slots, const pk_rows* q_out,
+                       const void* q_weight, const void* k_weight, float eps, const pk_rope* rope,
+                       int64_t tokens, int Hq, void* stream);
+
+/* pk_kv_cache_read -- tokens 0 .. kv_lens[i] - 1 of every request as rows
+ * row_start[i] + 0, 1, ... of k_out and v_out ([rows][Hkv][d], one dtype).
+ *   block_table  device int32 [n][max_blocks]: physical block of a request's
+ *                logical pages, clamped into [0, num_blocks)
+ *   kv_lens, row_start  device int32 [n]; lengths are clamped into
+ *                [0, max_blocks * page_size], rows outside of [0, rows) are not
+ *                written.  The requests' rows must not overlap.
+ * Errors: PK_EINVAL; PK_EUNSUPPORTED. */
+int pk_kv_cache_read(const pk_cache* cache, const int32_t* block_table, int32_t max_blocks,
+                     const int32_t* kv_lens, const int32_t* row_start, int32_t n,
+                     const pk_rows* k_out, const pk_rows* v_out, int64_t rows, void* stream);
+
+/* pk_tree_attn -- attention of the last T_i = q_start[i + 1] - q_start[i] tokens
+ * of every request (the drafted ones, whose rows are in the cache already) over
+ * its kv_lens[i] tokens.  All see the kv_lens[i] - T_i tokens of the context;
+ * among the drafted ones token t sees those whose bit is set in its mask word.
+ * A row that sees nothing is zero.  What a row does not see cannot reach it, be
+ * it infinite or NaN.
+ *   q         device [total_q][Hq][d] bf16, 16-byte aligned
+ *   q_start   device int32 [n + 1], not decreasing, within [0, total_q]
+ *   max_q     the most drafted tokens of a request (at least the largest T_i;
+ *             PK_EUNSUPPORTED above 64); tokens beyond it are not computed
+ *   tree_mask device uint64 [total_q]: bit j for drafted token j of the same
+ *             request; NULL: token t sees tokens 0 .. t
+ *   block_table, kv_lens: as for pk_kv_cache_read
+ *   out       device [total_q][Hq][d], out_dtype, 16-byte aligned
+ *   workspace device, 256-byte aligned, at least pk_tree_attn_workspace_bytes
+ *             for n, max_q and the head shape or larger ones.  ZERO-FILLED BEFORE
+ *             ITS FIRST USE; every call leaves it ready for the next.  Calls that
+ *             share one are ordered by the caller.
+ * The partial results of a request are put together in a fixed order: results
+ * repeat bit for bit.
+ * Errors: PK_EINVAL; PK_EUNSUPPORTED (page size, d, max_q). */
+#define PK_MAX_DRAFTS 64
+size_t pk_tree_attn_workspace_bytes(int32_t n, int32_t max_q, int Hq, int Hkv, int d);
+int pk_tree_attn(const pk_cache* cache, const void* q, const int32_t* q_start, int64_t total_q, int32_t max_q,
+                 const uint64_t* tree_mask, const int32_t* block_table, int32_t max_blocks,
+                 const int32_t* kv_lens, int32_t n, void* out, float scale, int Hq, int out_dtype,
+                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* pk_kv_cache_keep -- after the drafted tokens have been judged: drafted tokens
+ * keep[i][0] < keep[i][1] < ... < keep[i][keep_count[i] - 1] of request i (the
+ * accepted branch) become tokens 0, 1, ... behind its context, bit for bit, and
+ * new_lens[i] = kv_lens[i] - T_i + keep_count[i].
+ *   keep        device int32 [n][max_keep], rising in every row; numbers outside
+ *               of [0, T_i) are passed over
+ *   keep_count  device int32 [n]; clamped into [0, min(max_keep, T_i)]
+ *   new_lens    device int32 [n], not kv_lens itself
+ * Other arguments as for pk_tree_attn.  Errors: PK_EINVAL; PK_EUNSUPPORTED. */
+int pk_kv_cache_keep(const pk_cache* cache, const int32_t* block_table, int32_t max_blocks,
+                     const int32_t* kv_lens, const int32_t* q_start, int32_t n,
+                     const int32_t* keep, int32_t max_keep, const int32_t* keep_count,
+                     int32_t* new_lens, void* stream);
 
 /* Message of the last error on this thread ("" if none). */
 const char* pk_last_error(void);
