@@ -9,11 +9,12 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
 
-PK_BF16, PK_F32 = 0, 1
+PK_BF16, PK_F32, PK_F8 = 0, 1, 2
 PK_GROUP_ALIGN = 32
 PK_KV_BLOCK = 32
 
@@ -89,6 +90,16 @@ def lib():
     L.pk_plan_tune.argtypes = [vp, ci, i64]
     L.pk_plan_stat.restype = i64
     L.pk_plan_stat.argtypes = [vp, ci]
+    for name, types in (("pk_qk_norm_rope", [vp] * 6 + [f32, vp, i64, ci, ci, ci, vp]),
+                        ("pk_kv_cache_write", [vp, vp, vp, vp, i64, vp]),
+                        ("pk_qkv_cache_write", [vp] * 8 + [f32, vp, i64, ci, vp]),
+                        ("pk_kv_cache_read", [vp, vp, i32, vp, vp, i32, vp, vp, i64, vp]),
+                        ("pk_tree_attn", [vp, vp, vp, i64, i32, vp, vp, i32, vp, i32, vp, f32, ci, ci, vp, sz, vp]),
+                        ("pk_kv_cache_keep", [vp, vp, i32, vp, vp, i32, vp, i32, vp, vp, vp])):
+        getattr(L, name).restype = ci
+        getattr(L, name).argtypes = types
+    L.pk_tree_attn_workspace_bytes.restype = sz
+    L.pk_tree_attn_workspace_bytes.argtypes = [i32, i32, ci, ci, ci]
     L.pk_last_error.restype = ctypes.c_char_p
     L.pk_last_error.argtypes = []
     _torch = torch
@@ -105,7 +116,8 @@ EXPORTS = [
     "pk_padded_prefill_attn", "pk_padded_decode_attn", "pk_plan_stat", "pk_last_error",
     "pk_kv_append", "pk_packed_decode_attn_grown", "pk_regroup_due", "pk_trie_partition",
     "pk_pack_plan_tree", "pk_trie_tree", "pk_plan_tune", "pk_packed_decode_attn_static",
-    "pk_packed_mixed_step",
+    "pk_packed_mixed_step", "pk_qk_norm_rope", "pk_kv_cache_write", "pk_qkv_cache_write",
+    "pk_kv_cache_read", "pk_tree_attn", "pk_tree_attn_workspace_bytes", "pk_kv_cache_keep",
 ]
 STATIC_SCRATCH_BYTES = 16 << 20
 TUNE_DECODE_SPLIT = 0
@@ -421,3 +433,176 @@ def padded_decode_attn(plan, q, k_pages, v_pages, block_table, out, scale, works
     _check(rc, "pk_padded_decode_attn")
     plan._ws = workspace
     return out
+
+
+# --------------------------------------------------------------------------
+# a decode step on a paged cache: norm, rotation, cache, drafted tokens
+# --------------------------------------------------------------------------
+
+_ROWS = struct.Struct("Pqqi4x")         # pk_rows; a bytes object is handed on as it is (a ctypes.Structure takes 1 us to fill)
+_CACHE = struct.Struct("PPPqiiii")      # pk_cache
+_ROPE = struct.Struct("PPqPiiii")       # pk_rope
+
+
+def _need(ok, what):
+    if not ok:
+        raise PackInferError(what)
+
+
+def _rows(x, name, heads=None, d=None):
+    """pk_rows of a tensor [tokens, heads, d] (any strides, columns contiguous); None: a null pointer."""
+    if x is None:
+        return None
+    _need(x.dim() == 3 and (x.stride(2) == 1 or x.shape[2] == 1 or x.numel() == 0), f"{name} must be [tokens, heads, d] with contiguous columns")
+    _need(heads is None or tuple(x.shape[1:]) == (heads, d), f"{name} must have {heads} heads of {d} columns")
+    return _ROWS.pack(x.data_ptr(), x.stride(0), x.stride(1), _dtype_code(x))
+
+
+def _vector(x, name, dtype, n=None):
+    """Address of a contiguous tensor of the given type (and number of elements)."""
+    if x is None:
+        return None
+    _need(x.dtype == dtype and x.is_contiguous() and (n is None or x.numel() == n),
+          f"{name} must be contiguous, {dtype}" + ("" if n is None else f", {n} elements"))
+    return x.data_ptr()
+
+
+class KvCache:
+    """Paged cache of keys and values (pk_cache).  k: [num_blocks, Hkv, page_size, d]; v: [num_blocks, Hkv, page_size / 4,
+    d, 4], four tokens interleaved; with torch.float8_e4m3fn also scales: [num_blocks, Hkv, 2, page_size] of
+    torch.float8_e8m0fnu, and with torch.bfloat16 none."""
+
+    def __init__(self, k, v, scales=None):
+        lib()
+        f8 = k.dtype == _torch.float8_e4m3fn
+        _need(f8 or k.dtype == _torch.bfloat16, "a cache is torch.float8_e4m3fn or torch.bfloat16")
+        _need(k.dim() == 4, "k must be [num_blocks, Hkv, page_size, d]")
+        self.num_blocks, self.Hkv, self.page_size, self.d = k.shape
+        self.k, self.v, self.scales, self.dtype = k, v, scales, PK_F8 if f8 else PK_BF16
+        _need(v.dtype == k.dtype and tuple(v.shape) == (self.num_blocks, self.Hkv, self.page_size // 4, self.d, 4),
+              "v must be [num_blocks, Hkv, page_size / 4, d, 4] of k's type")
+        _need((scales is not None) == f8, "scales belong to a cache in 8 bits, and to no other")
+        _need(not f8 or (scales.dtype == _torch.float8_e8m0fnu and tuple(scales.shape) == (self.num_blocks, self.Hkv, 2, self.page_size)),
+              "scales must be [num_blocks, Hkv, 2, page_size] of torch.float8_e8m0fnu")
+        _need(all(x is None or x.is_contiguous() for x in (k, v, scales)), "the tensors of a cache must be contiguous")
+        self.raw = _CACHE.pack(k.data_ptr(), v.data_ptr(), scales.data_ptr() if f8 else 0, self.num_blocks, self.page_size, self.Hkv, self.d, self.dtype)
+
+
+def new_kv_cache(num_blocks, page_size, Hkv, d, dtype=PK_F8, device="cuda") -> KvCache:
+    """A cache of zeros."""
+    lib()
+    t = _torch.float8_e4m3fn if dtype == PK_F8 else _torch.bfloat16
+    zeros = lambda shape, t: _torch.zeros(shape, dtype=_torch.uint8 if t.itemsize == 1 else t, device=device).view(t)  # noqa: E731
+    return KvCache(zeros((num_blocks, Hkv, page_size, d), t), zeros((num_blocks, Hkv, page_size // 4, d, 4), t),
+                   zeros((num_blocks, Hkv, 2, page_size), _torch.float8_e8m0fnu) if dtype == PK_F8 else None)
+
+
+class Rope:
+    """Rotary positions (pk_rope).  table: fp32 [max_pos, 2, rot_dim / 2], cosines and sines; positions: int32 [tokens] or
+    [axes, tokens] (device); pair_axis: axis of every rotated pair (host, None: the first); interleaved: pairs are
+    columns (2p, 2p + 1) instead of (p, p + rot_dim / 2)."""
+
+    def __init__(self, table, positions, pair_axis=None, interleaved=False):
+        lib()
+        _need(table.dtype == _torch.float32 and table.dim() == 3 and table.shape[1] == 2 and table.is_contiguous(),
+              "table must be contiguous fp32 [max_pos, 2, rot_dim / 2]")
+        positions = positions if positions.dim() == 2 else positions[None]
+        _need(positions.dtype == _torch.int32 and positions.dim() == 2 and (positions.stride(1) == 1 or positions.shape[1] <= 1),
+              "positions must be int32 [axes, tokens]")
+        pairs = table.shape[2]
+        self.pair_axis = None if pair_axis is None else np.ascontiguousarray(pair_axis, dtype=np.uint8)
+        _need(self.pair_axis is None or self.pair_axis.shape == (pairs,), "pair_axis must name an axis for each of the pairs")
+        self.table, self.positions, self.tokens = table, positions, positions.shape[1]
+        self.raw = _ROPE.pack(table.data_ptr(), positions.data_ptr(), positions.stride(0), 0 if pair_axis is None else self.pair_axis.ctypes.data,
+                              table.shape[0], 2 * pairs, positions.shape[0], int(bool(interleaved)))
+
+
+def _raw_rope(rope, tokens):
+    if rope is None:
+        return None
+    _need(rope.tokens >= tokens, "the rotation has fewer positions than there are tokens")
+    return rope.raw
+
+
+def qk_norm_rope(q, k, q_out, k_out, q_weight=None, k_weight=None, eps=1e-6, rope: Optional[Rope] = None, stream=None):
+    """Norm (where there is a weight) and rotation of q [tokens, Hq, d] and k [tokens, Hkv, d] into q_out and k_out."""
+    L = lib()
+    tokens, Hq, d = q.shape
+    Hkv = k.shape[1]
+    _need(k.shape[0] == tokens and q_out.shape == q.shape and k_out.shape == k.shape, "q, k, q_out, k_out: shapes differ")
+    rc = L.pk_qk_norm_rope(_rows(q, "q"), _rows(k, "k", Hkv, d), _rows(q_out, "q_out"), _rows(k_out, "k_out"),
+                           _vector(q_weight, "q_weight", q.dtype, d), _vector(k_weight, "k_weight", q.dtype, d), float(eps),
+                           _raw_rope(rope, tokens), tokens, Hq, Hkv, d, _stream(stream))
+    _check(rc, "pk_qk_norm_rope")
+    return q_out, k_out
+
+
+def kv_cache_write(cache: KvCache, k, v, slots, stream=None):
+    """Rows of k and v [tokens, Hkv, d] into slots (int64 [tokens], -1: not written) of the cache."""
+    L = lib()
+    tokens = k.shape[0]
+    _need(v.shape[0] == tokens, "k and v have different numbers of tokens")
+    rc = L.pk_kv_cache_write(cache.raw, _rows(k, "k", cache.Hkv, cache.d), _rows(v, "v", cache.Hkv, cache.d),
+                             _vector(slots, "slots", _torch.int64, tokens), tokens, _stream(stream))
+    _check(rc, "pk_kv_cache_write")
+    return cache
+
+
+def qkv_cache_write(cache: KvCache, q, k, v, slots, q_out, q_weight=None, k_weight=None, eps=1e-6, rope: Optional[Rope] = None, stream=None):
+    """qk_norm_rope and kv_cache_write in one launch: q into q_out, k (normed and rotated) and v into the cache."""
+    L = lib()
+    tokens, Hq, d = q.shape
+    _need(k.shape[0] == tokens and v.shape[0] == tokens and q_out.shape == q.shape and d == cache.d, "q, k, v, q_out: shapes differ")
+    rc = L.pk_qkv_cache_write(cache.raw, _rows(q, "q"), _rows(k, "k", cache.Hkv, d), _rows(v, "v", cache.Hkv, d),
+                              _vector(slots, "slots", _torch.int64, tokens), _rows(q_out, "q_out"),
+                              _vector(q_weight, "q_weight", q.dtype, d), _vector(k_weight, "k_weight", q.dtype, d), float(eps),
+                              _raw_rope(rope, tokens), tokens, Hq, _stream(stream))
+    _check(rc, "pk_qkv_cache_write")
+    return q_out
+
+
+def kv_cache_read(cache: KvCache, block_table, kv_lens, row_start, k_out, v_out, stream=None):
+    """Tokens 0 .. kv_lens[i] - 1 of every request as rows row_start[i], ... of k_out and v_out [rows, Hkv, d]."""
+    L = lib()
+    n, max_blocks = block_table.shape
+    _need(v_out.shape == k_out.shape, "k_out and v_out: shapes differ")
+    rc = L.pk_kv_cache_read(cache.raw, _vector(block_table, "block_table", _torch.int32), max_blocks, _vector(kv_lens, "kv_lens", _torch.int32, n),
+                            _vector(row_start, "row_start", _torch.int32, n), n, _rows(k_out, "k_out", cache.Hkv, cache.d),
+                            _rows(v_out, "v_out", cache.Hkv, cache.d), k_out.shape[0], _stream(stream))
+    _check(rc, "pk_kv_cache_read")
+    return k_out, v_out
+
+
+def new_tree_workspace(n, max_q, Hq, Hkv, d, device="cuda"):
+    """Workspace of tree_attn for up to n requests of up to max_q drafted tokens; zeros, as its first use asks for."""
+    nbytes = max(256, int(lib().pk_tree_attn_workspace_bytes(n, max_q, Hq, Hkv, d)))
+    return _torch.zeros(nbytes, dtype=_torch.uint8, device=device)
+
+
+def tree_attn(cache: KvCache, q, q_start, max_q, tree_mask, block_table, kv_lens, out, scale, workspace, stream=None):
+    """Attention of the drafted tokens q [total, Hq, d] (request i: rows q_start[i] .. q_start[i + 1]) over the cache.
+    tree_mask: int64 [total], bit j = drafted token j of the same request is seen (None: those before and itself)."""
+    L = lib()
+    total, Hq, d = q.shape
+    n, max_blocks = block_table.shape
+    _need(q.dtype == _torch.bfloat16 and q.is_contiguous() and out.is_contiguous() and out.shape == q.shape and d == cache.d,
+          "q must be contiguous bf16 [total, Hq, d], out of the same shape")
+    rc = L.pk_tree_attn(cache.raw, q.data_ptr(), _vector(q_start, "q_start", _torch.int32, n + 1), total, int(max_q),
+                        _vector(tree_mask, "tree_mask", _torch.int64, total), _vector(block_table, "block_table", _torch.int32), max_blocks,
+                        _vector(kv_lens, "kv_lens", _torch.int32, n), n, out.data_ptr(), float(scale), Hq, _dtype_code(out),
+                        workspace.data_ptr(), workspace.nbytes, _stream(stream))
+    _check(rc, "pk_tree_attn")
+    return out
+
+
+def kv_cache_keep(cache: KvCache, block_table, kv_lens, q_start, keep, keep_count, new_lens, stream=None):
+    """Drafted tokens keep[i, :keep_count[i]] (rising) of every request move up behind its context; new_lens receives
+    the lengths with them."""
+    L = lib()
+    n, max_blocks = block_table.shape
+    _need(keep.dim() == 2 and keep.shape[0] == n, "keep must be [n, max_keep]")
+    rc = L.pk_kv_cache_keep(cache.raw, _vector(block_table, "block_table", _torch.int32), max_blocks, _vector(kv_lens, "kv_lens", _torch.int32, n),
+                            _vector(q_start, "q_start", _torch.int32, n + 1), n, _vector(keep, "keep", _torch.int32), keep.shape[1],
+                            _vector(keep_count, "keep_count", _torch.int32, n), _vector(new_lens, "new_lens", _torch.int32, n), _stream(stream))
+    _check(rc, "pk_kv_cache_keep")
+    return new_lens

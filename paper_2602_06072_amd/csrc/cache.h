@@ -1,0 +1,59 @@
+// Norm and rotation of queries and keys, the paged cache in 8 bits or bf16, attention of drafted tokens over
+// it: what the launches take.  Pointers are device pointers unless they say otherwise.
+#pragma once
+#include <cstdint>
+
+#include "kernels.h"
+
+namespace pk {
+
+constexpr int kMostPairs = 128;                     // rotated pairs of a row
+constexpr int kMostDrafts = 64;                     // drafted tokens of a request: bits of its mask words
+
+struct RowsView {                                   // [token][head][d], strides in elements, columns contiguous
+    void* data; int64_t token_stride, head_stride;
+};
+
+// The cache: K [blocks][Hkv][page][d], V [blocks][Hkv][page / 4][d][4], scales [blocks][Hkv][2][page] (K, V)
+struct CacheView {
+    void* k; void* v; uint8_t* scales;
+    int64_t num_blocks; int page, Hkv, d, f8;
+};
+
+struct TokenRowsArgs {
+    RowsView q, k, v, q_out, k_out;                 // no k_out: K and V go into the cache
+    const void* q_weight; const void* k_weight;     // null: no norm
+    float eps;
+    const float* table; const int32_t* positions;   // [max_pos][2][pairs]; [axes][tokens]
+    int64_t axis_stride; int32_t max_pos; int pairs; int interleaved;
+    uint8_t pair_axis[kMostPairs];
+    CacheView cache; const int64_t* slots;
+    int64_t tokens; int Hq, Hkv, d;
+    int in_f32, out_f32;
+};
+int launch_token_rows(const TokenRowsArgs& a, void* stream);
+
+struct CacheReadArgs {
+    CacheView cache; const int32_t* block_table; int32_t max_blocks;
+    const int32_t* kv_lens; const int32_t* row_start; int32_t n;
+    RowsView k_out, v_out; int64_t rows; int out_f32;
+};
+int launch_cache_read(const CacheReadArgs& a, void* stream);
+
+struct CacheKeepArgs {
+    CacheView cache; const int32_t* block_table; int32_t max_blocks;
+    const int32_t* kv_lens; const int32_t* q_start; int32_t n;
+    const int32_t* keep; int32_t max_keep; const int32_t* keep_count; int32_t* new_lens;
+};
+int launch_cache_keep(const CacheKeepArgs& a, void* stream);
+
+struct TreeArgs {
+    CacheView cache; const int32_t* block_table; int32_t max_blocks;
+    const void* q; const int32_t* q_start; int64_t total_q; int32_t max_q;
+    const uint64_t* mask;                           // [total_q]; null: every drafted token sees those before it and itself
+    const int32_t* kv_lens; int32_t n;
+    void* out; int out_f32; float scale; int Hq;
+};
+int launch_tree_attn(const TreeArgs& a, void* stream);
+
+}  // namespace pk
