@@ -1,6 +1,7 @@
 // Norm and rotation of queries and keys, the paged cache in 8 bits or bf16, attention of drafted tokens over
 // it: what the launches take.  Pointers are device pointers unless they say otherwise.
 #pragma once
+#include <cstddef>
 #include <cstdint>
 
 #include "kernels.h"
@@ -47,13 +48,29 @@ struct CacheKeepArgs {
 };
 int launch_cache_keep(const CacheKeepArgs& a, void* stream);
 
+// How a launch takes the rows of a (request, KV head): workgroups of row_groups * row_blocks * 16 rows, `chunks` of them; pieces of the
+// requests' keys, for each KV head and chunk `items` and one more a request at most, two partial results a piece at most.
+struct TreeShape {
+    int row_blocks, row_groups, chunks, items;
+    int rows() const { return 16 * row_blocks * row_groups; }
+    // both grow with n and max_q, so that a workspace serves every call of one head shape that is not larger than what it was made for
+    static size_t count_bytes(int64_t n, int Hkv, const TreeShape& s) { return static_cast<size_t>((n * Hkv * s.chunks * 4 + 255) / 256 * 256); }
+    static size_t partial_bytes(int Hkv, int d, int compute_units, const TreeShape& s);
+    static TreeShape of(int max_q, int Hq, int Hkv, int compute_units);
+};
+
 struct TreeArgs {
     CacheView cache; const int32_t* block_table; int32_t max_blocks;
     const void* q; const int32_t* q_start; int64_t total_q; int32_t max_q;
     const uint64_t* mask;                           // [total_q]; null: every drafted token sees those before it and itself
     const int32_t* kv_lens; int32_t n;
     void* out; int out_f32; float scale; int Hq;
+    uint32_t* arrived;                              // [n][Hkv][chunks], zero between launches (arrival.h)
+    float* part_lse; float* part_o;                 // [slots][Hkv][chunks][rows], [..][d]
+    // set by the launch
+    int heads_per_kv, subs, chunks, items, least_share;        // subs: sub-tiles of 16 keys in a page
+    FastDiv by_r, by_subs;
 };
-int launch_tree_attn(const TreeArgs& a, void* stream);
+int launch_tree_attn(TreeArgs a, const TreeShape& s, void* stream);
 
 }  // namespace pk

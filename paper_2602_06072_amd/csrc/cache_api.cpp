@@ -120,7 +120,36 @@ int cache_write_args(const char* who, const pk_cache* cache, const pk_rows* v, c
     return PK_OK;
 }
 
+// Compute units of the current device; 256 when there is none to ask (sizes can be queried without one)
+int compute_units() {
+    int dev = 0, cus = 0;
+    if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0) {
+        (void)hipGetLastError();
+        return 256;
+    }
+    return cus;
+}
+
+bool tree_sizes_ok(const int64_t n, const int64_t max_q, const int64_t Hq, const int64_t Hkv, const int64_t d) {
+    return n >= 0 && n <= 65535 && max_q >= 0 && max_q <= PK_MAX_DRAFTS && Hkv > 0 && Hkv <= 65535 && Hq > 0 && Hq <= 16384 && Hq % Hkv == 0 && (d == 64 || d == 128);
+}
+
 }  // namespace
+
+TreeShape TreeShape::of(const int max_q, const int Hq, const int Hkv, const int compute_units) {
+    const int rows = max_q * (Hq / Hkv);
+    TreeShape s{rows <= 16 ? 1 : 2, rows <= 32 ? 1 : rows <= 64 ? 2 : 4, 1, 0};
+    s.chunks = rows <= s.rows() ? 1 : (rows + s.rows() - 1) / s.rows();
+    const int heads = Hkv * s.chunks;
+    s.items = 2 * compute_units > heads ? 2 * compute_units / heads : 1;
+    return s;
+}
+
+// a share of the keys is at least 1 / items of all of them, and only requests of more than a share are cut: 2 * items slots hold the pieces of all
+size_t TreeShape::partial_bytes(const int Hkv, const int d, const int compute_units, const TreeShape& s) {
+    const int64_t heads = static_cast<int64_t>(Hkv) * s.chunks, most = heads > 2 * compute_units ? heads : 2 * compute_units;
+    return static_cast<size_t>((2 * most * s.rows() * (d + 1) * 4 + 255) / 256 * 256);
+}
 
 extern "C" int pk_qk_norm_rope(const pk_rows* q, const pk_rows* k, const pk_rows* q_out, const pk_rows* k_out,
                                const void* q_weight, const void* k_weight, float eps, const pk_rope* rope,
@@ -192,8 +221,12 @@ extern "C" int pk_kv_cache_read(const pk_cache* cache, const int32_t* block_tabl
 }
 
 extern "C" size_t pk_tree_attn_workspace_bytes(int32_t n, int32_t max_q, int Hq, int Hkv, int d) {
-    (void)n; (void)max_q; (void)Hq; (void)Hkv; (void)d;
-    return 256;
+    return guarded<size_t>(size_t{0}, size_t{0}, "pk_tree_attn_workspace_bytes", [&]() -> size_t {
+        if (!tree_sizes_ok(n, max_q, Hq, Hkv, d)) return 0;
+        const int cus = compute_units();
+        const TreeShape s = TreeShape::of(max_q, Hq, Hkv, cus);
+        return TreeShape::count_bytes(n, Hkv, s) + TreeShape::partial_bytes(Hkv, d, cus, s);
+    });
 }
 
 extern "C" int pk_tree_attn(const pk_cache* cache, const void* q, const int32_t* q_start, int64_t total_q, int32_t max_q,
@@ -213,14 +246,22 @@ extern "C" int pk_tree_attn(const pk_cache* cache, const void* q, const int32_t*
         if (!q || !out || !q_start) return refuse(who, {PK_EINVAL, "q, out or q_start is NULL"});
         if (!aligned(q, 16) || !aligned(out, 16)) return refuse(who, {PK_EINVAL, "q and out must be 16-byte aligned"});
         if (!workspace || !aligned(workspace, 256)) return refuse(who, {PK_EINVAL, "workspace is NULL or not 256-byte aligned"});
-        if (workspace_bytes < pk_tree_attn_workspace_bytes(n, max_q, Hq, cache->Hkv, cache->d))
+        const int cus = compute_units();
+        const TreeShape shape = TreeShape::of(max_q, Hq, cache->Hkv, cus);
+        const size_t partial = TreeShape::partial_bytes(cache->Hkv, cache->d, cus, shape);
+        workspace_bytes = workspace_bytes / 256 * 256;
+        if (workspace_bytes < TreeShape::count_bytes(n, cache->Hkv, shape) + partial)
             return refuse(who, {PK_EINVAL, "workspace smaller than pk_tree_attn_workspace_bytes"});
         TreeArgs a{};
         a.cache = view(*cache); a.block_table = block_table; a.max_blocks = max_blocks;
         a.q = q; a.q_start = q_start; a.total_q = total_q; a.max_q = max_q; a.mask = tree_mask;
         a.kv_lens = kv_lens; a.n = n;
         a.out = out; a.out_f32 = out_dtype == PK_F32; a.scale = scale; a.Hq = Hq;
-        return launched(who, launch_tree_attn(a, stream));
+        // counts at the front, partial results at the end: no call writes the counts of another
+        a.arrived = static_cast<uint32_t*>(workspace);
+        a.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + workspace_bytes - partial);
+        a.part_lse = a.part_o + partial / 4 / (cache->d + 1) * cache->d;
+        return launched(who, launch_tree_attn(a, shape, stream));
     });
 }
 
