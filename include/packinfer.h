@@ -565,8 +565,9 @@ int pk_qkv_cache_write(const pk_cache* cache, const pk_rows* q, const pk_rows* k
  *   block_table  device int32 [n][max_blocks]: physical block of a request's
  *                logical pages, clamped into [0, num_blocks)
  *   kv_lens, row_start  device int32 [n]; lengths are clamped into
- *                [0, max_blocks * page_size], rows outside of [0, rows) are not
- *                written.  The requests' rows must not overlap.
+ *                [0, max_blocks * page_size]; tokens whose row would be `rows` or
+ *                more are not written, nor is a request with a negative row_start.
+ *                The requests' rows must not overlap.
  * Errors: PK_EINVAL; PK_EUNSUPPORTED. */
 int pk_kv_cache_read(const pk_cache* cache, const int32_t* block_table, int32_t max_blocks,
                      const int32_t* kv_lens, const int32_t* row_start, int32_t n,
@@ -586,10 +587,11 @@ int pk_kv_cache_read(const pk_cache* cache, const int32_t* block_table, int32_t 
  *             request; NULL: token t sees tokens 0 .. t
  *   block_table, kv_lens: as for pk_kv_cache_read
  *   out       device [total_q][Hq][d], out_dtype, 16-byte aligned
- *   workspace device, 256-byte aligned, at least pk_tree_attn_workspace_bytes
- *             for n, max_q and the head shape or larger ones.  ZERO-FILLED BEFORE
- *             ITS FIRST USE; every call leaves it ready for the next.  Calls that
- *             share one are ordered by the caller.
+ *   workspace device, 256-byte aligned, at least pk_tree_attn_workspace_bytes.
+ *             ZERO-FILLED BEFORE ITS FIRST USE; every call leaves it ready for the
+ *             next.  One made for some n and max_q serves all calls of the same
+ *             head shape that have no more of either; all calls with it pass the
+ *             same workspace_bytes and are ordered by the caller.
  * The partial results of a request are put together in a fixed order: results
  * repeat bit for bit.
  * Errors: PK_EINVAL; PK_EUNSUPPORTED (page size, d, max_q). */

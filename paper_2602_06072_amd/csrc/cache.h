@@ -31,15 +31,18 @@ struct TokenRowsArgs {
     CacheView cache; const int64_t* slots;
     int64_t tokens; int Hq, Hkv, d;
     int in_f32, out_f32;
+    // set by the launch
+    int splits, axes_by_four; FastDiv by_splits; float one_by_d;       // waves that share a token's heads; whether four pairs in a row have one axis
 };
-int launch_token_rows(const TokenRowsArgs& a, void* stream);
+int launch_token_rows(TokenRowsArgs a, void* stream);
 
 struct CacheReadArgs {
     CacheView cache; const int32_t* block_table; int32_t max_blocks;
     const int32_t* kv_lens; const int32_t* row_start; int32_t n;
     RowsView k_out, v_out; int64_t rows; int out_f32;
+    int splits; FastDiv by_splits;                  // set by the launch: workgroups that share the heads of 64 tokens
 };
-int launch_cache_read(const CacheReadArgs& a, void* stream);
+int launch_cache_read(CacheReadArgs a, void* stream);
 
 struct CacheKeepArgs {
     CacheView cache; const int32_t* block_table; int32_t max_blocks;

@@ -1,96 +1,365 @@
-// Rows of a token: norm and rotation of queries and keys, and their way into the cache.
+// Rows of a token on their way between the projections, the cache and the attention: norm and rotation of queries and keys, quantised
+// writes, reads, and the moves of accepted tokens.  All of it is bound by memory (by latency in a decode step), one pass over the data.
+#include <type_traits>
+
 #include "cache_format.hip.h"
 
 namespace pk {
 namespace {
 
-__device__ __forceinline__ float load_element(const void* p, const int64_t i, const int f32) {
-    return f32 ? static_cast<const float*>(p)[i] : bf16_bits_to_float(static_cast<const uint16_t*>(p)[i]);
-}
-__device__ __forceinline__ void store_element(void* p, const int64_t i, const float x, const int f32) {
-    if (f32) static_cast<float*>(p)[i] = x;
-    else static_cast<uint16_t*>(p)[i] = float_to_bf16_bits(x);
+constexpr int kWaves = 4;
+
+// sum and maximum over aligned groups of LPR lanes (8, 16 or 32), in every lane of them
+template <int CTRL>
+__device__ __forceinline__ float dpp(const float x) { return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xF, 0xF, true)); }
+template <int LPR, class Op>
+__device__ __forceinline__ float over_row(float x, Op op) {
+    x = op(x, dpp<0xB1>(x));                        // quad_perm [1,0,3,2]
+    x = op(x, dpp<0x4E>(x));                        // quad_perm [2,3,0,1]
+    x = op(x, dpp<0x141>(x));                       // row_half_mirror: the other four of eight
+    if constexpr (LPR >= 16) x = op(x, dpp<0x140>(x));     // row_mirror: the other eight of sixteen
+    if constexpr (LPR >= 32) x = op(x, __shfl_xor(x, 16, 64));
+    return x;
 }
 
-// One wave for a row: y = x * rsqrt(mean(x^2) + eps) * w, then (a, b) -> (a cos - b sin, b cos + a sin) of every pair
-__global__ __launch_bounds__(64) void token_rows_kernel(TokenRowsArgs a) {
-    __shared__ float row[256];
-    const int64_t t = blockIdx.x;
-    const int lane = threadIdx.x, d = a.d;
-    int h = blockIdx.y;
-    const int what = h < a.Hq ? 0 : h < a.Hq + a.Hkv ? 1 : 2;      // query, key, value
-    h -= what == 0 ? 0 : what == 1 ? a.Hq : a.Hq + a.Hkv;
-    const RowsView& in = what == 0 ? a.q : what == 1 ? a.k : a.v;
-    const void* w = what == 0 ? a.q_weight : what == 1 ? a.k_weight : nullptr;
-    float sum = 0.f;
-    for (int c = lane; c < d; c += 64) {
-        const float x = load_element(in.data, t * in.token_stride + h * in.head_stride + c, a.in_f32);
-        row[c] = x;
-        sum = fmaf(x, x, sum);
+// Eight columns of a row: four from column `a` on and four from `b` on
+struct Eight { float a[4], b[4]; };
+template <bool F32>
+struct RawEight { std::conditional_t<F32, u32x4, uint2> a, b; };
+template <bool F32>
+__device__ __forceinline__ RawEight<F32> load_eight(const void* p, const int64_t at, const int a, const int b) {
+    using T = decltype(RawEight<F32>::a);
+    if constexpr (F32) {
+        const float* x = static_cast<const float*>(p) + at;
+        return {*reinterpret_cast<const T*>(x + a), *reinterpret_cast<const T*>(x + b)};
+    } else {
+        const uint16_t* x = static_cast<const uint16_t*>(p) + at;
+        return {*reinterpret_cast<const T*>(x + a), *reinterpret_cast<const T*>(x + b)};
     }
-    if (w) {
-        const float inv = 1.f / sqrtf(wave_sum(sum) / d + a.eps);
-        for (int c = lane; c < d; c += 64) row[c] = row[c] * inv * load_element(w, c, a.in_f32);
+}
+__device__ __forceinline__ float low_half(const uint32_t x) { return __uint_as_float(x << 16); }
+__device__ __forceinline__ float high_half(const uint32_t x) { return __uint_as_float(x & 0xFFFF0000u); }
+template <bool F32>
+__device__ __forceinline__ Eight widened(const RawEight<F32>& r) {
+    if constexpr (F32) return __builtin_bit_cast(Eight, r);
+    else return {{low_half(r.a.x), high_half(r.a.x), low_half(r.a.y), high_half(r.a.y)}, {low_half(r.b.x), high_half(r.b.x), low_half(r.b.y), high_half(r.b.y)}};
+}
+template <bool F32>
+__device__ __forceinline__ void store_eight(void* p, const int64_t at, const int a, const int b, const Eight& x) {
+    if constexpr (F32) {
+        float* o = static_cast<float*>(p) + at;
+        *reinterpret_cast<floatx4*>(o + a) = floatx4{x.a[0], x.a[1], x.a[2], x.a[3]};
+        *reinterpret_cast<floatx4*>(o + b) = floatx4{x.b[0], x.b[1], x.b[2], x.b[3]};
+    } else {
+        uint16_t* o = static_cast<uint16_t*>(p) + at;
+        *reinterpret_cast<uint2*>(o + a) = make_uint2(pack_bf16x2(x.a[0], x.a[1]), pack_bf16x2(x.a[2], x.a[3]));
+        *reinterpret_cast<uint2*>(o + b) = make_uint2(pack_bf16x2(x.b[0], x.b[1]), pack_bf16x2(x.b[2], x.b[3]));
     }
-    __syncthreads();
-    if (what < 2 && a.table)
-        for (int p = lane; p < a.pairs; p += 64) {
-            int pos = a.positions[a.pair_axis[p] * a.axis_stride + t];
-            pos = min(max(pos, 0), a.max_pos - 1);
-            const float* cs = a.table + static_cast<int64_t>(pos) * 2 * a.pairs + p;
-            const int i = a.interleaved ? 2 * p : p, j = a.interleaved ? 2 * p + 1 : p + a.pairs;
-            const float x = row[i], y = row[j];
-            row[i] = x * cs[0] - y * cs[a.pairs];
-            row[j] = y * cs[0] + x * cs[a.pairs];
-        }
-    __syncthreads();
-    if (what == 0 || a.k_out.data) {
-        const RowsView& out = what == 0 ? a.q_out : a.k_out;
-        for (int c = lane; c < d; c += 64) store_element(out.data, t * out.token_stride + h * out.head_stride + c, row[c], a.out_f32);
-        return;
-    }
-    const int64_t slot = a.slots[t];
-    if (slot < 0 || slot >= a.cache.num_blocks * a.cache.page) return;
-    const int64_t block = slot / a.cache.page;
-    const int off = static_cast<int>(slot % a.cache.page);
-    uint32_t largest = 0;
-    for (int c = lane; c < d; c += 64) largest = max(largest, finite_bits(row[c]));
-    for (int o = 32; o > 0; o >>= 1) largest = max(largest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(largest), o, 64)));
-    const uint32_t byte = scale_byte(largest);
-    for (int c = lane; c < d; c += 64) {
-        const int64_t i = what == 1 ? k_index(a.cache, block, off, h, c) : v_index(a.cache, block, off, h, c);
-        void* dst = what == 1 ? a.cache.k : a.cache.v;
-        if (a.cache.f8) static_cast<uint8_t*>(dst)[i] = static_cast<uint8_t>(pack_f8x2(row[c], 0.f, scale_inverse(byte)));
-        else static_cast<uint16_t*>(dst)[i] = float_to_bf16_bits(row[c]);
-    }
-    if (a.cache.f8 && lane == 0) a.cache.scales[scale_index(a.cache, block, off, h, what - 1)] = static_cast<uint8_t>(byte);
 }
 
-// One workgroup for a token of a request
-__global__ __launch_bounds__(64) void cache_read_kernel(CacheReadArgs a) {
-    const int i = blockIdx.y, lane = threadIdx.x;
-    const int64_t len = min(static_cast<int64_t>(a.kv_lens[i]), static_cast<int64_t>(a.max_blocks) * a.cache.page);
-    const CacheView& c = a.cache;
-    for (int64_t t = blockIdx.x; t < len; t += gridDim.x) {
-        const int64_t out_row = a.row_start[i] + t;
-        if (out_row < 0 || out_row >= a.rows) continue;
-        const int64_t block = block_of(c, a.block_table + static_cast<int64_t>(i) * a.max_blocks, static_cast<int>(t / c.page));
-        const int off = static_cast<int>(t % c.page);
-        for (int e = lane; e < c.Hkv * c.d; e += 64) {
-            const int h = e / c.d, col = e % c.d;
-            const int64_t ki = k_index(c, block, off, h, col), vi = v_index(c, block, off, h, col);
-            float k, v;
-            if (c.f8) {
-                const auto value = [](const void* p, int64_t at) { return __builtin_amdgcn_cvt_f32_fp8(static_cast<const uint8_t*>(p)[at], 0); };
-                k = value(c.k, ki) * scale_value(c.scales[scale_index(c, block, off, h, 0)]);
-                v = value(c.v, vi) * scale_value(c.scales[scale_index(c, block, off, h, 1)]);
-            } else {
-                k = load_element(c.k, ki, 0);
-                v = load_element(c.v, vi, 0);
+// permlane swaps: rows 16..31 of x with rows 0..15 of y (and 48..63 with 32..47); the upper half of x with the lower half of y
+__device__ __forceinline__ void swap16(uint32_t& x, uint32_t& y) {
+    const auto p = __builtin_amdgcn_permlane16_swap(x, y, false, false);
+    x = p[0]; y = p[1];
+}
+__device__ __forceinline__ void swap32(uint32_t& x, uint32_t& y) {
+    const auto p = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+    x = p[0]; y = p[1];
+}
+
+enum Kind { kQuery, kKey, kValue };
+
+// One wave for four consecutive tokens (two with LPR = 32), a head of theirs (two with LPR = 8) at a time: LPR lanes share a row, eight columns each.
+// A pair's two columns are in one lane (halves: four columns of either half), so that the rotation needs no exchange, and the cosines and sines of a
+// token are loaded once for all the heads that a wave takes.  Four tokens at once because the cache interleaves the values of four.
+template <int LPR, bool IN_F32, bool OUT_F32>
+__global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a) {
+    constexpr int TOKENS = LPR == 32 ? 2 : 4, HEADS = LPR == 8 ? 2 : 1, BATCH = 4;
+    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(blockIdx.x * kWaves + (threadIdx.x >> 6))), lane = threadIdx.x & 63;
+    const int group = a.by_splits(wave), split = wave - group * a.splits;
+    const int64_t t0 = static_cast<int64_t>(group) * TOKENS;
+    if (t0 >= a.tokens) return;
+    const int sub = lane / (64 / TOKENS), of = HEADS == 1 ? 0 : lane >> 3 & 1, x = lane % LPR;
+    const bool token_ok = t0 + sub < a.tokens, columns_ok = 8 * x < a.d;
+    const int64_t t = token_ok ? t0 + sub : a.tokens - 1;
+    const int steps_q = (a.Hq + HEADS - 1) / HEADS, steps_k = (a.Hkv + HEADS - 1) / HEADS, steps = steps_q + (a.k_out.data ? 1 : 2) * steps_k;
+    const int first = static_cast<int>(static_cast<int64_t>(steps) * split / a.splits), last = static_cast<int>(static_cast<int64_t>(steps) * (split + 1) / a.splits);
+
+    // columns of a row that is rotated, and of one that is not
+    const bool rotated = x < a.pairs / 4;
+    const int plain_a = columns_ok ? 8 * x : 0, plain_b = plain_a + 4;
+    const int turn_a = rotated && !a.interleaved ? 4 * x : plain_a, turn_b = rotated && !a.interleaved ? 4 * x + a.pairs : plain_b;
+    floatx4 cs = {1.f, 1.f, 1.f, 1.f}, sn = {0.f, 0.f, 0.f, 0.f};
+    if (a.table && rotated && first < steps_q + steps_k) {
+        const auto row = [&](const int axis) {
+            const int pos = a.positions[axis * a.axis_stride + t];
+            return a.table + static_cast<int64_t>(min(max(pos, 0), a.max_pos - 1)) * 2 * a.pairs + 4 * x;
+        };
+        if (a.axes_by_four) {                       // the four pairs of a lane have one axis
+            const float* r = row(a.pair_axis[4 * x]);
+            cs = *reinterpret_cast<const floatx4*>(r);
+            sn = *reinterpret_cast<const floatx4*>(r + a.pairs);
+        } else {
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                const float* r = row(a.pair_axis[4 * x + p]);
+                cs[p] = r[p];
+                sn[p] = r[a.pairs + p];
             }
-            store_element(a.k_out.data, out_row * a.k_out.token_stride + h * a.k_out.head_stride + col, k, a.out_f32);
-            store_element(a.v_out.data, out_row * a.v_out.token_stride + h * a.v_out.head_stride + col, v, a.out_f32);
         }
+    }
+    int64_t block = 0;
+    int off = 0;
+    bool slot_ok = false, whole = false;            // whole: the four tokens fill four interleaved places
+    if (!a.k_out.data && last > steps_q) {
+        const int64_t slot = a.slots[t];
+        slot_ok = token_ok && slot >= 0 && slot < a.cache.num_blocks * a.cache.page;
+        block = slot_ok ? slot / a.cache.page : 0;
+        off = slot_ok ? static_cast<int>(slot - block * a.cache.page) : 0;
+        whole = __all(slot_ok && (off & 3) == sub && __shfl(slot, lane & 15, 64) + sub == slot);
+    }
+
+    const auto run = [&](auto what, const int from, const int to, const int heads, const RowsView& in, const RowsView& out, const void* weight) {
+        constexpr Kind KIND = decltype(what)::value;
+        const bool turns = KIND != kValue;
+        const int ca = turns ? turn_a : plain_a, cb = turns ? turn_b : plain_b;
+        Eight w;
+        const bool normed = weight != nullptr;
+        if (normed && from < to) w = widened<IN_F32>(load_eight<IN_F32>(weight, 0, ca, cb));
+        for (int s0 = from; s0 < to; s0 += BATCH) {
+            RawEight<IN_F32> raw[BATCH];
+#pragma unroll
+            for (int s = 0; s < BATCH; ++s) {
+                const int h = min(HEADS * min(s0 + s, to - 1) + of, heads - 1);
+                raw[s] = load_eight<IN_F32>(in.data, t * in.token_stride + h * in.head_stride, ca, cb);
+            }
+#pragma unroll
+            for (int s = 0; s < BATCH; ++s) {
+                if (s0 + s >= to) break;
+                const int h = HEADS * (s0 + s) + of;
+                const bool row_ok = token_ok && columns_ok && h < heads;
+                Eight y = widened<IN_F32>(raw[s]);
+                if (!columns_ok) y = Eight{};
+                if (KIND != kValue && normed) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum = fmaf(y.a[e], y.a[e], fmaf(y.b[e], y.b[e], sum));
+                    sum = over_row<LPR>(sum, [](float p, float q) { return p + q; });
+                    const float inv = 1.f / sqrtf(fmaf(sum, a.one_by_d, a.eps));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { y.a[e] *= inv * w.a[e]; y.b[e] *= inv * w.b[e]; }
+                }
+                if (KIND != kValue && rotated) {
+                    const auto turn = [](float& p, float& q, const float c, const float n) {
+                        const float p0 = p, q0 = q;
+                        p = fmaf(p0, c, -q0 * n);
+                        q = fmaf(q0, c, p0 * n);
+                    };
+                    if (a.interleaved) {
+                        turn(y.a[0], y.a[1], cs[0], sn[0]);
+                        turn(y.a[2], y.a[3], cs[1], sn[1]);
+                        turn(y.b[0], y.b[1], cs[2], sn[2]);
+                        turn(y.b[2], y.b[3], cs[3], sn[3]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) turn(y.a[e], y.b[e], cs[e], sn[e]);
+                    }
+                }
+                if (KIND == kQuery || (KIND == kKey && a.k_out.data)) {
+                    if (row_ok) store_eight<OUT_F32>(out.data, t * out.token_stride + h * out.head_stride, ca, cb, y);
+                    continue;
+                }
+                if constexpr (LPR <= 16) {
+                    const bool cell_ok = row_ok && slot_ok;
+                    const int64_t base = (block * a.cache.Hkv + h) * a.cache.page;
+                    if (a.cache.f8) {
+                        float top = 0.f;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(__uint_as_float(finite_bits(y.a[e])), __uint_as_float(finite_bits(y.b[e]))));
+                        top = over_row<LPR>(top, [](float p, float q) { return fmaxf(p, q); });
+                        const uint32_t byte = scale_byte(__float_as_uint(top));
+                        const float inv = scale_inverse(byte);
+                        uint32_t c0 = pack_f8x2(y.a[0], y.a[1], inv) | pack_f8x2(y.a[2], y.a[3], inv) << 16;
+                        uint32_t c1 = pack_f8x2(y.b[0], y.b[1], inv) | pack_f8x2(y.b[2], y.b[3], inv) << 16;
+                        if (cell_ok && x == 0) a.cache.scales[2 * base + (KIND == kValue ? a.cache.page : 0) + off] = static_cast<uint8_t>(byte);
+                        if constexpr (KIND == kKey) {
+                            uint8_t* k = static_cast<uint8_t*>(a.cache.k) + (base + off) * a.d;
+                            if (cell_ok) {
+                                *reinterpret_cast<uint32_t*>(k + ca) = c0;
+                                *reinterpret_cast<uint32_t*>(k + cb) = c1;
+                            }
+                        } else if (whole) {
+                            // column pairs 0..3 of tokens 0..3 -> lane group s has pair s of all four tokens: 2 columns x 4 tokens, 8 bytes
+                            swap32(c0, c1);                        // groups 0, 1: pairs 0, 1 of tokens s, s + 2; groups 2, 3: pairs 2, 3 of tokens s - 2, s
+                            uint32_t even = __builtin_amdgcn_perm(c1, c0, 0x05040100u), odd = __builtin_amdgcn_perm(c1, c0, 0x07060302u);
+                            swap16(even, odd);                     // pair s of tokens 0, 2 and of tokens 1, 3
+                            const uint32_t lo = __builtin_amdgcn_perm(odd, even, 0x06020400u), hi = __builtin_amdgcn_perm(odd, even, 0x07030501u);
+                            uint8_t* v = static_cast<uint8_t*>(a.cache.v) + (base + (off & ~3)) * a.d + 4 * (8 * x + 2 * sub);
+                            if (columns_ok && h < heads) *reinterpret_cast<uint2*>(v) = make_uint2(lo, hi);
+                        } else if (cell_ok) {
+                            uint8_t* v = static_cast<uint8_t*>(a.cache.v) + (base + (off & ~3)) * a.d + 4 * 8 * x + (off & 3);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                v[4 * e] = static_cast<uint8_t>(c0 >> 8 * e);
+                                v[16 + 4 * e] = static_cast<uint8_t>(c1 >> 8 * e);
+                            }
+                        }
+                    } else {
+                        uint32_t p[4] = {pack_bf16x2(y.a[0], y.a[1]), pack_bf16x2(y.a[2], y.a[3]), pack_bf16x2(y.b[0], y.b[1]), pack_bf16x2(y.b[2], y.b[3])};
+                        if constexpr (KIND == kKey) {
+                            uint16_t* k = static_cast<uint16_t*>(a.cache.k) + (base + off) * a.d;
+                            if (cell_ok) {
+                                *reinterpret_cast<uint2*>(k + ca) = make_uint2(p[0], p[1]);
+                                *reinterpret_cast<uint2*>(k + cb) = make_uint2(p[2], p[3]);
+                            }
+                        } else if (whole) {                        // the same with pairs of 32 bits: lane group s has pair s of tokens 0..3
+                            swap32(p[0], p[2]);                    // groups 0, 1: pair 0 of tokens s, s + 2; groups 2, 3: pair 2 of tokens s - 2, s
+                            swap32(p[1], p[3]);                    // pairs 1, 3
+                            swap16(p[0], p[1]);                    // pair s of tokens 0, 1
+                            swap16(p[2], p[3]);                    // of tokens 2, 3
+                            uint16_t* v = static_cast<uint16_t*>(a.cache.v) + (base + (off & ~3)) * a.d + 4 * (8 * x + 2 * sub);
+                            if (columns_ok && h < heads)
+                                *reinterpret_cast<u32x4*>(v) = u32x4{__builtin_amdgcn_perm(p[1], p[0], 0x05040100u), __builtin_amdgcn_perm(p[3], p[2], 0x05040100u),
+                                                                     __builtin_amdgcn_perm(p[1], p[0], 0x07060302u), __builtin_amdgcn_perm(p[3], p[2], 0x07060302u)};
+                        } else if (cell_ok) {
+                            uint16_t* v = static_cast<uint16_t*>(a.cache.v) + (base + (off & ~3)) * a.d + 4 * 8 * x + (off & 3);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                v[8 * e] = static_cast<uint16_t>(p[e]);
+                                v[8 * e + 4] = static_cast<uint16_t>(p[e] >> 16);
+                            }
+                        }
+                    }
+                }
+            }
+        }
+    };
+    run(std::integral_constant<Kind, kQuery>{}, min(first, steps_q), min(last, steps_q), a.Hq, a.q, a.q_out, a.q_weight);
+    const int k0 = steps_q, k1 = steps_q + steps_k;
+    run(std::integral_constant<Kind, kKey>{}, min(max(first, k0), k1) - k0, min(max(last, k0), k1) - k0, a.Hkv, a.k, a.k_out, a.k_weight);
+    run(std::integral_constant<Kind, kValue>{}, max(first, k1) - k1, max(last, k1) - k1, a.Hkv, a.v, a.k_out, nullptr);
+}
+
+// The request that unit `item` of the launch belongs to, and its number there, where request i has units(i) of them: prefix sums of them all,
+// by every workgroup itself.  False: there are fewer.
+template <class Units>
+__device__ __forceinline__ bool find_unit(const int n, const int item, Units units, int& request, int& unit) {
+    __shared__ int sums[kWaves], found[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int each = (n + 64 * kWaves - 1) / (64 * kWaves), i0 = min(n, tid * each), i1 = min(n, i0 + each);
+    int mine = 0;
+    for (int i = i0; i < i1; ++i) mine += units(i);
+    int before = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(before, o, 64);
+        if (lane >= o) before += y;
+    }
+    if (lane == 63) sums[wave] = before;
+    if (tid == 0) found[0] = -1;
+    __syncthreads();
+    before -= mine;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+        if (w < wave) before += sums[w];
+    if (item >= before && item < before + mine)
+        for (int i = i0; i < i1; ++i) {
+            const int k = units(i);
+            if (item < before + k) { found[0] = i; found[1] = item - before; break; }
+            before += k;
+        }
+    __syncthreads();
+    request = __builtin_amdgcn_readfirstlane(found[0]);
+    unit = __builtin_amdgcn_readfirstlane(found[1]);
+    return request >= 0;
+}
+
+template <bool F32, int COUNT>
+__device__ __forceinline__ void store_row(void* p, const int64_t at, const float* x) {
+    if constexpr (F32) {
+#pragma unroll
+        for (int e = 0; e < COUNT; e += 4) *reinterpret_cast<floatx4*>(static_cast<float*>(p) + at + e) = floatx4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+    } else if constexpr (COUNT % 8 == 0) {
+#pragma unroll
+        for (int e = 0; e < COUNT; e += 8)
+            *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p) + at + e) = u32x4{pack_bf16x2(x[e], x[e + 1]), pack_bf16x2(x[e + 2], x[e + 3]), pack_bf16x2(x[e + 4], x[e + 5]), pack_bf16x2(x[e + 6], x[e + 7])};
+    } else {
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + at) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+    }
+}
+__device__ __forceinline__ void widen_codes(const uint32_t x, const float scale, float* y) {
+    y[0] = __builtin_amdgcn_cvt_f32_fp8(x, 0) * scale;
+    y[1] = __builtin_amdgcn_cvt_f32_fp8(x, 1) * scale;
+    y[2] = __builtin_amdgcn_cvt_f32_fp8(x, 2) * scale;
+    y[3] = __builtin_amdgcn_cvt_f32_fp8(x, 3) * scale;
+}
+
+// One workgroup for 64 tokens of a request and some of the heads, one wave for 16 tokens, which lie in one page, a head at a time.  K: 16-byte
+// chunks as they are.  V: a lane takes all four interleaved tokens of its columns, so that each of their rows is stored in whole lines.
+template <int D, bool F8, bool OUT_F32>
+__global__ __launch_bounds__(64 * kWaves) void cache_read_kernel(CacheReadArgs a) {
+    constexpr int PER = F8 ? 16 : 8, LANES = D / PER, ROWS = 64 / LANES, KC = 16 / ROWS;   // K: columns of a chunk, lanes and rows of a load, loads
+    constexpr int COLS = D / 16, VC = COLS * 4 / PER;                                     // V: columns of a lane, chunks
+    const CacheView& c = a.cache;
+    const int64_t most = static_cast<int64_t>(a.max_blocks) * c.page;
+    const auto length = [&](const int i) {          // tokens that have a row
+        const int64_t start = a.row_start[i];
+        return start < 0 ? 0 : static_cast<int>(max(min(min(static_cast<int64_t>(a.kv_lens[i]), most), a.rows - start), int64_t{0}));
+    };
+    int i, unit;
+    if (!find_unit(a.n, a.by_splits(static_cast<int>(blockIdx.x)), [&](const int y) { return (length(y) + 63) / 64; }, i, unit)) return;
+    const int split = static_cast<int>(blockIdx.x) % a.splits, h0 = c.Hkv * split / a.splits, h1 = c.Hkv * (split + 1) / a.splits;
+    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+    const int len = length(i), t0 = unit * 64 + wave * 16;
+    if (t0 >= len) return;
+    const int page = t0 / c.page, off = t0 - page * c.page;
+    const int64_t block = block_of(c, a.block_table + static_cast<int64_t>(i) * a.max_blocks, page);
+    const int64_t row0 = static_cast<int64_t>(a.row_start[i]) + t0;
+    const auto row_ok = [&](const int token) { return t0 + token < len; };
+    const int g = lane >> 4, x = lane & 15;
+#pragma unroll 2
+    for (int h = h0; h < h1; ++h) {
+        const int64_t base = (block * c.Hkv + h) * c.page, at = (base + off) * D * (F8 ? 1 : 2);
+        u32x4 k[KC], v[VC];
+        float ks[KC], vs[4];
+#pragma unroll
+        for (int y = 0; y < KC; ++y) k[y] = *reinterpret_cast<const u32x4*>(static_cast<const unsigned char*>(c.k) + at + 16 * (lane + 64 * y));
+#pragma unroll
+        for (int y = 0; y < VC; ++y) v[y] = *reinterpret_cast<const u32x4*>(static_cast<const unsigned char*>(c.v) + at + 16 * (VC * lane + y));
+        if constexpr (F8) {
+#pragma unroll
+            for (int y = 0; y < KC; ++y) ks[y] = scale_value(c.scales[2 * base + off + y * ROWS + lane / LANES]);
+            const uint32_t four = *reinterpret_cast<const uint32_t*>(c.scales + 2 * base + c.page + off + 4 * g);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) vs[e] = scale_value(four >> 8 * e & 0xFF);
+        }
+#pragma unroll
+        for (int y = 0; y < KC; ++y) {
+            float row[PER];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (F8) widen_codes(k[y][e], ks[y], row + 4 * e);
+                else { row[2 * e] = low_half(k[y][e]); row[2 * e + 1] = high_half(k[y][e]); }
+            }
+            const int token = y * ROWS + lane / LANES;
+            if (row_ok(token)) store_row<OUT_F32, PER>(a.k_out.data, (row0 + token) * a.k_out.token_stride + h * a.k_out.head_stride + lane % LANES * PER, row);
+        }
+        float rows[4][COLS];
+#pragma unroll
+        for (int col = 0; col < COLS; ++col) {
+            if constexpr (F8) {
+                float four[4];
+                widen_codes(v[col / 4][col % 4], 1.f, four);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) rows[e][col] = four[e] * vs[e];
+            } else {
+                const uint32_t lo = v[col / 2][2 * (col % 2)], hi = v[col / 2][2 * (col % 2) + 1];
+                rows[0][col] = low_half(lo); rows[1][col] = high_half(lo); rows[2][col] = low_half(hi); rows[3][col] = high_half(hi);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (row_ok(4 * g + e)) store_row<OUT_F32, COLS>(a.v_out.data, (row0 + 4 * g + e) * a.v_out.token_stride + h * a.v_out.head_stride + x * COLS, rows[e]);
     }
 }
 
@@ -119,16 +388,57 @@ __global__ __launch_bounds__(128) void cache_keep_kernel(CacheKeepArgs a) {
     }
 }
 
+template <int LPR>
+void launch_rows(const TokenRowsArgs& a, const dim3 grid, hipStream_t st) {
+    const dim3 block(64 * kWaves);
+    if (a.in_f32 && a.out_f32) hipLaunchKernelGGL((token_rows_kernel<LPR, true, true>), grid, block, 0, st, a);
+    else if (a.in_f32) hipLaunchKernelGGL((token_rows_kernel<LPR, true, false>), grid, block, 0, st, a);
+    else if (a.out_f32) hipLaunchKernelGGL((token_rows_kernel<LPR, false, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((token_rows_kernel<LPR, false, false>), grid, block, 0, st, a);
+}
+
+template <int D, bool F8>
+void launch_read(const CacheReadArgs& a, const dim3 grid, hipStream_t st) {
+    if (a.out_f32) hipLaunchKernelGGL((cache_read_kernel<D, F8, true>), grid, dim3(64 * kWaves), 0, st, a);
+    else hipLaunchKernelGGL((cache_read_kernel<D, F8, false>), grid, dim3(64 * kWaves), 0, st, a);
+}
+
 }  // namespace
 
-int launch_token_rows(const TokenRowsArgs& a, void* stream) {
-    const unsigned heads = static_cast<unsigned>(a.Hq + (a.k_out.data ? 1 : 2) * a.Hkv);
-    hipLaunchKernelGGL(token_rows_kernel, dim3(static_cast<unsigned>(a.tokens), heads), dim3(64), 0, static_cast<hipStream_t>(stream), a);
+int launch_token_rows(TokenRowsArgs a, void* stream) {
+    const int lanes = a.d <= 64 ? 8 : a.d <= 128 ? 16 : 32, tokens = lanes == 32 ? 2 : 4, heads = lanes == 8 ? 2 : 1;
+    const int64_t groups = (a.tokens + tokens - 1) / tokens;
+    const int steps = (a.Hq + heads - 1) / heads + (a.k_out.data ? 1 : 2) * ((a.Hkv + heads - 1) / heads);
+    // waves for a group of tokens: steps of eight heads, fewer where that leaves compute units without work
+    const int64_t wanted = 8192 / (groups < 8192 ? groups : 8192), eighths = (steps + 7) / 8;
+    const int64_t splits = wanted > eighths ? wanted : eighths;
+    a.splits = static_cast<int>(splits < steps ? splits : steps);
+    a.by_splits = FastDiv::by(static_cast<uint32_t>(a.splits));
+    a.one_by_d = 1.f / static_cast<float>(a.d);
+    a.axes_by_four = 1;
+    for (int p = 0; p < a.pairs; ++p)
+        if (a.pair_axis[p] != a.pair_axis[p & ~3]) a.axes_by_four = 0;
+    const int64_t workgroups = (groups * a.splits + kWaves - 1) / kWaves;
+    if (workgroups * kWaves > 0x7FFFFFFF) return static_cast<int>(hipErrorInvalidConfiguration);
+    const dim3 grid(static_cast<unsigned>(workgroups));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (lanes == 8) launch_rows<8>(a, grid, st);
+    else if (lanes == 16) launch_rows<16>(a, grid, st);
+    else launch_rows<32>(a, grid, st);
     return static_cast<int>(hipGetLastError());
 }
 
-int launch_cache_read(const CacheReadArgs& a, void* stream) {
-    hipLaunchKernelGGL(cache_read_kernel, dim3(1024, static_cast<unsigned>(a.n)), dim3(64), 0, static_cast<hipStream_t>(stream), a);
+int launch_cache_read(CacheReadArgs a, void* stream) {
+    const int64_t units = a.rows / 64 + a.n;        // at most: requests have rows of their own
+    // the heads of a unit over several workgroups where there are few units
+    const int64_t splits = 2048 / (units < 2048 ? units : 2048);
+    a.splits = static_cast<int>(splits < a.cache.Hkv ? splits : a.cache.Hkv);
+    a.by_splits = FastDiv::by(static_cast<uint32_t>(a.splits));
+    if (units * a.splits > 0x7FFFFFFF) return static_cast<int>(hipErrorInvalidConfiguration);
+    const dim3 grid(static_cast<unsigned>(units * a.splits));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (a.cache.d == 128) { if (a.cache.f8) launch_read<128, true>(a, grid, st); else launch_read<128, false>(a, grid, st); }
+    else { if (a.cache.f8) launch_read<64, true>(a, grid, st); else launch_read<64, false>(a, grid, st); }
     return static_cast<int>(hipGetLastError());
 }
 
