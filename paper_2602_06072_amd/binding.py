@@ -449,21 +449,27 @@ def _need(ok, what):
         raise PackInferError(what)
 
 
+# (checks on the way of every call name what they refuse only where they refuse: a formatted message takes as long as the check)
 def _rows(x, name, heads=None, d=None):
     """pk_rows of a tensor [tokens, heads, d] (any strides, columns contiguous); None: a null pointer."""
     if x is None:
         return None
-    _need(x.dim() == 3 and (x.stride(2) == 1 or x.shape[2] == 1 or x.numel() == 0), f"{name} must be [tokens, heads, d] with contiguous columns")
-    _need(heads is None or tuple(x.shape[1:]) == (heads, d), f"{name} must have {heads} heads of {d} columns")
-    return _ROWS.pack(x.data_ptr(), x.stride(0), x.stride(1), _dtype_code(x))
+    shape = x.shape
+    if len(shape) != 3 or (heads is not None and (shape[1] != heads or shape[2] != d)):
+        raise PackInferError(f"{name} must be [tokens, heads, d]" + ("" if heads is None else f" with {heads} heads of {d} columns"))
+    ts, hs, cs = x.stride()
+    if cs != 1 and shape[2] != 1 and x.numel() != 0:
+        raise PackInferError(f"{name} must have contiguous columns")
+    code = _dtype_codes.get(x.dtype)
+    return _ROWS.pack(x.data_ptr(), ts, hs, _dtype_code(x) if code is None else code)
 
 
 def _vector(x, name, dtype, n=None):
     """Address of a contiguous tensor of the given type (and number of elements)."""
     if x is None:
         return None
-    _need(x.dtype == dtype and x.is_contiguous() and (n is None or x.numel() == n),
-          f"{name} must be contiguous, {dtype}" + ("" if n is None else f", {n} elements"))
+    if x.dtype != dtype or not x.is_contiguous() or (n is not None and x.numel() != n):
+        raise PackInferError(f"{name} must be contiguous, {dtype}" + ("" if n is None else f", {n} elements"))
     return x.data_ptr()
 
 

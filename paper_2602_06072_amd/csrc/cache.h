@@ -51,14 +51,13 @@ struct CacheKeepArgs {
 };
 int launch_cache_keep(const CacheKeepArgs& a, void* stream);
 
-// How a launch takes the rows of a (request, KV head): workgroups of row_groups * row_blocks * 16 rows, `chunks` of them; pieces of the
-// requests' keys, for each KV head and chunk `items` and one more a request at most, two partial results a piece at most.
+// How a launch takes the rows of a (request, KV head): `chunks` workgroups of up to `rows` of them for every piece of the request's keys; `items` workgroups of a
+// KV head run at once, `rounds` times as many are made of more requests than that.
 struct TreeShape {
-    int row_blocks, row_groups, chunks, items;
-    int rows() const { return 16 * row_blocks * row_groups; }
+    int rows, chunks, items, rounds;
     // both grow with n and max_q, so that a workspace serves every call of one head shape that is not larger than what it was made for
-    static size_t count_bytes(int64_t n, int Hkv, const TreeShape& s) { return static_cast<size_t>((n * Hkv * s.chunks * 4 + 255) / 256 * 256); }
-    static size_t partial_bytes(int Hkv, int d, int compute_units, const TreeShape& s);
+    size_t count_bytes(int64_t n, int Hkv) const { return static_cast<size_t>((n * Hkv * chunks * 4 + 255) / 256 * 256); }
+    size_t partial_bytes(int Hkv, int d, int compute_units) const;
     static TreeShape of(int max_q, int Hq, int Hkv, int compute_units);
 };
 
@@ -69,9 +68,9 @@ struct TreeArgs {
     const int32_t* kv_lens; int32_t n;
     void* out; int out_f32; float scale; int Hq;
     uint32_t* arrived;                              // [n][Hkv][chunks], zero between launches (arrival.h)
-    float* part_lse; float* part_o;                 // [slots][Hkv][chunks][rows], [..][d]
+    float* part_lse; float* part_o;                 // [slots][Hkv][rows], [..][d]
     // set by the launch
-    int heads_per_kv, subs, chunks, items, least_share;        // subs: sub-tiles of 16 keys in a page
+    int heads_per_kv, subs, rows_of_chunk, chunks, items, rounds, least_share;     // subs: sub-tiles of 16 keys in a page; least_share: tiles of a piece
     FastDiv by_r, by_subs;
 };
 int launch_tree_attn(TreeArgs a, const TreeShape& s, void* stream);

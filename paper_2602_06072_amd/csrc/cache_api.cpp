@@ -52,6 +52,7 @@ Refusal check_cache(const pk_cache* c) {
     if (c->d != 64 && c->d != 128) return {PK_EUNSUPPORTED, "the cache is built for d in {64, 128}"};
     if (c->page_size <= 0 || c->page_size % 16 != 0) return {PK_EUNSUPPORTED, "page_size must be a multiple of 16"};
     if (c->Hkv <= 0 || c->Hkv > 65535 || c->num_blocks <= 0 || c->num_blocks > kMostTokens) return {PK_EINVAL, "need 0 < Hkv < 65536 and 0 < num_blocks < 2^31"};
+    if (c->num_blocks * c->Hkv > kMostTokens / c->page_size) return {PK_EUNSUPPORTED, "a cache of 2^31 rows (num_blocks * Hkv * page_size) or more"};
     if (!c->k || !c->v || (c->dtype == PK_F8 && !c->scales)) return {PK_EINVAL, "k, v or scales of the cache is NULL"};
     if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->scales, 16)) return {PK_EINVAL, "k, v and scales of the cache must be 16-byte aligned"};
     return {PK_OK, ""};
@@ -138,17 +139,16 @@ bool tree_sizes_ok(const int64_t n, const int64_t max_q, const int64_t Hq, const
 
 TreeShape TreeShape::of(const int max_q, const int Hq, const int Hkv, const int compute_units) {
     const int rows = max_q * (Hq / Hkv);
-    TreeShape s{rows <= 16 ? 1 : 2, rows <= 32 ? 1 : rows <= 64 ? 2 : 4, 1, 0};
-    s.chunks = rows <= s.rows() ? 1 : (rows + s.rows() - 1) / s.rows();
-    const int heads = Hkv * s.chunks;
-    s.items = 2 * compute_units > heads ? 2 * compute_units / heads : 1;
+    TreeShape s{rows <= 16 ? 16 : rows <= 32 ? 32 : 128, 1, 0, rows <= 32 ? 4 : 2};
+    s.chunks = rows <= s.rows ? 1 : (rows + s.rows - 1) / s.rows;
+    s.items = 2 * compute_units > Hkv ? 2 * compute_units / Hkv : 1;       // (two workgroups of a compute unit)
     return s;
 }
 
-// a share of the keys is at least 1 / items of all of them, and only requests of more than a share are cut: 2 * items slots hold the pieces of all
-size_t TreeShape::partial_bytes(const int Hkv, const int d, const int compute_units, const TreeShape& s) {
-    const int64_t heads = static_cast<int64_t>(Hkv) * s.chunks, most = heads > 2 * compute_units ? heads : 2 * compute_units;
-    return static_cast<size_t>((2 * most * s.rows() * (d + 1) * 4 + 255) / 256 * 256);
+// A piece has at least 1 / (items * rounds) of all tiles, and only requests of more than that are cut: twice as many slots hold the pieces of all.
+size_t TreeShape::partial_bytes(const int Hkv, const int d, const int compute_units) const {
+    const int64_t most = Hkv > 2 * compute_units ? Hkv : 2 * compute_units;
+    return static_cast<size_t>((2 * most * rounds * rows * (d + 1) * 4 + 255) / 256 * 256);
 }
 
 extern "C" int pk_qk_norm_rope(const pk_rows* q, const pk_rows* k, const pk_rows* q_out, const pk_rows* k_out,
@@ -225,7 +225,7 @@ extern "C" size_t pk_tree_attn_workspace_bytes(int32_t n, int32_t max_q, int Hq,
         if (!tree_sizes_ok(n, max_q, Hq, Hkv, d)) return 0;
         const int cus = compute_units();
         const TreeShape s = TreeShape::of(max_q, Hq, Hkv, cus);
-        return TreeShape::count_bytes(n, Hkv, s) + TreeShape::partial_bytes(Hkv, d, cus, s);
+        return s.count_bytes(n, Hkv) + s.partial_bytes(Hkv, d, cus);
     });
 }
 
@@ -248,9 +248,9 @@ extern "C" int pk_tree_attn(const pk_cache* cache, const void* q, const int32_t*
         if (!workspace || !aligned(workspace, 256)) return refuse(who, {PK_EINVAL, "workspace is NULL or not 256-byte aligned"});
         const int cus = compute_units();
         const TreeShape shape = TreeShape::of(max_q, Hq, cache->Hkv, cus);
-        const size_t partial = TreeShape::partial_bytes(cache->Hkv, cache->d, cus, shape);
+        const size_t partial = shape.partial_bytes(cache->Hkv, cache->d, cus);
         workspace_bytes = workspace_bytes / 256 * 256;
-        if (workspace_bytes < TreeShape::count_bytes(n, cache->Hkv, shape) + partial)
+        if (workspace_bytes < shape.count_bytes(n, cache->Hkv) + partial)
             return refuse(who, {PK_EINVAL, "workspace smaller than pk_tree_attn_workspace_bytes"});
         TreeArgs a{};
         a.cache = view(*cache); a.block_table = block_table; a.max_blocks = max_blocks;

@@ -23,73 +23,90 @@ __device__ __forceinline__ float max_of_lane_groups(float x) {
     return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
 }
 
-// What a workgroup works on: a piece of the tiles of a request.
+// Sum over the wave, in every lane; sums of the lanes up to each one
+__device__ __forceinline__ int wave_prefix(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);         // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);        // row_bcast 15 into rows 1 and 3, 31 into rows 2 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+    return x;
+}
+__device__ __forceinline__ int last_lane(const int x) { return __builtin_amdgcn_readlane(x, 63); }
+
+// What a workgroup works on: a piece of the tiles of a request, for some of its rows (a chunk).
 struct Piece {
-    int request, piece, pieces, slot;               // slot: of the request's first partial result
+    int request, piece, pieces, chunk, slot;        // slot: of the piece's partial result; those of a chunk's pieces are `chunks` apart
+    int chunks;
 };
 
-// Tiles of TOKENS keys that a request's rows have to visit (0: it has no rows), and pieces they are cut into.  A request with rows and no key
-// has one piece, which writes zeros.
+// Tiles of TOKENS keys that a request has, and chunks of rows that visit them (0: no rows).  A request with rows and no key has one piece, which writes zeros.
+struct Load { int tiles, chunks; };
 template <int TOKENS>
-__device__ __forceinline__ int tiles_of(const TreeArgs& a, const int i) {
+__device__ __forceinline__ Load load_of(const TreeArgs& a, const int i) {
     const int64_t most = static_cast<int64_t>(a.max_blocks) * a.cache.page;
     const int len = static_cast<int>(min(static_cast<int64_t>(max(a.kv_lens[i], 0)), most));
-    return a.q_start[i + 1] > a.q_start[i] ? (len + TOKENS - 1) / TOKENS : -1;
+    const int rows = max(min(a.q_start[i + 1] - a.q_start[i], a.max_q), 0) * a.heads_per_kv;
+    return {(len + TOKENS - 1) / TOKENS, (rows + a.rows_of_chunk - 1) / a.rows_of_chunk};
 }
-__device__ __forceinline__ int pieces_of(const int tiles, const int share) { return tiles < 0 ? 0 : max(1, (tiles + share - 1) / share); }
+__device__ __forceinline__ int pieces_of(const int tiles, const int share) { return max(1, (tiles + share - 1) / share); }
 
-// The piece number `item` of the launch, found from the lengths by every workgroup itself (no table to be made on the host, none to be
-// copied when lengths change): tiles of all requests, the share of a piece that follows from them, prefix sums of pieces and slots.
+// The workgroup's piece, number `item` of the launch, found from the lengths by every wave itself: no table to be made on the host, none to be copied when
+// lengths change.  A piece has at most `share` tiles.  The share is the smallest of eight with which all pieces run at once (a second, partly filled round of
+// workgroups is as long as the first); where there are more requests than that, it is made small enough for several rounds to even out.
 template <int TOKENS>
-__device__ __forceinline__ bool find_piece(const TreeArgs& a, const int item, Piece& out) {
-    __shared__ int sums[3][kWaves];
-    __shared__ Piece found;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int each = (a.n + 64 * kWaves - 1) / (64 * kWaves), i0 = min(a.n, tid * each), i1 = min(a.n, i0 + each);
+__device__ __forceinline__ bool find_piece(const TreeArgs& a, const int item, int* counts, Piece& out) {
+    constexpr int STEPS = 8;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int total = 0;
-    for (int i = i0; i < i1; ++i) total += max(0, tiles_of<TOKENS>(a, i));
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
-    if (lane == 0) sums[0][wave] = total;
-    if (tid == 0) found.pieces = 0;
-    __syncthreads();
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) total += sums[0][w];
-    const int share = max(a.least_share, (total + a.items - 1) / a.items);
-    int mine = 0, slots = 0;
-    for (int i = i0; i < i1; ++i) {
-        const int k = pieces_of(tiles_of<TOKENS>(a, i), share);
-        mine += k;
-        slots += k > 1 ? k : 0;
+    for (int i = lane; i < a.n; i += 64) {
+        const Load w = load_of<TOKENS>(a, i);
+        total += w.tiles * w.chunks;
     }
-    int before = mine, slots_before = slots;
+    total = last_lane(wave_prefix(total));
+    const auto candidate = [&](const int x) {       // an even share of all tiles, and 1/8, 2/8, .. more
+        return max(a.least_share, static_cast<int>((static_cast<int64_t>(total) * (8 + x) + 8 * a.items - 1) / (8 * a.items)));
+    };
+    int fit[STEPS / kWaves] = {};
+    for (int i = lane; i < a.n; i += 64) {
+        const Load w = load_of<TOKENS>(a, i);
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int x = __shfl_up(before, o, 64), y = __shfl_up(slots_before, o, 64);
-        if (lane >= o) { before += x; slots_before += y; }
+        for (int x = 0; x < STEPS / kWaves; ++x) fit[x] += w.chunks * pieces_of(w.tiles, candidate(wave + kWaves * x));
     }
-    if (lane == 63) { sums[1][wave] = before; sums[2][wave] = slots_before; }
-    __syncthreads();
-    before -= mine;
-    slots_before -= slots;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w)
-        if (w < wave) { before += sums[1][w]; slots_before += sums[2][w]; }
-    if (item >= before && item < before + mine) {
-        for (int i = i0; i < i1; ++i) {
-            const int k = pieces_of(tiles_of<TOKENS>(a, i), share);
-            if (item < before + k) { found = {i, item - before, k, slots_before}; break; }
-            before += k;
-            slots_before += k > 1 ? k : 0;
+    for (int x = 0; x < STEPS / kWaves; ++x) {
+        const int all = last_lane(wave_prefix(fit[x]));
+        if (lane == 0) counts[wave + kWaves * x] = all;
+    }
+    __syncthreads();
+    int share = max(a.least_share, (total + a.items * a.rounds - 1) / (a.items * a.rounds));
+#pragma unroll
+    for (int x = STEPS - 1; x >= 0; --x)
+        if (counts[x] <= a.items) share = candidate(x);
+    int before = 0, slots = 0;
+    for (int i0 = 0; i0 < a.n; i0 += 64) {
+        const int i = min(i0 + lane, a.n - 1);
+        Load w = load_of<TOKENS>(a, i);
+        if (i0 + lane >= a.n) w.chunks = 0;
+        const int k = pieces_of(w.tiles, share), mine = k * w.chunks, upto = wave_prefix(mine), slots_upto = wave_prefix(k > 1 ? mine : 0);
+        const uint64_t here = __ballot(item >= before + upto - mine && item < before + upto);
+        if (here != 0) {
+            const int from = __builtin_ctzll(here);
+            const auto of = [&](const int x) { return __builtin_amdgcn_readlane(x, from); };
+            const int local = item - before - of(upto - mine);
+            out.request = i0 + from;
+            out.pieces = of(k);
+            out.chunks = of(w.chunks);
+            out.piece = local / out.chunks;
+            out.chunk = local - out.piece * out.chunks;
+            out.slot = slots + of(slots_upto - (k > 1 ? mine : 0)) + local;
+            return true;
         }
+        before += last_lane(upto);
+        slots += last_lane(slots_upto);
     }
-    __syncthreads();
-    out.request = __builtin_amdgcn_readfirstlane(found.request);
-    out.piece = __builtin_amdgcn_readfirstlane(found.piece);
-    out.pieces = __builtin_amdgcn_readfirstlane(found.pieces);
-    out.slot = __builtin_amdgcn_readfirstlane(found.slot);
-    return out.pieces > 0;
+    return false;
 }
 
 // K and V of a tile of N sub-tiles (16 keys each) as they are in memory
@@ -97,7 +114,7 @@ template <int D, bool F8, int N>
 struct TileRegs {
     static constexpr int CH = F8 ? D / 64 : D / 32;  // 16-byte chunks of a lane in a sub-tile
     u32x4 k[N][CH], v[N][CH];
-    uint32_t ks[N], vs[N];                          // scale byte of key 16u + lane % 16; of keys 16u + 4 (lane / 16) + 0..3
+    uint32_t ks[N], vs[N];                          // scale bytes of keys 16u + n..n + 3, n = lane % 16 & 12 (a byte would be widened, and waited for, where it is loaded); 16u + 4 (lane / 16)..
 };
 
 // 4 codes -> 4 bf16 values times `scale`
@@ -113,7 +130,7 @@ template <int D, bool F8, int N>
 __device__ __forceinline__ bf16x8 k_operand(const TileRegs<D, F8, N>& r, const int u, const int s) {
     if constexpr (F8) {
         const u32x4 x = r.k[u][s / 2];
-        const float scale = scale_value(r.ks[u]);
+        const float scale = scale_value(r.ks[u] >> 8 * (threadIdx.x & 3) & 0xFF);
         return s % 2 == 0 ? operand(widen(x[0], scale), widen(x[1], scale)) : operand(widen(x[2], scale), widen(x[3], scale));
     } else {
         return __builtin_bit_cast(bf16x8, r.k[u][s]);
@@ -152,11 +169,9 @@ __device__ __forceinline__ void store4(const TreeArgs& a, const int64_t at, cons
 // 1 / l; a row that saw nothing is zero, one whose sum is no number stays one
 __device__ __forceinline__ float inverse_sum(const float l) { return l > 0.f || l != l ? 1.f / l : 0.f; }
 
-// What is no finite number in a word of V (four codes, or two bf16 numbers): all ones in its place
-template <bool F8>
+// All ones in the place of the bf16 numbers of a word that are not finite
 __device__ __forceinline__ uint32_t not_finite(const uint32_t x) {
-    if constexpr (F8) return ((((x & 0x7F7F7F7Fu) + 0x01010101u) >> 7) & 0x01010101u) * 0xFFu;
-    else return ((x & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((x & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+    return ((x & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((x & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
 }
 
 // Which of the keys key .. key + 3 a row sees, bit by bit: those of the context, of the drafted tokens those in its mask word, none from len on.
@@ -168,85 +183,313 @@ __device__ __forceinline__ uint32_t seen_of_four(const uint64_t bits, const int 
     return (context | drafted) & ((1u << min(max(len - key, 0), 4)) - 1);
 }
 
-// One workgroup for (piece, KV head, rows): ROWGROUPS of its four waves take 16 NB rows each, the waves of a row group take tiles of N sub-tiles
-// in turns, two in flight for each.
-template <int D, bool F8, int NB, int ROWGROUPS, int N, int WAVES_PER_SIMD>
-__global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(TreeArgs a) {
-    using Regs = TileRegs<D, F8, N>;
-    constexpr int CH = Regs::CH, TOKENS = 16 * N, KS = D / 32, VT = D / 16, SIZE = F8 ? 1 : 2;
-    constexpr int SHARERS = kWaves / ROWGROUPS, ROWS = 16 * NB * ROWGROUPS, PITCH = D + 4;
-    __shared__ __align__(16) float po[kWaves][16][PITCH];
-    __shared__ float pm[kWaves][16], pl[kWaves][16];
-    __shared__ int last;
+// Where a workgroup's rows and keys are
+struct Bounds {
+    int64_t q0;                                     // first drafted token's row of q
+    int rows, row0, rows_here;                      // rows of the request for a KV head; first one of the chunk, and how many
+    int len, ctx, tiles, t0, t1;                    // keys; those in front of the drafted tokens (negative: some have no place); tiles, the piece's
+    const int32_t* table;
+};
+template <int TOKENS>
+__device__ __forceinline__ Bounds bounds_of(const TreeArgs& a, const Piece& w) {
+    Bounds b;
+    const int i = w.request, asked = a.q_start[i + 1] - a.q_start[i];
+    b.q0 = min(max(static_cast<int64_t>(a.q_start[i]), int64_t{0}), a.total_q);
+    b.rows = static_cast<int>(min(static_cast<int64_t>(min(asked, a.max_q)), a.total_q - b.q0)) * a.heads_per_kv;
+    b.row0 = w.chunk * a.rows_of_chunk;
+    b.rows_here = min(b.rows - b.row0, a.rows_of_chunk);
+    b.len = static_cast<int>(min(static_cast<int64_t>(max(a.kv_lens[i], 0)), static_cast<int64_t>(a.max_blocks) * a.cache.page));
+    b.ctx = a.kv_lens[i] - asked;
+    b.tiles = (b.len + TOKENS - 1) / TOKENS;
+    b.t0 = static_cast<int>(static_cast<int64_t>(b.tiles) * w.piece / w.pieces);
+    b.t1 = static_cast<int>(static_cast<int64_t>(b.tiles) * (w.piece + 1) / w.pieces);
+    b.table = a.block_table + static_cast<int64_t>(i) * a.max_blocks;
+    return b;
+}
 
+// Where the sub-tiles of 16 keys (each in one page) of a tile are, a lane for each: first row of K and V, first byte of the scales.  Asked for a turn of
+// the loop before the tile's own requests, and before those of a tile that is used earlier, so that nothing waits for it.
+template <int N>
+__device__ __forceinline__ int ask_places(const TreeArgs& a, const Bounds& b, const int tile, const int first) {
+    const int sub = tile * N + first + static_cast<int>(threadIdx.x & 15);
+    return b.table[a.by_subs(min(sub, (b.len - 1) / 16))];         // (the entry as it is)
+}
+struct SubTile {
+    __amdgpu_buffer_rsrc_t k, v, s;                 // buffers of K, V and scales; empty past the end of the piece (zeros, no traffic)
+};
+// In lane u: row of K and V where sub-tile `first + u` of the tile begins (-1: past the end of the piece), and byte of its scales
+struct Rows { int row; uint32_t scale; };
+template <int N>
+__device__ __forceinline__ Rows rows_of(const TreeArgs& a, const Bounds& b, const int kvh, const int tile, const int first, const int entry) {
     const CacheView& c = a.cache;
-    const int kvh = blockIdx.x % c.Hkv, rest = blockIdx.x / c.Hkv, chunk = rest % a.chunks;
-    Piece w;
-    if (!find_piece<TOKENS>(a, rest / a.chunks, w)) return;
-    const int i = w.request;
+    const int sub = tile * N + first + static_cast<int>(threadIdx.x & 15), last = (b.len - 1) / 16, in = min(sub, last);
+    const int block = min(max(entry, 0), static_cast<int>(c.num_blocks - 1)), off = (in - a.by_subs(in) * a.subs) * 16;
+    const int row = (block * c.Hkv + kvh) * c.page + off;          // (a cache has fewer than 2^31 rows)
+    return {tile < b.t1 && sub <= last ? row : -1, 2 * static_cast<uint32_t>(row) - static_cast<uint32_t>(off)};
+}
+template <int D, bool F8>
+__device__ __forceinline__ SubTile sub_tile(const TreeArgs& a, const Rows& r, const int u) {
+    constexpr int SIZE = F8 ? 1 : 2;
+    const CacheView& c = a.cache;
+    const int row = __builtin_amdgcn_readlane(r.row, u);
+    const bool there = row >= 0;
+    const auto resource = [&](const void* base, const uint64_t byte, const int bytes) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(static_cast<const unsigned char*>(base) + byte), 0, there ? bytes : 0, 0x00020000);
+    };
+    const uint64_t at = static_cast<uint64_t>(static_cast<uint32_t>(there ? row : 0)) * (D * SIZE);
+    SubTile t;
+    t.k = resource(c.k, at, 16 * D * SIZE);
+    t.v = resource(c.v, at, 16 * D * SIZE);
+    if constexpr (F8) t.s = resource(c.scales, there ? static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(r.scale), u)) : 0u, c.page + 16);
+    return t;
+}
+__device__ __forceinline__ u32x4 load16(const __amdgpu_buffer_rsrc_t r, const int lane, const int at) {
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, lane, at, kNonTemporalLoad));
+}
+
+// What a wave has of 16 NB rows: lane (n, g) holds columns of row 16 b + n
+template <int D, int NB>
+struct Sums {
+    floatx4 o[NB][D / 16], l[NB];                   // sum of p v, relative to m; sum of p in every element
+    float m[NB];                                    // maximum of the scores (exponents of two)
+    __device__ __forceinline__ Sums() {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            m[b] = -INFINITY; l[b] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int t = 0; t < D / 16; ++t) o[b][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+};
+template <int D, int NB>
+struct Queries {
+    bf16x8 q[NB][D / 32];
+    uint64_t bits[NB];
+};
+template <int D, bool F8, int NB>
+__device__ __forceinline__ void load_queries(const TreeArgs& a, const Bounds& w, const int kvh, const int first_row, Queries<D, NB>& y) {
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {                  // rows beyond the last repeat it and are not stored
+        const int row = min(first_row + 16 * b + n, w.rows - 1), t = a.by_r(row), h = row - t * a.heads_per_kv;
+        const uint16_t* q = static_cast<const uint16_t*>(a.q) + ((w.q0 + t) * a.Hq + kvh * a.heads_per_kv + h) * D;
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) y.q[b][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(q + k_column<D, F8>(s, g)));
+        y.bits[b] = a.mask ? a.mask[w.q0 + t] : ~uint64_t{0} >> (63 - t);
+    }
+}
+
+// Probabilities of 16 N keys against a row, from their raw scores; what is summed up so far is brought to the new maximum.
+// `hidden`: bit x for key x that the row does not see (looked at with EDGE).
+template <int D, int N, bool EDGE>
+__device__ __forceinline__ void probabilities(const floatx4 (&s)[N], const uint32_t hidden, const float sl2, floatx4 (&o)[D / 16], floatx4& l, float& m, float (&p)[4 * N]) {
+#pragma unroll
+    for (int x = 0; x < 4 * N; ++x) p[x] = !EDGE || !(hidden >> x & 1) ? s[x / 4][x % 4] : -INFINITY;
+    float mx = p[0];
+#pragma unroll
+    for (int x = 1; x < 4 * N; ++x) mx = fmaxf(mx, p[x]);
+    const float m_new = fmaxf(m, max_of_lane_groups(mx) * sl2);
+    const float m_use = m_new == -INFINITY ? 0.f : m_new;
+    if (__any(m_new != m)) {
+        const float alpha = __builtin_amdgcn_exp2f(m - m_use);
+        l *= alpha;
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t) o[t] *= alpha;
+        m = m_new;
+    }
+#pragma unroll
+    for (int x = 0; x < 4 * N; ++x) p[x] = __builtin_amdgcn_exp2f(fmaf(p[x], sl2, -m_use));
+}
+
+// The product of a block of V columns with the probabilities of 32 keys, of which some rows do not see some: a probability of zero does not hide what is no
+// finite number in V, so such values leave the operand and come back for the rows that see them (how many of each kind).
+template <int NB, int D, int XN>
+__device__ __forceinline__ void product_with_hidden(const bf16x8 v, const uint32_t (&hidden)[NB], const int x, const bf16x8 (&pf)[NB][XN], Sums<D, NB>& y, const int t) {
+    const u32x4 words = __builtin_bit_cast(u32x4, v);
+    u32x4 clean;
+    uint32_t any = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t odd = not_finite(words[e]);
+        clean[e] = words[e] & ~odd;
+        any |= odd;
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) y.o[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, clean), pf[b][x], y.o[b][t], 0, 0, 0);
+    if (!__any(any != 0)) return;
+    for (int kind = 0; kind < 3; ++kind) {
+        const auto is = [&](const uint32_t half) { return kind == 0 ? (half & 0x7FFFu) > 0x7F80u : half == (kind == 1 ? 0x7F80u : 0xFF80u); };
+        u32x4 of_kind;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) of_kind[e] = (is(words[e] & 0xFFFFu) ? 0x3F80u : 0u) | (is(words[e] >> 16) ? 0x3F800000u : 0u);
+        const float value = kind == 0 ? __uint_as_float(0x7FC00000u) : kind == 1 ? INFINITY : -INFINITY;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            u32x4 seen;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) seen[e] = (hidden[b] >> (8 * x + 2 * e) & 1 ? 0u : 0x3F80u) | (hidden[b] >> (8 * x + 2 * e + 1) & 1 ? 0u : 0x3F800000u);
+            const floatx4 count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, of_kind), __builtin_bit_cast(bf16x8, seen), floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y.o[b][t][e] += count[e] > 0.f ? value : 0.f;
+        }
+    }
+}
+
+// Results of a workgroup: those of the `sharers` waves of a row group are put together in LDS and written; where the request has other pieces they are
+// partial results, and the workgroup that finishes last puts those together, in their order whichever it is.
+template <int D> constexpr int kPitch = D + 4;
+template <int D> constexpr int kJoinBytes = kWaves * 16 * (kPitch<D> + 2) * 4;
+template <int D, bool F8, int NB>
+__device__ __forceinline__ void finish(const TreeArgs& a, const Piece& w, const Bounds& bounds, const int kvh, const int row_groups, const int sharers, const Sums<D, NB>& y, unsigned char* lds, int* last) {
+    constexpr int CH = F8 ? D / 64 : D / 32, PITCH = kPitch<D>;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6)), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-    const int rowgroup = wave / SHARERS, sharer = wave % SHARERS;
-
-    const int64_t q0 = min(max(static_cast<int64_t>(a.q_start[i]), int64_t{0}), a.total_q);
-    const int asked = a.q_start[i + 1] - a.q_start[i];
-    const int rows = static_cast<int>(min(static_cast<int64_t>(min(asked, a.max_q)), a.total_q - q0)) * a.heads_per_kv, row0 = chunk * ROWS;
-    if (row0 >= rows) return;                       // (all pieces of the request alike)
-    const int len = static_cast<int>(min(static_cast<int64_t>(max(a.kv_lens[i], 0)), static_cast<int64_t>(a.max_blocks) * c.page));
-    const int ctx = a.kv_lens[i] - asked;           // (negative: some drafted tokens have no place)
-    const int tiles = (len + TOKENS - 1) / TOKENS;
-    const int t0 = static_cast<int>(static_cast<int64_t>(tiles) * w.piece / w.pieces), t1 = static_cast<int>(static_cast<int64_t>(tiles) * (w.piece + 1) / w.pieces);
-    const auto* table = reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(a.block_table + static_cast<int64_t>(i) * a.max_blocks));
-
-    floatx4 o[NB][VT], l[NB];                       // sum of p v, relative to m; sum of p in every element
-    float m[NB];
+    float* po = reinterpret_cast<float*>(lds);      // [wave][16][PITCH]
+    float* pm = po + kWaves * 16 * PITCH;           // [wave][16]
+    float* pl = pm + kWaves * 16;
+    const auto part_row = [&](const int piece) { return (static_cast<int64_t>(w.slot + (piece - w.piece) * w.chunks) * a.cache.Hkv + kvh) * a.rows_of_chunk; };
+    const auto out_at = [&](const int local, const int col) {
+        const int row = bounds.row0 + local, t = a.by_r(row);
+        return ((bounds.q0 + t) * a.Hq + kvh * a.heads_per_kv + row - t * a.heads_per_kv) * D + col;
+    };
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-        m[b] = -INFINITY; l[b] = floatx4{0.f, 0.f, 0.f, 0.f};
+        __syncthreads();
+        float* mine = po + (wave * 16 + n) * PITCH;
 #pragma unroll
-        for (int t = 0; t < VT; ++t) o[b][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int x = 0; x < CH; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (F8) *reinterpret_cast<floatx4*>(mine + 64 * x + 16 * g + 4 * e) = floatx4{y.o[b][4 * x][e], y.o[b][4 * x + 1][e], y.o[b][4 * x + 2][e], y.o[b][4 * x + 3][e]};
+                else *reinterpret_cast<floatx2*>(mine + 32 * x + 8 * g + 2 * e) = floatx2{y.o[b][2 * x][e], y.o[b][2 * x + 1][e]};
+            }
+        if (g == 0) { pm[wave * 16 + n] = y.m[b]; pl[wave * 16 + n] = y.l[b][0]; }
+        __syncthreads();
+        for (int x = threadIdx.x; x < row_groups * 16 * (D / 4); x += 64 * kWaves) {
+            const int of = x / (16 * (D / 4)), rn = x / (D / 4) % 16, col = 4 * (x % (D / 4)), local = (of * NB + b) * 16 + rn;
+            if (local >= bounds.rows_here) continue;
+            const int from = of * sharers * 16 + rn;
+            float top = -INFINITY;
+            for (int z = 0; z < sharers; ++z) top = fmaxf(top, pm[from + 16 * z]);
+            const float use = top == -INFINITY ? 0.f : top;
+            float sum = 0.f;
+            floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+            for (int z = 0; z < sharers; ++z) {
+                const float f = __builtin_amdgcn_exp2f(pm[from + 16 * z] - use);
+                const floatx4 v = *reinterpret_cast<const floatx4*>(po + (from + 16 * z) * PITCH + col);
+                sum = fmaf(f, pl[from + 16 * z], sum);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] = fmaf(f, v[e], acc[e]);
+            }
+            acc *= inverse_sum(sum);
+            if (w.pieces == 1) {
+                store4(a, out_at(local, col), acc);
+            } else {
+                const int64_t at = part_row(w.piece) + local;
+                publish4(a.part_o + at * D + col, acc);
+                if (col == 0) __hip_atomic_store(a.part_lse + at, sum > 0.f || sum != sum ? top + __builtin_amdgcn_logf(sum) : -INFINITY, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+        }
     }
+    if (w.pieces == 1) return;
+    // (decode_body.hip.h on the order of the stores and the count)
+    __builtin_amdgcn_s_waitcnt(0x0F70);            // vmcnt(0): this wave's partial results are in memory
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const int64_t group = (static_cast<int64_t>(w.request) * a.cache.Hkv + kvh) * a.chunks + w.chunk;
+        *last = arrives_last(TreeCount{a.arrived + group}, static_cast<uint32_t>(w.pieces));
+    }
+    __syncthreads();
+    if (*last == 0) return;
+    constexpr int BATCH = 4;
+    for (int x = threadIdx.x; x < bounds.rows_here * (D / 4); x += 64 * kWaves) {
+        const int local = x / (D / 4), col = 4 * (x % (D / 4));
+        float top = -INFINITY, sum = 0.f;
+        floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int p = 0; p < w.pieces; p += BATCH) {
+            float lse[BATCH];
+            floatx4 v[BATCH];
+#pragma unroll
+            for (int z = 0; z < BATCH; ++z) {
+                const int64_t at = part_row(min(p + z, w.pieces - 1)) + local;
+                lse[z] = __hip_atomic_load(a.part_lse + at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                v[z] = read_published4(a.part_o + at * D + col);
+            }
+            float top_new = top;
+#pragma unroll
+            for (int z = 0; z < BATCH; ++z) {
+                if (p + z >= w.pieces) { lse[z] = -INFINITY; v[z] = floatx4{0.f, 0.f, 0.f, 0.f}; }
+                top_new = fmaxf(top_new, lse[z]);
+            }
+            const float use = top_new == -INFINITY ? 0.f : top_new;
+            const float alpha = __builtin_amdgcn_exp2f(top - use);
+            sum *= alpha;
+            acc *= alpha;
+#pragma unroll
+            for (int z = 0; z < BATCH; ++z) {
+                const float f = __builtin_amdgcn_exp2f(lse[z] - use);
+                sum += f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] = fmaf(f, v[z][e], acc[e]);
+            }
+            top = top_new;
+        }
+        store4(a, out_at(local, col), acc * inverse_sum(sum));
+    }
+}
 
-    const int first_row = row0 + rowgroup * 16 * NB;
-    if (first_row < rows && t0 + sharer < t1) {
-        const int last_sub = (len - 1) / 16;
-        auto load = [&](Regs& r, const int tile) {
+// Up to 16 NB rows: bound by memory.  The four waves of a workgroup take tiles of N sub-tiles in turns, SETS tiles in flight in each, from memory into
+// registers and from there into the products.
+template <int D, bool F8, int NB, int N, int SETS, int WAVES_PER_SIMD>
+__global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(TreeArgs a) {
+    static_assert(SETS == 2 || SETS == 3, "sets");
+    using Regs = TileRegs<D, F8, N>;
+    constexpr int CH = Regs::CH, TOKENS = 16 * N, KS = D / 32, VT = D / 16, SIZE = F8 ? 1 : 2;
+    __shared__ __align__(16) unsigned char lds[kJoinBytes<D>];
+    __shared__ int counts[8], last;
+
+    const int kvh = blockIdx.x % a.cache.Hkv;
+    Piece w;
+    if (!find_piece<TOKENS>(a, blockIdx.x / a.cache.Hkv, counts, w)) return;
+    const Bounds bounds = bounds_of<TOKENS>(a, w);
+    if (bounds.rows_here <= 0) return;              // (total_q says so; all pieces of the request alike)
+    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6)), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int len = bounds.len, ctx = bounds.ctx, t1 = bounds.t1;
+
+    Sums<D, NB> y;
+    int tile = bounds.t0 + wave;
+    if (tile < t1) {
+        // requests a tile, whose places are known, and the places of the set's tile after that
+        auto load = [&](Regs& r, int& places, const int tile) {
+            const Rows rows = rows_of<N>(a, bounds, kvh, tile, 0, places);
+            places = ask_places<N>(a, bounds, tile + SETS * kWaves, 0);
 #pragma unroll
             for (int u = 0; u < N; ++u) {
-                const int sub = min(tile * N + u, last_sub);
-                const bool there = tile < t1 && tile * N + u <= last_sub;
-                const int page = a.by_subs(sub), off = (sub - page * a.subs) * 16;
-                const int block = min(max(static_cast<int>(table[page]), 0), static_cast<int>(c.num_blocks - 1));
-                const int64_t at = (static_cast<int64_t>(block) * c.Hkv + kvh) * c.page;
-                const auto resource = [&](const void* base, const int64_t byte, const int bytes) {
-                    return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(static_cast<const unsigned char*>(base) + byte), 0, there ? bytes : 0, 0x00020000);
-                };
-                const auto rk = resource(c.k, (at + off) * D * SIZE, 16 * D * SIZE), rv = resource(c.v, (at + off) * D * SIZE, 16 * D * SIZE);
+                const SubTile t = sub_tile<D, F8>(a, rows, u);
 #pragma unroll
-                for (int x = 0; x < CH; ++x) r.k[u][x] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, n * D * SIZE + 16 * g, 64 * x, kNonTemporalLoad));
+                for (int x = 0; x < CH; ++x) r.k[u][x] = load16(t.k, n * D * SIZE + 16 * g, 64 * x);
 #pragma unroll
-                for (int x = 0; x < CH; ++x) r.v[u][x] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, g * 4 * D * SIZE + 16 * n, 256 * x, kNonTemporalLoad));
+                for (int x = 0; x < CH; ++x) r.v[u][x] = load16(t.v, g * 4 * D * SIZE + 16 * n, 256 * x);
                 if constexpr (F8) {
-                    const auto rs = resource(c.scales, 2 * at + off, c.page + 16);
-                    r.ks[u] = __builtin_amdgcn_raw_buffer_load_b8(rs, n, 0, 0);
-                    r.vs[u] = __builtin_amdgcn_raw_buffer_load_b32(rs, 4 * g, c.page, 0);
+                    r.ks[u] = __builtin_amdgcn_raw_buffer_load_b32(t.s, n & 12, 0, 0);
+                    r.vs[u] = __builtin_amdgcn_raw_buffer_load_b32(t.s, 4 * g, a.cache.page, 0);
                 }
             }
         };
-        Regs r0, r1;
-        load(r0, t0 + sharer);
-        load(r1, t0 + sharer + SHARERS);
-
-        // rows of this lane's columns; rows beyond the last repeat it and are not stored
-        bf16x8 qf[NB][KS];
-        uint64_t bits[NB];
+        Regs r[SETS];
+        int places[SETS];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const int row = min(first_row + 16 * b + n, rows - 1), t = a.by_r(row), h = row - t * a.heads_per_kv;
-            const uint16_t* q = static_cast<const uint16_t*>(a.q) + ((q0 + t) * a.Hq + kvh * a.heads_per_kv + h) * D;
+        for (int s = 0; s < SETS; ++s) places[s] = ask_places<N>(a, bounds, tile + s * kWaves, 0);
+        load(r[0], places[0], tile);
+        Queries<D, NB> q;
+        load_queries<D, F8, NB>(a, bounds, kvh, bounds.row0, q);
+        // The rows are waited for here, with the first tile; left to the loop, its first products wait for all tiles in flight in every turn.
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int s = 0; s < KS; ++s) qf[b][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(q + k_column<D, F8>(s, g)));
-            bits[b] = a.mask ? a.mask[q0 + t] : ~uint64_t{0} >> (63 - t);
-        }
+        for (int s = 1; s < SETS; ++s) load(r[s], places[s], tile + s * kWaves);
+        __builtin_amdgcn_sched_barrier(0);
+        constexpr int OTHERS = (SETS - 1) * (N * (2 * CH + (F8 ? 2 : 0)) + 1);
+        static_assert(OTHERS < 64, "vmcnt");
+        __builtin_amdgcn_s_waitcnt(0x0F70 | (OTHERS & 0xF) | (OTHERS >> 4 << 14));
         const float sl2 = a.scale * kLog2e;
 
         // `edge`: some key of the tile is not seen by some row
@@ -261,41 +504,26 @@ __global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(
                 for (int k = 0; k < KS; ++k) {
                     const bf16x8 x = k_operand<D, F8, N>(r, u, k);
 #pragma unroll
-                    for (int b = 0; b < NB; ++b) s[b][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, qf[b][k], s[b][u], 0, 0, 0);
+                    for (int b = 0; b < NB; ++b) s[b][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q.q[b][k], s[b][u], 0, 0, 0);
                 }
                 if constexpr (F8) __builtin_amdgcn_sched_barrier(0);       // (bf16 copies of a sub-tile at a time: they are twice its size)
             }
             // lane (n, g) holds scores of its rows against keys TOKENS * tile + 16 u + 4 g + e
             const int key0 = tile * TOKENS + 4 * g;
-            uint32_t hidden[NB];                                   // keys that this lane's row does not see, bit 4 u + e
-            bool strange = false;                                  // V has something that is no finite number
+            uint32_t hidden[NB] = {};                              // keys that this lane's row does not see, bit 4 u + e
             if constexpr (EDGE) {
 #pragma unroll
                 for (int b = 0; b < NB; ++b) {
                     uint32_t seen = 0;
 #pragma unroll
-                    for (int u = 0; u < N; ++u) seen |= seen_of_four(bits[b], key0 + 16 * u, ctx, len) << 4 * u;
+                    for (int u = 0; u < N; ++u) seen |= seen_of_four(q.bits[b], key0 + 16 * u, ctx, len) << 4 * u;
                     hidden[b] = ~seen;
                 }
-                // A probability of zero does not hide what is no number: such values leave V here and come back below for the rows that see them.
-                uint32_t any = 0;
+                if constexpr (F8) {                                // a scale where there is no key may be anything
 #pragma unroll
-                for (int u = 0; u < N; ++u) {
-                    if constexpr (F8) {                            // a scale where there is no key may be anything
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (key0 + 16 * u + e >= len) r.vs[u] = (r.vs[u] & ~(0xFFu << 8 * e)) | 127u << 8 * e;
-                    }
-#pragma unroll
-                    for (int x = 0; x < CH; ++x)
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) {
-                            const uint32_t odd = not_finite<F8>(r.v[u][x][y]);
-                            r.v[u][x][y] &= ~odd;
-                            any |= odd;
-                        }
+                    for (int x = 0; x < 4 * N; ++x)
+                        if (key0 + 16 * (x / 4) + x % 4 >= len) r.vs[x / 4] = (r.vs[x / 4] & ~(0xFFu << 8 * (x % 4))) | 127u << 8 * (x % 4);
                 }
-                strange = __any(any != 0);
             }
             float factor[F8 ? N : 1][4];
             if constexpr (F8) {
@@ -308,33 +536,14 @@ __global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                float raw[4 * N];
-#pragma unroll
-                for (int x = 0; x < 4 * N; ++x) raw[x] = !EDGE || !(hidden[b] >> x & 1) ? s[b][x / 4][x % 4] : -INFINITY;
-                float mx = raw[0];
-#pragma unroll
-                for (int x = 1; x < 4 * N; ++x) mx = fmaxf(mx, raw[x]);
-                const float m_new = fmaxf(m[b], max_of_lane_groups(mx) * sl2);
-                const float m_use = m_new == -INFINITY ? 0.f : m_new;
-                if (__any(m_new != m[b])) {
-                    const float alpha = __builtin_amdgcn_exp2f(m[b] - m_use);
-                    l[b] *= alpha;
-#pragma unroll
-                    for (int t = 0; t < VT; ++t) o[b][t] *= alpha;
-                    m[b] = m_new;
-                }
+                float p[4 * N];
+                probabilities<D, N, EDGE>(s[b], hidden[b], sl2, y.o[b], y.l[b], y.m[b], p);
                 uint32_t pw[2 * N];
 #pragma unroll
-                for (int u = 0; u < N; ++u) {
-                    float p[4];
+                for (int x = 0; x < 4 * N; ++x)
+                    if constexpr (F8) p[x] *= factor[x / 4][x % 4];        // the scale of V, a power of two: it rounds nothing
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        p[e] = __builtin_amdgcn_exp2f(fmaf(raw[4 * u + e], sl2, -m_use));
-                        if constexpr (F8) p[e] *= factor[u][e];    // the scale of V, a power of two: it rounds nothing
-                    }
-                    pw[2 * u] = pack_bf16x2(p[0], p[1]);
-                    pw[2 * u + 1] = pack_bf16x2(p[2], p[3]);
-                }
+                for (int x = 0; x < 2 * N; ++x) pw[x] = pack_bf16x2(p[2 * x], p[2 * x + 1]);
 #pragma unroll
                 for (int x = 0; x < N / 2; ++x) pf[b][x] = __builtin_bit_cast(bf16x8, u32x4{pw[4 * x], pw[4 * x + 1], pw[4 * x + 2], pw[4 * x + 3]});
             }
@@ -350,178 +559,245 @@ __global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(
                     }
                 }
 #pragma unroll
-                for (int b = 0; b < NB; ++b) l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones), pf[b][x], l[b], 0, 0, 0);
+                for (int b = 0; b < NB; ++b) y.l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones), pf[b][x], y.l[b], 0, 0, 0);
 #pragma unroll
                 for (int t = 0; t < VT; ++t) {
                     const bf16x8 v = v_operand<D, F8, N>(r, x, t);
+                    if constexpr (EDGE) product_with_hidden<NB, D, N / 2>(v, hidden, x, pf, y, t);
+                    else {
 #pragma unroll
-                    for (int b = 0; b < NB; ++b) o[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[b][x], o[b][t], 0, 0, 0);
-                    if (F8 && t % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-                }
-            }
-            if constexpr (EDGE) {
-                if (strange) {                                     // how many such values of each kind a row sees in a column
-                    load(r, tile);                                 // (it is gone from the registers)
-                    Regs of_kind;
-                    for (int kind = 0; kind < (F8 ? 1 : 3); ++kind) {
-#pragma unroll
-                        for (int u = 0; u < N; ++u)
-#pragma unroll
-                            for (int x = 0; x < CH; ++x)
-#pragma unroll
-                                for (int y = 0; y < 4; ++y) {
-                                    const uint32_t v = r.v[u][x][y];
-                                    if constexpr (F8) {
-                                        of_kind.v[u][x][y] = ((((v & 0x7F7F7F7Fu) + 0x01010101u) >> 7) & 0x01010101u) * 0x38u;       // 0x38: one
-                                    } else {
-                                        const auto is = [&](const uint32_t half) { return kind == 0 ? (half & 0x7FFFu) > 0x7F80u : half == (kind == 1 ? 0x7F80u : 0xFF80u); };
-                                        of_kind.v[u][x][y] = (is(v & 0xFFFFu) ? 0x3F80u : 0u) | (is(v >> 16) ? 0x3F800000u : 0u);
-                                    }
-                                }
-                        const float value = kind == 0 ? __uint_as_float(0x7FC00000u) : kind == 1 ? INFINITY : -INFINITY;
-#pragma unroll
-                        for (int b = 0; b < NB; ++b) {
-                            bf16x8 seen[N / 2];
-#pragma unroll
-                            for (int x = 0; x < N / 2; ++x) {
-                                u32x4 one;
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) one[e] = (hidden[b] >> (8 * x + 2 * e) & 1 ? 0u : 0x3F80u) | (hidden[b] >> (8 * x + 2 * e + 1) & 1 ? 0u : 0x3F800000u);
-                                seen[x] = __builtin_bit_cast(bf16x8, one);
-                            }
-#pragma unroll
-                            for (int t = 0; t < VT; ++t) {
-                                floatx4 count = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                                for (int x = 0; x < N / 2; ++x) count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_operand<D, F8, N>(of_kind, x, t), seen[x], count, 0, 0, 0);
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) o[b][t][e] += count[e] > 0.f ? value : 0.f;
-                            }
-                        }
+                        for (int b = 0; b < NB; ++b) y.o[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[b][x], y.o[b][t], 0, 0, 0);
                     }
+                    if (F8 && t % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                 }
             }
         };
         // Tiles that every row sees whole, then the others (a tile or two of a request: the drafted tokens, the end), whose code needs the
         // registers of the second set.  Requests past the last tile have empty descriptors: behind a condition the compiler would wait for all of them.
         const int whole = min(max(min(ctx, len), 0) / TOKENS, t1);
-        int tile = t0 + sharer;
-        while (tile < whole) {
-            step(r0, tile, std::false_type{});
-            load(r0, tile + 2 * SHARERS);
-            tile += SHARERS;
-            if (tile >= whole) { r0 = r1; break; }
-            step(r1, tile, std::false_type{});
-            load(r1, tile + 2 * SHARERS);
-            tile += SHARERS;
+        const auto turn = [&](Regs& x, int& at) {
+            step(x, tile, std::false_type{});
+            load(x, at, tile + SETS * kWaves);
+            tile += kWaves;
+        };
+        for (;;) {                                                 // (left by jumps: a flag to leave by keeps all sets alive)
+            if (tile >= whole) goto others;
+            turn(r[0], places[0]);
+            if (tile >= whole) { r[0] = r[1]; goto others; }
+            turn(r[1], places[1]);
+            if constexpr (SETS == 3) {
+                if (tile >= whole) { r[0] = r[2]; goto others; }
+                turn(r[2], places[2]);
+            }
         }
+    others:
         while (tile < t1) {
-            step(r0, tile, std::true_type{});
-            tile += SHARERS;
-            load(r0, tile);
+            step(r[0], tile, std::true_type{});
+            tile += kWaves;
+            places[0] = ask_places<N>(a, bounds, tile, 0);
+            load(r[0], places[0], tile);
         }
     }
+    finish<D, F8, NB>(a, w, bounds, kvh, 1, kWaves, y, lds, &last);
+}
 
-    const int64_t group = (static_cast<int64_t>(i) * c.Hkv + kvh) * a.chunks + chunk;
-    const auto part_row = [&](const int piece) { return (static_cast<int64_t>(w.slot + piece) * c.Hkv + kvh) * a.chunks * ROWS + static_cast<int64_t>(chunk) * ROWS; };
-    const auto out_at = [&](const int row, const int col) {
-        const int t = a.by_r(row);
-        return ((q0 + t) * a.Hq + kvh * a.heads_per_kv + row - t * a.heads_per_kv) * D + col;
+// 4 codes of four tokens -> bf16 values times each one's scale
+__device__ __forceinline__ uint2 widen_each(const uint32_t x, const float (&s)[4]) {
+    const auto two = [&](auto high, const float p, const float q) {
+        constexpr bool HIGH = decltype(high)::value;
+        return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, q, HIGH)),
+                                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, p, HIGH)), 0x07060100u);
     };
-    const int rows_here = min(rows - row0, ROWS);
+    return make_uint2(two(std::false_type{}, s[0], s[1]), two(std::true_type{}, s[2], s[3]));
+}
+
+// More rows, 128 in a workgroup: bound by the matrix pipe and by what surrounds it.  The workgroup's waves bring a tile of 64 keys into LDS together, a
+// quarter each, as bf16 operands (the conversion is done once, not by every wave), two tiles at a time; every wave reads it for its 32 rows.  With 64 rows
+// and fewer two waves share 32 rows, half of a tile's keys each.
+constexpr int kWideRows = 128;
+template <int D, bool F8>
+__global__ __launch_bounds__(64 * kWaves, 2) void tree_attn_wide_kernel(TreeArgs a) {
+    constexpr int NB = 2, N = 4, TOKENS = 64, KS = D / 32, VT = D / 16, CH = F8 ? D / 64 : D / 32, SIZE = F8 ? 1 : 2;
+    constexpr int K_BYTES = N * KS * 1024, STAGE = 2 * K_BYTES;
+    __shared__ __align__(16) unsigned char lds[2 * STAGE > kJoinBytes<D> ? 2 * STAGE : kJoinBytes<D>];
+    __shared__ int counts[8], last;
+
+    const int kvh = blockIdx.x % a.cache.Hkv;
+    Piece w;
+    if (!find_piece<TOKENS>(a, blockIdx.x / a.cache.Hkv, counts, w)) return;
+    const Bounds bounds = bounds_of<TOKENS>(a, w);
+    if (bounds.rows_here <= 0) return;
+    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6)), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int len = bounds.len, ctx = bounds.ctx, t0 = bounds.t0, t1 = bounds.t1;
+    const int sharers = bounds.rows_here <= 64 ? 2 : 1, row_group = wave / sharers, half = wave % sharers;
+    const bool works = row_group * 32 < bounds.rows_here;
+
+    Sums<D, NB> y;
+    if (t0 < t1) {
+        // this wave's quarter of a tile: K or V of two sub-tiles
+        struct Quarter { u32x4 c[2][CH]; uint32_t s[2]; };
+        const int of_v = wave & 1, pair = wave >> 1;
+        const int lane_at = of_v ? g * 4 * D * SIZE + 16 * n : n * D * SIZE + 16 * g, chunk_at = of_v ? 256 : 64;
+        const int scale_lane = of_v ? 4 * g : n & 12, scale_at = of_v ? a.cache.page : 0;
+        auto load = [&](Quarter& r, int& places, const int tile) {
+            const Rows rows = rows_of<N>(a, bounds, kvh, tile, 2 * pair, places);
+            places = ask_places<N>(a, bounds, tile + 2, 2 * pair);
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        if (b > 0) __syncthreads();
+            for (int u = 0; u < 2; ++u) {
+                const SubTile t = sub_tile<D, F8>(a, rows, u);
 #pragma unroll
-        for (int x = 0; x < CH; ++x)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if constexpr (F8) *reinterpret_cast<floatx4*>(&po[wave][n][64 * x + 16 * g + 4 * e]) = floatx4{o[b][4 * x][e], o[b][4 * x + 1][e], o[b][4 * x + 2][e], o[b][4 * x + 3][e]};
-                else *reinterpret_cast<floatx2*>(&po[wave][n][32 * x + 8 * g + 2 * e]) = floatx2{o[b][2 * x][e], o[b][2 * x + 1][e]};
+                for (int x = 0; x < CH; ++x) r.c[u][x] = load16(of_v ? t.v : t.k, lane_at, chunk_at * x);
+                if constexpr (F8) r.s[u] = __builtin_amdgcn_raw_buffer_load_b32(t.s, scale_lane, scale_at, 0);
             }
-        if (g == 0) { pm[wave][n] = m[b]; pl[wave][n] = l[b][0]; }
-        __syncthreads();
-        for (int x = threadIdx.x; x < ROWGROUPS * 16 * (D / 4); x += 64 * kWaves) {
-            const int of = x / (16 * (D / 4)), rn = x / (D / 4) % 16, col = 4 * (x % (D / 4)), local = (of * NB + b) * 16 + rn;
-            if (local >= rows_here) continue;
-            float top = pm[of * SHARERS][rn];
+        };
+        const int whole = min(max(min(ctx, len), 0) / TOKENS, t1);
+        auto put = [&](const Quarter& r, const int stage) {
+            unsigned char* to = lds + stage * STAGE + of_v * K_BYTES + 16 * lane;
+            TileRegs<D, F8, 2> x;
+            if (!of_v) {
 #pragma unroll
-            for (int y = 1; y < SHARERS; ++y) top = fmaxf(top, pm[of * SHARERS + y][rn]);
-            const float use = top == -INFINITY ? 0.f : top;
-            float sum = 0.f;
-            floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+                for (int u = 0; u < 2; ++u) {
 #pragma unroll
-            for (int y = 0; y < SHARERS; ++y) {
-                const int from = of * SHARERS + y;
-                const float f = __builtin_amdgcn_exp2f(pm[from][rn] - use);
-                const floatx4 v = *reinterpret_cast<const floatx4*>(&po[from][rn][col]);
-                sum = fmaf(f, pl[from][rn], sum);
+                    for (int z = 0; z < CH; ++z) x.k[u][z] = r.c[u][z];
+                    x.ks[u] = r.s[u];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] = fmaf(f, v[e], acc[e]);
+                    for (int s = 0; s < KS; ++s) *reinterpret_cast<bf16x8*>(to + ((2 * pair + u) * KS + s) * 1024) = k_operand<D, F8, 2>(x, u, s);
+                }
+                return;
             }
-            acc *= inverse_sum(sum);
-            if (w.pieces == 1) {
-                store4(a, out_at(row0 + local, col), acc);
+            if constexpr (F8) {
+                float s[2][4];
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[u][e] = scale_value(r.s[u] >> 8 * e & 0xFF);
+#pragma unroll
+                for (int t = 0; t < VT; ++t)
+                    *reinterpret_cast<bf16x8*>(to + (pair * VT + t) * 1024) = operand(widen_each(r.c[0][t / 4][t % 4], s[0]), widen_each(r.c[1][t / 4][t % 4], s[1]));
             } else {
-                const int64_t at = part_row(w.piece) + local;
-                publish4(a.part_o + at * D + col, acc);
-                if (col == 0) __hip_atomic_store(a.part_lse + at, sum > 0.f || sum != sum ? top + __builtin_amdgcn_logf(sum) : -INFINITY, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int z = 0; z < CH; ++z) x.v[u][z] = r.c[u][z];
+#pragma unroll
+                for (int t = 0; t < VT; ++t) *reinterpret_cast<bf16x8*>(to + (pair * VT + t) * 1024) = v_operand<D, F8, 2>(x, 0, t);
             }
+        };
+        Quarter r0, r1;
+        int p0 = ask_places<N>(a, bounds, t0, 2 * pair), p1 = ask_places<N>(a, bounds, t0 + 1, 2 * pair);
+        load(r0, p0, t0);
+        Queries<D, NB> q;
+        load_queries<D, F8, NB>(a, bounds, kvh, bounds.row0 + (works ? row_group * 32 : 0), q);
+        __builtin_amdgcn_sched_barrier(0);
+        load(r1, p1, t0 + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        constexpr int SECOND = 2 * (CH + (F8 ? 1 : 0)) + 1;
+        __builtin_amdgcn_s_waitcnt(0x0F70 | (SECOND & 0xF) | (SECOND >> 4 << 14));     // (the rows too, tree_attn_kernel)
+        const float sl2 = a.scale * kLog2e;
+
+        // 32 keys of the tile, those of sub-tile pair x0
+        auto step = [&](const int tile, const int stage, const int x0, auto edge) {
+            constexpr int XN = 1, SN = 2 * XN;
+            constexpr bool EDGE = decltype(edge)::value;
+            const unsigned char* k = lds + stage * STAGE + 16 * lane + x0 * 2 * KS * 1024;
+            const unsigned char* v = lds + stage * STAGE + K_BYTES + 16 * lane + x0 * VT * 1024;
+            // operands are read RING steps ahead (all at once they would need the registers that there are)
+            constexpr int RING = 4, KF = SN * KS, VF = XN * VT;
+            bf16x8 ring[RING];
+            floatx4 s[NB][SN];
+#pragma unroll
+            for (int f = 0; f < RING; ++f) ring[f] = *reinterpret_cast<const bf16x8*>(k + f * 1024);
+#pragma unroll
+            for (int f = 0; f < KF; ++f) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+                    s[b][f / KS] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ring[f % RING], q.q[b][f % KS], f % KS == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : s[b][f / KS], 0, 0, 0);
+                ring[f % RING] = *reinterpret_cast<const bf16x8*>(f + RING < KF ? k + (f + RING) * 1024 : v + (f + RING - KF) * 1024);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            uint32_t hidden[NB] = {};
+            if constexpr (EDGE) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    uint32_t seen = 0;
+#pragma unroll
+                    for (int u = 0; u < SN; ++u) seen |= seen_of_four(q.bits[b], tile * TOKENS + 32 * x0 + 16 * u + 4 * g, ctx, len) << 4 * u;
+                    hidden[b] = ~seen;
+                }
+            }
+            bf16x8 pf[NB][XN];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                float p[4 * SN];
+                probabilities<D, SN, EDGE>(s[b], hidden[b], sl2, y.o[b], y.l[b], y.m[b], p);
+#pragma unroll
+                for (int x = 0; x < XN; ++x)
+                    pf[b][x] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(p[8 * x], p[8 * x + 1]), pack_bf16x2(p[8 * x + 2], p[8 * x + 3]),
+                                                                pack_bf16x2(p[8 * x + 4], p[8 * x + 5]), pack_bf16x2(p[8 * x + 6], p[8 * x + 7])});
+            }
+            const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
+#pragma unroll
+            for (int f = 0; f < VF; ++f) {
+                const int x = f / VT, t = f % VT;
+                if (t == 0) {
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) y.l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[b][x], y.l[b], 0, 0, 0);       // (of the rounded probabilities)
+                }
+                if constexpr (EDGE) product_with_hidden<NB, D, XN>(ring[f % RING], hidden, x, pf, y, t);
+                else {
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) y.o[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ring[f % RING], pf[b][x], y.o[b][t], 0, 0, 0);
+                }
+                if (f + RING < VF) ring[f % RING] = *reinterpret_cast<const bf16x8*>(v + (f + RING) * 1024);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        const int x0 = sharers == 1 ? 0 : half, x1 = sharers == 1 ? 2 : half + 1;
+        // LDS alone is waited for: the quarters on their way stay so
+        const auto all_here = [&] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+        put(r0, 0);
+        load(r0, p0, t0 + 2);
+        // Tiles that every row sees whole, then the others, as in tree_attn_kernel.  A tile is requested three turns before it is used: two of them in registers.
+        int tile = t0;
+        for (;;) {
+            if (tile >= whole) goto others;
+            all_here();
+            put(r1, 1);
+            load(r1, p1, tile + 3);
+            if (works) for (int x = x0; x < x1; ++x) step(tile, 0, x, std::false_type{});
+            ++tile;
+            if (tile >= whole) {
+                r1 = r0;
+                goto others;
+            }
+            all_here();
+            put(r0, 0);
+            load(r0, p0, tile + 3);
+            if (works) for (int x = x0; x < x1; ++x) step(tile, 1, x, std::false_type{});
+            ++tile;
+        }
+    others:
+        while (tile < t1) {
+            const int stage = (tile - t0) & 1;
+            all_here();
+            put(r1, stage ^ 1);
+            p1 = ask_places<N>(a, bounds, tile + 2, 2 * pair);
+            load(r1, p1, tile + 2);
+            if (works) for (int x = x0; x < x1; ++x) step(tile, stage, x, std::true_type{});
+            ++tile;
         }
     }
-    if (w.pieces == 1) return;
-    // The workgroup that finishes last puts the pieces together, in their order whichever it is (decode_body.hip.h on the order of stores and counts).
-    __builtin_amdgcn_s_waitcnt(0x0F70);            // vmcnt(0): this wave's partial results are in memory
-    __syncthreads();
-    if (threadIdx.x == 0) last = arrives_last(TreeCount{a.arrived + group}, static_cast<uint32_t>(w.pieces));
-    __syncthreads();
-    if (last == 0) return;
-    constexpr int BATCH = 4;
-    for (int x = threadIdx.x; x < rows_here * (D / 4); x += 64 * kWaves) {
-        const int local = x / (D / 4), col = 4 * (x % (D / 4));
-        float top = -INFINITY, sum = 0.f;
-        floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-        for (int p = 0; p < w.pieces; p += BATCH) {
-            float lse[BATCH];
-            floatx4 v[BATCH];
-#pragma unroll
-            for (int y = 0; y < BATCH; ++y) {
-                const int64_t at = part_row(min(p + y, w.pieces - 1)) + local;
-                lse[y] = __hip_atomic_load(a.part_lse + at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                v[y] = read_published4(a.part_o + at * D + col);
-            }
-            float top_new = top;
-#pragma unroll
-            for (int y = 0; y < BATCH; ++y) {
-                if (p + y >= w.pieces) { lse[y] = -INFINITY; v[y] = floatx4{0.f, 0.f, 0.f, 0.f}; }
-                top_new = fmaxf(top_new, lse[y]);
-            }
-            const float use = top_new == -INFINITY ? 0.f : top_new;
-            const float alpha = __builtin_amdgcn_exp2f(top - use);
-            sum *= alpha;
-            acc *= alpha;
-#pragma unroll
-            for (int y = 0; y < BATCH; ++y) {
-                const float f = __builtin_amdgcn_exp2f(lse[y] - use);
-                sum += f;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] = fmaf(f, v[y][e], acc[e]);
-            }
-            top = top_new;
-        }
-        store4(a, out_at(row0 + local, col), acc * inverse_sum(sum));
-    }
+    finish<D, F8, NB>(a, w, bounds, kvh, kWaves / sharers, sharers, y, lds, &last);
 }
 
 template <int D, bool F8>
-int launch(const TreeArgs& a, const TreeShape& s, const dim3 grid, hipStream_t st) {
+int launch(const TreeArgs& a, const int row_blocks, const dim3 grid, hipStream_t st) {
     const dim3 block(64 * kWaves);
     // sub-tiles in a tile: two tiles in flight, and with the accumulators of 16 or 32 rows within 256 registers (512 for 32 rows and d = 128 in bf16)
-    constexpr int N1 = F8 ? 4 : 256 / D, N2 = F8 && D == 64 ? 4 : 2, W2 = F8 || D == 64 ? 2 : 1;
-    if (s.row_blocks == 1) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 1, 1, N1, 2>), grid, block, 0, st, a);
-    else if (s.row_groups == 1) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 2, 1, N2, W2>), grid, block, 0, st, a);
-    else if (s.row_groups == 2) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 2, 2, N2, W2>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((tree_attn_kernel<D, F8, 2, 4, N2, W2>), grid, block, 0, st, a);
+    constexpr int N1 = D == 64 ? 4 : 2, S1 = F8 && D == 128 ? 3 : 2, N2 = F8 && D == 64 ? 4 : 2, W2 = F8 || D == 64 ? 2 : 1;
+    if (row_blocks == 1) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 1, N1, S1, 2>), grid, block, 0, st, a);
+    else if (row_blocks == 2) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 2, N2, 2, W2>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((tree_attn_wide_kernel<D, F8>), grid, block, 0, st, a);
     return static_cast<int>(hipGetLastError());
 }
 
@@ -532,15 +808,22 @@ int launch_tree_attn(TreeArgs a, const TreeShape& s, void* stream) {
     a.by_r = FastDiv::by(static_cast<uint32_t>(a.heads_per_kv));
     a.subs = a.cache.page / 16;
     a.by_subs = FastDiv::by(static_cast<uint32_t>(a.subs));
+    a.rows_of_chunk = s.rows;
     a.chunks = s.chunks;
     a.items = s.items;
+    a.rounds = s.rounds;
     a.least_share = 4;
-    const int64_t workgroups = (static_cast<int64_t>(a.items) + a.n) * a.chunks * a.cache.Hkv;
+    // Pieces of a KV head: with few requests the last of the shares that are looked at (15/8 of an even one) makes no more than run at once; otherwise those of
+    // several rounds, and one more for every (request, chunk).  (Workgroups that find no piece take 3 us, two at a time on a unit.)
+    const int64_t loads = static_cast<int64_t>(a.n) * a.chunks;
+    if (15 * loads <= 7 * a.items) a.rounds = 1;
+    const int64_t workgroups = (a.rounds == 1 ? a.items : static_cast<int64_t>(a.items) * a.rounds + loads) * a.cache.Hkv;
     if (workgroups > 0x7FFFFFFF) return static_cast<int>(hipErrorInvalidConfiguration);
     const dim3 grid(static_cast<unsigned>(workgroups));
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (a.cache.d == 128) return a.cache.f8 ? launch<128, true>(a, s, grid, st) : launch<128, false>(a, s, grid, st);
-    return a.cache.f8 ? launch<64, true>(a, s, grid, st) : launch<64, false>(a, s, grid, st);
+    const int row_blocks = s.rows / 16;
+    if (a.cache.d == 128) return a.cache.f8 ? launch<128, true>(a, row_blocks, grid, st) : launch<128, false>(a, row_blocks, grid, st);
+    return a.cache.f8 ? launch<64, true>(a, row_blocks, grid, st) : launch<64, false>(a, row_blocks, grid, st);
 }
 
 }  // namespace pk
