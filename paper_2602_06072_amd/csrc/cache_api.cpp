@@ -139,16 +139,16 @@ bool tree_sizes_ok(const int64_t n, const int64_t max_q, const int64_t Hq, const
 
 TreeShape TreeShape::of(const int max_q, const int Hq, const int Hkv, const int compute_units) {
     const int rows = max_q * (Hq / Hkv);
-    TreeShape s{rows <= 16 ? 16 : rows <= 32 ? 32 : 128, 1, 0, rows <= 32 ? 4 : 2};
+    TreeShape s{rows <= 16 ? 16 : rows <= 32 ? 32 : 128, 1, 0, rows <= 32 ? 8 : 5};
     s.chunks = rows <= s.rows ? 1 : (rows + s.rows - 1) / s.rows;
     s.items = 2 * compute_units > Hkv ? 2 * compute_units / Hkv : 1;       // (two workgroups of a compute unit)
     return s;
 }
 
-// A piece has at least 1 / (items * rounds) of all tiles, and only requests of more than that are cut: twice as many slots hold the pieces of all.
+// A piece has at least 4 / (items * rounds) of all tiles, and only requests of more than that are cut: twice as many slots hold the pieces of all.
 size_t TreeShape::partial_bytes(const int Hkv, const int d, const int compute_units) const {
     const int64_t most = Hkv > 2 * compute_units ? Hkv : 2 * compute_units;
-    return static_cast<size_t>((2 * most * rounds * rows * (d + 1) * 4 + 255) / 256 * 256);
+    return static_cast<size_t>(((rounds + 1) / 2 * most * rows * (d + 1) * 4 + 255) / 256 * 256);
 }
 
 extern "C" int pk_qk_norm_rope(const pk_rows* q, const pk_rows* k, const pk_rows* q_out, const pk_rows* k_out,
@@ -259,7 +259,9 @@ extern "C" int pk_tree_attn(const pk_cache* cache, const void* q, const int32_t*
         a.out = out; a.out_f32 = out_dtype == PK_F32; a.scale = scale; a.Hq = Hq;
         // counts at the front, partial results at the end: no call writes the counts of another
         a.arrived = static_cast<uint32_t*>(workspace);
-        a.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + workspace_bytes - partial);
+        char* end = static_cast<char*>(workspace) + workspace_bytes;
+        a.part_o = reinterpret_cast<float*>(end - partial);
+        a.pieces_of = reinterpret_cast<int2*>(end - partial - (static_cast<size_t>(n) * 8 + 255) / 256 * 256);
         a.part_lse = a.part_o + partial / 4 / (cache->d + 1) * cache->d;
         return launched(who, launch_tree_attn(a, shape, stream));
     });

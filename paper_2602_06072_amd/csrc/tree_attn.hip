@@ -52,11 +52,20 @@ __device__ __forceinline__ Load load_of(const TreeArgs& a, const int i) {
 }
 __device__ __forceinline__ int pieces_of(const int tiles, const int share) { return max(1, (tiles + share - 1) / share); }
 
-// The workgroup's piece, number `item` of the launch, found from the lengths by every wave itself: no table to be made on the host, none to be copied when
-// lengths change.  A piece has at most `share` tiles.  The share is the smallest of eight with which all pieces run at once (a second, partly filled round of
-// workgroups is as long as the first); where there are more requests than that, it is made small enough for several rounds to even out.
+// The pieces of a launch follow from the lengths, and every wave finds its own from them: no table to be made on the host, none to be copied when lengths
+// change.  A piece has at most `share` tiles.
+//
+// Few requests (a.rounds == 0): the share is the smallest of eight with which all pieces run at once (a second, partly filled round of workgroups takes as long as
+// the first).  The last of the eight, 15/8 of an even one, always does: a launch has as many workgroups as run at once.
+// More requests: a piece is at most a part of what a workgroup's place gets to do, and long pieces come first (of more than half of the share, of more than a
+// quarter, the others), so that the launch ends with short ones.
+struct Shares { int share, middle, last; };         // middle, last: number of the first piece of the second and third kind
+__device__ __forceinline__ int order_of(const Load w, const int share) {
+    const int k = pieces_of(w.tiles, share);
+    return k > 1 || 2 * w.tiles > share ? 0 : 4 * w.tiles > share ? 1 : 2;
+}
 template <int TOKENS>
-__device__ __forceinline__ bool find_piece(const TreeArgs& a, const int item, int* counts, Piece& out) {
+__device__ __forceinline__ Shares share_of(const TreeArgs& a, int* counts) {
     constexpr int STEPS = 8;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int total = 0;
@@ -65,6 +74,20 @@ __device__ __forceinline__ bool find_piece(const TreeArgs& a, const int item, in
         total += w.tiles * w.chunks;
     }
     total = last_lane(wave_prefix(total));
+    Shares s{};
+    if (a.rounds > 0) {
+        s.share = max(a.least_share, static_cast<int>((4 * static_cast<int64_t>(total) + a.items * a.rounds - 1) / (a.items * a.rounds)));
+        int longs = 0, middles = 0;
+        for (int i = lane; i < a.n; i += 64) {
+            const Load w = load_of<TOKENS>(a, i);
+            const int k = w.chunks * pieces_of(w.tiles, s.share), o = order_of(w, s.share);
+            longs += o == 0 ? k : 0;
+            middles += o == 1 ? k : 0;
+        }
+        s.middle = last_lane(wave_prefix(longs));
+        s.last = s.middle + last_lane(wave_prefix(middles));
+        return s;
+    }
     const auto candidate = [&](const int x) {       // an even share of all tiles, and 1/8, 2/8, .. more
         return max(a.least_share, static_cast<int>((static_cast<int64_t>(total) * (8 + x) + 8 * a.items - 1) / (8 * a.items)));
     };
@@ -80,16 +103,23 @@ __device__ __forceinline__ bool find_piece(const TreeArgs& a, const int item, in
         if (lane == 0) counts[wave + kWaves * x] = all;
     }
     __syncthreads();
-    int share = max(a.least_share, (total + a.items * a.rounds - 1) / (a.items * a.rounds));
+    s.share = candidate(STEPS - 1);
 #pragma unroll
-    for (int x = STEPS - 1; x >= 0; --x)
-        if (counts[x] <= a.items) share = candidate(x);
-    int before = 0, slots = 0;
+    for (int x = STEPS - 2; x >= 0; --x)
+        if (counts[x] <= a.items) s.share = candidate(x);
+    return s;
+}
+// Piece number `item` of a KV head; false: there are fewer
+template <int TOKENS>
+__device__ __forceinline__ bool find_piece(const TreeArgs& a, const int item, const Shares& s, Piece& out) {
+    const int lane = threadIdx.x & 63;
+    const int order = a.rounds == 0 ? -1 : item < s.middle ? 0 : item < s.last ? 1 : 2;
+    int before = order < 1 ? 0 : order == 1 ? s.middle : s.last, slots = 0;        // (only requests of the first kind are cut)
     for (int i0 = 0; i0 < a.n; i0 += 64) {
         const int i = min(i0 + lane, a.n - 1);
         Load w = load_of<TOKENS>(a, i);
-        if (i0 + lane >= a.n) w.chunks = 0;
-        const int k = pieces_of(w.tiles, share), mine = k * w.chunks, upto = wave_prefix(mine), slots_upto = wave_prefix(k > 1 ? mine : 0);
+        if (i0 + lane >= a.n || (order >= 0 && order_of(w, s.share) != order)) w.chunks = 0;
+        const int k = pieces_of(w.tiles, s.share), mine = k * w.chunks, upto = wave_prefix(mine), slots_upto = wave_prefix(k > 1 ? mine : 0);
         const uint64_t here = __ballot(item >= before + upto - mine && item < before + upto);
         if (here != 0) {
             const int from = __builtin_ctzll(here);
@@ -107,6 +137,30 @@ __device__ __forceinline__ bool find_piece(const TreeArgs& a, const int item, in
         slots += last_lane(slots_upto);
     }
     return false;
+}
+
+// The kernel's arguments, to be read anew: kept in registers over the loop of pieces they would leave too few scalar ones for the loop of tiles inside (trees of 64
+// requests 674 -> 756 us)
+__device__ __forceinline__ const TreeArgs& kernel_args() {
+    auto p = (const __attribute__((address_space(4))) TreeArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const TreeArgs*)p;
+}
+
+// Runs `work(arguments, piece, KV head)` for the workgroup's pieces: the one of its number and, where there are more pieces than workgroups, those as many numbers on.
+// Workgroups go round-robin over the XCDs: with eight KV heads an XCD keeps to one, and the chunks of its rows find its keys in the L2.
+template <int TOKENS, class Work>
+__device__ __forceinline__ void run_pieces(int* counts, Work work) {
+    const Shares shares = share_of<TOKENS>(kernel_args(), counts);
+    for (int item = blockIdx.x;; item += gridDim.x) {
+        const TreeArgs& a = kernel_args();
+        Piece w;
+        const int rest = item / a.cache.Hkv, kvh = item - rest * a.cache.Hkv;
+        if (!find_piece<TOKENS>(a, rest, shares, w)) return;
+        work(a, w, kvh);
+        if (a.rounds == 0) return;
+        __syncthreads();
+    }
 }
 
 // K and V of a tile of N sub-tiles (16 keys each) as they are in memory
@@ -146,28 +200,20 @@ __device__ __forceinline__ bf16x8 v_operand(const TileRegs<D, F8, N>& r, const i
     }
 }
 
-__device__ __forceinline__ void publish4(float* p, const floatx4 x) {
-    uint64_t* q = reinterpret_cast<uint64_t*>(p);
-    __hip_atomic_store(q, __builtin_bit_cast(uint64_t, floatx2{x[0], x[1]}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __hip_atomic_store(q + 1, __builtin_bit_cast(uint64_t, floatx2{x[2], x[3]}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ floatx4 read_published4(const float* p) {
-    const uint64_t* q = reinterpret_cast<const uint64_t*>(p);
-    const floatx2 a = __builtin_bit_cast(floatx2, __hip_atomic_load(q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-    const floatx2 b = __builtin_bit_cast(floatx2, __hip_atomic_load(q + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-    return floatx4{a[0], a[1], b[0], b[1]};
-}
-struct TreeCount {
-    uint32_t* x;
-    __device__ __forceinline__ uint32_t next(const uint32_t limit) const { return __builtin_amdgcn_atomic_inc32(x, limit, __ATOMIC_RELAXED, "agent"); }
-};
-
+// Partial results that another workgroup of the same launch reads are written through to memory, and read past what an L2 has of an earlier launch
+// (decode_body.hip.h on the order of such stores and the count)
+constexpr int kDeviceScope = 16;                    // cache policy of a buffer load: the scope bit that a relaxed atomic load at device scope has
 __device__ __forceinline__ void store4(const TreeArgs& a, const int64_t at, const floatx4 x) {
     if (a.out_f32) *reinterpret_cast<floatx4*>(static_cast<float*>(a.out) + at) = x;
     else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
 }
 // 1 / l; a row that saw nothing is zero, one whose sum is no number stays one
 __device__ __forceinline__ float inverse_sum(const float l) { return l > 0.f || l != l ? 1.f / l : 0.f; }
+
+struct TreeCount {
+    uint32_t* x;
+    __device__ __forceinline__ uint32_t next(const uint32_t limit) const { return __builtin_amdgcn_atomic_inc32(x, limit, __ATOMIC_RELAXED, "agent"); }
+};
 
 // All ones in the place of the bf16 numbers of a word that are not finite
 __device__ __forceinline__ uint32_t not_finite(const uint32_t x) {
@@ -279,18 +325,29 @@ __device__ __forceinline__ void load_queries(const TreeArgs& a, const Bounds& w,
     }
 }
 
-// Probabilities of 16 N keys against a row, from their raw scores; what is summed up so far is brought to the new maximum.
-// `hidden`: bit x for key x that the row does not see (looked at with EDGE).
-template <int D, int N, bool EDGE>
+// Probabilities of 16 N keys against a row, from their raw scores.  `hidden`: bit x for key x that the row does not see (looked at with EDGE).
+// LAZY: they are relative to m, which need not be the maximum: bf16 and fp32 hold 2^8 as well as 1, so what is summed up so far is brought to a new
+// maximum only when a probability reaches that (m = -inf in front of a wave's first tile: they are infinite then).  A maximum across the lanes for
+// every tile costs as much as the exponents' arithmetic.
+constexpr float kMostProbability = 256.f;
+template <int D, int N, bool EDGE, bool LAZY>
 __device__ __forceinline__ void probabilities(const floatx4 (&s)[N], const uint32_t hidden, const float sl2, floatx4 (&o)[D / 16], floatx4& l, float& m, float (&p)[4 * N]) {
+    const auto raw = [&](const int x) { return !EDGE || !(hidden >> x & 1) ? s[x / 4][x % 4] : -INFINITY; };
+    if constexpr (LAZY && !EDGE) {
+        float top = 0.f;
 #pragma unroll
-    for (int x = 0; x < 4 * N; ++x) p[x] = !EDGE || !(hidden >> x & 1) ? s[x / 4][x % 4] : -INFINITY;
-    float mx = p[0];
+        for (int x = 0; x < 4 * N; ++x) {
+            p[x] = __builtin_amdgcn_exp2f(fmaf(raw(x), sl2, -m));
+            top = fmaxf(top, p[x]);
+        }
+        if (!__any(!(top < kMostProbability))) return;
+    }
+    float mx = raw(0);
 #pragma unroll
-    for (int x = 1; x < 4 * N; ++x) mx = fmaxf(mx, p[x]);
+    for (int x = 1; x < 4 * N; ++x) mx = fmaxf(mx, raw(x));
     const float m_new = fmaxf(m, max_of_lane_groups(mx) * sl2);
     const float m_use = m_new == -INFINITY ? 0.f : m_new;
-    if (__any(m_new != m)) {
+    if (LAZY || __any(m_new != m)) {
         const float alpha = __builtin_amdgcn_exp2f(m - m_use);
         l *= alpha;
 #pragma unroll
@@ -298,7 +355,7 @@ __device__ __forceinline__ void probabilities(const floatx4 (&s)[N], const uint3
         m = m_new;
     }
 #pragma unroll
-    for (int x = 0; x < 4 * N; ++x) p[x] = __builtin_amdgcn_exp2f(fmaf(p[x], sl2, -m_use));
+    for (int x = 0; x < 4 * N; ++x) p[x] = __builtin_amdgcn_exp2f(fmaf(raw(x), sl2, -m_use));
 }
 
 // The product of a block of V columns with the probabilities of 32 keys, of which some rows do not see some: a probability of zero does not hide what is no
@@ -335,11 +392,45 @@ __device__ __forceinline__ void product_with_hidden(const bf16x8 v, const uint32
     }
 }
 
+// Four columns of a row from the partial results of its pieces: sum of exp(lse) o over sum of exp(lse), eight pieces on their way at a time
+template <class Read>
+__device__ __forceinline__ floatx4 merged(const int pieces, Read read) {
+    constexpr int BATCH = 8;
+    float top = -INFINITY, sum = 0.f;
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < pieces; p += BATCH) {
+        float lse[BATCH];
+        floatx4 o[BATCH];
+#pragma unroll
+        for (int z = 0; z < BATCH; ++z) read(min(p + z, pieces - 1), lse[z], o[z]);
+        float top_new = top;
+#pragma unroll
+        for (int z = 0; z < BATCH; ++z) {
+            if (p + z >= pieces) { lse[z] = -INFINITY; o[z] = floatx4{0.f, 0.f, 0.f, 0.f}; }
+            top_new = fmaxf(top_new, lse[z]);
+        }
+        const float use = top_new == -INFINITY ? 0.f : top_new;
+        const float alpha = __builtin_amdgcn_exp2f(top - use);
+        sum *= alpha;
+        acc *= alpha;
+#pragma unroll
+        for (int z = 0; z < BATCH; ++z) {
+            const float f = __builtin_amdgcn_exp2f(lse[z] - use);
+            sum += f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] = fmaf(f, o[z][e], acc[e]);
+        }
+        top = top_new;
+    }
+    return acc * inverse_sum(sum);
+}
+
 // Results of a workgroup: those of the `sharers` waves of a row group are put together in LDS and written; where the request has other pieces they are
-// partial results, and the workgroup that finishes last puts those together, in their order whichever it is.
+// partial results.  HERE (few rows): the workgroup that finishes last puts those together, in their order whichever it is; otherwise a second launch does
+// (tree_merge_kernel): reads past the caches take 2 us each, and one workgroup's worth of them 6 to 16 us for 32 to 128 rows.
 template <int D> constexpr int kPitch = D + 4;
 template <int D> constexpr int kJoinBytes = kWaves * 16 * (kPitch<D> + 2) * 4;
-template <int D, bool F8, int NB>
+template <int D, bool F8, int NB, bool HERE>
 __device__ __forceinline__ void finish(const TreeArgs& a, const Piece& w, const Bounds& bounds, const int kvh, const int row_groups, const int sharers, const Sums<D, NB>& y, unsigned char* lds, int* last) {
     constexpr int CH = F8 ? D / 64 : D / 32, PITCH = kPitch<D>;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6)), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
@@ -385,10 +476,20 @@ __device__ __forceinline__ void finish(const TreeArgs& a, const Piece& w, const 
                 store4(a, out_at(local, col), acc);
             } else {
                 const int64_t at = part_row(w.piece) + local;
-                publish4(a.part_o + at * D + col, acc);
-                if (col == 0) __hip_atomic_store(a.part_lse + at, sum > 0.f || sum != sum ? top + __builtin_amdgcn_logf(sum) : -INFINITY, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                const float lse = sum > 0.f || sum != sum ? top + __builtin_amdgcn_logf(sum) : -INFINITY;
+                if constexpr (HERE) {
+                    write_through(a.part_o + at * D + col, __builtin_bit_cast(u32x4, acc));
+                    if (col == 0) __hip_atomic_store(a.part_lse + at, lse, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                } else {
+                    *reinterpret_cast<floatx4*>(a.part_o + at * D + col) = acc;
+                    if (col == 0) a.part_lse[at] = lse;
+                }
             }
         }
+    }
+    if constexpr (!HERE) {
+        if (w.piece == 0 && w.chunk == 0 && kvh == 0 && threadIdx.x == 0) a.pieces_of[w.request] = make_int2(w.pieces, w.slot);
+        return;
     }
     if (w.pieces == 1) return;
     // (decode_body.hip.h on the order of the stores and the count)
@@ -400,56 +501,30 @@ __device__ __forceinline__ void finish(const TreeArgs& a, const Piece& w, const 
     }
     __syncthreads();
     if (*last == 0) return;
-    constexpr int BATCH = 4;
+    const int apart = w.chunks * a.cache.Hkv * a.rows_of_chunk;    // rows from a piece to the next
+    const auto o_rows = __builtin_amdgcn_make_buffer_rsrc(a.part_o + part_row(0) * D, 0, 0x7FFFFFFF, 0x00020000);
+    const auto lse_rows = __builtin_amdgcn_make_buffer_rsrc(a.part_lse + part_row(0), 0, 0x7FFFFFFF, 0x00020000);
     for (int x = threadIdx.x; x < bounds.rows_here * (D / 4); x += 64 * kWaves) {
         const int local = x / (D / 4), col = 4 * (x % (D / 4));
-        float top = -INFINITY, sum = 0.f;
-        floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-        for (int p = 0; p < w.pieces; p += BATCH) {
-            float lse[BATCH];
-            floatx4 v[BATCH];
-#pragma unroll
-            for (int z = 0; z < BATCH; ++z) {
-                const int64_t at = part_row(min(p + z, w.pieces - 1)) + local;
-                lse[z] = __hip_atomic_load(a.part_lse + at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                v[z] = read_published4(a.part_o + at * D + col);
-            }
-            float top_new = top;
-#pragma unroll
-            for (int z = 0; z < BATCH; ++z) {
-                if (p + z >= w.pieces) { lse[z] = -INFINITY; v[z] = floatx4{0.f, 0.f, 0.f, 0.f}; }
-                top_new = fmaxf(top_new, lse[z]);
-            }
-            const float use = top_new == -INFINITY ? 0.f : top_new;
-            const float alpha = __builtin_amdgcn_exp2f(top - use);
-            sum *= alpha;
-            acc *= alpha;
-#pragma unroll
-            for (int z = 0; z < BATCH; ++z) {
-                const float f = __builtin_amdgcn_exp2f(lse[z] - use);
-                sum += f;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] = fmaf(f, v[z][e], acc[e]);
-            }
-            top = top_new;
-        }
-        store4(a, out_at(local, col), acc * inverse_sum(sum));
+        store4(a, out_at(local, col), merged(w.pieces, [&](const int p, float& lse, floatx4& o) {
+            const int at = p * apart + local;
+            lse = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(lse_rows, at * 4, 0, kDeviceScope));
+            o = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(o_rows, (at * D + col) * 4, 0, kDeviceScope));
+        }));
     }
 }
 
 // Up to 16 NB rows: bound by memory.  The four waves of a workgroup take tiles of N sub-tiles in turns, SETS tiles in flight in each, from memory into
 // registers and from there into the products.
 template <int D, bool F8, int NB, int N, int SETS, int WAVES_PER_SIMD>
-__global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(TreeArgs a) {
+__global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(TreeArgs) {
     static_assert(SETS == 2 || SETS == 3, "sets");
     using Regs = TileRegs<D, F8, N>;
     constexpr int CH = Regs::CH, TOKENS = 16 * N, KS = D / 32, VT = D / 16, SIZE = F8 ? 1 : 2;
     __shared__ __align__(16) unsigned char lds[kJoinBytes<D>];
     __shared__ int counts[8], last;
 
-    const int kvh = blockIdx.x % a.cache.Hkv;
-    Piece w;
-    if (!find_piece<TOKENS>(a, blockIdx.x / a.cache.Hkv, counts, w)) return;
+    run_pieces<TOKENS>(counts, [&](const TreeArgs& a, const Piece& w, const int kvh) {
     const Bounds bounds = bounds_of<TOKENS>(a, w);
     if (bounds.rows_here <= 0) return;              // (total_q says so; all pieces of the request alike)
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6)), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
@@ -537,7 +612,7 @@ __global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 float p[4 * N];
-                probabilities<D, N, EDGE>(s[b], hidden[b], sl2, y.o[b], y.l[b], y.m[b], p);
+                probabilities<D, N, EDGE, false>(s[b], hidden[b], sl2, y.o[b], y.l[b], y.m[b], p);
                 uint32_t pw[2 * N];
 #pragma unroll
                 for (int x = 0; x < 4 * N; ++x)
@@ -598,7 +673,8 @@ __global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(
             load(r[0], places[0], tile);
         }
     }
-    finish<D, F8, NB>(a, w, bounds, kvh, 1, kWaves, y, lds, &last);
+    finish<D, F8, NB, NB == 1>(a, w, bounds, kvh, 1, kWaves, y, lds, &last);
+    });
 }
 
 // 4 codes of four tokens -> bf16 values times each one's scale
@@ -616,15 +692,13 @@ __device__ __forceinline__ uint2 widen_each(const uint32_t x, const float (&s)[4
 // and fewer two waves share 32 rows, half of a tile's keys each.
 constexpr int kWideRows = 128;
 template <int D, bool F8>
-__global__ __launch_bounds__(64 * kWaves, 2) void tree_attn_wide_kernel(TreeArgs a) {
+__global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void tree_attn_wide_kernel(TreeArgs) {
     constexpr int NB = 2, N = 4, TOKENS = 64, KS = D / 32, VT = D / 16, CH = F8 ? D / 64 : D / 32, SIZE = F8 ? 1 : 2;
     constexpr int K_BYTES = N * KS * 1024, STAGE = 2 * K_BYTES;
     __shared__ __align__(16) unsigned char lds[2 * STAGE > kJoinBytes<D> ? 2 * STAGE : kJoinBytes<D>];
     __shared__ int counts[8], last;
 
-    const int kvh = blockIdx.x % a.cache.Hkv;
-    Piece w;
-    if (!find_piece<TOKENS>(a, blockIdx.x / a.cache.Hkv, counts, w)) return;
+    run_pieces<TOKENS>(counts, [&](const TreeArgs& a, const Piece& w, const int kvh) {
     const Bounds bounds = bounds_of<TOKENS>(a, w);
     if (bounds.rows_here <= 0) return;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6)), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
@@ -729,7 +803,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_attn_wide_kernel(TreeArgs
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 float p[4 * SN];
-                probabilities<D, SN, EDGE>(s[b], hidden[b], sl2, y.o[b], y.l[b], y.m[b], p);
+                probabilities<D, SN, EDGE, true>(s[b], hidden[b], sl2, y.o[b], y.l[b], y.m[b], p);
 #pragma unroll
                 for (int x = 0; x < XN; ++x)
                     pf[b][x] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(p[8 * x], p[8 * x + 1]), pack_bf16x2(p[8 * x + 2], p[8 * x + 3]),
@@ -787,17 +861,49 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_attn_wide_kernel(TreeArgs
             ++tile;
         }
     }
-    finish<D, F8, NB>(a, w, bounds, kvh, kWaves / sharers, sharers, y, lds, &last);
+    finish<D, F8, NB, false>(a, w, bounds, kvh, kWaves / sharers, sharers, y, lds, &last);
+    });
+}
+
+// Puts the pieces of a request together: one workgroup for (request, KV head, chunk, slice of its rows); nothing to do where there is one piece.
+template <int D>
+__global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a) {
+    int rest = blockIdx.x;
+    const auto take = [&](const int of) { const int x = rest % of; rest /= of; return x; };
+    const int slice = take(a.slices), kvh = take(a.cache.Hkv), chunk = take(a.chunks), i = rest;
+    const int asked = a.q_start[i + 1] - a.q_start[i];
+    const int64_t q0 = min(max(static_cast<int64_t>(a.q_start[i]), int64_t{0}), a.total_q);
+    const int rows = static_cast<int>(min(static_cast<int64_t>(min(asked, a.max_q)), a.total_q - q0)) * a.heads_per_kv;
+    const int here = min(rows - chunk * a.rows_of_chunk, a.rows_of_chunk);
+    if (here <= 0) return;
+    const int2 p = a.pieces_of[i];
+    if (p.x == 1) return;
+    const int chunks = (rows + a.rows_of_chunk - 1) / a.rows_of_chunk;
+    const auto part_row = [&](const int piece) { return (static_cast<int64_t>(p.y + piece * chunks + chunk) * a.cache.Hkv + kvh) * a.rows_of_chunk; };
+    for (int x = slice * 256 + threadIdx.x; x < here * (D / 4); x += a.slices * 256) {
+        const int local = x / (D / 4), col = 4 * (x % (D / 4)), row = chunk * a.rows_of_chunk + local, t = a.by_r(row);
+        store4(a, ((q0 + t) * a.Hq + kvh * a.heads_per_kv + row - t * a.heads_per_kv) * D + col, merged(p.x, [&](const int piece, float& lse, floatx4& o) {
+            const int64_t at = part_row(piece) + local;
+            lse = a.part_lse[at];
+            o = *reinterpret_cast<const floatx4*>(a.part_o + at * D + col);
+        }));
+    }
 }
 
 template <int D, bool F8>
 int launch(const TreeArgs& a, const int row_blocks, const dim3 grid, hipStream_t st) {
     const dim3 block(64 * kWaves);
     // sub-tiles in a tile: two tiles in flight, and with the accumulators of 16 or 32 rows within 256 registers (512 for 32 rows and d = 128 in bf16)
-    constexpr int N1 = D == 64 ? 4 : 2, S1 = F8 && D == 128 ? 3 : 2, N2 = F8 && D == 64 ? 4 : 2, W2 = F8 || D == 64 ? 2 : 1;
-    if (row_blocks == 1) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 1, N1, S1, 2>), grid, block, 0, st, a);
+    constexpr int N1 = D == 64 ? 4 : 2, S1 = 2, N2 = F8 && D == 64 ? 4 : 2, W1 = D == 64 && F8 || D == 128 && F8 ? 3 : 2, W2 = F8 ? 2 : D == 64 ? 3 : 1;
+    if (row_blocks == 1) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 1, N1, S1, W1>), grid, block, 0, st, a);
     else if (row_blocks == 2) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 2, N2, 2, W2>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((tree_attn_wide_kernel<D, F8>), grid, block, 0, st, a);
+    const int keys = 16 * (row_blocks == 1 ? N1 : row_blocks == 2 ? N2 : 4);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess || row_blocks == 1) return static_cast<int>(e);
+    if (static_cast<int64_t>(a.max_blocks) * a.cache.page <= static_cast<int64_t>(a.least_share) * keys) return 0;       // no request can have two pieces
+    const int64_t groups = static_cast<int64_t>(a.n) * a.chunks * a.cache.Hkv;
+    if (groups * a.slices > 0x7FFFFFFF) return static_cast<int>(hipErrorInvalidConfiguration);
+    hipLaunchKernelGGL((tree_merge_kernel<D>), dim3(static_cast<unsigned>(groups * a.slices)), dim3(256), 0, st, a);
     return static_cast<int>(hipGetLastError());
 }
 
@@ -812,13 +918,15 @@ int launch_tree_attn(TreeArgs a, const TreeShape& s, void* stream) {
     a.chunks = s.chunks;
     a.items = s.items;
     a.rounds = s.rounds;
-    a.least_share = 4;
-    // Pieces of a KV head: with few requests the last of the shares that are looked at (15/8 of an even one) makes no more than run at once; otherwise those of
-    // several rounds, and one more for every (request, chunk).  (Workgroups that find no piece take 3 us, two at a time on a unit.)
+    // At least 256 keys to a piece: four users' tokens 13.1 us, with 128 15.6, with 512 13.4; 64-token trees of six requests 44, 55, 50.
+    a.least_share = s.rows == 128 || a.cache.d == 64 ? 4 : 8;
     const int64_t loads = static_cast<int64_t>(a.n) * a.chunks;
-    if (15 * loads <= 7 * a.items) a.rounds = 1;
-    const int64_t workgroups = (a.rounds == 1 ? a.items : static_cast<int64_t>(a.items) * a.rounds + loads) * a.cache.Hkv;
-    if (workgroups > 0x7FFFFFFF) return static_cast<int>(hipErrorInvalidConfiguration);
+    if (15 * loads <= 7 * a.items) a.rounds = 0;
+    // (workgroups without a piece take 3 us, two at a time on a unit: there are no more of them than a round)
+    const int64_t workgroups = (a.rounds == 0 ? a.items : loads + a.items / 2) * a.cache.Hkv;
+    // the merge: up to 2048 workgroups, of 8 rows and more each
+    const int64_t groups = static_cast<int64_t>(a.n) * a.chunks * a.cache.Hkv, slices = 2048 / (groups < 2048 ? groups : 2048);
+    a.slices = static_cast<int>(slices < s.rows / 8 ? slices : s.rows / 8);
     const dim3 grid(static_cast<unsigned>(workgroups));
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int row_blocks = s.rows / 16;
