@@ -56,7 +56,7 @@ int launch_cache_keep(const CacheKeepArgs& a, void* stream);
 // How a launch takes the rows of a (request, KV head): `chunks` workgroups of up to `rows` of them for every piece of the request's keys; `items` workgroups of a
 // KV head run at once; of more requests than that a piece has at most 4 / rounds of what a workgroup's place gets to do.
 struct TreeShape {
-    int rows, chunks, items, rounds;
+    int rows, chunks, items, rounds, alone_chunks;  // alone_chunks: chunks of 32 rows (16 with no more), where a wave has a request
     // both grow with n and max_q, so that a workspace serves every call of one head shape that is not larger than what it was made for
     size_t count_bytes(int64_t n, int Hkv) const { return static_cast<size_t>((n * Hkv * chunks * 4 + 255) / 256 * 256 + (n * 8 + 255) / 256 * 256); }
     size_t partial_bytes(int Hkv, int d, int compute_units) const;
@@ -73,7 +73,7 @@ struct TreeArgs {
     int2* pieces_of;                                // [n] pieces of a request and slot of the first one, for the merge in a launch of its own
     float* part_lse; float* part_o;                 // [slots][Hkv][rows], [..][d]
     // set by the launch
-    int heads_per_kv, subs, rows_of_chunk, chunks, items, rounds, least_share, slices;     // subs: sub-tiles of 16 keys in a page; least_share: tiles of a piece
+    int heads_per_kv, subs, rows_of_chunk, chunks, items, rounds, least_share, least_of_many, slices, whole;     // subs: sub-tiles of 16 keys in a page; least_share: tiles of a piece
     FastDiv by_r, by_subs;
 };
 int launch_tree_attn(TreeArgs a, const TreeShape& s, void* stream);

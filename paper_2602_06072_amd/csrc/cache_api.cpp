@@ -139,7 +139,7 @@ bool tree_sizes_ok(const int64_t n, const int64_t max_q, const int64_t Hq, const
 
 TreeShape TreeShape::of(const int max_q, const int Hq, const int Hkv, const int compute_units) {
     const int rows = max_q * (Hq / Hkv);
-    TreeShape s{rows <= 16 ? 16 : rows <= 32 ? 32 : 128, 1, 0, rows <= 32 ? 8 : 5};
+    TreeShape s{rows <= 16 ? 16 : rows <= 32 ? 32 : 128, 1, 0, rows <= 32 ? 8 : 5, (rows + 31) / 32};
     s.chunks = rows <= s.rows ? 1 : (rows + s.rows - 1) / s.rows;
     s.items = 2 * compute_units > Hkv ? 2 * compute_units / Hkv : 1;       // (two workgroups of a compute unit)
     return s;

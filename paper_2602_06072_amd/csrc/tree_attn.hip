@@ -55,11 +55,10 @@ __device__ __forceinline__ int pieces_of(const int tiles, const int share) { ret
 // The pieces of a launch follow from the lengths, and every wave finds its own from them: no table to be made on the host, none to be copied when lengths
 // change.  A piece has at most `share` tiles.
 //
-// Few requests (a.rounds == 0): the share is the smallest of eight with which all pieces run at once (a second, partly filled round of workgroups takes as long as
-// the first).  The last of the eight, 15/8 of an even one, always does: a launch has as many workgroups as run at once.
-// More requests: a piece is at most a part of what a workgroup's place gets to do, and long pieces come first (of more than half of the share, of more than a
+// Where one round of workgroups may hold them all, the share is the smallest of eight with which it does (a second, partly filled round takes as long as the
+// first).  Otherwise a piece is at most a part of what a workgroup's place gets to do, and long pieces come first (of more than half of the share, of more than a
 // quarter, the others), so that the launch ends with short ones.
-struct Shares { int share, middle, last; };         // middle, last: number of the first piece of the second and third kind
+struct Shares { int share, middle, last; };         // middle, last: number of the first piece of the second and third kind; middle < 0: the one round, in the order of requests
 __device__ __forceinline__ int order_of(const Load w, const int share) {
     const int k = pieces_of(w.tiles, share);
     return k > 1 || 2 * w.tiles > share ? 0 : 4 * w.tiles > share ? 1 : 2;
@@ -68,52 +67,55 @@ template <int TOKENS>
 __device__ __forceinline__ Shares share_of(const TreeArgs& a, int* counts) {
     constexpr int STEPS = 8;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int total = 0;
+    int total = 0, loads = 0;
     for (int i = lane; i < a.n; i += 64) {
         const Load w = load_of<TOKENS>(a, i);
         total += w.tiles * w.chunks;
+        loads += w.chunks;
     }
     total = last_lane(wave_prefix(total));
-    Shares s{};
-    if (a.rounds > 0) {
-        s.share = max(a.least_share, static_cast<int>((4 * static_cast<int64_t>(total) + a.items * a.rounds - 1) / (a.items * a.rounds)));
-        int longs = 0, middles = 0;
+    loads = last_lane(wave_prefix(loads));
+    Shares s{0, -1, 0};
+    if (loads <= a.items) {
+        // eighths of an even share; with 7/15 of the places taken by uncut requests the 15 below always hold all
+        const auto candidate = [&](const int x) {
+            const int eighths = x < 3 ? 8 + x : x < 6 ? 6 + 2 * x : 4 * x - 4;     // 8, 9, 10, 12, 14, 16, 20, 24
+            return max(a.least_share, static_cast<int>((static_cast<int64_t>(total) * eighths + 8 * a.items - 1) / (8 * a.items)));
+        };
+        int fit[STEPS / kWaves] = {};
         for (int i = lane; i < a.n; i += 64) {
             const Load w = load_of<TOKENS>(a, i);
-            const int k = w.chunks * pieces_of(w.tiles, s.share), o = order_of(w, s.share);
-            longs += o == 0 ? k : 0;
-            middles += o == 1 ? k : 0;
+#pragma unroll
+            for (int x = 0; x < STEPS / kWaves; ++x) fit[x] += w.chunks * pieces_of(w.tiles, candidate(wave + kWaves * x));
         }
-        s.middle = last_lane(wave_prefix(longs));
-        s.last = s.middle + last_lane(wave_prefix(middles));
-        return s;
+#pragma unroll
+        for (int x = 0; x < STEPS / kWaves; ++x) {
+            const int all = last_lane(wave_prefix(fit[x]));
+            if (lane == 0) counts[wave + kWaves * x] = all;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int x = STEPS - 1; x >= 0; --x)
+            if (counts[x] <= a.items) s.share = candidate(x);
+        if (s.share > 0) return s;
     }
-    const auto candidate = [&](const int x) {       // an even share of all tiles, and 1/8, 2/8, .. more
-        return max(a.least_share, static_cast<int>((static_cast<int64_t>(total) * (8 + x) + 8 * a.items - 1) / (8 * a.items)));
-    };
-    int fit[STEPS / kWaves] = {};
+    s.share = max(a.least_of_many, static_cast<int>((4 * static_cast<int64_t>(total) + a.items * a.rounds - 1) / (a.items * a.rounds)));
+    int longs = 0, middles = 0;
     for (int i = lane; i < a.n; i += 64) {
         const Load w = load_of<TOKENS>(a, i);
-#pragma unroll
-        for (int x = 0; x < STEPS / kWaves; ++x) fit[x] += w.chunks * pieces_of(w.tiles, candidate(wave + kWaves * x));
+        const int k = w.chunks * pieces_of(w.tiles, s.share), o = order_of(w, s.share);
+        longs += o == 0 ? k : 0;
+        middles += o == 1 ? k : 0;
     }
-#pragma unroll
-    for (int x = 0; x < STEPS / kWaves; ++x) {
-        const int all = last_lane(wave_prefix(fit[x]));
-        if (lane == 0) counts[wave + kWaves * x] = all;
-    }
-    __syncthreads();
-    s.share = candidate(STEPS - 1);
-#pragma unroll
-    for (int x = STEPS - 2; x >= 0; --x)
-        if (counts[x] <= a.items) s.share = candidate(x);
+    s.middle = last_lane(wave_prefix(longs));
+    s.last = s.middle + last_lane(wave_prefix(middles));
     return s;
 }
 // Piece number `item` of a KV head; false: there are fewer
 template <int TOKENS>
 __device__ __forceinline__ bool find_piece(const TreeArgs& a, const int item, const Shares& s, Piece& out) {
     const int lane = threadIdx.x & 63;
-    const int order = a.rounds == 0 ? -1 : item < s.middle ? 0 : item < s.last ? 1 : 2;
+    const int order = s.middle < 0 ? -1 : item < s.middle ? 0 : item < s.last ? 1 : 2;
     int before = order < 1 ? 0 : order == 1 ? s.middle : s.last, slots = 0;        // (only requests of the first kind are cut)
     for (int i0 = 0; i0 < a.n; i0 += 64) {
         const int i = min(i0 + lane, a.n - 1);
@@ -151,6 +153,11 @@ __device__ __forceinline__ const TreeArgs& kernel_args() {
 // Workgroups go round-robin over the XCDs: with eight KV heads an XCD keeps to one, and the chunks of its rows find its keys in the L2.
 template <int TOKENS, class Work>
 __device__ __forceinline__ void run_pieces(int* counts, Work work) {
+    if (const TreeArgs& a = kernel_args(); a.whole) {              // no request can have two pieces
+        const int rest = blockIdx.x / a.cache.Hkv, i = rest / a.chunks;
+        work(a, Piece{i, 0, 1, rest - i * a.chunks, 0, a.chunks}, static_cast<int>(blockIdx.x) - rest * a.cache.Hkv);
+        return;
+    }
     const Shares shares = share_of<TOKENS>(kernel_args(), counts);
     for (int item = blockIdx.x;; item += gridDim.x) {
         const TreeArgs& a = kernel_args();
@@ -158,7 +165,7 @@ __device__ __forceinline__ void run_pieces(int* counts, Work work) {
         const int rest = item / a.cache.Hkv, kvh = item - rest * a.cache.Hkv;
         if (!find_piece<TOKENS>(a, rest, shares, w)) return;
         work(a, w, kvh);
-        if (a.rounds == 0) return;
+        if (shares.middle < 0) return;
         __syncthreads();
     }
 }
@@ -430,7 +437,7 @@ __device__ __forceinline__ floatx4 merged(const int pieces, Read read) {
 // (tree_merge_kernel): reads past the caches take 2 us each, and one workgroup's worth of them 6 to 16 us for 32 to 128 rows.
 template <int D> constexpr int kPitch = D + 4;
 template <int D> constexpr int kJoinBytes = kWaves * 16 * (kPitch<D> + 2) * 4;
-template <int D, bool F8, int NB, bool HERE>
+template <int D, bool F8, int NB, bool HERE, bool ALONE = false>
 __device__ __forceinline__ void finish(const TreeArgs& a, const Piece& w, const Bounds& bounds, const int kvh, const int row_groups, const int sharers, const Sums<D, NB>& y, unsigned char* lds, int* last) {
     constexpr int CH = F8 ? D / 64 : D / 32, PITCH = kPitch<D>;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6)), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
@@ -442,9 +449,12 @@ __device__ __forceinline__ void finish(const TreeArgs& a, const Piece& w, const 
         const int row = bounds.row0 + local, t = a.by_r(row);
         return ((bounds.q0 + t) * a.Hq + kvh * a.heads_per_kv + row - t * a.heads_per_kv) * D + col;
     };
+    // (a wave alone: LDS works through the accesses of a wave in their order, the compiler alone must leave them in it)
+    const auto sync = [] { if constexpr (ALONE) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); else __syncthreads(); };
+    const int thread = ALONE ? lane : threadIdx.x, threads = ALONE ? 64 : 64 * kWaves, first_wave = ALONE ? wave : 0;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-        __syncthreads();
+        sync();
         float* mine = po + (wave * 16 + n) * PITCH;
 #pragma unroll
         for (int x = 0; x < CH; ++x)
@@ -454,11 +464,11 @@ __device__ __forceinline__ void finish(const TreeArgs& a, const Piece& w, const 
                 else *reinterpret_cast<floatx2*>(mine + 32 * x + 8 * g + 2 * e) = floatx2{y.o[b][2 * x][e], y.o[b][2 * x + 1][e]};
             }
         if (g == 0) { pm[wave * 16 + n] = y.m[b]; pl[wave * 16 + n] = y.l[b][0]; }
-        __syncthreads();
-        for (int x = threadIdx.x; x < row_groups * 16 * (D / 4); x += 64 * kWaves) {
+        sync();
+        for (int x = thread; x < row_groups * 16 * (D / 4); x += threads) {
             const int of = x / (16 * (D / 4)), rn = x / (D / 4) % 16, col = 4 * (x % (D / 4)), local = (of * NB + b) * 16 + rn;
             if (local >= bounds.rows_here) continue;
-            const int from = of * sharers * 16 + rn;
+            const int from = (first_wave + of * sharers) * 16 + rn;
             float top = -INFINITY;
             for (int z = 0; z < sharers; ++z) top = fmaxf(top, pm[from + 16 * z]);
             const float use = top == -INFINITY ? 0.f : top;
@@ -487,6 +497,7 @@ __device__ __forceinline__ void finish(const TreeArgs& a, const Piece& w, const 
             }
         }
     }
+    if constexpr (ALONE) return;
     if constexpr (!HERE) {
         if (w.piece == 0 && w.chunk == 0 && kvh == 0 && threadIdx.x == 0) a.pieces_of[w.request] = make_int2(w.pieces, w.slot);
         return;
@@ -515,28 +526,28 @@ __device__ __forceinline__ void finish(const TreeArgs& a, const Piece& w, const 
 }
 
 // Up to 16 NB rows: bound by memory.  The four waves of a workgroup take tiles of N sub-tiles in turns, SETS tiles in flight in each, from memory into
-// registers and from there into the products.
-template <int D, bool F8, int NB, int N, int SETS, int WAVES_PER_SIMD>
+// registers and from there into the products.  ALONE: every wave has a request (and rows) of its own, all of whose tiles it takes.
+template <int D, bool F8, int NB, int N, int SETS, int WAVES_PER_SIMD, bool ALONE = false>
 __global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(TreeArgs) {
-    static_assert(SETS == 2 || SETS == 3, "sets");
+    static_assert(SETS == 2, "sets");
     using Regs = TileRegs<D, F8, N>;
-    constexpr int CH = Regs::CH, TOKENS = 16 * N, KS = D / 32, VT = D / 16, SIZE = F8 ? 1 : 2;
+    constexpr int CH = Regs::CH, TOKENS = 16 * N, KS = D / 32, VT = D / 16, SIZE = F8 ? 1 : 2, STRIDE = ALONE ? 1 : kWaves;
     __shared__ __align__(16) unsigned char lds[kJoinBytes<D>];
     __shared__ int counts[8], last;
 
-    run_pieces<TOKENS>(counts, [&](const TreeArgs& a, const Piece& w, const int kvh) {
-    const Bounds bounds = bounds_of<TOKENS>(a, w);
-    if (bounds.rows_here <= 0) return;              // (total_q says so; all pieces of the request alike)
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6)), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const auto work = [&](const TreeArgs& a, const Piece& w, const int kvh) {
+    const Bounds bounds = bounds_of<TOKENS>(a, w);
+    if (bounds.rows_here <= 0) return;              // (no rows, or total_q says so; all pieces of the request alike)
     const int len = bounds.len, ctx = bounds.ctx, t1 = bounds.t1;
 
     Sums<D, NB> y;
-    int tile = bounds.t0 + wave;
+    int tile = bounds.t0 + (ALONE ? 0 : wave);
     if (tile < t1) {
         // requests a tile, whose places are known, and the places of the set's tile after that
         auto load = [&](Regs& r, int& places, const int tile) {
             const Rows rows = rows_of<N>(a, bounds, kvh, tile, 0, places);
-            places = ask_places<N>(a, bounds, tile + SETS * kWaves, 0);
+            places = ask_places<N>(a, bounds, tile + SETS * STRIDE, 0);
 #pragma unroll
             for (int u = 0; u < N; ++u) {
                 const SubTile t = sub_tile<D, F8>(a, rows, u);
@@ -553,14 +564,14 @@ __global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(
         Regs r[SETS];
         int places[SETS];
 #pragma unroll
-        for (int s = 0; s < SETS; ++s) places[s] = ask_places<N>(a, bounds, tile + s * kWaves, 0);
+        for (int s = 0; s < SETS; ++s) places[s] = ask_places<N>(a, bounds, tile + s * STRIDE, 0);
         load(r[0], places[0], tile);
         Queries<D, NB> q;
         load_queries<D, F8, NB>(a, bounds, kvh, bounds.row0, q);
         // The rows are waited for here, with the first tile; left to the loop, its first products wait for all tiles in flight in every turn.
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int s = 1; s < SETS; ++s) load(r[s], places[s], tile + s * kWaves);
+        for (int s = 1; s < SETS; ++s) load(r[s], places[s], tile + s * STRIDE);
         __builtin_amdgcn_sched_barrier(0);
         constexpr int OTHERS = (SETS - 1) * (N * (2 * CH + (F8 ? 2 : 0)) + 1);
         static_assert(OTHERS < 64, "vmcnt");
@@ -652,29 +663,32 @@ __global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(
         const int whole = min(max(min(ctx, len), 0) / TOKENS, t1);
         const auto turn = [&](Regs& x, int& at) {
             step(x, tile, std::false_type{});
-            load(x, at, tile + SETS * kWaves);
-            tile += kWaves;
+            load(x, at, tile + SETS * STRIDE);
+            tile += STRIDE;
         };
         for (;;) {                                                 // (left by jumps: a flag to leave by keeps all sets alive)
             if (tile >= whole) goto others;
             turn(r[0], places[0]);
             if (tile >= whole) { r[0] = r[1]; goto others; }
             turn(r[1], places[1]);
-            if constexpr (SETS == 3) {
-                if (tile >= whole) { r[0] = r[2]; goto others; }
-                turn(r[2], places[2]);
-            }
         }
     others:
         while (tile < t1) {
             step(r[0], tile, std::true_type{});
-            tile += kWaves;
+            tile += STRIDE;
             places[0] = ask_places<N>(a, bounds, tile, 0);
             load(r[0], places[0], tile);
         }
     }
-    finish<D, F8, NB, NB == 1>(a, w, bounds, kvh, 1, kWaves, y, lds, &last);
-    });
+    finish<D, F8, NB, NB == 1, ALONE>(a, w, bounds, kvh, 1, ALONE ? 1 : kWaves, y, lds, &last);
+    };
+    if constexpr (ALONE) {
+        const TreeArgs& a = kernel_args();
+        const int item = blockIdx.x * kWaves + wave, rest = item / a.cache.Hkv, i = rest / a.chunks;
+        if (i < a.n) work(a, Piece{i, 0, 1, rest - i * a.chunks, 0, a.chunks}, item - rest * a.cache.Hkv);
+    } else {
+        run_pieces<TOKENS>(counts, work);
+    }
 }
 
 // 4 codes of four tokens -> bf16 values times each one's scale
@@ -692,7 +706,7 @@ __device__ __forceinline__ uint2 widen_each(const uint32_t x, const float (&s)[4
 // and fewer two waves share 32 rows, half of a tile's keys each.
 constexpr int kWideRows = 128;
 template <int D, bool F8>
-__global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void tree_attn_wide_kernel(TreeArgs) {
+__global__ __launch_bounds__(64 * kWaves, D == 64 && F8 ? 3 : 2) void tree_attn_wide_kernel(TreeArgs) {
     constexpr int NB = 2, N = 4, TOKENS = 64, KS = D / 32, VT = D / 16, CH = F8 ? D / 64 : D / 32, SIZE = F8 ? 1 : 2;
     constexpr int K_BYTES = N * KS * 1024, STAGE = 2 * K_BYTES;
     __shared__ __align__(16) unsigned char lds[2 * STAGE > kJoinBytes<D> ? 2 * STAGE : kJoinBytes<D>];
@@ -890,18 +904,40 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a) {
     }
 }
 
+// sub-tiles in a tile: two tiles in flight, and with the accumulators of 16 or 32 rows within 256 registers (512 for 32 rows and d = 128 in bf16)
+template <int D, bool F8> constexpr int kSubTiles1 = D == 64 ? 4 : 2;
+template <int D, bool F8> constexpr int kSubTiles2 = F8 && D == 64 ? 4 : 2;
+template <int D, bool F8> constexpr int kWavesOf2 = F8 || D == 64 ? 2 : 1;
+constexpr int kLeastKeys = 256;                     // keys of a piece at least: four users' tokens 13.1 us, with 128 15.6, with 512 13.4; 51-token trees of six requests 44, 55, 50
+
 template <int D, bool F8>
-int launch(const TreeArgs& a, const int row_blocks, const dim3 grid, hipStream_t st) {
+int launch(TreeArgs a, const TreeShape& s, hipStream_t st) {
     const dim3 block(64 * kWaves);
-    // sub-tiles in a tile: two tiles in flight, and with the accumulators of 16 or 32 rows within 256 registers (512 for 32 rows and d = 128 in bf16)
-    constexpr int N1 = D == 64 ? 4 : 2, S1 = 2, N2 = F8 && D == 64 ? 4 : 2, W1 = D == 64 && F8 || D == 128 && F8 ? 3 : 2, W2 = F8 ? 2 : D == 64 ? 3 : 1;
-    if (row_blocks == 1) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 1, N1, S1, W1>), grid, block, 0, st, a);
-    else if (row_blocks == 2) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 2, N2, 2, W2>), grid, block, 0, st, a);
+    const int row_blocks = s.rows / 16, keys = 16 * (row_blocks == 1 ? kSubTiles1<D, F8> : row_blocks == 2 ? kSubTiles2<D, F8> : 4);
+    a.least_share = kLeastKeys / keys;
+    const int64_t loads = static_cast<int64_t>(a.n) * a.chunks, most_keys = static_cast<int64_t>(a.max_blocks) * a.cache.page;
+    a.whole = most_keys <= kLeastKeys;              // no request can have two pieces: nothing to be found out, nothing to be put together
+    a.least_of_many = (s.rows == 128 ? 4 : 1) * a.least_share;     // (cut into more, the partial results of 128 rows are more bytes than the keys)
+    // Short requests, and more of them than workgroups run at once: a wave for every request and 32 rows.
+    if (const int64_t units = static_cast<int64_t>(a.n) * a.cache.Hkv * s.alone_chunks; a.whole && loads > a.items && units <= 0x7FFFFFFF) {
+        a.chunks = s.alone_chunks;
+        a.rows_of_chunk = s.rows == 16 ? 16 : 32;
+        const dim3 grid(static_cast<unsigned>((units + kWaves - 1) / kWaves));
+        if (row_blocks == 1) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 1, kSubTiles1<D, F8>, 2, 2, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((tree_attn_kernel<D, F8, 2, kSubTiles2<D, F8>, 2, kWavesOf2<D, F8>, true>), grid, block, 0, st, a);
+        return static_cast<int>(hipGetLastError());
+    }
+    // (workgroups without a piece take 3 us, two at a time on a unit: there are no more of them than half a round)
+    const int64_t workgroups = (a.whole ? loads : loads <= a.items / 2 ? a.items : loads + a.items / 2) * a.cache.Hkv;
+    if (workgroups > 0x7FFFFFFF) return static_cast<int>(hipErrorInvalidConfiguration);
+    const dim3 grid(static_cast<unsigned>(workgroups));
+    if (row_blocks == 1) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 1, kSubTiles1<D, F8>, 2, 2>), grid, block, 0, st, a);
+    else if (row_blocks == 2) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 2, kSubTiles2<D, F8>, 2, kWavesOf2<D, F8>>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((tree_attn_wide_kernel<D, F8>), grid, block, 0, st, a);
-    const int keys = 16 * (row_blocks == 1 ? N1 : row_blocks == 2 ? N2 : 4);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess || row_blocks == 1) return static_cast<int>(e);
-    if (static_cast<int64_t>(a.max_blocks) * a.cache.page <= static_cast<int64_t>(a.least_share) * keys) return 0;       // no request can have two pieces
-    const int64_t groups = static_cast<int64_t>(a.n) * a.chunks * a.cache.Hkv;
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess || row_blocks == 1 || a.whole) return static_cast<int>(e);
+    // the merge: up to 2048 workgroups, of 8 rows and more each
+    const int64_t groups = loads * a.cache.Hkv, slices = 2048 / (groups < 2048 ? groups : 2048);
+    a.slices = static_cast<int>(slices < s.rows / 8 ? slices : s.rows / 8);
     if (groups * a.slices > 0x7FFFFFFF) return static_cast<int>(hipErrorInvalidConfiguration);
     hipLaunchKernelGGL((tree_merge_kernel<D>), dim3(static_cast<unsigned>(groups * a.slices)), dim3(256), 0, st, a);
     return static_cast<int>(hipGetLastError());
@@ -918,20 +954,9 @@ int launch_tree_attn(TreeArgs a, const TreeShape& s, void* stream) {
     a.chunks = s.chunks;
     a.items = s.items;
     a.rounds = s.rounds;
-    // At least 256 keys to a piece: four users' tokens 13.1 us, with 128 15.6, with 512 13.4; 64-token trees of six requests 44, 55, 50.
-    a.least_share = s.rows == 128 || a.cache.d == 64 ? 4 : 8;
-    const int64_t loads = static_cast<int64_t>(a.n) * a.chunks;
-    if (15 * loads <= 7 * a.items) a.rounds = 0;
-    // (workgroups without a piece take 3 us, two at a time on a unit: there are no more of them than a round)
-    const int64_t workgroups = (a.rounds == 0 ? a.items : loads + a.items / 2) * a.cache.Hkv;
-    // the merge: up to 2048 workgroups, of 8 rows and more each
-    const int64_t groups = static_cast<int64_t>(a.n) * a.chunks * a.cache.Hkv, slices = 2048 / (groups < 2048 ? groups : 2048);
-    a.slices = static_cast<int>(slices < s.rows / 8 ? slices : s.rows / 8);
-    const dim3 grid(static_cast<unsigned>(workgroups));
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const int row_blocks = s.rows / 16;
-    if (a.cache.d == 128) return a.cache.f8 ? launch<128, true>(a, row_blocks, grid, st) : launch<128, false>(a, row_blocks, grid, st);
-    return a.cache.f8 ? launch<64, true>(a, row_blocks, grid, st) : launch<64, false>(a, row_blocks, grid, st);
+    if (a.cache.d == 128) return a.cache.f8 ? launch<128, true>(a, s, st) : launch<128, false>(a, s, st);
+    return a.cache.f8 ? launch<64, true>(a, s, st) : launch<64, false>(a, s, st);
 }
 
 }  // namespace pk
