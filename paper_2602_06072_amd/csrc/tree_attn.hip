@@ -666,13 +666,15 @@ __global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(
             load(x, at, tile + SETS * STRIDE);
             tile += STRIDE;
         };
-        for (;;) {                                                 // (left by jumps: a flag to leave by keeps all sets alive)
-            if (tile >= whole) goto others;
+        // (the loop has one way out: from another in the middle the compiler would take the younger set for the one that it has to wait for)
+        while (tile + STRIDE < whole) {
             turn(r[0], places[0]);
-            if (tile >= whole) { r[0] = r[1]; goto others; }
             turn(r[1], places[1]);
         }
-    others:
+        if (tile < whole) {
+            turn(r[0], places[0]);
+            r[0] = r[1];
+        }
         while (tile < t1) {
             step(r[0], tile, std::true_type{});
             tile += STRIDE;
@@ -847,24 +849,21 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 && F8 ? 3 : 2) void tree_attn_
         load(r0, p0, t0 + 2);
         // Tiles that every row sees whole, then the others, as in tree_attn_kernel.  A tile is requested three turns before it is used: two of them in registers.
         int tile = t0;
-        for (;;) {
-            if (tile >= whole) goto others;
+        const auto turn = [&](Quarter& r, int& p, const int stage) {
             all_here();
-            put(r1, 1);
-            load(r1, p1, tile + 3);
-            if (works) for (int x = x0; x < x1; ++x) step(tile, 0, x, std::false_type{});
+            put(r, stage ^ 1);
+            load(r, p, tile + 3);
+            if (works) for (int x = x0; x < x1; ++x) step(tile, stage, x, std::false_type{});
             ++tile;
-            if (tile >= whole) {
-                r1 = r0;
-                goto others;
-            }
-            all_here();
-            put(r0, 0);
-            load(r0, p0, tile + 3);
-            if (works) for (int x = x0; x < x1; ++x) step(tile, 1, x, std::false_type{});
-            ++tile;
+        };
+        while (tile + 1 < whole) {                                 // (one way out, as there)
+            turn(r1, p1, 0);
+            turn(r0, p0, 1);
         }
-    others:
+        if (tile < whole) {
+            turn(r1, p1, 0);
+            r1 = r0;
+        }
         while (tile < t1) {
             const int stage = (tile - t0) & 1;
             all_here();
