@@ -73,7 +73,9 @@ struct TreeArgs {
     int2* pieces_of;                                // [n] pieces of a request and slot of the first one, for the merge in a launch of its own
     float* part_lse; float* part_o;                 // [slots][Hkv][rows], [..][d]
     // set by the launch
-    int heads_per_kv, subs, rows_of_chunk, chunks, items, rounds, least_share, least_of_many, slices, whole;     // subs: sub-tiles of 16 keys in a page; least_share: tiles of a piece
+    int heads_per_kv, subs, most_keys, chunk_shift, chunks, items, slices, whole;  // subs: sub-tiles of 16 keys in a page; chunk_shift: rows of a chunk, log2
+    float rounds, least_per_share, least_per_many;
+    FastDiv by_hkv, by_chunks;
     FastDiv by_r, by_subs;
 };
 int launch_tree_attn(TreeArgs a, const TreeShape& s, void* stream);

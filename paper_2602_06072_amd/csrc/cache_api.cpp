@@ -148,7 +148,7 @@ TreeShape TreeShape::of(const int max_q, const int Hq, const int Hkv, const int 
 // A piece has at least 4 / (items * rounds) of all tiles, and only requests of more than that are cut: twice as many slots hold the pieces of all.
 size_t TreeShape::partial_bytes(const int Hkv, const int d, const int compute_units) const {
     const int64_t most = Hkv > 2 * compute_units ? Hkv : 2 * compute_units;
-    return static_cast<size_t>(((rounds + 1) / 2 * most * rows * (d + 1) * 4 + 255) / 256 * 256);
+    return static_cast<size_t>((((rounds + 1) / 2 * most + 64) * rows * (d + 1) * 4 + 255) / 256 * 256);
 }
 
 extern "C" int pk_qk_norm_rope(const pk_rows* q, const pk_rows* k, const pk_rows* q_out, const pk_rows* k_out,

@@ -41,87 +41,90 @@ struct Piece {
     int chunks;
 };
 
+// The pieces of a launch follow from the lengths, and every wave finds its own from them: no table to be made on the host, none to be copied when lengths
+// change.  All of it is on the way to the first load, and its instructions come from memory in every launch: no division by a variable, and few instructions
+// (with integer divisions and eight candidates for the share 4.5 to 9 us, half of a short launch).
+//
 // Tiles of TOKENS keys that a request has, and chunks of rows that visit them (0: no rows).  A request with rows and no key has one piece, which writes zeros.
 struct Load { int tiles, chunks; };
 template <int TOKENS>
 __device__ __forceinline__ Load load_of(const TreeArgs& a, const int i) {
-    const int64_t most = static_cast<int64_t>(a.max_blocks) * a.cache.page;
-    const int len = static_cast<int>(min(static_cast<int64_t>(max(a.kv_lens[i], 0)), most));
-    const int rows = max(min(a.q_start[i + 1] - a.q_start[i], a.max_q), 0) * a.heads_per_kv;
-    return {(len + TOKENS - 1) / TOKENS, (rows + a.rows_of_chunk - 1) / a.rows_of_chunk};
+    const int in = min(i, a.n - 1), q0 = a.q_start[in], q1 = a.q_start[in + 1], len = min(max(a.kv_lens[in], 0), a.most_keys);
+    const int rows = i < a.n ? max(min(q1 - q0, a.max_q), 0) * a.heads_per_kv : 0;
+    return {(len + TOKENS - 1) / TOKENS, (rows + (1 << a.chunk_shift) - 1) >> a.chunk_shift};
 }
-__device__ __forceinline__ int pieces_of(const int tiles, const int share) { return max(1, (tiles + share - 1) / share); }
+// Pieces of a request, of `share` tiles and fewer.  Which side a division falls to that just comes out does not matter: every wave of every launch has the same.
+struct Shares {
+    float per_share;                                // 1 / share
+    int middle, last;                               // number of the first piece of the second and third kind; middle < 0: pieces in the order of requests
+};
+__device__ __forceinline__ int pieces_of(const int tiles, const float per_share) { return max(1, static_cast<int>(ceilf(static_cast<float>(tiles) * per_share))); }
 
-// The pieces of a launch follow from the lengths, and every wave finds its own from them: no table to be made on the host, none to be copied when lengths
-// change.  A piece has at most `share` tiles.
-//
-// Where one round of workgroups may hold them all, the share is the smallest of eight with which it does (a second, partly filled round takes as long as the
-// first).  Otherwise a piece is at most a part of what a workgroup's place gets to do, and long pieces come first (of more than half of the share, of more than a
-// quarter, the others), so that the launch ends with short ones.
-struct Shares { int share, middle, last; };         // middle, last: number of the first piece of the second and third kind; middle < 0: the one round, in the order of requests
-__device__ __forceinline__ int order_of(const Load w, const int share) {
-    const int k = pieces_of(w.tiles, share);
-    return k > 1 || 2 * w.tiles > share ? 0 : 4 * w.tiles > share ? 1 : 2;
+// Where one round of workgroups may hold all pieces, the share is the smallest of three with which it does (a second, partly filled round takes as long as the
+// first): a cut request has half a piece more than its tiles make, on average, and one more at most.  Otherwise a piece is a part of what a workgroup's place gets to
+// do, and long pieces come first (of more than half of the share, of more than a quarter, the others), so that the launch ends with short ones.
+__device__ __forceinline__ int kind_of(const int tiles, const float per_share) { return (2.f * tiles * per_share > 1.f ? 0 : 1) + (4.f * tiles * per_share > 1.f ? 0 : 1); }
+// The first 64 KEPT requests are read once, all at a time, and kept; beside streaming workgroups every further read takes 2 us and more.
+template <int KEPT> struct Loads { Load of[KEPT]; };
+template <int TOKENS, int KEPT>
+__device__ __forceinline__ Loads<KEPT> read_loads(const TreeArgs& a) {
+    Loads<KEPT> l{};
+#pragma unroll
+    for (int u = 0; u < KEPT; ++u)
+        if (64 * u < a.n) l.of[u] = load_of<TOKENS>(a, 64 * u + static_cast<int>(threadIdx.x & 63));
+    return l;
 }
-template <int TOKENS>
-__device__ __forceinline__ Shares share_of(const TreeArgs& a, int* counts) {
-    constexpr int STEPS = 8;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// each(first number, load of this lane's request) for 64 requests at a time, until it says that it is enough
+template <int TOKENS, int KEPT, class Each>
+__device__ __forceinline__ void for_loads(const TreeArgs& a, const Loads<KEPT>& l, Each each) {
+#pragma unroll
+    for (int u = 0; u < KEPT; ++u)
+        if (64 * u >= a.n || each(64 * u, l.of[u])) return;
+    for (int i0 = 64 * KEPT; i0 < a.n; i0 += 64)
+        if (each(i0, load_of<TOKENS>(a, i0 + static_cast<int>(threadIdx.x & 63)))) return;
+}
+template <int TOKENS, int KEPT>
+__device__ __forceinline__ Shares share_of(const TreeArgs& a, const Loads<KEPT>& l) {
     int total = 0, loads = 0;
-    for (int i = lane; i < a.n; i += 64) {
-        const Load w = load_of<TOKENS>(a, i);
+    for_loads<TOKENS>(a, l, [&](int, const Load w) {
         total += w.tiles * w.chunks;
         loads += w.chunks;
-    }
+        return false;
+    });
     total = last_lane(wave_prefix(total));
     loads = last_lane(wave_prefix(loads));
-    Shares s{0, -1, 0};
-    if (loads <= a.items) {
-        // eighths of an even share; with 7/15 of the places taken by uncut requests the 15 below always hold all
-        const auto candidate = [&](const int x) {
-            const int eighths = x < 3 ? 8 + x : x < 6 ? 6 + 2 * x : 4 * x - 4;     // 8, 9, 10, 12, 14, 16, 20, 24
-            return max(a.least_share, static_cast<int>((static_cast<int64_t>(total) * eighths + 8 * a.items - 1) / (8 * a.items)));
-        };
-        int fit[STEPS / kWaves] = {};
-        for (int i = lane; i < a.n; i += 64) {
-            const Load w = load_of<TOKENS>(a, i);
-#pragma unroll
-            for (int x = 0; x < STEPS / kWaves; ++x) fit[x] += w.chunks * pieces_of(w.tiles, candidate(wave + kWaves * x));
-        }
-#pragma unroll
-        for (int x = 0; x < STEPS / kWaves; ++x) {
-            const int all = last_lane(wave_prefix(fit[x]));
-            if (lane == 0) counts[wave + kWaves * x] = all;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int x = STEPS - 1; x >= 0; --x)
-            if (counts[x] <= a.items) s.share = candidate(x);
-        if (s.share > 0) return s;
+    const float least = a.least_per_share, tiles = static_cast<float>(max(total, 1)), places = static_cast<float>(a.items), taken = static_cast<float>(loads);
+    Shares s{0.f, -1, 0};
+    const bool one_round = taken <= 0.75f * places;
+    // the two shares to be looked at, or how many pieces are long and half as long
+    s.per_share = one_round ? min(least, (places - 0.5f * taken) / tiles) : min(a.least_per_many, places * a.rounds / tiles);
+    const float more = min(least, (places - 0.7f * taken) / tiles);
+    int first = 0, second = 0;
+    for_loads<TOKENS>(a, l, [&](int, const Load w) {
+        const int k = w.chunks * pieces_of(w.tiles, s.per_share), kind = kind_of(w.tiles, s.per_share);
+        first += one_round || kind == 0 ? k : 0;
+        second += one_round ? w.chunks * pieces_of(w.tiles, more) : kind == 1 ? k : 0;
+        return false;
+    });
+    first = last_lane(wave_prefix(first));
+    second = last_lane(wave_prefix(second));
+    if (one_round) {
+        if (first > a.items) s.per_share = second <= a.items ? more : min(least, (places - taken) / tiles);
+    } else {
+        s.middle = first;
+        s.last = first + second;
     }
-    s.share = max(a.least_of_many, static_cast<int>((4 * static_cast<int64_t>(total) + a.items * a.rounds - 1) / (a.items * a.rounds)));
-    int longs = 0, middles = 0;
-    for (int i = lane; i < a.n; i += 64) {
-        const Load w = load_of<TOKENS>(a, i);
-        const int k = w.chunks * pieces_of(w.tiles, s.share), o = order_of(w, s.share);
-        longs += o == 0 ? k : 0;
-        middles += o == 1 ? k : 0;
-    }
-    s.middle = last_lane(wave_prefix(longs));
-    s.last = s.middle + last_lane(wave_prefix(middles));
     return s;
 }
 // Piece number `item` of a KV head; false: there are fewer
-template <int TOKENS>
-__device__ __forceinline__ bool find_piece(const TreeArgs& a, const int item, const Shares& s, Piece& out) {
-    const int lane = threadIdx.x & 63;
-    const int order = s.middle < 0 ? -1 : item < s.middle ? 0 : item < s.last ? 1 : 2;
-    int before = order < 1 ? 0 : order == 1 ? s.middle : s.last, slots = 0;        // (only requests of the first kind are cut)
-    for (int i0 = 0; i0 < a.n; i0 += 64) {
-        const int i = min(i0 + lane, a.n - 1);
-        Load w = load_of<TOKENS>(a, i);
-        if (i0 + lane >= a.n || (order >= 0 && order_of(w, s.share) != order)) w.chunks = 0;
-        const int k = pieces_of(w.tiles, s.share), mine = k * w.chunks, upto = wave_prefix(mine), slots_upto = wave_prefix(k > 1 ? mine : 0);
+template <int TOKENS, int KEPT>
+__device__ __forceinline__ bool find_piece(const TreeArgs& a, const Loads<KEPT>& l, const int item, const Shares& s, Piece& out) {
+    const int kind = s.middle < 0 ? -1 : item < s.middle ? 0 : item < s.last ? 1 : 2;
+    int before = kind < 1 ? 0 : kind == 1 ? s.middle : s.last, slots = 0;          // (only requests of the first kind are cut)
+    bool found = false;
+    for_loads<TOKENS>(a, l, [&](const int i0, const Load w) {
+        const int k = pieces_of(w.tiles, s.per_share), mine = kind >= 0 && kind_of(w.tiles, s.per_share) != kind ? 0 : k * w.chunks;
+        const int upto = wave_prefix(mine), slots_upto = wave_prefix(k > 1 ? mine : 0);
         const uint64_t here = __ballot(item >= before + upto - mine && item < before + upto);
         if (here != 0) {
             const int from = __builtin_ctzll(here);
@@ -130,15 +133,16 @@ __device__ __forceinline__ bool find_piece(const TreeArgs& a, const int item, co
             out.request = i0 + from;
             out.pieces = of(k);
             out.chunks = of(w.chunks);
-            out.piece = local / out.chunks;
+            out.piece = static_cast<int>((static_cast<float>(local) + 0.5f) / static_cast<float>(out.chunks));       // (the chunks of a piece one after the other)
             out.chunk = local - out.piece * out.chunks;
             out.slot = slots + of(slots_upto - (k > 1 ? mine : 0)) + local;
-            return true;
+            return found = true;
         }
         before += last_lane(upto);
         slots += last_lane(slots_upto);
-    }
-    return false;
+        return false;
+    });
+    return found;
 }
 
 // The kernel's arguments, to be read anew: kept in registers over the loop of pieces they would leave too few scalar ones for the loop of tiles inside (trees of 64
@@ -151,19 +155,20 @@ __device__ __forceinline__ const TreeArgs& kernel_args() {
 
 // Runs `work(arguments, piece, KV head)` for the workgroup's pieces: the one of its number and, where there are more pieces than workgroups, those as many numbers on.
 // Workgroups go round-robin over the XCDs: with eight KV heads an XCD keeps to one, and the chunks of its rows find its keys in the L2.
-template <int TOKENS, class Work>
-__device__ __forceinline__ void run_pieces(int* counts, Work work) {
+template <int TOKENS, int KEPT, class Work>
+__device__ __forceinline__ void run_pieces(Work work) {
     if (const TreeArgs& a = kernel_args(); a.whole) {              // no request can have two pieces
-        const int rest = blockIdx.x / a.cache.Hkv, i = rest / a.chunks;
+        const int rest = a.by_hkv(blockIdx.x), i = a.by_chunks(rest);
         work(a, Piece{i, 0, 1, rest - i * a.chunks, 0, a.chunks}, static_cast<int>(blockIdx.x) - rest * a.cache.Hkv);
         return;
     }
-    const Shares shares = share_of<TOKENS>(kernel_args(), counts);
+    const Loads<KEPT> loads = read_loads<TOKENS, KEPT>(kernel_args());
+    const Shares shares = share_of<TOKENS>(kernel_args(), loads);
     for (int item = blockIdx.x;; item += gridDim.x) {
         const TreeArgs& a = kernel_args();
         Piece w;
-        const int rest = item / a.cache.Hkv, kvh = item - rest * a.cache.Hkv;
-        if (!find_piece<TOKENS>(a, rest, shares, w)) return;
+        const int rest = a.by_hkv(item), kvh = item - rest * a.cache.Hkv;
+        if (!find_piece<TOKENS>(a, loads, rest, shares, w)) return;
         work(a, w, kvh);
         if (shares.middle < 0) return;
         __syncthreads();
@@ -249,13 +254,20 @@ __device__ __forceinline__ Bounds bounds_of(const TreeArgs& a, const Piece& w) {
     const int i = w.request, asked = a.q_start[i + 1] - a.q_start[i];
     b.q0 = min(max(static_cast<int64_t>(a.q_start[i]), int64_t{0}), a.total_q);
     b.rows = static_cast<int>(min(static_cast<int64_t>(min(asked, a.max_q)), a.total_q - b.q0)) * a.heads_per_kv;
-    b.row0 = w.chunk * a.rows_of_chunk;
-    b.rows_here = min(b.rows - b.row0, a.rows_of_chunk);
-    b.len = static_cast<int>(min(static_cast<int64_t>(max(a.kv_lens[i], 0)), static_cast<int64_t>(a.max_blocks) * a.cache.page));
+    b.row0 = w.chunk << a.chunk_shift;
+    b.rows_here = min(b.rows - b.row0, 1 << a.chunk_shift);
+    b.len = min(max(a.kv_lens[i], 0), a.most_keys);
     b.ctx = a.kv_lens[i] - asked;
     b.tiles = (b.len + TOKENS - 1) / TOKENS;
-    b.t0 = static_cast<int>(static_cast<int64_t>(b.tiles) * w.piece / w.pieces);
-    b.t1 = static_cast<int>(static_cast<int64_t>(b.tiles) * (w.piece + 1) / w.pieces);
+    // pieces of as many tiles but the last, which may have fewer (or none): the smallest number of which `pieces` are enough
+    int each = b.tiles;
+    if (w.pieces > 1) {
+        each = static_cast<int>(static_cast<float>(b.tiles) / static_cast<float>(w.pieces));
+        each += each * w.pieces < b.tiles ? 1 : 0;
+        each += each * w.pieces < b.tiles ? 1 : 0;
+    }
+    b.t0 = min(w.piece * each, b.tiles);
+    b.t1 = min(b.t0 + each, b.tiles);
     b.table = a.block_table + static_cast<int64_t>(i) * a.max_blocks;
     return b;
 }
@@ -444,7 +456,7 @@ __device__ __forceinline__ void finish(const TreeArgs& a, const Piece& w, const 
     float* po = reinterpret_cast<float*>(lds);      // [wave][16][PITCH]
     float* pm = po + kWaves * 16 * PITCH;           // [wave][16]
     float* pl = pm + kWaves * 16;
-    const auto part_row = [&](const int piece) { return (static_cast<int64_t>(w.slot + (piece - w.piece) * w.chunks) * a.cache.Hkv + kvh) * a.rows_of_chunk; };
+    const auto part_row = [&](const int piece) { return (static_cast<int64_t>(w.slot + (piece - w.piece) * w.chunks) * a.cache.Hkv + kvh) * (1 << a.chunk_shift); };
     const auto out_at = [&](const int local, const int col) {
         const int row = bounds.row0 + local, t = a.by_r(row);
         return ((bounds.q0 + t) * a.Hq + kvh * a.heads_per_kv + row - t * a.heads_per_kv) * D + col;
@@ -512,7 +524,7 @@ __device__ __forceinline__ void finish(const TreeArgs& a, const Piece& w, const 
     }
     __syncthreads();
     if (*last == 0) return;
-    const int apart = w.chunks * a.cache.Hkv * a.rows_of_chunk;    // rows from a piece to the next
+    const int apart = w.chunks * a.cache.Hkv * (1 << a.chunk_shift);    // rows from a piece to the next
     const auto o_rows = __builtin_amdgcn_make_buffer_rsrc(a.part_o + part_row(0) * D, 0, 0x7FFFFFFF, 0x00020000);
     const auto lse_rows = __builtin_amdgcn_make_buffer_rsrc(a.part_lse + part_row(0), 0, 0x7FFFFFFF, 0x00020000);
     for (int x = threadIdx.x; x < bounds.rows_here * (D / 4); x += 64 * kWaves) {
@@ -533,7 +545,7 @@ __global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(
     using Regs = TileRegs<D, F8, N>;
     constexpr int CH = Regs::CH, TOKENS = 16 * N, KS = D / 32, VT = D / 16, SIZE = F8 ? 1 : 2, STRIDE = ALONE ? 1 : kWaves;
     __shared__ __align__(16) unsigned char lds[kJoinBytes<D>];
-    __shared__ int counts[8], last;
+    __shared__ int last;
 
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6)), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const auto work = [&](const TreeArgs& a, const Piece& w, const int kvh) {
@@ -686,10 +698,10 @@ __global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(
     };
     if constexpr (ALONE) {
         const TreeArgs& a = kernel_args();
-        const int item = blockIdx.x * kWaves + wave, rest = item / a.cache.Hkv, i = rest / a.chunks;
+        const int item = blockIdx.x * kWaves + wave, rest = a.by_hkv(item), i = a.by_chunks(rest);
         if (i < a.n) work(a, Piece{i, 0, 1, rest - i * a.chunks, 0, a.chunks}, item - rest * a.cache.Hkv);
     } else {
-        run_pieces<TOKENS>(counts, work);
+        run_pieces<TOKENS, 4>(work);
     }
 }
 
@@ -712,9 +724,9 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 && F8 ? 3 : 2) void tree_attn_
     constexpr int NB = 2, N = 4, TOKENS = 64, KS = D / 32, VT = D / 16, CH = F8 ? D / 64 : D / 32, SIZE = F8 ? 1 : 2;
     constexpr int K_BYTES = N * KS * 1024, STAGE = 2 * K_BYTES;
     __shared__ __align__(16) unsigned char lds[2 * STAGE > kJoinBytes<D> ? 2 * STAGE : kJoinBytes<D>];
-    __shared__ int counts[8], last;
+    __shared__ int last;
 
-    run_pieces<TOKENS>(counts, [&](const TreeArgs& a, const Piece& w, const int kvh) {
+    run_pieces<TOKENS, 2>([&](const TreeArgs& a, const Piece& w, const int kvh) {
     const Bounds bounds = bounds_of<TOKENS>(a, w);
     if (bounds.rows_here <= 0) return;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6)), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
@@ -887,14 +899,14 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a) {
     const int asked = a.q_start[i + 1] - a.q_start[i];
     const int64_t q0 = min(max(static_cast<int64_t>(a.q_start[i]), int64_t{0}), a.total_q);
     const int rows = static_cast<int>(min(static_cast<int64_t>(min(asked, a.max_q)), a.total_q - q0)) * a.heads_per_kv;
-    const int here = min(rows - chunk * a.rows_of_chunk, a.rows_of_chunk);
+    const int here = min(rows - chunk * (1 << a.chunk_shift), (1 << a.chunk_shift));
     if (here <= 0) return;
     const int2 p = a.pieces_of[i];
     if (p.x == 1) return;
-    const int chunks = (rows + a.rows_of_chunk - 1) / a.rows_of_chunk;
-    const auto part_row = [&](const int piece) { return (static_cast<int64_t>(p.y + piece * chunks + chunk) * a.cache.Hkv + kvh) * a.rows_of_chunk; };
+    const int chunks = (rows + (1 << a.chunk_shift) - 1) / (1 << a.chunk_shift);
+    const auto part_row = [&](const int piece) { return (static_cast<int64_t>(p.y + piece * chunks + chunk) * a.cache.Hkv + kvh) * (1 << a.chunk_shift); };
     for (int x = slice * 256 + threadIdx.x; x < here * (D / 4); x += a.slices * 256) {
-        const int local = x / (D / 4), col = 4 * (x % (D / 4)), row = chunk * a.rows_of_chunk + local, t = a.by_r(row);
+        const int local = x / (D / 4), col = 4 * (x % (D / 4)), row = chunk * (1 << a.chunk_shift) + local, t = a.by_r(row);
         store4(a, ((q0 + t) * a.Hq + kvh * a.heads_per_kv + row - t * a.heads_per_kv) * D + col, merged(p.x, [&](const int piece, float& lse, floatx4& o) {
             const int64_t at = part_row(piece) + local;
             lse = a.part_lse[at];
@@ -913,14 +925,15 @@ template <int D, bool F8>
 int launch(TreeArgs a, const TreeShape& s, hipStream_t st) {
     const dim3 block(64 * kWaves);
     const int row_blocks = s.rows / 16, keys = 16 * (row_blocks == 1 ? kSubTiles1<D, F8> : row_blocks == 2 ? kSubTiles2<D, F8> : 4);
-    a.least_share = kLeastKeys / keys;
+    a.least_per_share = static_cast<float>(keys) / kLeastKeys;
     const int64_t loads = static_cast<int64_t>(a.n) * a.chunks, most_keys = static_cast<int64_t>(a.max_blocks) * a.cache.page;
     a.whole = most_keys <= kLeastKeys;              // no request can have two pieces: nothing to be found out, nothing to be put together
-    a.least_of_many = (s.rows == 128 ? 4 : 1) * a.least_share;     // (cut into more, the partial results of 128 rows are more bytes than the keys)
+    a.least_per_many = a.least_per_share / (s.rows == 128 ? 4 : 1);        // (cut into more, the partial results of 128 rows are more bytes than the keys)
     // Short requests, and more of them than workgroups run at once: a wave for every request and 32 rows.
     if (const int64_t units = static_cast<int64_t>(a.n) * a.cache.Hkv * s.alone_chunks; a.whole && loads > a.items && units <= 0x7FFFFFFF) {
         a.chunks = s.alone_chunks;
-        a.rows_of_chunk = s.rows == 16 ? 16 : 32;
+        a.chunk_shift = s.rows == 16 ? 4 : 5;
+        a.by_chunks = FastDiv::by(static_cast<uint32_t>(a.chunks));
         const dim3 grid(static_cast<unsigned>((units + kWaves - 1) / kWaves));
         if (row_blocks == 1) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 1, kSubTiles1<D, F8>, 2, 2, true>), grid, block, 0, st, a);
         else hipLaunchKernelGGL((tree_attn_kernel<D, F8, 2, kSubTiles2<D, F8>, 2, kWavesOf2<D, F8>, true>), grid, block, 0, st, a);
@@ -949,10 +962,13 @@ int launch_tree_attn(TreeArgs a, const TreeShape& s, void* stream) {
     a.by_r = FastDiv::by(static_cast<uint32_t>(a.heads_per_kv));
     a.subs = a.cache.page / 16;
     a.by_subs = FastDiv::by(static_cast<uint32_t>(a.subs));
-    a.rows_of_chunk = s.rows;
+    a.chunk_shift = s.rows == 16 ? 4 : s.rows == 32 ? 5 : 7;
     a.chunks = s.chunks;
+    a.by_chunks = FastDiv::by(static_cast<uint32_t>(a.chunks));
+    a.by_hkv = FastDiv::by(static_cast<uint32_t>(a.cache.Hkv));
+    a.most_keys = a.max_blocks * a.cache.page;      // (fewer than 2^31)
     a.items = s.items;
-    a.rounds = s.rounds;
+    a.rounds = s.rounds / 4.f;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (a.cache.d == 128) return a.cache.f8 ? launch<128, true>(a, s, st) : launch<128, false>(a, s, st);
     return a.cache.f8 ? launch<64, true>(a, s, st) : launch<64, false>(a, s, st);
