@@ -34,7 +34,7 @@ struct TokenRowsArgs {
     int64_t tokens; int Hq, Hkv, d;
     int in_f32, out_f32;
     // set by the launch
-    int splits, axes_by_four; FastDiv by_splits; float one_by_d;       // waves that share a token's heads; whether four pairs in a row have one axis
+    int splits, axes_by_four; FastDiv by_splits; double by_d;       // waves that share a token's heads; whether four pairs in a row have one axis
 };
 int launch_token_rows(TokenRowsArgs a, void* stream);
 
@@ -50,8 +50,9 @@ struct CacheKeepArgs {
     CacheView cache; const int32_t* block_table; int32_t max_blocks;
     const int32_t* kv_lens; const int32_t* q_start; int32_t n;
     const int32_t* keep; int32_t max_keep; const int32_t* keep_count; int32_t* new_lens;
+    FastDiv by_page;
 };
-int launch_cache_keep(const CacheKeepArgs& a, void* stream);
+int launch_cache_keep(CacheKeepArgs a, void* stream);
 
 // How a launch takes the rows of a (request, KV head): `chunks` workgroups of up to `rows` of them for every piece of the request's keys; `items` workgroups of a
 // KV head run at once; of more requests than that a piece has at most 4 / rounds of what a workgroup's place gets to do.

@@ -11,13 +11,21 @@ constexpr int kWaves = 4;
 
 // sum and maximum over aligned groups of LPR lanes (8, 16 or 32), in every lane of them
 template <int CTRL>
-__device__ __forceinline__ float dpp(const float x) { return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xF, 0xF, true)); }
-template <int LPR, class Op>
-__device__ __forceinline__ float over_row(float x, Op op) {
-    x = op(x, dpp<0xB1>(x));                        // quad_perm [1,0,3,2]
-    x = op(x, dpp<0x4E>(x));                        // quad_perm [2,3,0,1]
-    x = op(x, dpp<0x141>(x));                       // row_half_mirror: the other four of eight
-    if constexpr (LPR >= 16) x = op(x, dpp<0x140>(x));     // row_mirror: the other eight of sixteen
+__device__ __forceinline__ uint32_t dpp(const uint32_t x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xF, 0xF, true); }
+template <int CTRL, class T>
+__device__ __forceinline__ T from_lane(const T x) {
+    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(T, dpp<CTRL>(__builtin_bit_cast(uint32_t, x)));
+    else {
+        const uint2 y = __builtin_bit_cast(uint2, x);
+        return __builtin_bit_cast(T, make_uint2(dpp<CTRL>(y.x), dpp<CTRL>(y.y)));
+    }
+}
+template <int LPR, class T, class Op>
+__device__ __forceinline__ T over_row(T x, Op op) {
+    x = op(x, from_lane<0xB1>(x));                  // quad_perm [1,0,3,2]
+    x = op(x, from_lane<0x4E>(x));                  // quad_perm [2,3,0,1]
+    x = op(x, from_lane<0x141>(x));                 // row_half_mirror: the other four of eight
+    if constexpr (LPR >= 16) x = op(x, from_lane<0x140>(x));       // row_mirror: the other eight of sixteen
     if constexpr (LPR >= 32) x = op(x, __shfl_xor(x, 16, 64));
     return x;
 }
@@ -67,12 +75,57 @@ __device__ __forceinline__ void swap32(uint32_t& x, uint32_t& y) {
     x = p[0]; y = p[1];
 }
 
-enum Kind { kQuery, kKey, kValue };
+// x as a float that rounds to fewer bits as x itself does: toward zero, with an odd last bit where anything was cut off (an infinity where x is out of range)
+__device__ __forceinline__ float odd_float(const double x) {
+    const float f = static_cast<float>(x);
+    const double back = f;
+    uint32_t b = __float_as_uint(f);
+    if (fabs(back) > fabs(x) && fabsf(f) < INFINITY) b -= 1;
+    if (back != x && fabsf(f) < INFINITY) b |= 1;
+    return __uint_as_float(b);
+}
+__device__ __forceinline__ float odd_float(const float x) { return x; }
+
+// Norm and rotation of a lane's eight columns in T
+template <class T, int LPR>
+__device__ __forceinline__ void norm_and_turn(Eight& row, const bool normed, const Eight& w, const T by_d, const T eps, const bool rotated, const bool interleaved,
+                                              const floatx4 cs, const floatx4 sn) {
+    T y[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { y[e] = row.a[e]; y[4 + e] = row.b[e]; }
+    if (normed) {
+        T sum = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum = fma(y[e], y[e], fma(y[4 + e], y[4 + e], sum));
+        sum = over_row<LPR>(sum, [](const T p, const T q) { return p + q; });
+        const T inv = T(1) / sqrt(fma(sum, by_d, eps));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { y[e] *= inv * w.a[e]; y[4 + e] *= inv * w.b[e]; }
+    }
+    if (rotated) {
+        const auto turn = [&](const int i, const int j, const T c, const T n) {
+            const T p = y[i], q = y[j];
+            y[i] = fma(p, c, -q * n);
+            y[j] = fma(q, c, p * n);
+        };
+        if (interleaved) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) turn(2 * e, 2 * e + 1, cs[e], sn[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) turn(e, 4 + e, cs[e], sn[e]);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { row.a[e] = odd_float(y[e]); row.b[e] = odd_float(y[4 + e]); }
+}
+
+enum Kind { kQuery, kKey, kCachedKey, kCachedValue };
 
 // One wave for four consecutive tokens (two with LPR = 32), a head of theirs (two with LPR = 8) at a time: LPR lanes share a row, eight columns each.
 // A pair's two columns are in one lane (halves: four columns of either half), so that the rotation needs no exchange, and the cosines and sines of a
 // token are loaded once for all the heads that a wave takes.  Four tokens at once because the cache interleaves the values of four.
-template <int LPR, bool IN_F32, bool OUT_F32>
+template <int LPR, bool IN_F32, bool OUT_F32, bool CACHED>
 __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a) {
     constexpr int TOKENS = LPR == 32 ? 2 : 4, HEADS = LPR == 8 ? 2 : 1, BATCH = 4;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(blockIdx.x * kWaves + (threadIdx.x >> 6))), lane = threadIdx.x & 63;
@@ -82,7 +135,7 @@ __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a
     const int sub = lane / (64 / TOKENS), of = HEADS == 1 ? 0 : lane >> 3 & 1, x = lane % LPR;
     const bool token_ok = t0 + sub < a.tokens, columns_ok = 8 * x < a.d;
     const int64_t t = token_ok ? t0 + sub : a.tokens - 1;
-    const int steps_q = (a.Hq + HEADS - 1) / HEADS, steps_k = (a.Hkv + HEADS - 1) / HEADS, steps = steps_q + (a.k_out.data ? 1 : 2) * steps_k;
+    const int steps_q = (a.Hq + HEADS - 1) / HEADS, steps_k = (a.Hkv + HEADS - 1) / HEADS, steps = steps_q + (CACHED ? 2 : 1) * steps_k;
     const int first = static_cast<int>(static_cast<int64_t>(steps) * split / a.splits), last = static_cast<int>(static_cast<int64_t>(steps) * (split + 1) / a.splits);
 
     // columns of a row that is rotated, and of one that is not
@@ -111,7 +164,7 @@ __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a
     int64_t block = 0;
     int off = 0;
     bool slot_ok = false, whole = false;            // whole: the four tokens fill four interleaved places
-    if (!a.k_out.data && last > steps_q) {
+    if (CACHED && last > steps_q) {
         const int64_t slot = a.slots[t];
         slot_ok = token_ok && slot >= 0 && slot < a.cache.num_blocks * a.cache.page;
         block = slot_ok ? slot / a.cache.page : 0;
@@ -121,7 +174,7 @@ __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a
 
     const auto run = [&](auto what, const int from, const int to, const int heads, const RowsView& in, const RowsView& out, const void* weight) {
         constexpr Kind KIND = decltype(what)::value;
-        const bool turns = KIND != kValue;
+        constexpr bool turns = KIND != kCachedValue;
         const int ca = turns ? turn_a : plain_a, cb = turns ? turn_b : plain_b;
         Eight w;
         const bool normed = weight != nullptr;
@@ -140,36 +193,13 @@ __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a
                 const bool row_ok = token_ok && columns_ok && h < heads;
                 Eight y = widened<IN_F32>(raw[s]);
                 if (!columns_ok) y = Eight{};
-                if (KIND != kValue && normed) {
-                    float sum = 0.f;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) sum = fmaf(y.a[e], y.a[e], fmaf(y.b[e], y.b[e], sum));
-                    sum = over_row<LPR>(sum, [](float p, float q) { return p + q; });
-                    const float inv = 1.f / sqrtf(fmaf(sum, a.one_by_d, a.eps));
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) { y.a[e] *= inv * w.a[e]; y.b[e] *= inv * w.b[e]; }
-                }
-                if (KIND != kValue && rotated) {
-                    const auto turn = [](float& p, float& q, const float c, const float n) {
-                        const float p0 = p, q0 = q;
-                        p = fmaf(p0, c, -q0 * n);
-                        q = fmaf(q0, c, p0 * n);
-                    };
-                    if (a.interleaved) {
-                        turn(y.a[0], y.a[1], cs[0], sn[0]);
-                        turn(y.a[2], y.a[3], cs[1], sn[1]);
-                        turn(y.b[0], y.b[1], cs[2], sn[2]);
-                        turn(y.b[2], y.b[3], cs[3], sn[3]);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) turn(y.a[e], y.b[e], cs[e], sn[e]);
-                    }
-                }
-                if (KIND == kQuery || (KIND == kKey && a.k_out.data)) {
+                // A key of the cache in 64 bits: it is stored with few bits, and one that lies by the middle between two of them goes to the nearer (in 32 bits
+                // some three in a million go to the other, which 8 bits hold 6% apart).  Eight lanes' work of 80 rows, and no time at any size.
+                if (KIND == kCachedKey && (normed || a.table)) norm_and_turn<double, LPR>(y, normed, w, a.by_d, a.eps, rotated, a.interleaved, cs, sn);
+                else if (turns) norm_and_turn<float, LPR>(y, normed, w, static_cast<float>(a.by_d), a.eps, rotated, a.interleaved, cs, sn);
+                if constexpr (KIND == kQuery || KIND == kKey) {
                     if (row_ok) store_eight<OUT_F32>(out.data, t * out.token_stride + h * out.head_stride, ca, cb, y);
-                    continue;
-                }
-                if constexpr (LPR <= 16) {
+                } else {
                     const bool cell_ok = row_ok && slot_ok;
                     const int64_t base = (block * a.cache.Hkv + h) * a.cache.page;
                     if (a.cache.f8) {
@@ -181,8 +211,8 @@ __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a
                         const float inv = scale_inverse(byte);
                         uint32_t c0 = pack_f8x2(y.a[0], y.a[1], inv) | pack_f8x2(y.a[2], y.a[3], inv) << 16;
                         uint32_t c1 = pack_f8x2(y.b[0], y.b[1], inv) | pack_f8x2(y.b[2], y.b[3], inv) << 16;
-                        if (cell_ok && x == 0) a.cache.scales[2 * base + (KIND == kValue ? a.cache.page : 0) + off] = static_cast<uint8_t>(byte);
-                        if constexpr (KIND == kKey) {
+                        if (cell_ok && x == 0) a.cache.scales[2 * base + (KIND == kCachedValue ? a.cache.page : 0) + off] = static_cast<uint8_t>(byte);
+                        if constexpr (KIND == kCachedKey) {
                             uint8_t* k = static_cast<uint8_t*>(a.cache.k) + (base + off) * a.d;
                             if (cell_ok) {
                                 *reinterpret_cast<uint32_t*>(k + ca) = c0;
@@ -206,7 +236,7 @@ __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a
                         }
                     } else {
                         uint32_t p[4] = {pack_bf16x2(y.a[0], y.a[1]), pack_bf16x2(y.a[2], y.a[3]), pack_bf16x2(y.b[0], y.b[1]), pack_bf16x2(y.b[2], y.b[3])};
-                        if constexpr (KIND == kKey) {
+                        if constexpr (KIND == kCachedKey) {
                             uint16_t* k = static_cast<uint16_t*>(a.cache.k) + (base + off) * a.d;
                             if (cell_ok) {
                                 *reinterpret_cast<uint2*>(k + ca) = make_uint2(p[0], p[1]);
@@ -236,8 +266,8 @@ __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a
     };
     run(std::integral_constant<Kind, kQuery>{}, min(first, steps_q), min(last, steps_q), a.Hq, a.q, a.q_out, a.q_weight);
     const int k0 = steps_q, k1 = steps_q + steps_k;
-    run(std::integral_constant<Kind, kKey>{}, min(max(first, k0), k1) - k0, min(max(last, k0), k1) - k0, a.Hkv, a.k, a.k_out, a.k_weight);
-    run(std::integral_constant<Kind, kValue>{}, max(first, k1) - k1, max(last, k1) - k1, a.Hkv, a.v, a.k_out, nullptr);
+    run(std::integral_constant<Kind, CACHED ? kCachedKey : kKey>{}, min(max(first, k0), k1) - k0, min(max(last, k0), k1) - k0, a.Hkv, a.k, a.k_out, a.k_weight);
+    if constexpr (CACHED) run(std::integral_constant<Kind, kCachedValue>{}, max(first, k1) - k1, max(last, k1) - k1, a.Hkv, a.v, a.k_out, nullptr);
 }
 
 // The request that unit `item` of the launch belongs to, and its number there, where request i has units(i) of them: prefix sums of them all,
@@ -363,38 +393,61 @@ __global__ __launch_bounds__(64 * kWaves) void cache_read_kernel(CacheReadArgs a
     }
 }
 
-// One workgroup for a (request, KV head).  A lane moves the same columns of every kept row, first to last: what it overwrites are rows that it
-// has moved already or that nobody keeps, since keep[j] >= j, and no other lane touches them.
+// One workgroup for a (request, KV head), a lane for a column.  Bound by latency: lengths and numbers, then pages, then the rows, each of them read for eight rows at
+// a time.  All of them may be read before the first is stored, since keep rises: a kept row lies behind every place that an earlier one moves to.
 template <class T>
 __global__ __launch_bounds__(128) void cache_keep_kernel(CacheKeepArgs a) {
+    constexpr int BATCH = 8;
     const int i = blockIdx.x, h = blockIdx.y, lane = threadIdx.x;
     const CacheView& c = a.cache;
-    const int drafts = a.q_start[i + 1] - a.q_start[i];
-    const int base = a.kv_lens[i] - drafts;
+    const int drafts = a.q_start[i + 1] - a.q_start[i], base = a.kv_lens[i] - drafts;
     const int count = min(max(min(a.keep_count[i], a.max_keep), 0), max(drafts, 0));
     if (h == 0 && lane == 0) a.new_lens[i] = base + count;
     const int32_t* row = a.block_table + static_cast<int64_t>(i) * a.max_blocks;
+    const int32_t* keep = a.keep + static_cast<int64_t>(i) * a.max_keep;
     const int end = static_cast<int>(min(static_cast<int64_t>(a.max_blocks) * c.page, static_cast<int64_t>(0x7FFFFFFF)));
-    for (int j = 0; j < count; ++j) {
-        const int from = a.keep[static_cast<int64_t>(i) * a.max_keep + j];
-        if (from <= j || from >= drafts || base + j < 0 || base + from >= end) continue;      // in its place already, or no drafted token
-        const int s = base + from, t = base + j;
-        const int64_t sb = block_of(c, row, s / c.page), tb = block_of(c, row, t / c.page);
-        if (lane < c.d) {
-            static_cast<T*>(c.k)[k_index(c, tb, t % c.page, h, lane)] = static_cast<const T*>(c.k)[k_index(c, sb, s % c.page, h, lane)];
-            static_cast<T*>(c.v)[v_index(c, tb, t % c.page, h, lane)] = static_cast<const T*>(c.v)[v_index(c, sb, s % c.page, h, lane)];
+    if (end == 0 || lane >= c.d) return;
+    T* k = static_cast<T*>(c.k);
+    T* v = static_cast<T*>(c.v);
+    for (int j0 = 0; j0 < count; j0 += BATCH) {
+        bool moves[BATCH];
+        int64_t from[BATCH], to[BATCH];             // physical block
+        int from_off[BATCH], to_off[BATCH];
+        T kept_k[BATCH], kept_v[BATCH];
+        uint8_t scale[BATCH];
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+            const int j = min(j0 + u, count - 1), f = keep[j];
+            moves[u] = j0 + u < count && f > j && f < drafts && base + j >= 0 && base + f < end;     // not in its place already, and a drafted token
+            const int s = moves[u] ? base + f : 0, t = moves[u] ? base + j : 0, sp = a.by_page(s), tp = a.by_page(t);
+            from[u] = block_of(c, row, sp);
+            to[u] = block_of(c, row, tp);
+            from_off[u] = s - sp * c.page;
+            to_off[u] = t - tp * c.page;
         }
-        if (c.f8 && lane < 2) c.scales[scale_index(c, tb, t % c.page, h, lane)] = c.scales[scale_index(c, sb, s % c.page, h, lane)];
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+            kept_k[u] = k[k_index(c, from[u], from_off[u], h, lane)];
+            kept_v[u] = v[v_index(c, from[u], from_off[u], h, lane)];
+            scale[u] = c.f8 && lane < 2 ? c.scales[scale_index(c, from[u], from_off[u], h, lane)] : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+            if (!moves[u]) continue;
+            k[k_index(c, to[u], to_off[u], h, lane)] = kept_k[u];
+            v[v_index(c, to[u], to_off[u], h, lane)] = kept_v[u];
+            if (c.f8 && lane < 2) c.scales[scale_index(c, to[u], to_off[u], h, lane)] = scale[u];
+        }
     }
 }
 
-template <int LPR>
+template <int LPR, bool CACHED>
 void launch_rows(const TokenRowsArgs& a, const dim3 grid, hipStream_t st) {
     const dim3 block(64 * kWaves);
-    if (a.in_f32 && a.out_f32) hipLaunchKernelGGL((token_rows_kernel<LPR, true, true>), grid, block, 0, st, a);
-    else if (a.in_f32) hipLaunchKernelGGL((token_rows_kernel<LPR, true, false>), grid, block, 0, st, a);
-    else if (a.out_f32) hipLaunchKernelGGL((token_rows_kernel<LPR, false, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((token_rows_kernel<LPR, false, false>), grid, block, 0, st, a);
+    if (a.in_f32 && a.out_f32) hipLaunchKernelGGL((token_rows_kernel<LPR, true, true, CACHED>), grid, block, 0, st, a);
+    else if (a.in_f32) hipLaunchKernelGGL((token_rows_kernel<LPR, true, false, CACHED>), grid, block, 0, st, a);
+    else if (a.out_f32) hipLaunchKernelGGL((token_rows_kernel<LPR, false, true, CACHED>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((token_rows_kernel<LPR, false, false, CACHED>), grid, block, 0, st, a);
 }
 
 template <int D, bool F8>
@@ -414,7 +467,7 @@ int launch_token_rows(TokenRowsArgs a, void* stream) {
     const int64_t splits = wanted > eighths ? wanted : eighths;
     a.splits = static_cast<int>(splits < steps ? splits : steps);
     a.by_splits = FastDiv::by(static_cast<uint32_t>(a.splits));
-    a.one_by_d = 1.f / static_cast<float>(a.d);
+    a.by_d = 1. / a.d;
     a.axes_by_four = 1;
     for (int p = 0; p < a.pairs; ++p)
         if (a.pair_axis[p] != a.pair_axis[p & ~3]) a.axes_by_four = 0;
@@ -422,9 +475,10 @@ int launch_token_rows(TokenRowsArgs a, void* stream) {
     if (workgroups * kWaves > 0x7FFFFFFF) return static_cast<int>(hipErrorInvalidConfiguration);
     const dim3 grid(static_cast<unsigned>(workgroups));
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (lanes == 8) launch_rows<8>(a, grid, st);
-    else if (lanes == 16) launch_rows<16>(a, grid, st);
-    else launch_rows<32>(a, grid, st);
+    const bool cached = !a.k_out.data;              // (rows of a cache have 64 or 128 columns)
+    if (lanes == 8) cached ? launch_rows<8, true>(a, grid, st) : launch_rows<8, false>(a, grid, st);
+    else if (lanes == 16) cached ? launch_rows<16, true>(a, grid, st) : launch_rows<16, false>(a, grid, st);
+    else launch_rows<32, false>(a, grid, st);
     return static_cast<int>(hipGetLastError());
 }
 
@@ -442,7 +496,8 @@ int launch_cache_read(CacheReadArgs a, void* stream) {
     return static_cast<int>(hipGetLastError());
 }
 
-int launch_cache_keep(const CacheKeepArgs& a, void* stream) {
+int launch_cache_keep(CacheKeepArgs a, void* stream) {
+    a.by_page = FastDiv::by(static_cast<uint32_t>(a.cache.page));
     const dim3 grid(static_cast<unsigned>(a.n), static_cast<unsigned>(a.cache.Hkv));
     if (a.cache.f8) hipLaunchKernelGGL(cache_keep_kernel<uint8_t>, grid, dim3(128), 0, static_cast<hipStream_t>(stream), a);
     else hipLaunchKernelGGL(cache_keep_kernel<uint16_t>, grid, dim3(128), 0, static_cast<hipStream_t>(stream), a);
