@@ -324,12 +324,13 @@ __device__ __forceinline__ void widen_codes(const uint32_t x, const float scale,
     y[3] = __builtin_amdgcn_cvt_f32_fp8(x, 3) * scale;
 }
 
-// One workgroup for 64 tokens of a request and some of the heads, one wave for 16 tokens, which lie in one page, a head at a time.  K: 16-byte
-// chunks as they are.  V: a lane takes all four interleaved tokens of its columns, so that each of their rows is stored in whole lines.
+// One workgroup for 64 tokens of a request and some of the heads, one wave for 16 tokens, which lie in one page, a head at a time.  Bound by memory.  Lanes take
+// columns so that the wave stores whole lines of the rows, 16 bytes a lane where a row has as many: K as it lies, V all four interleaved tokens of a few columns.
 template <int D, bool F8, bool OUT_F32>
 __global__ __launch_bounds__(64 * kWaves) void cache_read_kernel(CacheReadArgs a) {
-    constexpr int PER = F8 ? 16 : 8, LANES = D / PER, ROWS = 64 / LANES, KC = 16 / ROWS;   // K: columns of a chunk, lanes and rows of a load, loads
-    constexpr int COLS = D / 16, VC = COLS * 4 / PER;                                     // V: columns of a lane, chunks
+    constexpr int SIZE = F8 ? 1 : 2, PER = OUT_F32 ? 4 : 8, LANES = D / PER, ROWS = 64 / LANES, KC = 16 / ROWS;          // K: columns of a lane, lanes and rows of a load, loads
+    constexpr int COLS = OUT_F32 ? 4 : D / 16, GROUPS = D / 16 / COLS, VC = COLS * 4 * SIZE / 16;                        // V: columns in a row of a lane, how often, 16-byte chunks of each
+    using KChunk = std::conditional_t<PER * SIZE == 16, u32x4, std::conditional_t<PER * SIZE == 8, uint2, uint32_t>>;
     const CacheView& c = a.cache;
     const int64_t most = static_cast<int64_t>(a.max_blocks) * c.page;
     const auto length = [&](const int i) {          // tokens that have a row
@@ -349,13 +350,16 @@ __global__ __launch_bounds__(64 * kWaves) void cache_read_kernel(CacheReadArgs a
     const int g = lane >> 4, x = lane & 15;
 #pragma unroll 2
     for (int h = h0; h < h1; ++h) {
-        const int64_t base = (block * c.Hkv + h) * c.page, at = (base + off) * D * (F8 ? 1 : 2);
-        u32x4 k[KC], v[VC];
+        const int64_t base = (block * c.Hkv + h) * c.page, at = (base + off) * D * SIZE;
+        KChunk k[KC];
+        u32x4 v[GROUPS][VC];
         float ks[KC], vs[4];
 #pragma unroll
-        for (int y = 0; y < KC; ++y) k[y] = *reinterpret_cast<const u32x4*>(static_cast<const unsigned char*>(c.k) + at + 16 * (lane + 64 * y));
+        for (int y = 0; y < KC; ++y) k[y] = *reinterpret_cast<const KChunk*>(static_cast<const unsigned char*>(c.k) + at + static_cast<int>(sizeof(KChunk)) * (lane + 64 * y));
 #pragma unroll
-        for (int y = 0; y < VC; ++y) v[y] = *reinterpret_cast<const u32x4*>(static_cast<const unsigned char*>(c.v) + at + 16 * (VC * lane + y));
+        for (int p = 0; p < GROUPS; ++p)
+#pragma unroll
+            for (int y = 0; y < VC; ++y) v[p][y] = *reinterpret_cast<const u32x4*>(static_cast<const unsigned char*>(c.v) + at + g * 4 * D * SIZE + 16 * (VC * (16 * p + x) + y));
         if constexpr (F8) {
 #pragma unroll
             for (int y = 0; y < KC; ++y) ks[y] = scale_value(c.scales[2 * base + off + y * ROWS + lane / LANES]);
@@ -365,31 +369,36 @@ __global__ __launch_bounds__(64 * kWaves) void cache_read_kernel(CacheReadArgs a
         }
 #pragma unroll
         for (int y = 0; y < KC; ++y) {
+            uint32_t words[sizeof(KChunk) / 4];
+            __builtin_memcpy(words, &k[y], sizeof(KChunk));
             float row[PER];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if constexpr (F8) widen_codes(k[y][e], ks[y], row + 4 * e);
-                else { row[2 * e] = low_half(k[y][e]); row[2 * e + 1] = high_half(k[y][e]); }
+            for (int e = 0; e < static_cast<int>(sizeof(KChunk)) / 4; ++e) {
+                if constexpr (F8) widen_codes(words[e], ks[y], row + 4 * e);
+                else { row[2 * e] = low_half(words[e]); row[2 * e + 1] = high_half(words[e]); }
             }
             const int token = y * ROWS + lane / LANES;
             if (row_ok(token)) store_row<OUT_F32, PER>(a.k_out.data, (row0 + token) * a.k_out.token_stride + h * a.k_out.head_stride + lane % LANES * PER, row);
         }
-        float rows[4][COLS];
 #pragma unroll
-        for (int col = 0; col < COLS; ++col) {
-            if constexpr (F8) {
-                float four[4];
-                widen_codes(v[col / 4][col % 4], 1.f, four);
+        for (int p = 0; p < GROUPS; ++p) {
+            float rows[4][COLS];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) rows[e][col] = four[e] * vs[e];
-            } else {
-                const uint32_t lo = v[col / 2][2 * (col % 2)], hi = v[col / 2][2 * (col % 2) + 1];
-                rows[0][col] = low_half(lo); rows[1][col] = high_half(lo); rows[2][col] = low_half(hi); rows[3][col] = high_half(hi);
+            for (int col = 0; col < COLS; ++col) {
+                if constexpr (F8) {
+                    float four[4];
+                    widen_codes(v[p][col / 4][col % 4], 1.f, four);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) rows[e][col] = four[e] * vs[e];
+                } else {
+                    const uint32_t lo = v[p][col / 2][2 * (col % 2)], hi = v[p][col / 2][2 * (col % 2) + 1];
+                    rows[0][col] = low_half(lo); rows[1][col] = high_half(lo); rows[2][col] = low_half(hi); rows[3][col] = high_half(hi);
+                }
             }
-        }
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (row_ok(4 * g + e)) store_row<OUT_F32, COLS>(a.v_out.data, (row0 + 4 * g + e) * a.v_out.token_stride + h * a.v_out.head_stride + x * COLS, rows[e]);
+            for (int e = 0; e < 4; ++e)
+                if (row_ok(4 * g + e)) store_row<OUT_F32, COLS>(a.v_out.data, (row0 + 4 * g + e) * a.v_out.token_stride + h * a.v_out.head_stride + (16 * p + x) * COLS, rows[e]);
+        }
     }
 }
 
