@@ -34,9 +34,10 @@ __device__ __forceinline__ T over_row(T x, Op op) {
 struct Eight { float a[4], b[4]; };
 template <bool F32>
 struct RawEight { std::conditional_t<F32, u32x4, uint2> a, b; };
-template <bool F32>
+template <bool F32, bool ADJACENT = false>
 __device__ __forceinline__ RawEight<F32> load_eight(const void* p, const int64_t at, const int a, const int b) {
     using T = decltype(RawEight<F32>::a);
+    if constexpr (ADJACENT && !F32) return __builtin_bit_cast(RawEight<F32>, *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p) + at + a));
     if constexpr (F32) {
         const float* x = static_cast<const float*>(p) + at;
         return {*reinterpret_cast<const T*>(x + a), *reinterpret_cast<const T*>(x + b)};
@@ -121,13 +122,16 @@ __device__ __forceinline__ void norm_and_turn(Eight& row, const bool normed, con
 }
 
 enum Kind { kQuery, kKey, kCachedKey, kCachedValue };
+// What a launch does: rows to rows; queries to rows, keys and values into the cache; keys and values into the cache as they are
+enum Mode { kRows, kProjected, kWrite };
 
 // One wave for four consecutive tokens (two with LPR = 32), a head of theirs (two with LPR = 8) at a time: LPR lanes share a row, eight columns each.
 // A pair's two columns are in one lane (halves: four columns of either half), so that the rotation needs no exchange, and the cosines and sines of a
 // token are loaded once for all the heads that a wave takes.  Four tokens at once because the cache interleaves the values of four.
-template <int LPR, bool IN_F32, bool OUT_F32, bool CACHED>
+template <int LPR, bool IN_F32, bool OUT_F32, Mode MODE>
 __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a) {
-    constexpr int TOKENS = LPR == 32 ? 2 : 4, HEADS = LPR == 8 ? 2 : 1, BATCH = 4;
+    constexpr int TOKENS = LPR == 32 ? 2 : 4, HEADS = LPR == 8 ? 2 : 1, BATCH = MODE == kWrite ? 8 : 4;
+    constexpr bool CACHED = MODE != kRows;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(blockIdx.x * kWaves + (threadIdx.x >> 6))), lane = threadIdx.x & 63;
     const int group = a.by_splits(wave), split = wave - group * a.splits;
     const int64_t t0 = static_cast<int64_t>(group) * TOKENS;
@@ -174,17 +178,17 @@ __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a
 
     const auto run = [&](auto what, const int from, const int to, const int heads, const RowsView& in, const RowsView& out, const void* weight) {
         constexpr Kind KIND = decltype(what)::value;
-        constexpr bool turns = KIND != kCachedValue;
+        constexpr bool turns = KIND != kCachedValue && MODE != kWrite;
         const int ca = turns ? turn_a : plain_a, cb = turns ? turn_b : plain_b;
         Eight w;
-        const bool normed = weight != nullptr;
+        const bool normed = turns && weight != nullptr;
         if (normed && from < to) w = widened<IN_F32>(load_eight<IN_F32>(weight, 0, ca, cb));
         for (int s0 = from; s0 < to; s0 += BATCH) {
             RawEight<IN_F32> raw[BATCH];
 #pragma unroll
             for (int s = 0; s < BATCH; ++s) {
                 const int h = min(HEADS * min(s0 + s, to - 1) + of, heads - 1);
-                raw[s] = load_eight<IN_F32>(in.data, t * in.token_stride + h * in.head_stride, ca, cb);
+                raw[s] = load_eight<IN_F32, !turns>(in.data, t * in.token_stride + h * in.head_stride, ca, cb);
             }
 #pragma unroll
             for (int s = 0; s < BATCH; ++s) {
@@ -195,7 +199,7 @@ __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a
                 if (!columns_ok) y = Eight{};
                 // A key of the cache in 64 bits: it is stored with few bits, and one that lies by the middle between two of them goes to the nearer (in 32 bits
                 // some three in a million go to the other, which 8 bits hold 6% apart).  Eight lanes' work of 80 rows, and no time at any size.
-                if (KIND == kCachedKey && (normed || a.table)) norm_and_turn<double, LPR>(y, normed, w, a.by_d, a.eps, rotated, a.interleaved, cs, sn);
+                if (turns && KIND == kCachedKey) norm_and_turn<double, LPR>(y, normed, w, a.by_d, a.eps, rotated, a.interleaved, cs, sn);
                 else if (turns) norm_and_turn<float, LPR>(y, normed, w, static_cast<float>(a.by_d), a.eps, rotated, a.interleaved, cs, sn);
                 if constexpr (KIND == kQuery || KIND == kKey) {
                     if (row_ok) store_eight<OUT_F32>(out.data, t * out.token_stride + h * out.head_stride, ca, cb, y);
@@ -214,7 +218,8 @@ __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a
                         if (cell_ok && x == 0) a.cache.scales[2 * base + (KIND == kCachedValue ? a.cache.page : 0) + off] = static_cast<uint8_t>(byte);
                         if constexpr (KIND == kCachedKey) {
                             uint8_t* k = static_cast<uint8_t*>(a.cache.k) + (base + off) * a.d;
-                            if (cell_ok) {
+                            if (!turns && cell_ok) *reinterpret_cast<uint2*>(k + ca) = make_uint2(c0, c1);
+                            if (turns && cell_ok) {
                                 *reinterpret_cast<uint32_t*>(k + ca) = c0;
                                 *reinterpret_cast<uint32_t*>(k + cb) = c1;
                             }
@@ -238,7 +243,8 @@ __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a
                         uint32_t p[4] = {pack_bf16x2(y.a[0], y.a[1]), pack_bf16x2(y.a[2], y.a[3]), pack_bf16x2(y.b[0], y.b[1]), pack_bf16x2(y.b[2], y.b[3])};
                         if constexpr (KIND == kCachedKey) {
                             uint16_t* k = static_cast<uint16_t*>(a.cache.k) + (base + off) * a.d;
-                            if (cell_ok) {
+                            if (!turns && cell_ok) *reinterpret_cast<u32x4*>(k + ca) = u32x4{p[0], p[1], p[2], p[3]};
+                            if (turns && cell_ok) {
                                 *reinterpret_cast<uint2*>(k + ca) = make_uint2(p[0], p[1]);
                                 *reinterpret_cast<uint2*>(k + cb) = make_uint2(p[2], p[3]);
                             }
@@ -264,7 +270,7 @@ __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a
             }
         }
     };
-    run(std::integral_constant<Kind, kQuery>{}, min(first, steps_q), min(last, steps_q), a.Hq, a.q, a.q_out, a.q_weight);
+    if constexpr (MODE != kWrite) run(std::integral_constant<Kind, kQuery>{}, min(first, steps_q), min(last, steps_q), a.Hq, a.q, a.q_out, a.q_weight);
     const int k0 = steps_q, k1 = steps_q + steps_k;
     run(std::integral_constant<Kind, CACHED ? kCachedKey : kKey>{}, min(max(first, k0), k1) - k0, min(max(last, k0), k1) - k0, a.Hkv, a.k, a.k_out, a.k_weight);
     if constexpr (CACHED) run(std::integral_constant<Kind, kCachedValue>{}, max(first, k1) - k1, max(last, k1) - k1, a.Hkv, a.v, a.k_out, nullptr);
@@ -450,13 +456,14 @@ __global__ __launch_bounds__(128) void cache_keep_kernel(CacheKeepArgs a) {
     }
 }
 
-template <int LPR, bool CACHED>
+template <int LPR, Mode MODE>
 void launch_rows(const TokenRowsArgs& a, const dim3 grid, hipStream_t st) {
     const dim3 block(64 * kWaves);
-    if (a.in_f32 && a.out_f32) hipLaunchKernelGGL((token_rows_kernel<LPR, true, true, CACHED>), grid, block, 0, st, a);
-    else if (a.in_f32) hipLaunchKernelGGL((token_rows_kernel<LPR, true, false, CACHED>), grid, block, 0, st, a);
-    else if (a.out_f32) hipLaunchKernelGGL((token_rows_kernel<LPR, false, true, CACHED>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((token_rows_kernel<LPR, false, false, CACHED>), grid, block, 0, st, a);
+    constexpr bool F32 = MODE != kWrite;            // (a write has no rows to put out)
+    if (a.in_f32 && a.out_f32) hipLaunchKernelGGL((token_rows_kernel<LPR, true, F32, MODE>), grid, block, 0, st, a);
+    else if (a.in_f32) hipLaunchKernelGGL((token_rows_kernel<LPR, true, false, MODE>), grid, block, 0, st, a);
+    else if (a.out_f32) hipLaunchKernelGGL((token_rows_kernel<LPR, false, F32, MODE>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((token_rows_kernel<LPR, false, false, MODE>), grid, block, 0, st, a);
 }
 
 template <int D, bool F8>
@@ -484,10 +491,11 @@ int launch_token_rows(TokenRowsArgs a, void* stream) {
     if (workgroups * kWaves > 0x7FFFFFFF) return static_cast<int>(hipErrorInvalidConfiguration);
     const dim3 grid(static_cast<unsigned>(workgroups));
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const bool cached = !a.k_out.data;              // (rows of a cache have 64 or 128 columns)
-    if (lanes == 8) cached ? launch_rows<8, true>(a, grid, st) : launch_rows<8, false>(a, grid, st);
-    else if (lanes == 16) cached ? launch_rows<16, true>(a, grid, st) : launch_rows<16, false>(a, grid, st);
-    else launch_rows<32, false>(a, grid, st);
+    // a cache has rows of 64 or 128 columns
+    const Mode mode = a.k_out.data ? kRows : a.Hq == 0 && !a.table && !a.k_weight ? kWrite : kProjected;
+    if (lanes == 8) mode == kRows ? launch_rows<8, kRows>(a, grid, st) : mode == kWrite ? launch_rows<8, kWrite>(a, grid, st) : launch_rows<8, kProjected>(a, grid, st);
+    else if (lanes == 16) mode == kRows ? launch_rows<16, kRows>(a, grid, st) : mode == kWrite ? launch_rows<16, kWrite>(a, grid, st) : launch_rows<16, kProjected>(a, grid, st);
+    else launch_rows<32, kRows>(a, grid, st);
     return static_cast<int>(hipGetLastError());
 }
 
