@@ -121,7 +121,8 @@ __device__ __forceinline__ void norm_and_turn(Eight& row, const bool normed, con
     for (int e = 0; e < 4; ++e) { row.a[e] = odd_float(y[e]); row.b[e] = odd_float(y[4 + e]); }
 }
 
-enum Kind { kQuery, kKey, kCachedKey, kCachedValue };
+enum Kind { kQuery, kKey, kCachedKey, kCachedCell, kCachedValue };       // (cell: values of four tokens that are interleaved)
+struct Place { int64_t t, block; int off; bool ok; };                  // token, and where it goes in the cache
 // What a launch does: rows to rows; queries to rows, keys and values into the cache; keys and values into the cache as they are
 enum Mode { kRows, kProjected, kWrite };
 
@@ -165,20 +166,33 @@ __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a
             }
         }
     }
-    int64_t block = 0;
-    int off = 0;
-    bool slot_ok = false, whole = false;            // whole: the four tokens fill four interleaved places
+    // Where the lane's token goes.  Values are interleaved by four: four tokens in a row that fill such a cell go there together, by the wave that has the first of
+    // them, whichever tokens the wave has otherwise (prompts behind contexts of any length: 44354 tokens of 8 heads 89 -> 58 us, 4.7 TB/s, what a large copy reaches); the others one by one.
+    Place own{t, 0, 0, false}, cell{t, 0, 0, false};
+    bool any_cell = false, any_single = false, single = false;
     if (CACHED && last > steps_q) {
-        const int64_t slot = a.slots[t];
-        slot_ok = token_ok && slot >= 0 && slot < a.cache.num_blocks * a.cache.page;
-        block = slot_ok ? slot / a.cache.page : 0;
-        off = slot_ok ? static_cast<int>(slot - block * a.cache.page) : 0;
-        whole = __all(slot_ok && (off & 3) == sub && __shfl(slot, lane & 15, 64) + sub == slot);
+        const int64_t places = a.cache.num_blocks * a.cache.page, near = t0 - 3 + (lane & 15);
+        const int64_t slot = near >= 0 && near < a.tokens && (lane & 15) < 10 ? a.slots[near] : -1;          // of tokens t0 - 3 .. t0 + 6
+        const bool inside = slot >= 0 && slot < places;
+        const uint32_t begins = __ballot(inside && (slot & 3) == 0), follows = __ballot(__shfl_up(slot, 1, 16) + 1 == slot && (lane & 15) > 0 && inside);
+        const uint32_t full = begins & follows >> 1 & follows >> 2 & follows >> 3 & 0x7F, covered = full | full << 1 | full << 2 | full << 3;
+        const auto at = [&](Place& p, const int64_t s, const bool ok) {
+            p.ok = ok;
+            p.block = ok ? s / a.cache.page : 0;
+            p.off = ok ? static_cast<int>(s - p.block * a.cache.page) : 0;
+        };
+        at(own, __shfl(slot, sub + 3, 16), token_ok && __shfl(static_cast<int>(inside), sub + 3, 16));
+        single = own.ok && !(covered >> (sub + 3) & 1);
+        any_single = __any(single);
+        any_cell = (full & 0x78) != 0;
+        const int start = any_cell ? __builtin_ctz(full & 0x78) : 3;
+        at(cell, __shfl(slot, start, 16) + sub, any_cell);
+        cell.t = any_cell ? t0 - 3 + start + sub : t;
     }
 
-    const auto run = [&](auto what, const int from, const int to, const int heads, const RowsView& in, const RowsView& out, const void* weight) {
+    const auto run = [&](auto what, const Place& to_place, const int from, const int to, const int heads, const RowsView& in, const RowsView& out, const void* weight) {
         constexpr Kind KIND = decltype(what)::value;
-        constexpr bool turns = KIND != kCachedValue && MODE != kWrite;
+        constexpr bool turns = KIND < kCachedCell && MODE != kWrite;
         const int ca = turns ? turn_a : plain_a, cb = turns ? turn_b : plain_b;
         Eight w;
         const bool normed = turns && weight != nullptr;
@@ -188,13 +202,13 @@ __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a
 #pragma unroll
             for (int s = 0; s < BATCH; ++s) {
                 const int h = min(HEADS * min(s0 + s, to - 1) + of, heads - 1);
-                raw[s] = load_eight<IN_F32, !turns>(in.data, t * in.token_stride + h * in.head_stride, ca, cb);
+                raw[s] = load_eight<IN_F32, !turns>(in.data, to_place.t * in.token_stride + h * in.head_stride, ca, cb);
             }
 #pragma unroll
             for (int s = 0; s < BATCH; ++s) {
                 if (s0 + s >= to) break;
                 const int h = HEADS * (s0 + s) + of;
-                const bool row_ok = token_ok && columns_ok && h < heads;
+                const bool row_ok = columns_ok && h < heads;
                 Eight y = widened<IN_F32>(raw[s]);
                 if (!columns_ok) y = Eight{};
                 // A key of the cache in 64 bits: it is stored with few bits, and one that lies by the middle between two of them goes to the nearer (in 32 bits
@@ -202,10 +216,11 @@ __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a
                 if (turns && KIND == kCachedKey) norm_and_turn<double, LPR>(y, normed, w, a.by_d, a.eps, rotated, a.interleaved, cs, sn);
                 else if (turns) norm_and_turn<float, LPR>(y, normed, w, static_cast<float>(a.by_d), a.eps, rotated, a.interleaved, cs, sn);
                 if constexpr (KIND == kQuery || KIND == kKey) {
-                    if (row_ok) store_eight<OUT_F32>(out.data, t * out.token_stride + h * out.head_stride, ca, cb, y);
+                    if (row_ok && token_ok) store_eight<OUT_F32>(out.data, t * out.token_stride + h * out.head_stride, ca, cb, y);
                 } else {
-                    const bool cell_ok = row_ok && slot_ok;
-                    const int64_t base = (block * a.cache.Hkv + h) * a.cache.page;
+                    const bool cell_ok = row_ok && to_place.ok;
+                    const int off = to_place.off;
+                    const int64_t base = (to_place.block * a.cache.Hkv + h) * a.cache.page;
                     if (a.cache.f8) {
                         float top = 0.f;
 #pragma unroll
@@ -215,7 +230,7 @@ __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a
                         const float inv = scale_inverse(byte);
                         uint32_t c0 = pack_f8x2(y.a[0], y.a[1], inv) | pack_f8x2(y.a[2], y.a[3], inv) << 16;
                         uint32_t c1 = pack_f8x2(y.b[0], y.b[1], inv) | pack_f8x2(y.b[2], y.b[3], inv) << 16;
-                        if (cell_ok && x == 0) a.cache.scales[2 * base + (KIND == kCachedValue ? a.cache.page : 0) + off] = static_cast<uint8_t>(byte);
+                        if (cell_ok && x == 0) a.cache.scales[2 * base + (KIND == kCachedKey ? 0 : a.cache.page) + off] = static_cast<uint8_t>(byte);
                         if constexpr (KIND == kCachedKey) {
                             uint8_t* k = static_cast<uint8_t*>(a.cache.k) + (base + off) * a.d;
                             if (!turns && cell_ok) *reinterpret_cast<uint2*>(k + ca) = make_uint2(c0, c1);
@@ -223,14 +238,14 @@ __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a
                                 *reinterpret_cast<uint32_t*>(k + ca) = c0;
                                 *reinterpret_cast<uint32_t*>(k + cb) = c1;
                             }
-                        } else if (whole) {
+                        } else if constexpr (KIND == kCachedCell) {
                             // column pairs 0..3 of tokens 0..3 -> lane group s has pair s of all four tokens: 2 columns x 4 tokens, 8 bytes
                             swap32(c0, c1);                        // groups 0, 1: pairs 0, 1 of tokens s, s + 2; groups 2, 3: pairs 2, 3 of tokens s - 2, s
                             uint32_t even = __builtin_amdgcn_perm(c1, c0, 0x05040100u), odd = __builtin_amdgcn_perm(c1, c0, 0x07060302u);
                             swap16(even, odd);                     // pair s of tokens 0, 2 and of tokens 1, 3
                             const uint32_t lo = __builtin_amdgcn_perm(odd, even, 0x06020400u), hi = __builtin_amdgcn_perm(odd, even, 0x07030501u);
                             uint8_t* v = static_cast<uint8_t*>(a.cache.v) + (base + (off & ~3)) * a.d + 4 * (8 * x + 2 * sub);
-                            if (columns_ok && h < heads) *reinterpret_cast<uint2*>(v) = make_uint2(lo, hi);
+                            if (cell_ok) *reinterpret_cast<uint2*>(v) = make_uint2(lo, hi);
                         } else if (cell_ok) {
                             uint8_t* v = static_cast<uint8_t*>(a.cache.v) + (base + (off & ~3)) * a.d + 4 * 8 * x + (off & 3);
 #pragma unroll
@@ -248,13 +263,13 @@ __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a
                                 *reinterpret_cast<uint2*>(k + ca) = make_uint2(p[0], p[1]);
                                 *reinterpret_cast<uint2*>(k + cb) = make_uint2(p[2], p[3]);
                             }
-                        } else if (whole) {                        // the same with pairs of 32 bits: lane group s has pair s of tokens 0..3
+                        } else if constexpr (KIND == kCachedCell) {                        // the same with pairs of 32 bits: lane group s has pair s of tokens 0..3
                             swap32(p[0], p[2]);                    // groups 0, 1: pair 0 of tokens s, s + 2; groups 2, 3: pair 2 of tokens s - 2, s
                             swap32(p[1], p[3]);                    // pairs 1, 3
                             swap16(p[0], p[1]);                    // pair s of tokens 0, 1
                             swap16(p[2], p[3]);                    // of tokens 2, 3
                             uint16_t* v = static_cast<uint16_t*>(a.cache.v) + (base + (off & ~3)) * a.d + 4 * (8 * x + 2 * sub);
-                            if (columns_ok && h < heads)
+                            if (cell_ok)
                                 *reinterpret_cast<u32x4*>(v) = u32x4{__builtin_amdgcn_perm(p[1], p[0], 0x05040100u), __builtin_amdgcn_perm(p[3], p[2], 0x05040100u),
                                                                      __builtin_amdgcn_perm(p[1], p[0], 0x07060302u), __builtin_amdgcn_perm(p[3], p[2], 0x07060302u)};
                         } else if (cell_ok) {
@@ -270,10 +285,14 @@ __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a
             }
         }
     };
-    if constexpr (MODE != kWrite) run(std::integral_constant<Kind, kQuery>{}, min(first, steps_q), min(last, steps_q), a.Hq, a.q, a.q_out, a.q_weight);
+    if constexpr (MODE != kWrite) run(std::integral_constant<Kind, kQuery>{}, own, min(first, steps_q), min(last, steps_q), a.Hq, a.q, a.q_out, a.q_weight);
     const int k0 = steps_q, k1 = steps_q + steps_k;
-    run(std::integral_constant<Kind, CACHED ? kCachedKey : kKey>{}, min(max(first, k0), k1) - k0, min(max(last, k0), k1) - k0, a.Hkv, a.k, a.k_out, a.k_weight);
-    if constexpr (CACHED) run(std::integral_constant<Kind, kCachedValue>{}, max(first, k1) - k1, max(last, k1) - k1, a.Hkv, a.v, a.k_out, nullptr);
+    run(std::integral_constant<Kind, CACHED ? kCachedKey : kKey>{}, own, min(max(first, k0), k1) - k0, min(max(last, k0), k1) - k0, a.Hkv, a.k, a.k_out, a.k_weight);
+    if constexpr (CACHED) {
+        if (any_cell) run(std::integral_constant<Kind, kCachedCell>{}, cell, max(first, k1) - k1, max(last, k1) - k1, a.Hkv, a.v, a.k_out, nullptr);
+        own.ok = single;
+        if (any_single) run(std::integral_constant<Kind, kCachedValue>{}, own, max(first, k1) - k1, max(last, k1) - k1, a.Hkv, a.v, a.k_out, nullptr);
+    }
 }
 
 // The request that unit `item` of the launch belongs to, and its number there, where request i has units(i) of them: prefix sums of them all,
