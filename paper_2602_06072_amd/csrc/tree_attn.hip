@@ -4,7 +4,15 @@
 // transposed problem with v_mfma_f32_16x16x32_bf16: S^T = K Q^T (A: 16 keys, B: 16 rows), O^T += V^T P^T (A: 16 columns, B: 16 rows), so
 // that the scores of a row sit in four lanes and P^T leaves the first product as the operand of the second.  The cache is laid out for it:
 // a lane's bytes of a K row are one token's (its scale goes in with the conversion to bf16, which is exact), and a dword of V is a column of
-// the four keys whose scores the lane holds, so nothing goes through LDS on its way from memory to the matrix pipe.
+// the four keys whose scores the lane holds, so that with few rows nothing goes through LDS on its way from memory to the matrix pipe.
+//
+// With u = rows and L = keys of a request a launch reads (2 d + 2) L bytes a KV head (4 d L from bf16) and computes 4 d u L operations: memory bounds it up to some
+// 100 rows, the matrix pipe beyond.  Measured (MI355X, cache in 8 bits, 8 KV heads of 128 columns): 256 single tokens behind 32 .. 16384 tokens with 32 heads 352 us,
+// 6.1 TB/s; 128 trees with 64 heads 153 us and 8 for the merge, of 97 for the whole step's bytes; 64 trees of up to 64 tokens with 64 heads 640 us, 0.74 PFLOP/s
+// of the pairs that are seen (a product of large matrices reaches 1.34).
+//
+// Roundings: K and V to bf16 are exact (4 bits of fraction and a power of two); probabilities are rounded to bf16 for the matrix pipe, half a unit of 2^-8, and
+// their sum is that of the rounded ones; scores, sums, accumulators and partial results have 32 bits.
 #include "arrival.h"
 #include "cache_format.hip.h"
 
@@ -537,164 +545,164 @@ __device__ __forceinline__ void finish(const TreeArgs& a, const Piece& w, const 
     }
 }
 
-// Up to 16 NB rows: bound by memory.  The four waves of a workgroup take tiles of N sub-tiles in turns, SETS tiles in flight in each, from memory into
+// Up to 16 NB rows: bound by memory, in short launches by latency (four single tokens behind 300 .. 3000 tokens 11.4 us: the pieces found 2 to 3, first tile 1 to 3,
+// tiles 2, last one 2, results and merge 2 to 4).  The four waves of a workgroup take tiles of N sub-tiles in turns, SETS tiles in flight in each, from memory into
 // registers and from there into the products.  ALONE: every wave has a request (and rows) of its own, all of whose tiles it takes.
-template <int D, bool F8, int NB, int N, int SETS, int WAVES_PER_SIMD, bool ALONE = false>
+template <int D, bool F8, int NB, int N, int WAVES_PER_SIMD, bool ALONE = false>
 __global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(TreeArgs) {
-    static_assert(SETS == 2, "sets");
     using Regs = TileRegs<D, F8, N>;
-    constexpr int CH = Regs::CH, TOKENS = 16 * N, KS = D / 32, VT = D / 16, SIZE = F8 ? 1 : 2, STRIDE = ALONE ? 1 : kWaves;
+    constexpr int SETS = 2, CH = Regs::CH, TOKENS = 16 * N, KS = D / 32, VT = D / 16, SIZE = F8 ? 1 : 2, STRIDE = ALONE ? 1 : kWaves;
     __shared__ __align__(16) unsigned char lds[kJoinBytes<D>];
     __shared__ int last;
 
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6)), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const auto work = [&](const TreeArgs& a, const Piece& w, const int kvh) {
-    const Bounds bounds = bounds_of<TOKENS>(a, w);
-    if (bounds.rows_here <= 0) return;              // (no rows, or total_q says so; all pieces of the request alike)
-    const int len = bounds.len, ctx = bounds.ctx, t1 = bounds.t1;
+        const Bounds bounds = bounds_of<TOKENS>(a, w);
+        if (bounds.rows_here <= 0) return;              // (no rows, or total_q says so; all pieces of the request alike)
+        const int len = bounds.len, ctx = bounds.ctx, t1 = bounds.t1;
 
-    Sums<D, NB> y;
-    int tile = bounds.t0 + (ALONE ? 0 : wave);
-    if (tile < t1) {
-        // requests a tile, whose places are known, and the places of the set's tile after that
-        auto load = [&](Regs& r, int& places, const int tile) {
-            const Rows rows = rows_of<N>(a, bounds, kvh, tile, 0, places);
-            places = ask_places<N>(a, bounds, tile + SETS * STRIDE, 0);
+        Sums<D, NB> y;
+        int tile = bounds.t0 + (ALONE ? 0 : wave);
+        if (tile < t1) {
+            // requests a tile, whose places are known, and the places of the set's tile after that
+            auto load = [&](Regs& r, int& places, const int tile) {
+                const Rows rows = rows_of<N>(a, bounds, kvh, tile, 0, places);
+                places = ask_places<N>(a, bounds, tile + SETS * STRIDE, 0);
 #pragma unroll
-            for (int u = 0; u < N; ++u) {
-                const SubTile t = sub_tile<D, F8>(a, rows, u);
+                for (int u = 0; u < N; ++u) {
+                    const SubTile t = sub_tile<D, F8>(a, rows, u);
 #pragma unroll
-                for (int x = 0; x < CH; ++x) r.k[u][x] = load16(t.k, n * D * SIZE + 16 * g, 64 * x);
+                    for (int x = 0; x < CH; ++x) r.k[u][x] = load16(t.k, n * D * SIZE + 16 * g, 64 * x);
 #pragma unroll
-                for (int x = 0; x < CH; ++x) r.v[u][x] = load16(t.v, g * 4 * D * SIZE + 16 * n, 256 * x);
-                if constexpr (F8) {
-                    r.ks[u] = __builtin_amdgcn_raw_buffer_load_b32(t.s, n & 12, 0, 0);
-                    r.vs[u] = __builtin_amdgcn_raw_buffer_load_b32(t.s, 4 * g, a.cache.page, 0);
+                    for (int x = 0; x < CH; ++x) r.v[u][x] = load16(t.v, g * 4 * D * SIZE + 16 * n, 256 * x);
+                    if constexpr (F8) {
+                        r.ks[u] = __builtin_amdgcn_raw_buffer_load_b32(t.s, n & 12, 0, 0);
+                        r.vs[u] = __builtin_amdgcn_raw_buffer_load_b32(t.s, 4 * g, a.cache.page, 0);
+                    }
                 }
-            }
-        };
-        Regs r[SETS];
-        int places[SETS];
+            };
+            Regs r[SETS];
+            int places[SETS];
 #pragma unroll
-        for (int s = 0; s < SETS; ++s) places[s] = ask_places<N>(a, bounds, tile + s * STRIDE, 0);
-        load(r[0], places[0], tile);
-        Queries<D, NB> q;
-        load_queries<D, F8, NB>(a, bounds, kvh, bounds.row0, q);
-        // The rows are waited for here, with the first tile; left to the loop, its first products wait for all tiles in flight in every turn.
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int s = 1; s < SETS; ++s) load(r[s], places[s], tile + s * STRIDE);
-        __builtin_amdgcn_sched_barrier(0);
-        constexpr int OTHERS = (SETS - 1) * (N * (2 * CH + (F8 ? 2 : 0)) + 1);
-        static_assert(OTHERS < 64, "vmcnt");
-        __builtin_amdgcn_s_waitcnt(0x0F70 | (OTHERS & 0xF) | (OTHERS >> 4 << 14));
-        const float sl2 = a.scale * kLog2e;
-
-        // `edge`: some key of the tile is not seen by some row
-        auto step = [&](Regs& r, const int tile, auto edge) {
-            constexpr bool EDGE = decltype(edge)::value;
-            floatx4 s[NB][N];
-#pragma unroll
-            for (int u = 0; u < N; ++u) {
-#pragma unroll
-                for (int b = 0; b < NB; ++b) s[b][u] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                    const bf16x8 x = k_operand<D, F8, N>(r, u, k);
-#pragma unroll
-                    for (int b = 0; b < NB; ++b) s[b][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q.q[b][k], s[b][u], 0, 0, 0);
-                }
-                if constexpr (F8) __builtin_amdgcn_sched_barrier(0);       // (bf16 copies of a sub-tile at a time: they are twice its size)
-            }
-            // lane (n, g) holds scores of its rows against keys TOKENS * tile + 16 u + 4 g + e
-            const int key0 = tile * TOKENS + 4 * g;
-            uint32_t hidden[NB] = {};                              // keys that this lane's row does not see, bit 4 u + e
-            if constexpr (EDGE) {
-#pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    uint32_t seen = 0;
-#pragma unroll
-                    for (int u = 0; u < N; ++u) seen |= seen_of_four(q.bits[b], key0 + 16 * u, ctx, len) << 4 * u;
-                    hidden[b] = ~seen;
-                }
-                if constexpr (F8) {                                // a scale where there is no key may be anything
-#pragma unroll
-                    for (int x = 0; x < 4 * N; ++x)
-                        if (key0 + 16 * (x / 4) + x % 4 >= len) r.vs[x / 4] = (r.vs[x / 4] & ~(0xFFu << 8 * (x % 4))) | 127u << 8 * (x % 4);
-                }
-            }
-            float factor[F8 ? N : 1][4];
-            if constexpr (F8) {
-#pragma unroll
-                for (int u = 0; u < N; ++u)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) factor[u][e] = scale_value(r.vs[u] >> 8 * e & 0xFF);
-            }
-            bf16x8 pf[NB][N / 2];
+            for (int s = 0; s < SETS; ++s) places[s] = ask_places<N>(a, bounds, tile + s * STRIDE, 0);
+            load(r[0], places[0], tile);
+            Queries<D, NB> q;
+            load_queries<D, F8, NB>(a, bounds, kvh, bounds.row0, q);
+            // The rows are waited for here, with the first tile; left to the loop, its first products wait for all tiles in flight in every turn.
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                float p[4 * N];
-                probabilities<D, N, EDGE, false>(s[b], hidden[b], sl2, y.o[b], y.l[b], y.m[b], p);
-                uint32_t pw[2 * N];
+            for (int s = 1; s < SETS; ++s) load(r[s], places[s], tile + s * STRIDE);
+            __builtin_amdgcn_sched_barrier(0);
+            constexpr int OTHERS = (SETS - 1) * (N * (2 * CH + (F8 ? 2 : 0)) + 1);
+            static_assert(OTHERS < 64, "vmcnt");
+            __builtin_amdgcn_s_waitcnt(0x0F70 | (OTHERS & 0xF) | (OTHERS >> 4 << 14));
+            const float sl2 = a.scale * kLog2e;
+
+            // `edge`: some key of the tile is not seen by some row
+            auto step = [&](Regs& r, const int tile, auto edge) {
+                constexpr bool EDGE = decltype(edge)::value;
+                floatx4 s[NB][N];
 #pragma unroll
-                for (int x = 0; x < 4 * N; ++x)
-                    if constexpr (F8) p[x] *= factor[x / 4][x % 4];        // the scale of V, a power of two: it rounds nothing
+                for (int u = 0; u < N; ++u) {
 #pragma unroll
-                for (int x = 0; x < 2 * N; ++x) pw[x] = pack_bf16x2(p[2 * x], p[2 * x + 1]);
+                    for (int b = 0; b < NB; ++b) s[b][u] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int x = 0; x < N / 2; ++x) pf[b][x] = __builtin_bit_cast(bf16x8, u32x4{pw[4 * x], pw[4 * x + 1], pw[4 * x + 2], pw[4 * x + 3]});
-            }
+                    for (int k = 0; k < KS; ++k) {
+                        const bf16x8 x = k_operand<D, F8, N>(r, u, k);
 #pragma unroll
-            for (int x = 0; x < N / 2; ++x) {
-                // sums of the ROUNDED probabilities (their error cancels in part) from the matrix pipe: every row of A holds the inverse scales
-                u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+                        for (int b = 0; b < NB; ++b) s[b][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q.q[b][k], s[b][u], 0, 0, 0);
+                    }
+                    if constexpr (F8) __builtin_amdgcn_sched_barrier(0);       // (bf16 copies of a sub-tile at a time: they are twice its size)
+                }
+                // lane (n, g) holds scores of its rows against keys TOKENS * tile + 16 u + 4 g + e
+                const int key0 = tile * TOKENS + 4 * g;
+                uint32_t hidden[NB] = {};                              // keys that this lane's row does not see, bit 4 u + e
+                if constexpr (EDGE) {
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
+                        uint32_t seen = 0;
+#pragma unroll
+                        for (int u = 0; u < N; ++u) seen |= seen_of_four(q.bits[b], key0 + 16 * u, ctx, len) << 4 * u;
+                        hidden[b] = ~seen;
+                    }
+                    if constexpr (F8) {                                // a scale where there is no key may be anything
+#pragma unroll
+                        for (int x = 0; x < 4 * N; ++x)
+                            if (key0 + 16 * (x / 4) + x % 4 >= len) r.vs[x / 4] = (r.vs[x / 4] & ~(0xFFu << 8 * (x % 4))) | 127u << 8 * (x % 4);
+                    }
+                }
+                float factor[F8 ? N : 1][4];
                 if constexpr (F8) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t two = r.vs[2 * x + e / 2] >> 16 * (e % 2);
-                        ones[e] = (254u - (two & 0xFF)) << 7 | (254u - (two >> 8 & 0xFF)) << 23;
-                    }
+                    for (int u = 0; u < N; ++u)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) factor[u][e] = scale_value(r.vs[u] >> 8 * e & 0xFF);
+                }
+                bf16x8 pf[NB][N / 2];
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    float p[4 * N];
+                    probabilities<D, N, EDGE, false>(s[b], hidden[b], sl2, y.o[b], y.l[b], y.m[b], p);
+                    uint32_t pw[2 * N];
+#pragma unroll
+                    for (int x = 0; x < 4 * N; ++x)
+                        if constexpr (F8) p[x] *= factor[x / 4][x % 4];        // the scale of V, a power of two: it rounds nothing
+#pragma unroll
+                    for (int x = 0; x < 2 * N; ++x) pw[x] = pack_bf16x2(p[2 * x], p[2 * x + 1]);
+#pragma unroll
+                    for (int x = 0; x < N / 2; ++x) pf[b][x] = __builtin_bit_cast(bf16x8, u32x4{pw[4 * x], pw[4 * x + 1], pw[4 * x + 2], pw[4 * x + 3]});
                 }
 #pragma unroll
-                for (int b = 0; b < NB; ++b) y.l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones), pf[b][x], y.l[b], 0, 0, 0);
+                for (int x = 0; x < N / 2; ++x) {
+                    // sums of the ROUNDED probabilities (their error cancels in part) from the matrix pipe: every row of A holds the inverse scales
+                    u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+                    if constexpr (F8) {
 #pragma unroll
-                for (int t = 0; t < VT; ++t) {
-                    const bf16x8 v = v_operand<D, F8, N>(r, x, t);
-                    if constexpr (EDGE) product_with_hidden<NB, D, N / 2>(v, hidden, x, pf, y, t);
-                    else {
-#pragma unroll
-                        for (int b = 0; b < NB; ++b) y.o[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[b][x], y.o[b][t], 0, 0, 0);
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t two = r.vs[2 * x + e / 2] >> 16 * (e % 2);
+                            ones[e] = (254u - (two & 0xFF)) << 7 | (254u - (two >> 8 & 0xFF)) << 23;
+                        }
                     }
-                    if (F8 && t % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) y.l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones), pf[b][x], y.l[b], 0, 0, 0);
+#pragma unroll
+                    for (int t = 0; t < VT; ++t) {
+                        const bf16x8 v = v_operand<D, F8, N>(r, x, t);
+                        if constexpr (EDGE) product_with_hidden<NB, D, N / 2>(v, hidden, x, pf, y, t);
+                        else {
+#pragma unroll
+                            for (int b = 0; b < NB; ++b) y.o[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[b][x], y.o[b][t], 0, 0, 0);
+                        }
+                        if (F8 && t % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
+            };
+            // Tiles that every row sees whole, then the others (a tile or two of a request: the drafted tokens, the end), whose code needs the
+            // registers of the second set.  Requests past the last tile have empty descriptors: behind a condition the compiler would wait for all of them.
+            const int whole = min(max(min(ctx, len), 0) / TOKENS, t1);
+            const auto turn = [&](Regs& x, int& at) {
+                step(x, tile, std::false_type{});
+                load(x, at, tile + SETS * STRIDE);
+                tile += STRIDE;
+            };
+            // (the loop has one way out: from another in the middle the compiler would take the younger set for the one that it has to wait for)
+            while (tile + STRIDE < whole) {
+                turn(r[0], places[0]);
+                turn(r[1], places[1]);
             }
-        };
-        // Tiles that every row sees whole, then the others (a tile or two of a request: the drafted tokens, the end), whose code needs the
-        // registers of the second set.  Requests past the last tile have empty descriptors: behind a condition the compiler would wait for all of them.
-        const int whole = min(max(min(ctx, len), 0) / TOKENS, t1);
-        const auto turn = [&](Regs& x, int& at) {
-            step(x, tile, std::false_type{});
-            load(x, at, tile + SETS * STRIDE);
-            tile += STRIDE;
-        };
-        // (the loop has one way out: from another in the middle the compiler would take the younger set for the one that it has to wait for)
-        while (tile + STRIDE < whole) {
-            turn(r[0], places[0]);
-            turn(r[1], places[1]);
+            if (tile < whole) {
+                turn(r[0], places[0]);
+                r[0] = r[1];
+            }
+            while (tile < t1) {
+                step(r[0], tile, std::true_type{});
+                tile += STRIDE;
+                places[0] = ask_places<N>(a, bounds, tile, 0);
+                load(r[0], places[0], tile);
+            }
         }
-        if (tile < whole) {
-            turn(r[0], places[0]);
-            r[0] = r[1];
-        }
-        while (tile < t1) {
-            step(r[0], tile, std::true_type{});
-            tile += STRIDE;
-            places[0] = ask_places<N>(a, bounds, tile, 0);
-            load(r[0], places[0], tile);
-        }
-    }
-    finish<D, F8, NB, NB == 1, ALONE>(a, w, bounds, kvh, 1, ALONE ? 1 : kWaves, y, lds, &last);
+        finish<D, F8, NB, NB == 1, ALONE>(a, w, bounds, kvh, 1, ALONE ? 1 : kWaves, y, lds, &last);
     };
     if constexpr (ALONE) {
         const TreeArgs& a = kernel_args();
@@ -715,7 +723,9 @@ __device__ __forceinline__ uint2 widen_each(const uint32_t x, const float (&s)[4
     return make_uint2(two(std::false_type{}, s[0], s[1]), two(std::true_type{}, s[2], s[3]));
 }
 
-// More rows, 128 in a workgroup: bound by the matrix pipe and by what surrounds it.  The workgroup's waves bring a tile of 64 keys into LDS together, a
+// More rows, 128 in a workgroup: bound by the matrix pipe and what surrounds it (for 32 keys and 32 rows 34 MFMAs of 16 cycles, 16 exponentials of 16, some 60 other
+// instructions of 4 and 16 KiB out of LDS, 128 cycles of the unit).  Four waves: with eight (64 KiB shared by twice the rows) 736 instead of 691 us, and operands read
+// two, six or eight steps ahead instead of four 641 to 647 instead of 640.  The workgroup's waves bring a tile of 64 keys into LDS together, a
 // quarter each, as bf16 operands (the conversion is done once, not by every wave), two tiles at a time; every wave reads it for its 32 rows.  With 64 rows
 // and fewer two waves share 32 rows, half of a tile's keys each.
 constexpr int kWideRows = 128;
@@ -727,166 +737,170 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 && F8 ? 3 : 2) void tree_attn_
     __shared__ int last;
 
     run_pieces<TOKENS, 2>([&](const TreeArgs& a, const Piece& w, const int kvh) {
-    const Bounds bounds = bounds_of<TOKENS>(a, w);
-    if (bounds.rows_here <= 0) return;
-    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6)), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-    const int len = bounds.len, ctx = bounds.ctx, t0 = bounds.t0, t1 = bounds.t1;
-    const int sharers = bounds.rows_here <= 64 ? 2 : 1, row_group = wave / sharers, half = wave % sharers;
-    const bool works = row_group * 32 < bounds.rows_here;
+        const Bounds bounds = bounds_of<TOKENS>(a, w);
+        if (bounds.rows_here <= 0) return;
+        const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6)), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+        const int len = bounds.len, ctx = bounds.ctx, t0 = bounds.t0, t1 = bounds.t1;
+        const int sharers = bounds.rows_here <= 64 ? 2 : 1, row_group = wave / sharers, half = wave % sharers;
+        const bool works = row_group * 32 < bounds.rows_here;
 
-    Sums<D, NB> y;
-    if (t0 < t1) {
-        // this wave's quarter of a tile: K or V of two sub-tiles
-        struct Quarter { u32x4 c[2][CH]; uint32_t s[2]; };
-        const int of_v = wave & 1, pair = wave >> 1;
-        const int lane_at = of_v ? g * 4 * D * SIZE + 16 * n : n * D * SIZE + 16 * g, chunk_at = of_v ? 256 : 64;
-        const int scale_lane = of_v ? 4 * g : n & 12, scale_at = of_v ? a.cache.page : 0;
-        auto load = [&](Quarter& r, int& places, const int tile) {
-            const Rows rows = rows_of<N>(a, bounds, kvh, tile, 2 * pair, places);
-            places = ask_places<N>(a, bounds, tile + 2, 2 * pair);
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const SubTile t = sub_tile<D, F8>(a, rows, u);
-#pragma unroll
-                for (int x = 0; x < CH; ++x) r.c[u][x] = load16(of_v ? t.v : t.k, lane_at, chunk_at * x);
-                if constexpr (F8) r.s[u] = __builtin_amdgcn_raw_buffer_load_b32(t.s, scale_lane, scale_at, 0);
-            }
-        };
-        const int whole = min(max(min(ctx, len), 0) / TOKENS, t1);
-        auto put = [&](const Quarter& r, const int stage) {
-            unsigned char* to = lds + stage * STAGE + of_v * K_BYTES + 16 * lane;
-            TileRegs<D, F8, 2> x;
-            if (!of_v) {
+        Sums<D, NB> y;
+        if (t0 < t1) {
+            // this wave's quarter of a tile: K or V of two sub-tiles
+            struct Quarter { u32x4 c[2][CH]; uint32_t s[2]; };
+            const int of_v = wave & 1, pair = wave >> 1;
+            const int lane_at = of_v ? g * 4 * D * SIZE + 16 * n : n * D * SIZE + 16 * g, chunk_at = of_v ? 256 : 64;
+            const int scale_lane = of_v ? 4 * g : n & 12, scale_at = of_v ? a.cache.page : 0;
+            auto load = [&](Quarter& r, int& places, const int tile) {
+                const Rows rows = rows_of<N>(a, bounds, kvh, tile, 2 * pair, places);
+                places = ask_places<N>(a, bounds, tile + 2, 2 * pair);
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
+                    const SubTile t = sub_tile<D, F8>(a, rows, u);
 #pragma unroll
-                    for (int z = 0; z < CH; ++z) x.k[u][z] = r.c[u][z];
-                    x.ks[u] = r.s[u];
-#pragma unroll
-                    for (int s = 0; s < KS; ++s) *reinterpret_cast<bf16x8*>(to + ((2 * pair + u) * KS + s) * 1024) = k_operand<D, F8, 2>(x, u, s);
+                    for (int x = 0; x < CH; ++x) r.c[u][x] = load16(of_v ? t.v : t.k, lane_at, chunk_at * x);
+                    if constexpr (F8) r.s[u] = __builtin_amdgcn_raw_buffer_load_b32(t.s, scale_lane, scale_at, 0);
                 }
-                return;
-            }
-            if constexpr (F8) {
-                float s[2][4];
+            };
+            const int whole = min(max(min(ctx, len), 0) / TOKENS, t1);
+            auto put = [&](const Quarter& r, const int stage) {
+                unsigned char* to = lds + stage * STAGE + of_v * K_BYTES + 16 * lane;
+                TileRegs<D, F8, 2> x;
+                if (!of_v) {
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
+                    for (int u = 0; u < 2; ++u) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[u][e] = scale_value(r.s[u] >> 8 * e & 0xFF);
+                        for (int z = 0; z < CH; ++z) x.k[u][z] = r.c[u][z];
+                        x.ks[u] = r.s[u];
 #pragma unroll
-                for (int t = 0; t < VT; ++t)
-                    *reinterpret_cast<bf16x8*>(to + (pair * VT + t) * 1024) = operand(widen_each(r.c[0][t / 4][t % 4], s[0]), widen_each(r.c[1][t / 4][t % 4], s[1]));
-            } else {
+                        for (int s = 0; s < KS; ++s) *reinterpret_cast<bf16x8*>(to + ((2 * pair + u) * KS + s) * 1024) = k_operand<D, F8, 2>(x, u, s);
+                    }
+                    return;
+                }
+                if constexpr (F8) {
+                    float s[2][4];
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
+                    for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int z = 0; z < CH; ++z) x.v[u][z] = r.c[u][z];
+                        for (int e = 0; e < 4; ++e) s[u][e] = scale_value(r.s[u] >> 8 * e & 0xFF);
 #pragma unroll
-                for (int t = 0; t < VT; ++t) *reinterpret_cast<bf16x8*>(to + (pair * VT + t) * 1024) = v_operand<D, F8, 2>(x, 0, t);
-            }
-        };
-        Quarter r0, r1;
-        int p0 = ask_places<N>(a, bounds, t0, 2 * pair), p1 = ask_places<N>(a, bounds, t0 + 1, 2 * pair);
-        load(r0, p0, t0);
-        Queries<D, NB> q;
-        load_queries<D, F8, NB>(a, bounds, kvh, bounds.row0 + (works ? row_group * 32 : 0), q);
-        __builtin_amdgcn_sched_barrier(0);
-        load(r1, p1, t0 + 1);
-        __builtin_amdgcn_sched_barrier(0);
-        constexpr int SECOND = 2 * (CH + (F8 ? 1 : 0)) + 1;
-        __builtin_amdgcn_s_waitcnt(0x0F70 | (SECOND & 0xF) | (SECOND >> 4 << 14));     // (the rows too, tree_attn_kernel)
-        const float sl2 = a.scale * kLog2e;
+                    for (int t = 0; t < VT; ++t)
+                        *reinterpret_cast<bf16x8*>(to + (pair * VT + t) * 1024) = operand(widen_each(r.c[0][t / 4][t % 4], s[0]), widen_each(r.c[1][t / 4][t % 4], s[1]));
+                } else {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int z = 0; z < CH; ++z) x.v[u][z] = r.c[u][z];
+#pragma unroll
+                    for (int t = 0; t < VT; ++t) *reinterpret_cast<bf16x8*>(to + (pair * VT + t) * 1024) = v_operand<D, F8, 2>(x, 0, t);
+                }
+            };
+            Quarter r0, r1;
+            int p0 = ask_places<N>(a, bounds, t0, 2 * pair), p1 = ask_places<N>(a, bounds, t0 + 1, 2 * pair);
+            load(r0, p0, t0);
+            Queries<D, NB> q;
+            load_queries<D, F8, NB>(a, bounds, kvh, bounds.row0 + (works ? row_group * 32 : 0), q);
+            __builtin_amdgcn_sched_barrier(0);
+            load(r1, p1, t0 + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            constexpr int SECOND = 2 * (CH + (F8 ? 1 : 0)) + 1;
+            __builtin_amdgcn_s_waitcnt(0x0F70 | (SECOND & 0xF) | (SECOND >> 4 << 14));     // (the rows too, tree_attn_kernel)
+            const float sl2 = a.scale * kLog2e;
 
-        // 32 keys of the tile, those of sub-tile pair x0
-        auto step = [&](const int tile, const int stage, const int x0, auto edge) {
-            constexpr int XN = 1, SN = 2 * XN;
-            constexpr bool EDGE = decltype(edge)::value;
-            const unsigned char* k = lds + stage * STAGE + 16 * lane + x0 * 2 * KS * 1024;
-            const unsigned char* v = lds + stage * STAGE + K_BYTES + 16 * lane + x0 * VT * 1024;
-            // operands are read RING steps ahead (all at once they would need the registers that there are)
-            constexpr int RING = 4, KF = SN * KS, VF = XN * VT;
-            bf16x8 ring[RING];
-            floatx4 s[NB][SN];
+            // 32 keys of the tile, those of sub-tile pair x0
+            auto step = [&](const int tile, const int stage, const int x0, auto edge) {
+                constexpr int XN = 1, SN = 2 * XN;
+                constexpr bool EDGE = decltype(edge)::value;
+                const unsigned char* k = lds + stage * STAGE + 16 * lane + x0 * 2 * KS * 1024;
+                const unsigned char* v = lds + stage * STAGE + K_BYTES + 16 * lane + x0 * VT * 1024;
+                // operands are read RING steps ahead (all at once they would need the registers that there are)
+                constexpr int RING = 4, KF = SN * KS, VF = XN * VT;
+                bf16x8 ring[RING];
+                floatx4 s[NB][SN];
 #pragma unroll
-            for (int f = 0; f < RING; ++f) ring[f] = *reinterpret_cast<const bf16x8*>(k + f * 1024);
+                for (int f = 0; f < RING; ++f) ring[f] = *reinterpret_cast<const bf16x8*>(k + f * 1024);
 #pragma unroll
-            for (int f = 0; f < KF; ++f) {
+                for (int f = 0; f < KF; ++f) {
 #pragma unroll
-                for (int b = 0; b < NB; ++b)
-                    s[b][f / KS] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ring[f % RING], q.q[b][f % KS], f % KS == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : s[b][f / KS], 0, 0, 0);
-                ring[f % RING] = *reinterpret_cast<const bf16x8*>(f + RING < KF ? k + (f + RING) * 1024 : v + (f + RING - KF) * 1024);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            uint32_t hidden[NB] = {};
-            if constexpr (EDGE) {
+                    for (int b = 0; b < NB; ++b)
+                        s[b][f / KS] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ring[f % RING], q.q[b][f % KS], f % KS == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : s[b][f / KS], 0, 0, 0);
+                    ring[f % RING] = *reinterpret_cast<const bf16x8*>(f + RING < KF ? k + (f + RING) * 1024 : v + (f + RING - KF) * 1024);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                __builtin_amdgcn_s_setprio(0);
+                uint32_t hidden[NB] = {};
+                if constexpr (EDGE) {
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
+                        uint32_t seen = 0;
+#pragma unroll
+                        for (int u = 0; u < SN; ++u) seen |= seen_of_four(q.bits[b], tile * TOKENS + 32 * x0 + 16 * u + 4 * g, ctx, len) << 4 * u;
+                        hidden[b] = ~seen;
+                    }
+                }
+                bf16x8 pf[NB][XN];
 #pragma unroll
                 for (int b = 0; b < NB; ++b) {
-                    uint32_t seen = 0;
+                    float p[4 * SN];
+                    probabilities<D, SN, EDGE, true>(s[b], hidden[b], sl2, y.o[b], y.l[b], y.m[b], p);
 #pragma unroll
-                    for (int u = 0; u < SN; ++u) seen |= seen_of_four(q.bits[b], tile * TOKENS + 32 * x0 + 16 * u + 4 * g, ctx, len) << 4 * u;
-                    hidden[b] = ~seen;
+                    for (int x = 0; x < XN; ++x)
+                        pf[b][x] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(p[8 * x], p[8 * x + 1]), pack_bf16x2(p[8 * x + 2], p[8 * x + 3]),
+                                                                    pack_bf16x2(p[8 * x + 4], p[8 * x + 5]), pack_bf16x2(p[8 * x + 6], p[8 * x + 7])});
                 }
-            }
-            bf16x8 pf[NB][XN];
+                __builtin_amdgcn_s_setprio(1);
+                const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                float p[4 * SN];
-                probabilities<D, SN, EDGE, true>(s[b], hidden[b], sl2, y.o[b], y.l[b], y.m[b], p);
+                for (int f = 0; f < VF; ++f) {
+                    const int x = f / VT, t = f % VT;
+                    if (t == 0) {
 #pragma unroll
-                for (int x = 0; x < XN; ++x)
-                    pf[b][x] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(p[8 * x], p[8 * x + 1]), pack_bf16x2(p[8 * x + 2], p[8 * x + 3]),
-                                                                pack_bf16x2(p[8 * x + 4], p[8 * x + 5]), pack_bf16x2(p[8 * x + 6], p[8 * x + 7])});
-            }
-            const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
+                        for (int b = 0; b < NB; ++b) y.l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[b][x], y.l[b], 0, 0, 0);       // (of the rounded probabilities)
+                    }
+                    if constexpr (EDGE) product_with_hidden<NB, D, XN>(ring[f % RING], hidden, x, pf, y, t);
+                    else {
 #pragma unroll
-            for (int f = 0; f < VF; ++f) {
-                const int x = f / VT, t = f % VT;
-                if (t == 0) {
-#pragma unroll
-                    for (int b = 0; b < NB; ++b) y.l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[b][x], y.l[b], 0, 0, 0);       // (of the rounded probabilities)
+                        for (int b = 0; b < NB; ++b) y.o[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ring[f % RING], pf[b][x], y.o[b][t], 0, 0, 0);
+                    }
+                    if (f + RING < VF) ring[f % RING] = *reinterpret_cast<const bf16x8*>(v + (f + RING) * 1024);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                if constexpr (EDGE) product_with_hidden<NB, D, XN>(ring[f % RING], hidden, x, pf, y, t);
-                else {
-#pragma unroll
-                    for (int b = 0; b < NB; ++b) y.o[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ring[f % RING], pf[b][x], y.o[b][t], 0, 0, 0);
-                }
-                if (f + RING < VF) ring[f % RING] = *reinterpret_cast<const bf16x8*>(v + (f + RING) * 1024);
-                __builtin_amdgcn_sched_barrier(0);
+            };
+            const int x0 = sharers == 1 ? 0 : half, x1 = sharers == 1 ? 2 : half + 1;
+            // Whatever feeds the matrix pipe and the copies goes before the other wave's softmax (trees of 64 requests 648 -> 640 us)
+            __builtin_amdgcn_s_setprio(1);
+            // LDS alone is waited for: the quarters on their way stay so
+            const auto all_here = [&] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+            put(r0, 0);
+            load(r0, p0, t0 + 2);
+            // Tiles that every row sees whole, then the others, as in tree_attn_kernel.  A tile is requested three turns before it is used: two of them in registers.
+            int tile = t0;
+            const auto turn = [&](Quarter& r, int& p, const int stage) {
+                all_here();
+                put(r, stage ^ 1);
+                load(r, p, tile + 3);
+                if (works) for (int x = x0; x < x1; ++x) step(tile, stage, x, std::false_type{});
+                ++tile;
+            };
+            while (tile + 1 < whole) {                                 // (one way out, as there)
+                turn(r1, p1, 0);
+                turn(r0, p0, 1);
             }
-        };
-        const int x0 = sharers == 1 ? 0 : half, x1 = sharers == 1 ? 2 : half + 1;
-        // LDS alone is waited for: the quarters on their way stay so
-        const auto all_here = [&] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
-        put(r0, 0);
-        load(r0, p0, t0 + 2);
-        // Tiles that every row sees whole, then the others, as in tree_attn_kernel.  A tile is requested three turns before it is used: two of them in registers.
-        int tile = t0;
-        const auto turn = [&](Quarter& r, int& p, const int stage) {
-            all_here();
-            put(r, stage ^ 1);
-            load(r, p, tile + 3);
-            if (works) for (int x = x0; x < x1; ++x) step(tile, stage, x, std::false_type{});
-            ++tile;
-        };
-        while (tile + 1 < whole) {                                 // (one way out, as there)
-            turn(r1, p1, 0);
-            turn(r0, p0, 1);
+            if (tile < whole) {
+                turn(r1, p1, 0);
+                r1 = r0;
+            }
+            while (tile < t1) {
+                const int stage = (tile - t0) & 1;
+                all_here();
+                put(r1, stage ^ 1);
+                p1 = ask_places<N>(a, bounds, tile + 2, 2 * pair);
+                load(r1, p1, tile + 2);
+                if (works) for (int x = x0; x < x1; ++x) step(tile, stage, x, std::true_type{});
+                ++tile;
+            }
         }
-        if (tile < whole) {
-            turn(r1, p1, 0);
-            r1 = r0;
-        }
-        while (tile < t1) {
-            const int stage = (tile - t0) & 1;
-            all_here();
-            put(r1, stage ^ 1);
-            p1 = ask_places<N>(a, bounds, tile + 2, 2 * pair);
-            load(r1, p1, tile + 2);
-            if (works) for (int x = x0; x < x1; ++x) step(tile, stage, x, std::true_type{});
-            ++tile;
-        }
-    }
-    finish<D, F8, NB, false>(a, w, bounds, kvh, kWaves / sharers, sharers, y, lds, &last);
+        finish<D, F8, NB, false>(a, w, bounds, kvh, kWaves / sharers, sharers, y, lds, &last);
     });
 }
 
@@ -919,7 +933,7 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a) {
 template <int D, bool F8> constexpr int kSubTiles1 = D == 64 ? 4 : 2;
 template <int D, bool F8> constexpr int kSubTiles2 = F8 && D == 64 ? 4 : 2;
 template <int D, bool F8> constexpr int kWavesOf2 = F8 || D == 64 ? 2 : 1;
-constexpr int kLeastKeys = 256;                     // keys of a piece at least: four users' tokens 13.1 us, with 128 15.6, with 512 13.4; 51-token trees of six requests 44, 55, 50
+constexpr int kLeastKeys = 256;                     // keys of a piece at least: when four users' tokens took 13.1 us, they took 15.6 with 128 and 13.4 with 512; 51-token trees of six requests 44, 55, 50
 
 template <int D, bool F8>
 int launch(TreeArgs a, const TreeShape& s, hipStream_t st) {
@@ -935,16 +949,16 @@ int launch(TreeArgs a, const TreeShape& s, hipStream_t st) {
         a.chunk_shift = s.rows == 16 ? 4 : 5;
         a.by_chunks = FastDiv::by(static_cast<uint32_t>(a.chunks));
         const dim3 grid(static_cast<unsigned>((units + kWaves - 1) / kWaves));
-        if (row_blocks == 1) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 1, kSubTiles1<D, F8>, 2, 2, true>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((tree_attn_kernel<D, F8, 2, kSubTiles2<D, F8>, 2, kWavesOf2<D, F8>, true>), grid, block, 0, st, a);
+        if (row_blocks == 1) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 1, kSubTiles1<D, F8>, 2, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((tree_attn_kernel<D, F8, 2, kSubTiles2<D, F8>, kWavesOf2<D, F8>, true>), grid, block, 0, st, a);
         return static_cast<int>(hipGetLastError());
     }
     // (workgroups without a piece take 3 us, two at a time on a unit: there are no more of them than half a round)
     const int64_t workgroups = (a.whole ? loads : loads <= a.items / 2 ? a.items : loads + a.items / 2) * a.cache.Hkv;
     if (workgroups > 0x7FFFFFFF) return static_cast<int>(hipErrorInvalidConfiguration);
     const dim3 grid(static_cast<unsigned>(workgroups));
-    if (row_blocks == 1) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 1, kSubTiles1<D, F8>, 2, 2>), grid, block, 0, st, a);
-    else if (row_blocks == 2) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 2, kSubTiles2<D, F8>, 2, kWavesOf2<D, F8>>), grid, block, 0, st, a);
+    if (row_blocks == 1) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 1, kSubTiles1<D, F8>, 2>), grid, block, 0, st, a);
+    else if (row_blocks == 2) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 2, kSubTiles2<D, F8>, kWavesOf2<D, F8>>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((tree_attn_wide_kernel<D, F8>), grid, block, 0, st, a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess || row_blocks == 1 || a.whole) return static_cast<int>(e);
     // the merge: up to 2048 workgroups, of 8 rows and more each
