@@ -553,8 +553,8 @@ int pk_kv_cache_write(const pk_cache* cache, const pk_rows* k, const pk_rows* v,
                       int64_t tokens, void* stream);
 
 /* pk_qkv_cache_write -- pk_qk_norm_rope and pk_kv_cache_write in one launch: q
- * goes to q_out, k is normed, rotated and written to the cache from fp32
- * without a rounding in between, v is written.  q, k and v of one dtype. */
+ * goes to q_out, k is normed and rotated in fp64 and rounded once, to what the
+ * cache holds, v is written.  q, k and v of one dtype. */
 int pk_qkv_cache_write(const pk_cache* cache, const pk_rows* q, const pk_rows* k, const pk_rows* v,
                        const int64_t* slots, const pk_rows* q_out,
                        const void* q_weight, const void* k_weight, float eps, const pk_rope* rope,
