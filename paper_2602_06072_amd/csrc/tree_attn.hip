@@ -235,9 +235,11 @@ struct TreeCount {
     __device__ __forceinline__ uint32_t next(const uint32_t limit) const { return __builtin_amdgcn_atomic_inc32(x, limit, __ATOMIC_RELAXED, "agent"); }
 };
 
-// All ones in the place of the bf16 numbers of a word that are not finite
+// All ones in the place of the bf16 numbers of a word that are not finite: an exponent of ones and one more is the sign of a half, and that is spread
 __device__ __forceinline__ uint32_t not_finite(const uint32_t x) {
-    return ((x & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((x & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+    typedef short i16x2 __attribute__((ext_vector_type(2)));
+    const i16x2 y = __builtin_bit_cast(i16x2, (x & 0x7F807F80u) + 0x00800080u);
+    return __builtin_bit_cast(uint32_t, y >> 15);
 }
 
 // Which of the keys key .. key + 3 a row sees, bit by bit: those of the context, of the drafted tokens those in its mask word, none from len on.
