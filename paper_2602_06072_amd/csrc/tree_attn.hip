@@ -8,7 +8,7 @@
 //
 // With u = rows and L = keys of a request a launch reads (2 d + 2) L bytes a KV head (4 d L from bf16) and computes 4 d u L operations: memory bounds it up to some
 // 100 rows, the matrix pipe beyond.  Measured (MI355X, cache in 8 bits, 8 KV heads of 128 columns): 256 single tokens behind 32 .. 16384 tokens with 32 heads 352 us,
-// 6.1 TB/s; 128 trees with 64 heads 153 us and 8 for the merge, of 97 for the whole step's bytes; 64 trees of up to 64 tokens with 64 heads 640 us, 0.74 PFLOP/s
+// 6.1 TB/s; 128 trees with 64 heads 149 us and 8 for the merge, of 97 for the whole step's bytes; 64 trees of up to 64 tokens with 64 heads 637 us, 0.74 PFLOP/s
 // of the pairs that are seen (a product of large matrices reaches 1.34).
 //
 // Roundings: K and V to bf16 are exact (4 bits of fraction and a power of two); probabilities are rounded to bf16 for the matrix pipe, half a unit of 2^-8, and

@@ -81,6 +81,18 @@ def test_batches_of_every_kind(n, top, most, Hq, Hkv, d, page, cache):
     dense(s, None, chain)
 
 
+@pytest.mark.parametrize("cache", [pk.PK_F8, pk.PK_BF16])
+@pytest.mark.parametrize("n, top, most, Hq, Hkv, d", [(100, 60, 20, 40, 8, 64), (80, 100, 17, 64, 8, 128), (70, 4, 64, 16, 8, 64), (90, 0, 33, 32, 8, 128)])
+def test_many_short_trees(n, top, most, Hq, Hkv, d, cache):
+    """Tables of 256 keys and fewer: no request has two pieces.  Two chunks of rows, a second one of a few rows, contexts of nothing."""
+    ctx, drafts = ragged(3 * n, n, top, most)
+    s = step.make(most, ctx, drafts, Hq, Hkv, d, 16, cache)
+    assert s["table"].shape[1] * 16 <= 256
+    for kind in ("tree", "bits"):
+        mask = step.masks(s, kind)
+        dense(s, mask, step.call(s, mask))
+
+
 @pytest.mark.parametrize("Hq, Hkv, drafts", [(8, 8, 2), (16, 4, 6), (32, 2, 12)])
 def test_the_width_of_the_table_changes_no_result_beyond_rounding(Hq, Hkv, drafts):
     """A wide table allows long requests, so that a launch is laid out for them; the requests are the same short ones."""
