@@ -31,17 +31,23 @@ __device__ __forceinline__ float max_of_lane_groups(float x) {
     return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
 }
 
-// Sum over the wave, in every lane; sums of the lanes up to each one
-__device__ __forceinline__ int wave_prefix(int x) {
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);         // row_shr 1, 2, 4, 8
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);        // row_bcast 15 into rows 1 and 3, 31 into rows 2 and 3
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+// Sums of the lanes up to each one; the last lane's in all of them
+template <int CTRL, int ROWS, class T>
+__device__ __forceinline__ T from_before(const T x) {      // of a lane before this one, or 0
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, ROWS, 0xF, ROWS == 0xF));
+}
+template <class T>
+__device__ __forceinline__ T wave_prefix(T x) {
+    x += from_before<0x111, 0xF>(x);                // row_shr 1, 2, 4, 8
+    x += from_before<0x112, 0xF>(x);
+    x += from_before<0x114, 0xF>(x);
+    x += from_before<0x118, 0xF>(x);
+    x += from_before<0x142, 0xA>(x);                // row_bcast 15 into rows 1 and 3, 31 into rows 2 and 3
+    x += from_before<0x143, 0xC>(x);
     return x;
 }
-__device__ __forceinline__ int last_lane(const int x) { return __builtin_amdgcn_readlane(x, 63); }
+template <class T>
+__device__ __forceinline__ T last_lane(const T x) { return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63)); }
 
 // What a workgroup works on: a piece of the tiles of a request, for some of its rows (a chunk).
 struct Piece {
@@ -93,15 +99,16 @@ __device__ __forceinline__ void for_loads(const TreeArgs& a, const Loads<KEPT>& 
 }
 template <int TOKENS, int KEPT>
 __device__ __forceinline__ Shares share_of(const TreeArgs& a, const Loads<KEPT>& l) {
-    int total = 0, loads = 0;
+    float tiles = 0.f;                              // (of requests that share their pages there may be more than 2^31)
+    int loads = 0;
     for_loads<TOKENS>(a, l, [&](int, const Load w) {
-        total += w.tiles * w.chunks;
+        tiles = fmaf(static_cast<float>(w.tiles), static_cast<float>(w.chunks), tiles);
         loads += w.chunks;
         return false;
     });
-    total = last_lane(wave_prefix(total));
+    tiles = fmaxf(last_lane(wave_prefix(tiles)), 1.f);
     loads = last_lane(wave_prefix(loads));
-    const float least = a.least_per_share, tiles = static_cast<float>(max(total, 1)), places = static_cast<float>(a.items), taken = static_cast<float>(loads);
+    const float least = a.least_per_share, places = static_cast<float>(a.items), taken = static_cast<float>(loads);
     Shares s{0.f, -1, 0};
     const bool one_round = taken <= 0.75f * places;
     // the two shares to be looked at, or how many pieces are long and half as long

@@ -220,3 +220,34 @@ def test_many_kept_tokens(T, kept, page, cache):
     for x, y in zip(step.token_major(s["c"]), want):
         assert np.array_equal(x, y, equal_nan=True)
     assert new.tolist() == [s["lens"][i] - T + min(int(count[i]), now, T) for i in range(n)]
+
+
+@pytest.mark.parametrize("cache, blocks", [(pk.PK_F8, 290_000), (pk.PK_BF16, 150_000)])
+def test_a_cache_of_more_than_four_gib(cache, blocks):
+    """Every call on the last pages of a cache whose K and V are longer than 2^32 bytes each, against the same pages of a small one."""
+    g, Hkv, d, page, n, T = step.gen(9), 8, 128, 16, 3, 5
+    far, near = pk.new_kv_cache(blocks, page, Hkv, d, cache), pk.new_kv_cache(12, page, Hkv, d, cache)
+    assert far.k.nbytes > 1 << 32
+    table = torch.arange(12, dtype=torch.int32, device=DEV).view(n, 4).flip(0).contiguous()
+    lens = torch.tensor([64, 37, 20], dtype=torch.int32, device=DEV)
+    rows = step.randn(g, 12 * page, Hkv, d), step.randn(g, 12 * page, Hkv, d)
+    q, w = step.randn(g, n * T, 16, d), step.randn(g, d)
+    q_start = torch.arange(0, n * T + 1, T, dtype=torch.int32, device=DEV)
+    rope = pk.Rope(step.table_of(64, d), torch.arange(n * T, dtype=torch.int32, device=DEV))
+    keep = torch.tensor([[1, 3], [0, 4], [2, 3]], dtype=torch.int32, device=DEV)
+    results = []
+    for c, first in ((near, 0), (far, blocks - 12)):
+        slots = torch.arange(12 * page, device=DEV) + first * page
+        pk.kv_cache_write(c, *rows, slots)
+        at = table + first
+        new = torch.cat([at[i].long()[(torch.arange(T, device=DEV) + int(lens[i]) - T) // page] * page + (torch.arange(T, device=DEV) + int(lens[i]) - T) % page for i in range(n)])
+        qo, out, after = torch.empty_like(q), torch.empty_like(q), torch.empty_like(lens)
+        pk.qkv_cache_write(c, q, rows[0][:n * T], rows[1][:n * T], new, qo, w, w, 1e-6, rope)
+        pk.tree_attn(c, qo, q_start, T, None, at, lens, out, d ** -0.5, pk.new_tree_workspace(n, T, 16, Hkv, d))
+        pk.kv_cache_keep(c, at, lens, q_start, keep, torch.full_like(lens, 2), after)
+        k, v = (torch.zeros(128, Hkv, d, device=DEV) for _ in "kv")
+        pk.kv_cache_read(c, at, after, torch.tensor([0, 64, 101], dtype=torch.int32, device=DEV), k, v)
+        results.append((qo, out, after, k, v))
+    for x, y in zip(*results):
+        assert torch.equal(x, y)
+    assert (results[0][3] != 0).any() and (results[0][1] != 0).any()
