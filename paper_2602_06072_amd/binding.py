@@ -17,6 +17,7 @@ import numpy as np
 PK_BF16, PK_F32, PK_F8 = 0, 1, 2
 PK_GROUP_ALIGN = 32
 PK_KV_BLOCK = 32
+PK_MAX_DRAFTS = 64
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpackinfer.so")
@@ -601,10 +602,16 @@ def tree_attn(cache: KvCache, q, q_start, max_q, tree_mask, block_table, kv_lens
     return out
 
 
-def kv_cache_keep(cache: KvCache, block_table, kv_lens, q_start, keep, keep_count, new_lens, stream=None):
+def kv_cache_keep(cache: KvCache, block_table, kv_lens, q_start, keep, keep_count, new_lens, *more, stream=None):
     """Drafted tokens keep[i, :keep_count[i]] (rising) of every request move up behind its context; new_lens receives
-    the lengths with them."""
+    the lengths with them.  The bound max_q of tree_attn may stand in front of keep."""
     L = lib()
+    if not isinstance(keep, _torch.Tensor):
+        _need(len(more) > 0, "kv_cache_keep takes [max_q], keep, keep_count and new_lens")
+        max_q, keep, keep_count, new_lens, more = int(keep), keep_count, new_lens, more[0], more[1:]
+        _need(0 <= max_q <= PK_MAX_DRAFTS, "need 0 <= max_q <= 64")
+    _need(len(more) < 2 and not (more and stream is not None), "kv_cache_keep: one stream behind new_lens")
+    stream = more[0] if more else stream
     n, max_blocks = block_table.shape
     _need(keep.dim() == 2 and keep.shape[0] == n, "keep must be [n, max_keep]")
     rc = L.pk_kv_cache_keep(cache.raw, _vector(block_table, "block_table", _torch.int32), max_blocks, _vector(kv_lens, "kv_lens", _torch.int32, n),
