@@ -331,7 +331,7 @@ def _run_own(s):
     pk.tree_attn(s["cache"], s["q"], s["q_start"], s["max_q"], s["mask"], s["block_table"], s["lens"], s["out"], s["scale"], s["ws"])
     if op == "tree":
         return s["out"]
-    pk.kv_cache_keep(s["cache"], s["block_table"], s["lens"], s["q_start"], s["keep"], s["count"], s["new_lens"])
+    pk.kv_cache_keep(s["cache"], s["block_table"], s["lens"], s["q_start"], s["max_q"], s["keep"], s["count"], s["new_lens"])
     return _step_outputs(s)
 
 
