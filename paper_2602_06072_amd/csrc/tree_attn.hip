@@ -11,8 +11,9 @@
 // 6.1 TB/s; 128 trees with 64 heads 149 us and 8 for the merge, of 97 for the whole step's bytes; 64 trees of up to 64 tokens with 64 heads 637 us, 0.74 PFLOP/s
 // of the pairs that are seen (a product of large matrices reaches 1.34).
 //
-// Roundings: K and V to bf16 are exact (4 bits of fraction and a power of two); probabilities are rounded to bf16 for the matrix pipe, half a unit of 2^-8, and
-// their sum is that of the rounded ones; scores, sums, accumulators and partial results have 32 bits.
+// Roundings: K and V to bf16 are exact (4 bits of fraction and a power of two; below 2^-126 multiples of 2^-133); probabilities are rounded to bf16 for the matrix
+// pipe, half a unit of 2^-8, whatever the type of the output, and their sum is that of the rounded ones; scores, sums, accumulators and partial results have 32 bits.
+// The scales of V stay out of the probabilities: times 2^-126 a probability would be a denormal of a bit or none, and a row of zeros would lose its weight.
 #include "arrival.h"
 #include "cache_format.hip.h"
 
@@ -203,6 +204,15 @@ __device__ __forceinline__ uint2 widen(const uint32_t x, const float scale) {
     return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false)),
                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true)));
 }
+// 4 codes of four tokens -> bf16 values times each one's scale
+__device__ __forceinline__ uint2 widen_each(const uint32_t x, const float (&s)[4]) {
+    const auto two = [&](auto high, const float p, const float q) {
+        constexpr bool HIGH = decltype(high)::value;
+        return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, q, HIGH)),
+                                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, p, HIGH)), 0x07060100u);
+    };
+    return make_uint2(two(std::false_type{}, s[0], s[1]), two(std::true_type{}, s[2], s[3]));
+}
 __device__ __forceinline__ bf16x8 operand(const uint2 a, const uint2 b) { return __builtin_bit_cast(bf16x8, u32x4{a.x, a.y, b.x, b.y}); }
 
 // Operands of the products.  K: columns of step s and lane group g; V: column of A row m in block t.
@@ -217,10 +227,23 @@ __device__ __forceinline__ bf16x8 k_operand(const TileRegs<D, F8, N>& r, const i
         return __builtin_bit_cast(bf16x8, r.k[u][s]);
     }
 }
-template <int D, bool F8, int N>
-__device__ __forceinline__ bf16x8 v_operand(const TileRegs<D, F8, N>& r, const int b, const int t) {
+// scales of the keys of V that a lane has
+template <bool F8, int N> struct ValueScales { float of[F8 ? N : 1][4]; };
+template <bool F8, int N>
+__device__ __forceinline__ ValueScales<F8, N> value_scales(const uint32_t (&bytes)[N]) {
+    ValueScales<F8, N> s;
     if constexpr (F8) {
-        return operand(widen(r.v[2 * b][t / 4][t % 4], 1.f), widen(r.v[2 * b + 1][t / 4][t % 4], 1.f));
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s.of[u][e] = scale_value(bytes[u] >> 8 * e & 0xFF);
+    }
+    return s;
+}
+template <int D, bool F8, int N>
+__device__ __forceinline__ bf16x8 v_operand(const TileRegs<D, F8, N>& r, const ValueScales<F8, N>& s, const int b, const int t) {
+    if constexpr (F8) {
+        return operand(widen_each(r.v[2 * b][t / 4][t % 4], s.of[2 * b]), widen_each(r.v[2 * b + 1][t / 4][t % 4], s.of[2 * b + 1]));
     } else {
         const u32x4 x = r.v[2 * b][t / 2], y = r.v[2 * b + 1][t / 2];
         return t % 2 == 0 ? __builtin_bit_cast(bf16x8, u32x4{x[0], x[1], y[0], y[1]}) : __builtin_bit_cast(bf16x8, u32x4{x[2], x[3], y[2], y[3]});
@@ -634,18 +657,6 @@ __global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(
                         for (int u = 0; u < N; ++u) seen |= seen_of_four(q.bits[b], key0 + 16 * u, ctx, len) << 4 * u;
                         hidden[b] = ~seen;
                     }
-                    if constexpr (F8) {                                // a scale where there is no key may be anything
-#pragma unroll
-                        for (int x = 0; x < 4 * N; ++x)
-                            if (key0 + 16 * (x / 4) + x % 4 >= len) r.vs[x / 4] = (r.vs[x / 4] & ~(0xFFu << 8 * (x % 4))) | 127u << 8 * (x % 4);
-                    }
-                }
-                float factor[F8 ? N : 1][4];
-                if constexpr (F8) {
-#pragma unroll
-                    for (int u = 0; u < N; ++u)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) factor[u][e] = scale_value(r.vs[u] >> 8 * e & 0xFF);
                 }
                 bf16x8 pf[NB][N / 2];
                 __builtin_amdgcn_sched_barrier(0);
@@ -655,29 +666,20 @@ __global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(
                     probabilities<D, N, EDGE, false>(s[b], hidden[b], sl2, y.o[b], y.l[b], y.m[b], p);
                     uint32_t pw[2 * N];
 #pragma unroll
-                    for (int x = 0; x < 4 * N; ++x)
-                        if constexpr (F8) p[x] *= factor[x / 4][x % 4];        // the scale of V, a power of two: it rounds nothing
-#pragma unroll
                     for (int x = 0; x < 2 * N; ++x) pw[x] = pack_bf16x2(p[2 * x], p[2 * x + 1]);
 #pragma unroll
                     for (int x = 0; x < N / 2; ++x) pf[b][x] = __builtin_bit_cast(bf16x8, u32x4{pw[4 * x], pw[4 * x + 1], pw[4 * x + 2], pw[4 * x + 3]});
                 }
+                const ValueScales<F8, N> scales = value_scales<F8>(r.vs);
 #pragma unroll
                 for (int x = 0; x < N / 2; ++x) {
-                    // sums of the ROUNDED probabilities (their error cancels in part) from the matrix pipe: every row of A holds the inverse scales
-                    u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
-                    if constexpr (F8) {
+                    // sums of the ROUNDED probabilities (their error cancels in part) from the matrix pipe
+                    const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint32_t two = r.vs[2 * x + e / 2] >> 16 * (e % 2);
-                            ones[e] = (254u - (two & 0xFF)) << 7 | (254u - (two >> 8 & 0xFF)) << 23;
-                        }
-                    }
-#pragma unroll
-                    for (int b = 0; b < NB; ++b) y.l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones), pf[b][x], y.l[b], 0, 0, 0);
+                    for (int b = 0; b < NB; ++b) y.l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[b][x], y.l[b], 0, 0, 0);
 #pragma unroll
                     for (int t = 0; t < VT; ++t) {
-                        const bf16x8 v = v_operand<D, F8, N>(r, x, t);
+                        const bf16x8 v = v_operand<D, F8, N>(r, scales, x, t);
                         if constexpr (EDGE) product_with_hidden<NB, D, N / 2>(v, hidden, x, pf, y, t);
                         else {
 #pragma unroll
@@ -720,16 +722,6 @@ __global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(
     } else {
         run_pieces<TOKENS, 4>(work);
     }
-}
-
-// 4 codes of four tokens -> bf16 values times each one's scale
-__device__ __forceinline__ uint2 widen_each(const uint32_t x, const float (&s)[4]) {
-    const auto two = [&](auto high, const float p, const float q) {
-        constexpr bool HIGH = decltype(high)::value;
-        return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, q, HIGH)),
-                                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, p, HIGH)), 0x07060100u);
-    };
-    return make_uint2(two(std::false_type{}, s[0], s[1]), two(std::true_type{}, s[2], s[3]));
 }
 
 // More rows, 128 in a workgroup: bound by the matrix pipe and what surrounds it (for 32 keys and 32 rows 34 MFMAs of 16 cycles, 16 exponentials of 16, some 60 other
@@ -786,23 +778,14 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 && F8 ? 3 : 2) void tree_attn_
                     }
                     return;
                 }
-                if constexpr (F8) {
-                    float s[2][4];
 #pragma unroll
-                    for (int u = 0; u < 2; ++u)
+                for (int u = 0; u < 2; ++u) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[u][e] = scale_value(r.s[u] >> 8 * e & 0xFF);
-#pragma unroll
-                    for (int t = 0; t < VT; ++t)
-                        *reinterpret_cast<bf16x8*>(to + (pair * VT + t) * 1024) = operand(widen_each(r.c[0][t / 4][t % 4], s[0]), widen_each(r.c[1][t / 4][t % 4], s[1]));
-                } else {
-#pragma unroll
-                    for (int u = 0; u < 2; ++u)
-#pragma unroll
-                        for (int z = 0; z < CH; ++z) x.v[u][z] = r.c[u][z];
-#pragma unroll
-                    for (int t = 0; t < VT; ++t) *reinterpret_cast<bf16x8*>(to + (pair * VT + t) * 1024) = v_operand<D, F8, 2>(x, 0, t);
+                    for (int z = 0; z < CH; ++z) x.v[u][z] = r.c[u][z];
                 }
+                const ValueScales<F8, 2> scales = value_scales<F8>(r.s);
+#pragma unroll
+                for (int t = 0; t < VT; ++t) *reinterpret_cast<bf16x8*>(to + (pair * VT + t) * 1024) = v_operand<D, F8, 2>(x, scales, 0, t);
             };
             Quarter r0, r1;
             int p0 = ask_places<N>(a, bounds, t0, 2 * pair), p1 = ask_places<N>(a, bounds, t0 + 1, 2 * pair);
