@@ -496,12 +496,12 @@ class KvCache:
 
 
 def new_kv_cache(num_blocks, page_size, Hkv, d, dtype=PK_F8, device="cuda") -> KvCache:
-    """A cache of zeros."""
+    """A cache of zeros (with the scale that rows of zeros have)."""
     lib()
     t = _torch.float8_e4m3fn if dtype == PK_F8 else _torch.bfloat16
-    zeros = lambda shape, t: _torch.zeros(shape, dtype=_torch.uint8 if t.itemsize == 1 else t, device=device).view(t)  # noqa: E731
-    return KvCache(zeros((num_blocks, Hkv, page_size, d), t), zeros((num_blocks, Hkv, page_size // 4, d, 4), t),
-                   zeros((num_blocks, Hkv, 2, page_size), _torch.float8_e8m0fnu) if dtype == PK_F8 else None)
+    zeros = lambda shape: _torch.zeros(shape, dtype=_torch.uint8 if t.itemsize == 1 else t, device=device).view(t)  # noqa: E731
+    scales = _torch.ones((num_blocks, Hkv, 2, page_size), dtype=_torch.uint8, device=device).view(_torch.float8_e8m0fnu) if dtype == PK_F8 else None
+    return KvCache(zeros((num_blocks, Hkv, page_size, d)), zeros((num_blocks, Hkv, page_size // 4, d, 4)), scales)
 
 
 class Rope:

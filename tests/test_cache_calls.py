@@ -24,3 +24,11 @@ def test_keep_takes_the_bound_of_the_drafted_tokens_or_not():
     for args in ((5, *what[:2]), (-1, *what), (65, *what), (5, *what, Stream, Stream), (*what, Stream, Stream)):
         with pytest.raises(pk.PackInferError):
             pk.kv_cache_keep(*where, *args)
+
+
+def test_a_new_cache_holds_rows_of_zeros_as_the_format_has_them():
+    c = pk.new_kv_cache(3, 32, 2, 64, device="cpu")
+    assert (c.k.view(torch.uint8) == 0).all() and (c.v.view(torch.uint8) == 0).all()
+    assert (c.scales.view(torch.uint8) == 1).all()                 # 2^-126, the smallest scale: byte 0 stands for none
+    b = pk.new_kv_cache(3, 32, 2, 64, pk.PK_BF16, device="cpu")
+    assert b.scales is None and (b.k == 0).all() and (b.v == 0).all()
