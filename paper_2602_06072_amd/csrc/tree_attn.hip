@@ -386,7 +386,7 @@ __device__ __forceinline__ void load_queries(const TreeArgs& a, const Bounds& w,
 
 // Probabilities of 16 N keys against a row, from their raw scores.  `hidden`: bit x for key x that the row does not see (looked at with EDGE).
 // LAZY: they are relative to m, which need not be the maximum: bf16 and fp32 hold 2^8 as well as 1, so what is summed up so far is brought to a new
-// maximum only when a probability reaches that (m = -inf in front of a wave's first tile: they are infinite then).  A maximum across the lanes for
+// maximum only when a probability reaches that, and as long as m is -inf (a wave's first tile, scores of -inf).  A maximum across the lanes for
 // every tile costs as much as the exponents' arithmetic.
 constexpr float kMostProbability = 256.f;
 template <int D, int N, bool EDGE, bool LAZY>
@@ -399,7 +399,7 @@ __device__ __forceinline__ void probabilities(const floatx4 (&s)[N], const uint3
             p[x] = __builtin_amdgcn_exp2f(fmaf(raw(x), sl2, -m));
             top = fmaxf(top, p[x]);
         }
-        if (!__any(!(top < kMostProbability))) return;
+        if (!__any(!(top < kMostProbability) || m == -INFINITY)) return;
     }
     float mx = raw(0);
 #pragma unroll

@@ -111,3 +111,30 @@ def test_the_smallest_scale_of_k(drafts, heads):
     pk.kv_cache_write(s["c"], k, v, s["at"])
     bytes_of(s, 0)(torch.arange(0, 700, 3, device=DEV), 1)
     paths.dense(s, None, step.call(s, None))
+
+
+@pytest.mark.parametrize("first, last", [(0, 32), (0, 64), (64, 700), (0, 1490)])
+@pytest.mark.parametrize("drafts, heads", ROWS + [(17, 8)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_keys_whose_scores_are_minus_infinity_have_no_weight(drafts, heads, first, last, d):
+    """Infinite keys of a bf16 cache, at the front and where pieces begin; the others' results are finite."""
+    s = one_request(drafts, 1500 + drafts, drafts, heads, d, pk.PK_BF16)
+    k, v = rows_of(s, d)
+    k[first:last, :, 0] = -float("inf")
+    pk.kv_cache_write(s["c"], k, v, s["at"])
+    paths.dense(s, None, step.call(s, None))
+
+
+@pytest.mark.parametrize("keys, slope", [(300, 0.2), (600, 0.09), (1500, 0.03), (300, -0.2), (64, 0.9), (64, -0.9)])
+@pytest.mark.parametrize("cache", [pk.PK_F8, pk.PK_BF16])
+@pytest.mark.parametrize("drafts, heads", ROWS + [(17, 8)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_scores_that_rise_and_fall_from_tile_to_tile(drafts, heads, cache, keys, slope, d):
+    """Scores up to 60 that change by less and by more than 2^8 from one half-tile of 32 keys to the next, in the order of the keys.  fp32
+    sums of four products at a time err by 60 * 2^-24 each, 32 of them at most, half of it one way: 6e-5 of the 1e-4 that there are."""
+    s = one_request(drafts + keys, keys, drafts, heads, d, cache)
+    k, v = rows_of(s, d)
+    ramp = slope * torch.arange(keys, device=DEV)
+    k[..., 0] = ((ramp - ramp.mean()) * d ** 0.5 / 8)[:, None]
+    pk.kv_cache_write(s["c"], k, v, s["at"])
+    paths.dense(s, None, step.call(s, None))
