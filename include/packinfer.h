@@ -589,9 +589,9 @@ int pk_kv_cache_read(const pk_cache* cache, const int32_t* block_table, int32_t 
  *   out       device [total_q][Hq][d], out_dtype, 16-byte aligned
  *   workspace device, 256-byte aligned, at least pk_tree_attn_workspace_bytes.
  *             ZERO-FILLED BEFORE ITS FIRST USE; every call leaves it ready for the
- *             next.  One made for some n and max_q serves all calls of the same
- *             head shape that have no more of either; all calls with it pass the
- *             same workspace_bytes and are ordered by the caller.
+ *             next.  One workspace serves all calls with the same Hkv for which it is
+ *             large enough (PK_EINVAL otherwise), whatever it was made for; the
+ *             caller orders them.
  * The partial results of a request are put together in a fixed order: results
  * repeat bit for bit.
  * Errors: PK_EINVAL; PK_EUNSUPPORTED (page size, d, max_q). */

@@ -58,10 +58,24 @@ int launch_cache_keep(CacheKeepArgs a, void* stream);
 // KV head run at once; of more requests than that a piece has at most 4 / rounds of what a workgroup's place gets to do.
 struct TreeShape {
     int rows, chunks, items, rounds, alone_chunks;  // alone_chunks: chunks of 32 rows (16 with no more), where a wave has a request
-    // both grow with n and max_q, so that a workspace serves every call of one head shape that is not larger than what it was made for
-    size_t count_bytes(int64_t n, int Hkv) const { return static_cast<size_t>((n * Hkv * chunks * 4 + 255) / 256 * 256 + (n * 8 + 255) / 256 * 256); }
-    size_t partial_bytes(int Hkv, int d, int compute_units) const;
+    int64_t rows_of_slots(int Hkv, int compute_units) const { return slots(rounds, Hkv, compute_units) * rows; }
+    size_t partial_bytes(int Hkv, int d, int compute_units) const { return whole256(rows_of_slots(Hkv, compute_units) * (d + 1) * 4); }
+    // Counts of arrivals, one for every slot where up to 16 rows are joined in the launch.  They come first in a workspace, and how many there are depends
+    // neither on n nor on max_q: no call, whatever the others were, has its counts where another one has written something else.
+    static size_t count_bytes(int Hkv, int compute_units) { return whole256(slots(kRoundsOfFewRows, Hkv, compute_units) * 4); }
+    static size_t pieces_bytes(int64_t n) { return whole256(n * 8); }
     static TreeShape of(int max_q, int Hq, int Hkv, int compute_units);
+
+    static constexpr int kRoundsOfFewRows = 8;      // (of up to 32 rows)
+
+private:
+    // Pieces of cut requests, all KV heads together.  A piece has at least 4 / (items * rounds) of all tiles, and only requests of more than that are cut:
+    // twice as many slots hold the pieces of all.
+    static int64_t slots(int rounds, int Hkv, int compute_units) {
+        const int64_t most = Hkv > 2 * compute_units ? Hkv : 2 * compute_units;
+        return (rounds + 1) / 2 * most + 64;
+    }
+    static size_t whole256(int64_t bytes) { return static_cast<size_t>((bytes + 255) / 256 * 256); }
 };
 
 struct TreeArgs {
@@ -70,7 +84,7 @@ struct TreeArgs {
     const uint64_t* mask;                           // [total_q]; null: every drafted token sees those before it and itself
     const int32_t* kv_lens; int32_t n;
     void* out; int out_f32; float scale; int Hq;
-    uint32_t* arrived;                              // [n][Hkv][chunks], zero between launches (arrival.h)
+    uint32_t* arrived;                              // [slots][Hkv], a request's at its first slot; zero between launches (arrival.h)
     int2* pieces_of;                                // [n] pieces of a request and slot of the first one, for the merge in a launch of its own
     float* part_lse; float* part_o;                 // [slots][Hkv][rows], [..][d]
     // set by the launch

@@ -139,16 +139,10 @@ bool tree_sizes_ok(const int64_t n, const int64_t max_q, const int64_t Hq, const
 
 TreeShape TreeShape::of(const int max_q, const int Hq, const int Hkv, const int compute_units) {
     const int rows = max_q * (Hq / Hkv);
-    TreeShape s{rows <= 16 ? 16 : rows <= 32 ? 32 : 128, 1, 0, rows <= 32 ? 8 : 5, (rows + 31) / 32};
+    TreeShape s{rows <= 16 ? 16 : rows <= 32 ? 32 : 128, 1, 0, rows <= 32 ? kRoundsOfFewRows : 5, (rows + 31) / 32};
     s.chunks = rows <= s.rows ? 1 : (rows + s.rows - 1) / s.rows;
     s.items = 2 * compute_units > Hkv ? 2 * compute_units / Hkv : 1;       // (two workgroups of a compute unit)
     return s;
-}
-
-// A piece has at least 4 / (items * rounds) of all tiles, and only requests of more than that are cut: twice as many slots hold the pieces of all.
-size_t TreeShape::partial_bytes(const int Hkv, const int d, const int compute_units) const {
-    const int64_t most = Hkv > 2 * compute_units ? Hkv : 2 * compute_units;
-    return static_cast<size_t>((((rounds + 1) / 2 * most + 64) * rows * (d + 1) * 4 + 255) / 256 * 256);
 }
 
 extern "C" int pk_qk_norm_rope(const pk_rows* q, const pk_rows* k, const pk_rows* q_out, const pk_rows* k_out,
@@ -225,7 +219,7 @@ extern "C" size_t pk_tree_attn_workspace_bytes(int32_t n, int32_t max_q, int Hq,
         if (!tree_sizes_ok(n, max_q, Hq, Hkv, d)) return 0;
         const int cus = compute_units();
         const TreeShape s = TreeShape::of(max_q, Hq, Hkv, cus);
-        return s.count_bytes(n, Hkv) + s.partial_bytes(Hkv, d, cus);
+        return TreeShape::count_bytes(Hkv, cus) + s.partial_bytes(Hkv, d, cus) + TreeShape::pieces_bytes(n);
     });
 }
 
@@ -248,21 +242,19 @@ extern "C" int pk_tree_attn(const pk_cache* cache, const void* q, const int32_t*
         if (!workspace || !aligned(workspace, 256)) return refuse(who, {PK_EINVAL, "workspace is NULL or not 256-byte aligned"});
         const int cus = compute_units();
         const TreeShape shape = TreeShape::of(max_q, Hq, cache->Hkv, cus);
-        const size_t partial = shape.partial_bytes(cache->Hkv, cache->d, cus);
-        workspace_bytes = workspace_bytes / 256 * 256;
-        if (workspace_bytes < shape.count_bytes(n, cache->Hkv) + partial)
+        const size_t counts = TreeShape::count_bytes(cache->Hkv, cus), partial = shape.partial_bytes(cache->Hkv, cache->d, cus);
+        if (workspace_bytes < counts + partial + TreeShape::pieces_bytes(n))
             return refuse(who, {PK_EINVAL, "workspace smaller than pk_tree_attn_workspace_bytes"});
         TreeArgs a{};
         a.cache = view(*cache); a.block_table = block_table; a.max_blocks = max_blocks;
         a.q = q; a.q_start = q_start; a.total_q = total_q; a.max_q = max_q; a.mask = tree_mask;
         a.kv_lens = kv_lens; a.n = n;
         a.out = out; a.out_f32 = out_dtype == PK_F32; a.scale = scale; a.Hq = Hq;
-        // counts at the front, partial results at the end: no call writes the counts of another
-        a.arrived = static_cast<uint32_t*>(workspace);
-        char* end = static_cast<char*>(workspace) + workspace_bytes;
-        a.part_o = reinterpret_cast<float*>(end - partial);
-        a.pieces_of = reinterpret_cast<int2*>(end - partial - (static_cast<size_t>(n) * 8 + 255) / 256 * 256);
-        a.part_lse = a.part_o + partial / 4 / (cache->d + 1) * cache->d;
+        char* at = static_cast<char*>(workspace);
+        a.arrived = reinterpret_cast<uint32_t*>(at);
+        a.part_o = reinterpret_cast<float*>(at + counts);
+        a.part_lse = a.part_o + shape.rows_of_slots(cache->Hkv, cus) * cache->d;
+        a.pieces_of = reinterpret_cast<int2*>(at + counts + partial);
         return launched(who, launch_tree_attn(a, shape, stream));
     });
 }

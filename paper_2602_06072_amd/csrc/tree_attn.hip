@@ -559,7 +559,7 @@ __device__ __forceinline__ void finish(const TreeArgs& a, const Piece& w, const 
     __builtin_amdgcn_s_waitcnt(0x0F70);            // vmcnt(0): this wave's partial results are in memory
     __syncthreads();
     if (threadIdx.x == 0) {
-        const int64_t group = (static_cast<int64_t>(w.request) * a.cache.Hkv + kvh) * a.chunks + w.chunk;
+        const int64_t group = static_cast<int64_t>(w.slot - w.piece * w.chunks) * a.cache.Hkv + kvh;
         *last = arrives_last(TreeCount{a.arrived + group}, static_cast<uint32_t>(w.pieces));
     }
     __syncthreads();

@@ -32,3 +32,12 @@ def test_a_new_cache_holds_rows_of_zeros_as_the_format_has_them():
     assert (c.scales.view(torch.uint8) == 1).all()                 # 2^-126, the smallest scale: byte 0 stands for none
     b = pk.new_kv_cache(3, 32, 2, 64, pk.PK_BF16, device="cpu")
     assert b.scales is None and (b.k == 0).all() and (b.v == 0).all()
+
+
+@pytest.mark.parametrize("Hq, Hkv, d", [(32, 8, 128), (16, 1, 64), (64, 64, 64), (2048, 1024, 128)])
+def test_the_counts_of_a_workspace_do_not_grow_with_requests(Hq, Hkv, d):
+    """What has to be zero lies at the front and is as long for every call: more requests take the eight bytes that each call writes before it reads them."""
+    size = pk.lib().pk_tree_attn_workspace_bytes
+    for max_q in (1, 5, 64):
+        assert size(65535, max_q, Hq, Hkv, d) - size(1, max_q, Hq, Hkv, d) == 65535 * 8 // 256 * 256
+    assert size(1, 64, Hq, Hkv, d) >= size(1, 1, Hq, Hkv, d) > 0
