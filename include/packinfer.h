@@ -482,8 +482,8 @@ int pk_plan_tune(pk_plan* plan, int knob, int64_t value);
 
 /* Rows [token][head][d] in device memory; strides in elements, the d columns of
  * a row contiguous.  dtype PK_BF16 or PK_F32.  data and both strides are whole
- * multiples of 16 bytes (PK_EINVAL otherwise); strides are not negative, those
- * of outputs keep rows apart.  An output may be its own input (same data and
+ * multiples of 16 bytes (PK_EINVAL otherwise); strides are not negative, lead
+ * over no more than 2^59 elements, and those of outputs keep rows apart.  An output may be its own input (same data and
  * strides), and otherwise does not overlap any input. */
 typedef struct pk_rows {
     void* data;

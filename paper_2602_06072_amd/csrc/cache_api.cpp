@@ -26,7 +26,7 @@ int launched(const char* who, const int e) {
 bool aligned(const void* p, const size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
 constexpr int64_t kMostTokens = 0x7FFFFFFF;
-constexpr int64_t kMostStride = int64_t{1} << 40;   // elements: products with token numbers stay within 64 bits
+constexpr int64_t kMostExtent = int64_t{1} << 59;   // elements that one stride may lead to: two of them in bytes stay within 64 bits
 
 Refusal check_rows(const pk_rows* r, const char* name, const int64_t tokens, const int heads, const int d, const int dtype, const bool output) {
     const std::string n = name;
@@ -36,7 +36,7 @@ Refusal check_rows(const pk_rows* r, const char* name, const int64_t tokens, con
     const int unit = r->dtype == PK_F32 ? 4 : 8;
     if (!aligned(r->data, 16) || r->token_stride % unit != 0 || r->head_stride % unit != 0)
         return {PK_EINVAL, n + ": address and strides must be multiples of 16 bytes"};
-    if (r->token_stride < 0 || r->head_stride < 0 || r->token_stride > kMostStride || r->head_stride > kMostStride)
+    if (r->token_stride < 0 || r->head_stride < 0 || r->token_stride > kMostExtent / (tokens > 0 ? tokens : 1) || r->head_stride > kMostExtent / heads)
         return {PK_EINVAL, n + ": stride out of range"};
     if (output) {                                   // rows that lie apart one way or the other: heads inside tokens or tokens inside heads
         const bool heads_inside = (heads == 1 || r->head_stride >= d) && (tokens <= 1 || r->token_stride >= (heads - 1) * r->head_stride + d);
@@ -63,6 +63,7 @@ Refusal check_rope(const pk_rope* r, const int d) {
     if (!r->table || !r->positions) return {PK_EINVAL, "table or positions of the rotation is NULL"};
     if (!aligned(r->table, 16)) return {PK_EINVAL, "the table of the rotation must be 16-byte aligned"};
     if (r->max_pos <= 0 || r->n_axes <= 0 || r->n_axes > 255 || r->axis_stride < 0) return {PK_EINVAL, "need max_pos > 0, 0 < n_axes < 256, axis_stride >= 0"};
+    if (r->axis_stride > kMostExtent / r->n_axes) return {PK_EINVAL, "axis_stride out of range"};
     if (r->rot_dim <= 0 || r->rot_dim > d) return {PK_EINVAL, "need 0 < rot_dim <= d"};
     if (r->rot_dim % 16 != 0) return {PK_EUNSUPPORTED, "rot_dim must be a multiple of 16"};
     if (r->interleaved != 0 && r->interleaved != 1) return {PK_EINVAL, "interleaved must be 0 or 1"};

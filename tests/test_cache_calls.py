@@ -3,6 +3,9 @@ import pytest
 import torch
 
 from paper_2602_06072_amd import binding as pk
+from tests.test_cache_refusals import cache, refused, rope, rows
+
+EINVAL, P = -1, 1 << 20
 
 
 def empty_keep(n=0):
@@ -41,3 +44,26 @@ def test_the_counts_of_a_workspace_do_not_grow_with_requests(Hq, Hkv, d):
     for max_q in (1, 5, 64):
         assert size(65535, max_q, Hq, Hkv, d) - size(1, max_q, Hq, Hkv, d) == 65535 * 8 // 256 * 256
     assert size(1, 64, Hq, Hkv, d) >= size(1, 1, Hq, Hkv, d) > 0
+
+
+@pytest.mark.parametrize("tokens, ts, hs", [((1 << 31) - 1, 1 << 29, 128), (1 << 20, 1 << 40, 128), (4, 1 << 58, 128), (1, 1 << 62, 128), (4, 4096, 1 << 57)])
+def test_strides_whose_products_leave_64_bits_are_refused(tokens, ts, hs):
+    far, near = rows(ts=ts, hs=hs), rows(ts=4096)
+    L = pk.lib()
+    for q, k, q_out, k_out in ((far, near, near, near), (near, far, near, near), (near, near, far, near), (near, near, near, far)):
+        refused(L.pk_qk_norm_rope(q, k, q_out, k_out, None, None, 0.0, None, tokens, 8, 8, 128, None), EINVAL, "stride out of range")
+    refused(L.pk_kv_cache_write(cache(), rows(), far, P, tokens, None), EINVAL, "stride out of range")
+    refused(L.pk_kv_cache_read(cache(), P, 4, P, P, 3, near, far, tokens, None), EINVAL, "stride out of range")
+
+
+def test_strides_are_accepted_up_to_the_bound():
+    """The next argument is refused: the strides were not."""
+    L, most = pk.lib(), (1 << 59) // ((1 << 31) - 1) // 8 * 8
+    for ts, hs, tokens in ((most, 1 << 56, (1 << 31) - 1), (1 << 59, 128, 1), (1 << 40, 1 << 41, 1 << 19)):
+        far = rows(ts=ts, hs=hs)
+        refused(L.pk_qk_norm_rope(far, far, None, None, None, None, 0.0, None, tokens, 8, 8, 128, None), EINVAL, "q_out is NULL")
+
+
+@pytest.mark.parametrize("stride, axes", [(1 << 62, 3), ((1 << 59) + 4, 1), ((1 << 63) - 1, 255)])
+def test_axis_strides_whose_products_leave_64_bits_are_refused(stride, axes):
+    refused(pk.lib().pk_qk_norm_rope(rows(ts=4096), rows(), rows(ts=4096), rows(), None, None, 0.0, rope(stride=stride, axes=axes), 4, 32, 8, 128, None), EINVAL, "axis_stride")
