@@ -440,9 +440,10 @@ __global__ __launch_bounds__(128) void cache_keep_kernel(CacheKeepArgs a) {
     constexpr int BATCH = 8;
     const int i = blockIdx.x, h = blockIdx.y, lane = threadIdx.x;
     const CacheView& c = a.cache;
-    const int drafts = a.q_start[i + 1] - a.q_start[i], base = a.kv_lens[i] - drafts;
-    const int count = min(max(min(a.keep_count[i], a.max_keep), 0), max(drafts, 0));
-    if (h == 0 && lane == 0) a.new_lens[i] = base + count;
+    // (64 bits: whatever the arrays hold, no sum leads past the table)
+    const int64_t drafts = static_cast<int64_t>(a.q_start[i + 1]) - a.q_start[i], base = a.kv_lens[i] - drafts;
+    const int count = static_cast<int>(min(static_cast<int64_t>(max(min(a.keep_count[i], a.max_keep), 0)), max(drafts, int64_t{0})));
+    if (h == 0 && lane == 0) a.new_lens[i] = static_cast<int32_t>(base + count);
     const int32_t* row = a.block_table + static_cast<int64_t>(i) * a.max_blocks;
     const int32_t* keep = a.keep + static_cast<int64_t>(i) * a.max_keep;
     const int end = static_cast<int>(min(static_cast<int64_t>(a.max_blocks) * c.page, static_cast<int64_t>(0x7FFFFFFF)));
@@ -459,7 +460,7 @@ __global__ __launch_bounds__(128) void cache_keep_kernel(CacheKeepArgs a) {
         for (int u = 0; u < BATCH; ++u) {
             const int j = min(j0 + u, count - 1), f = keep[j];
             moves[u] = j0 + u < count && f > j && f < drafts && base + j >= 0 && base + f < end;     // not in its place already, and a drafted token
-            const int s = moves[u] ? base + f : 0, t = moves[u] ? base + j : 0, sp = a.by_page(s), tp = a.by_page(t);
+            const int s = moves[u] ? static_cast<int>(base + f) : 0, t = moves[u] ? static_cast<int>(base + j) : 0, sp = a.by_page(s), tp = a.by_page(t);
             from[u] = block_of(c, row, sp);
             to[u] = block_of(c, row, tp);
             from_off[u] = s - sp * c.page;
