@@ -609,7 +609,7 @@ int pk_tree_attn(const pk_cache* cache, const void* q, const int32_t* q_start, i
  *   keep        device int32 [n][max_keep], rising in every row; numbers outside
  *               of [0, T_i) are passed over
  *   keep_count  device int32 [n]; clamped into [0, min(max_keep, T_i)]
- *   new_lens    device int32 [n], not kv_lens itself
+ *   new_lens    device int32 [n], not kv_lens itself nor in another of the arrays
  * Other arguments as for pk_tree_attn.  Errors: PK_EINVAL; PK_EUNSUPPORTED. */
 int pk_kv_cache_keep(const pk_cache* cache, const int32_t* block_table, int32_t max_blocks,
                      const int32_t* kv_lens, const int32_t* q_start, int32_t n,

@@ -271,7 +271,14 @@ extern "C" int pk_kv_cache_keep(const pk_cache* cache, const int32_t* block_tabl
         if (max_keep < 0) return refuse(who, {PK_EINVAL, "max_keep is negative"});
         if (n == 0) return PK_OK;
         if (!q_start || (!keep && max_keep > 0) || !keep_count || !new_lens) return refuse(who, {PK_EINVAL, "q_start, keep, keep_count or new_lens is NULL"});
-        if (new_lens == kv_lens) return refuse(who, {PK_EINVAL, "new_lens must not be kv_lens itself"});
+        // (a workgroup writes a request's new length while those of its other heads still read)
+        const auto meets = [&](const void* p, const int64_t words) {
+            const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(new_lens);
+            return x < y + static_cast<uintptr_t>(n) * 4 && y < x + static_cast<uintptr_t>(words) * 4;
+        };
+        if (meets(kv_lens, n) || meets(q_start, n + 1) || meets(keep_count, n) || meets(keep, static_cast<int64_t>(n) * max_keep) ||
+            meets(block_table, static_cast<int64_t>(n) * max_blocks))
+            return refuse(who, {PK_EINVAL, "new_lens must not be kv_lens itself nor lie in another of the arrays"});
         CacheKeepArgs a{};
         a.cache = view(*cache); a.block_table = block_table; a.max_blocks = max_blocks;
         a.kv_lens = kv_lens; a.q_start = q_start; a.n = n;

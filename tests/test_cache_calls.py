@@ -67,3 +67,20 @@ def test_strides_are_accepted_up_to_the_bound():
 @pytest.mark.parametrize("stride, axes", [(1 << 62, 3), ((1 << 59) + 4, 1), ((1 << 63) - 1, 255)])
 def test_axis_strides_whose_products_leave_64_bits_are_refused(stride, axes):
     refused(pk.lib().pk_qk_norm_rope(rows(ts=4096), rows(), rows(ts=4096), rows(), None, None, 0.0, rope(stride=stride, axes=axes), 4, 32, 8, 128, None), EINVAL, "axis_stride")
+
+
+@pytest.mark.parametrize("name, words", [("lens", 3), ("start", 4), ("count", 3), ("keep", 15), ("table", 12)])
+def test_new_lengths_inside_of_an_array_that_is_read_are_refused(name, words):
+    """3 requests, 5 kept tokens, 4 pages each: places in front of, in and behind every array."""
+    at = dict(lens=P, start=P + 4096, count=P + 8192, keep=P + 12288, table=P + 16384)
+
+    def keep(new, max_keep=5):
+        return pk.lib().pk_kv_cache_keep(cache(), at["table"], 4, at["lens"], at["start"], 3, at["keep"], max_keep, at["count"], new, None)
+    for word in (-2, 0, words - 1):
+        refused(keep(at[name] + 4 * word), EINVAL, "new_lens must not be")
+    if torch.cuda.is_available():
+        return                                                     # (the others would be launched)
+    for word in (-3, words):
+        refused(keep(at[name] + 4 * word), -4, "")
+    if name == "keep":
+        refused(keep(at["keep"], 0), -4, "")                       # of no columns: nothing is read there
