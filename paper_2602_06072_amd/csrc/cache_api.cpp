@@ -58,9 +58,9 @@ Refusal check_cache(const pk_cache* c) {
     return {PK_OK, ""};
 }
 
-Refusal check_rope(const pk_rope* r, const int d) {
+Refusal check_rope(const pk_rope* r, const int64_t tokens, const int d) {
     if (!r) return {PK_OK, ""};
-    if (!r->table || !r->positions) return {PK_EINVAL, "table or positions of the rotation is NULL"};
+    if (!r->table || (!r->positions && tokens > 0)) return {PK_EINVAL, "table or positions of the rotation is NULL"};
     if (!aligned(r->table, 16)) return {PK_EINVAL, "the table of the rotation must be 16-byte aligned"};
     if (r->max_pos <= 0 || r->n_axes <= 0 || r->n_axes > 255 || r->axis_stride < 0) return {PK_EINVAL, "need max_pos > 0, 0 < n_axes < 256, axis_stride >= 0"};
     if (r->axis_stride > kMostExtent / r->n_axes) return {PK_EINVAL, "axis_stride out of range"};
@@ -75,7 +75,8 @@ Refusal check_rope(const pk_rope* r, const int d) {
 Refusal check_table(const int32_t* block_table, const int32_t max_blocks, const int32_t* kv_lens, const int32_t n, const pk_cache& c) {
     if (n < 0 || n > 65535) return {PK_EINVAL, "need 0 <= n < 65536"};
     if (n > 0 && (!block_table || !kv_lens)) return {PK_EINVAL, "block_table or kv_lens is NULL"};
-    if (max_blocks <= 0 || static_cast<int64_t>(max_blocks) * c.page_size > kMostTokens) return {PK_EINVAL, "need max_blocks > 0 and fewer than 2^31 tokens a request"};
+    if (n > 0 && max_blocks <= 0) return {PK_EINVAL, "need max_blocks > 0"};
+    if (max_blocks < 0 || static_cast<int64_t>(max_blocks) * c.page_size > kMostTokens) return {PK_EINVAL, "max_blocks is negative, or 2^31 tokens a request and more"};
     return {PK_OK, ""};
 }
 
@@ -106,7 +107,7 @@ int norm_rope_args(const char* who, const pk_rows* q, const pk_rows* k, const pk
     PK_CHECK(check_rows(q_out, "q_out", tokens, Hq, d, q_out->dtype, true));
     if ((q_weight || k_weight) && !(std::isfinite(eps) && eps >= 0.f)) return refuse(who, {PK_EINVAL, "eps must be finite and not negative"});
     if (!aligned(q_weight, 16) || !aligned(k_weight, 16)) return refuse(who, {PK_EINVAL, "weights must be 16-byte aligned"});
-    PK_CHECK(check_rope(rope, d));
+    PK_CHECK(check_rope(rope, tokens, d));
     a.q = view(*q); a.k = view(*k); a.q_out = view(*q_out);
     a.q_weight = q_weight; a.k_weight = k_weight; a.eps = eps;
     a.tokens = tokens; a.Hq = Hq; a.Hkv = Hkv; a.d = d;

@@ -84,3 +84,23 @@ def test_new_lengths_inside_of_an_array_that_is_read_are_refused(name, words):
         refused(keep(at[name] + 4 * word), -4, "")
     if name == "keep":
         refused(keep(at["keep"], 0), -4, "")                       # of no columns: nothing is read there
+
+
+def test_batches_of_nothing_are_no_work_for_the_binding():
+    """Tensors without elements, whose addresses are null: no tokens, no requests, tables without columns."""
+    f = lambda *shape, dtype=torch.bfloat16: torch.zeros(*shape, dtype=dtype)  # noqa: E731
+    i32 = lambda *shape: torch.zeros(*shape, dtype=torch.int32)  # noqa: E731
+    c, q, k = pk.new_kv_cache(4, 16, 2, 64, device="cpu"), f(0, 8, 64), f(0, 2, 64)
+    slots, rope = f(0, dtype=torch.int64), pk.Rope(f(4, 2, 32, dtype=torch.float32), i32(0))
+    assert rope.positions.data_ptr() == 0
+    w = f(64)
+    assert pk.qk_norm_rope(q, k, q.clone(), k.clone(), w, w, 1e-6, rope, stream=Stream)
+    assert pk.kv_cache_write(c, k, k, slots, stream=Stream) is c
+    assert pk.qkv_cache_write(c, q, k, k, slots, q, w, w, 1e-6, rope, stream=Stream) is q
+    for table in (i32(0, 3), i32(0, 0)):
+        assert pk.kv_cache_read(c, table, i32(0), i32(0), k, k, stream=Stream)
+        ws = pk.new_tree_workspace(0, 0, 8, 2, 64, device="cpu")
+        assert pk.tree_attn(c, q, i32(1), 0, None, table, i32(0), q, 0.1, ws, stream=Stream) is q
+        lens = i32(0)
+        assert pk.kv_cache_keep(c, table, i32(0), i32(1), i32(0, 0), i32(0), lens, stream=Stream) is lens
+    assert pk.tree_attn(c, q, i32(4), 5, f(0, dtype=torch.int64), i32(3, 2), i32(3), q, 0.1, ws, stream=Stream) is q     # requests without drafted tokens
