@@ -452,7 +452,8 @@ def _need(ok, what):
 
 # (checks on the way of every call name what they refuse only where they refuse: a formatted message takes as long as the check)
 def _rows(x, name, heads=None, d=None):
-    """pk_rows of a tensor [tokens, heads, d] (any strides, columns contiguous); None: a null pointer."""
+    """pk_rows of a tensor [tokens, heads, d] (any strides, columns contiguous); None: a null pointer.  A stride that leads
+    nowhere, of one token or one head, may be anything in a tensor."""
     if x is None:
         return None
     shape = x.shape
@@ -462,7 +463,7 @@ def _rows(x, name, heads=None, d=None):
     if cs != 1 and shape[2] != 1 and x.numel() != 0:
         raise PackInferError(f"{name} must have contiguous columns")
     code = _dtype_codes.get(x.dtype)
-    return _ROWS.pack(x.data_ptr(), ts, hs, _dtype_code(x) if code is None else code)
+    return _ROWS.pack(x.data_ptr(), ts if shape[0] > 1 else 0, hs if shape[1] > 1 else 0, _dtype_code(x) if code is None else code)
 
 
 def _vector(x, name, dtype, n=None):

@@ -104,3 +104,16 @@ def test_batches_of_nothing_are_no_work_for_the_binding():
         lens = i32(0)
         assert pk.kv_cache_keep(c, table, i32(0), i32(1), i32(0, 0), i32(0), lens, stream=Stream) is lens
     assert pk.tree_attn(c, q, i32(4), 5, f(0, dtype=torch.int64), i32(3, 2), i32(3), q, 0.1, ws, stream=Stream) is q     # requests without drafted tokens
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_strides_of_one_token_and_of_one_head_do_not_matter(dtype):
+    base = torch.zeros(5, 3, 131, dtype=dtype)                     # rows of an odd number of columns
+    one_token, one_head, one_row = base[2:3, :, :128], torch.zeros(5, 131 * 8, dtype=dtype)[:, None, :128].as_strided((5, 1, 128), (1048, 131, 1)), base[1:2, 1:2, :128]
+    unpacked = lambda x: pk._ROWS.unpack(pk._rows(x, "x"))[1:3]  # noqa: E731
+    assert unpacked(one_token) == (0, 131) and unpacked(one_head) == (1048, 0) and unpacked(one_row) == (0, 0)
+    row = torch.empty_strided((1, 1, 128), (77, 5, 1), dtype=dtype).zero_()
+    L, r = pk.lib(), pk._rows(row, "row")
+    refused(L.pk_qk_norm_rope(r, r, r, None, None, None, 0.0, None, 1, 1, 1, 128, None), EINVAL, "k_out is NULL")      # (the others were accepted)
+    far = rows(ts=77, hs=5)
+    refused(L.pk_qk_norm_rope(far, r, r, r, None, None, 0.0, None, 1, 1, 1, 128, None), EINVAL, "multiples of 16 bytes")   # as the header says
