@@ -935,9 +935,11 @@ int launch(TreeArgs a, const TreeShape& s, hipStream_t st) {
     const int64_t loads = static_cast<int64_t>(a.n) * a.chunks, most_keys = static_cast<int64_t>(a.max_blocks) * a.cache.page;
     a.whole = most_keys <= kLeastKeys;              // no request can have two pieces: nothing to be found out, nothing to be put together
     a.least_per_many = a.least_per_share / (s.rows == 128 ? 4 : 1);        // (cut into more, the partial results of 128 rows are more bytes than the keys)
-    // Short requests, and more of them than workgroups run at once: a wave for every request and 32 rows (300 requests of up to 17 tokens behind 60, 64 and 8 heads, 73 us and
-    // 142 by 128 rows; of up to 60, 272 and 344), but not for more than 32 rows of 64 columns, where a tile is converted in half the time (40 and 8 heads, up to 60 tokens, 134 and 102; 33, 80 and 86).
-    if (const int64_t units = static_cast<int64_t>(a.n) * a.cache.Hkv * s.alone_chunks; a.whole && (s.rows <= 32 || D == 128) && loads > a.items && units <= 0x7FFFFFFF) {
+    // Short requests, and more of them than workgroups run at once: a wave for every request and 32 rows (300 requests of up to 17 tokens behind 60, 64 and 8 heads of 128
+    // columns, 73 us and 142 by 128 rows; of up to 60, 272 and 344).  More than 32 rows of 64 columns in 8 bits stay with workgroups, which convert a tile once and not for
+    // every 32 rows: over 71 launches (70 or 300 requests behind up to 4, 60 or 180 tokens, four head shapes) they take 0.99 of the waves' time in the mean, 0.79 where the
+    // last 128 rows are more than 96, 1.09 where they are up to 32.  From bf16 nothing is converted, and they would take 1.25 of it.
+    if (const int64_t units = static_cast<int64_t>(a.n) * a.cache.Hkv * s.alone_chunks; a.whole && (s.rows <= 32 || D == 128 || !F8) && loads > a.items && units <= 0x7FFFFFFF) {
         a.chunks = s.alone_chunks;
         a.chunk_shift = s.rows == 16 ? 4 : 5;
         a.by_chunks = FastDiv::by(static_cast<uint32_t>(a.chunks));
