@@ -521,7 +521,10 @@ typedef struct pk_rope {
  * exponent bytes: b stands for 2^(b - 127), 1 <= b <= 254.  A row's byte is the
  * smallest whose scale s keeps its largest finite magnitude within 448 s, and
  * the code of x is x / s rounded to nearest even: dividing is exact, and what a
- * code stands for, code * s, is a bf16 number.  NaN and infinities become NaN.
+ * code stands for, code * s, is a bf16 number (but for the ends of the range: below
+ * 2^-126 bf16 has multiples of 2^-133, and 2^128, to which magnitudes from 1.9375
+ * * 2^127 on are rounded, is read as infinite).  A row of zeros has b = 1.  NaN and
+ * infinities become NaN.
  * Slot number s of the cache is token s % page_size of block s / page_size. */
 typedef struct pk_cache {
     void* k;
@@ -593,7 +596,11 @@ int pk_kv_cache_read(const pk_cache* cache, const int32_t* block_table, int32_t 
  *             large enough (PK_EINVAL otherwise), whatever it was made for; the
  *             caller orders them.
  * The partial results of a request are put together in a fixed order: results
- * repeat bit for bit.
+ * repeat bit for bit.  Probabilities are rounded to bf16 for the matrix pipe,
+ * whatever out_dtype is: a result is off by up to 2^-8 of sum p |v|, on the whole
+ * by 1e-3 of its norm; PK_F32 output leaves out its own rounding alone.  Scores
+ * and sums have 32 bits: where the largest score is s, sums of exp(score - s) v, in
+ * parts times up to 2^8, have to stay below 2^128.
  * Errors: PK_EINVAL; PK_EUNSUPPORTED (page size, d, max_q). */
 #define PK_MAX_DRAFTS 64
 size_t pk_tree_attn_workspace_bytes(int32_t n, int32_t max_q, int Hq, int Hkv, int d);

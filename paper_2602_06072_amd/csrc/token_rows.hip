@@ -3,9 +3,11 @@
 //
 // With x the row of a token's head: y = w x / sqrt(mean(x^2) + eps), pairs (a, b) of y turned to (a c - b s, b c + a s); into the cache as codes of E4M3 (nearest, ties to
 // even) times 2^E, the smallest E >= -126 that holds the row's largest finite magnitude within 448.  Sums and products have 32 bits, those of cached keys 64.
-// Measured (MI355X): 22011 tokens of 32 + 8 heads of 128 columns, bf16, 85 us, 5.4 TB/s; 44354 tokens of 8 heads of K and V into the cache 58 us, 4.7 TB/s (a large
-// copy 4.8); 307114 tokens of 8 heads read as bf16 rows 365 us, 5.2 TB/s, two thirds of it stores.  Stores past the caches take 72 instead of 85 us and
-// cost the next reader of the rows as much and more (2048 tokens and a pass over them 18.5 and 19.4 us, 16384 103 and 112).
+// Measured (MI355X): 22011 tokens of 32 + 8 heads of 128 columns, bf16, 85 us, 5.4 TB/s; 44354 tokens of 8 heads of K and V into the cache in 8 bits 58 us, 4.8 TB/s (a large
+// copy 4.8), 69 to 84 us right behind the read of the whole cache, from fp32 rows 101, into a bf16 cache 71; 307114 tokens of 8 heads read as bf16 rows 365 to 384 us, 5 TB/s, two
+// thirds of it stores, as fp32 rows 687, from a bf16 cache 503; norm, rotation and write of 22011 tokens in one launch 140 us, 3.6 TB/s, of 1080 tokens in runs of 4 .. 12 15 to 17,
+// where the bytes take 4: values outside of whole cells go one by one.  Stores past the caches take 72 instead of 85 us and cost the next reader of the rows as much and more
+// (2048 tokens and a pass over them 18.5 and 19.4 us, 16384 103 and 112).
 #include <type_traits>
 
 #include "cache_format.hip.h"
@@ -173,7 +175,7 @@ __global__ __launch_bounds__(64 * kWaves) void token_rows_kernel(TokenRowsArgs a
         }
     }
     // Where the lane's token goes.  Values are interleaved by four: four tokens in a row that fill such a cell go there together, by the wave that has the first of
-    // them, whichever tokens the wave has otherwise (prompts behind contexts of any length: 44354 tokens of 8 heads 89 -> 58 us, 4.7 TB/s, what a large copy reaches); the others one by one.
+    // them, whichever tokens the wave has otherwise (prompts behind contexts of any length: 44354 tokens of 8 heads 89 -> 58 us); the others one by one.
     Place own{t, 0, 0, false}, cell{t, 0, 0, false};
     bool any_cell = false, any_single = false, single = false;
     if (CACHED && last > steps_q) {

@@ -7,9 +7,9 @@
 // the four keys whose scores the lane holds, so that with few rows nothing goes through LDS on its way from memory to the matrix pipe.
 //
 // With u = rows and L = keys of a request a launch reads (2 d + 2) L bytes a KV head (4 d L from bf16) and computes 4 d u L operations: memory bounds it up to some
-// 100 rows, the matrix pipe beyond.  Measured (MI355X, cache in 8 bits, 8 KV heads of 128 columns): 256 single tokens behind 32 .. 16384 tokens with 32 heads 352 us,
-// 6.1 TB/s; 128 trees with 64 heads 149 us and 8 for the merge, of 97 for the whole step's bytes; 64 trees of up to 64 tokens with 64 heads 637 us, 0.74 PFLOP/s
-// of the pairs that are seen (a product of large matrices reaches 1.34).
+// 100 rows, the matrix pipe beyond.  Measured (MI355X, cache in 8 bits, 8 KV heads of 128 columns): 256 single tokens behind 32 .. 16384 tokens with 32 heads 353 us,
+// 6.1 TB/s; 128 trees of 4 .. 12 tokens with 32 heads 145 to 153 us and 8 for the merge, where the bytes take 94; 64 trees of up to 64 tokens with 64 heads 630 to 674
+// us, 0.70 to 0.75 PFLOP/s of the pairs that are seen (a product of large matrices reaches 1.34); from a bf16 cache 228 us with the merge, of 184, and 779.
 //
 // Roundings: K and V to bf16 are exact (4 bits of fraction and a power of two; below 2^-126 multiples of 2^-133); probabilities are rounded to bf16 for the matrix
 // pipe, half a unit of 2^-8, whatever the type of the output, and their sum is that of the rounded ones; scores, sums, accumulators and partial results have 32 bits.
@@ -577,7 +577,7 @@ __device__ __forceinline__ void finish(const TreeArgs& a, const Piece& w, const 
     }
 }
 
-// Up to 16 NB rows: bound by memory, in short launches by latency (four single tokens behind 300 .. 3000 tokens 11.4 us: the pieces found 2 to 3, first tile 1 to 3,
+// Up to 16 NB rows: bound by memory, in short launches by latency (four single tokens behind 300 .. 3000 tokens 11 us: the pieces found 2 to 3, first tile 1 to 3,
 // tiles 2, last one 2, results and merge 2 to 4).  The four waves of a workgroup take tiles of N sub-tiles in turns, SETS tiles in flight in each, from memory into
 // registers and from there into the products.  ALONE: every wave has a request (and rows) of its own, all of whose tiles it takes.
 template <int D, bool F8, int NB, int N, int WAVES_PER_SIMD, bool ALONE = false>
