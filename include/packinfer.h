@@ -588,7 +588,8 @@ int pk_kv_cache_read(const pk_cache* cache, const int32_t* block_table, int32_t 
  *             PK_EUNSUPPORTED above 64); tokens beyond it are not computed
  *   tree_mask device uint64 [total_q]: bit j for drafted token j of the same
  *             request; NULL: token t sees tokens 0 .. t
- *   block_table, kv_lens: as for pk_kv_cache_read
+ *   block_table, kv_lens: as for pk_kv_cache_read (tokens of a length that the
+ *             table has no pages for are not there, drafted ones first)
  *   out       device [total_q][Hq][d], out_dtype, 16-byte aligned
  *   workspace device, 256-byte aligned, at least pk_tree_attn_workspace_bytes.
  *             ZERO-FILLED BEFORE ITS FIRST USE; every call leaves it ready for the
