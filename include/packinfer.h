@@ -46,7 +46,7 @@
  *     point catches host exceptions (PK_ENOMEM when host memory runs out).
  *   - dtype: PK_BF16 (MFMA path) or PK_F32 (plain-FMA debug path).  The calls
  *     of the second half of this file (norm, rotation, paged cache, drafted
- *     tokens) need no plan; their lengths and tables are device arrays, which
+ *     tokens, branching and judging) need no plan; their lengths and tables are device arrays, which
  *     the kernels bound by the sizes given on the host.
  *     out_dtype: PK_BF16 or PK_F32 for the attention outputs.
  */
@@ -623,6 +623,161 @@ int pk_kv_cache_keep(const pk_cache* cache, const int32_t* block_table, int32_t 
                      const int32_t* kv_lens, const int32_t* q_start, int32_t n,
                      const int32_t* keep, int32_t max_keep, const int32_t* keep_count,
                      int32_t* new_lens, void* stream);
+
+/* ========================================================================
+ * Branching and judging around that step: requests that come from one another
+ * share pages, pages are handed out, copied and moved on the device, and the
+ * drafted tokens that stay are found from the target's logits.
+ *
+ *   pk_kv_pages_select   a new batch out of rows of the old one: forked,
+ *                        reordered and finished requests
+ *   pk_kv_pages_reserve  pages for the next tokens of every request; a shared
+ *                        page that would be written is replaced by a copy
+ *   pk_kv_pages_compact  the pages in use get the lowest numbers
+ *   pk_kv_cache_copy     pages of one layer's cache
+ *   pk_shared_tree_attn  pk_tree_attn that reads shared pages once
+ *   pk_draft_verify      which drafted tokens stay, and the token behind them
+ *
+ * Nothing here allocates or reads lengths on the host: a step of all of them
+ * can be captured in a graph.
+ *
+ * The pages of a batch.  One batch serves all layers; what has to be copied is
+ * therefore a list, which pk_kv_cache_copy takes for each layer's cache.
+ *   block_table  device int32 [n][max_blocks]: the blocks of a request's pages
+ *   lens         device int32 [n]: its tokens
+ *   pages        device int32 [n]: entries of its row that it holds (at least
+ *                those of its tokens; more where room was reserved)
+ *   refs         device int32 [num_blocks]: how many requests hold a block;
+ *                0: it is free.  A caller may count itself in for blocks that are
+ *                to outlive the requests (a prefix that is kept).
+ * Lengths and pages are clamped into what a row has room for; entries outside
+ * of [0, num_blocks) are carried along and counted nowhere.
+ * ======================================================================== */
+
+/* pk_kv_pages_select -- request i of the new batch is request from[i] of the old
+ * one (several times the same: forks; from[i] outside of [0, n): an empty
+ * request) with the pages of its tokens; room that was reserved beyond them is
+ * given up.  refs changes by what the new batch holds less what the old one
+ * held, so a request that is not taken over is freed.
+ *   from, new_lens, new_pages  device int32 [n_new]; new_table [n_new][max_blocks],
+ *             whose entries behind a request's pages are left as they are
+ * No output overlaps an input or another output.  Errors: PK_EINVAL. */
+int pk_kv_pages_select(const int32_t* block_table, const int32_t* lens, const int32_t* pages, int32_t n, int32_t max_blocks,
+                       const int32_t* from, int32_t n_new, int32_t* new_table, int32_t* new_lens, int32_t* new_pages,
+                       int32_t* refs, int64_t num_blocks, int32_t page_size, void* stream);
+
+/* pk_kv_pages_reserve -- every request gets pages for lens[i] + grow[i] tokens (no
+ * more than max_blocks of them), in the order of requests the free blocks of
+ * the lowest numbers.  Where its next token goes to a page that holds tokens
+ * and that others hold too, the page is replaced by a free block and noted for
+ * copying: copy_src[i] -> copy_dst[i] (-1: nothing to copy), its block before its
+ * other new ones.  If all holders of such a page grow in this call, the one of
+ * the highest number keeps it.
+ *   served    device int32 [n]: 1, or 0 where blocks run out: from the first request on for
+ *             which they do, none that needs one (or keeps a page that others
+ *             would have had to leave) gets any, and it is left as it was
+ *   grow      device int32 [n], at least 0 (less counts as 0)
+ *   workspace device, 256-byte aligned, at least pk_kv_pages_workspace_bytes.
+ *             ZERO-FILLED BEFORE ITS FIRST USE; every call leaves it ready for the
+ *             next, also of another of these calls; the caller orders them.
+ * A row must not name a block twice.  Errors: PK_EINVAL. */
+size_t pk_kv_pages_workspace_bytes(int64_t num_blocks);
+int pk_kv_pages_reserve(int32_t* block_table, const int32_t* lens, int32_t* pages, int32_t n, int32_t max_blocks,
+                        const int32_t* grow, int32_t* refs, int64_t num_blocks, int32_t page_size,
+                        int32_t* served, int32_t* copy_src, int32_t* copy_dst,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* pk_kv_pages_compact -- with U blocks in use, those of the numbers U and up move to
+ * the free ones below U: the k-th of them to the k-th, both by rising number, for
+ * k < max_moves (the rest by further calls).  copy_src[k] -> copy_dst[k] are
+ * the moves, -1 behind the last one; no block is in both lists.
+ *   new_table  block_table with the new numbers (entries behind a request's pages are not
+ *              written); may be block_table itself
+ *   new_refs   [num_blocks]; not refs itself
+ *   copy_src, copy_dst  device int32 [max_moves]
+ * workspace as for pk_kv_pages_reserve.  Errors: PK_EINVAL. */
+int pk_kv_pages_compact(const int32_t* block_table, const int32_t* pages, int32_t n, int32_t max_blocks,
+                        const int32_t* refs, int64_t num_blocks, int32_t* new_table, int32_t* new_refs,
+                        int32_t* copy_src, int32_t* copy_dst, int32_t max_moves,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* pk_kv_cache_copy -- block copy_src[i] of `from` to block copy_dst[i] of `to`, keys,
+ * values and scales, for i < count; pairs with a number that the cache does not
+ * have (-1) are passed over.  `to` may be `from`, or another cache of its dtype, page
+ * size and head shape (of another size, to move requests there) that does not
+ * overlap it.  No block is written twice, or read and written, in one call.
+ * Errors: PK_EINVAL; PK_EUNSUPPORTED. */
+int pk_kv_cache_copy(const pk_cache* from, const pk_cache* to, const int32_t* copy_src, const int32_t* copy_dst,
+                     int32_t count, void* stream);
+
+/* pk_shared_tree_attn -- pk_tree_attn for a batch in which neighbouring requests have
+ * their leading pages in common (as pk_kv_pages_select leaves forks): those keys are read
+ * once for all of them.
+ *   family_start  device int32 [families + 1], not decreasing: family g is
+ *             requests family_start[g] .. family_start[g + 1] - 1; requests in
+ *             none share nothing
+ *   families  0 .. n
+ * How many pages a family shares is found from its rows of block_table: the
+ * result is that of pk_tree_attn whatever the families are, but for the order of
+ * the sums.  It repeats bit for bit.
+ *   workspace as for pk_tree_attn, of at least
+ *             pk_shared_tree_attn_workspace_bytes; not to be shared with
+ *             pk_tree_attn
+ * Other arguments and errors as for pk_tree_attn. */
+size_t pk_shared_tree_attn_workspace_bytes(int32_t n, int32_t max_q, int64_t total_q, int Hq, int Hkv, int d);
+int pk_shared_tree_attn(const pk_cache* cache, const void* q, const int32_t* q_start, int64_t total_q, int32_t max_q,
+                        const uint64_t* tree_mask, const int32_t* block_table, int32_t max_blocks,
+                        const int32_t* kv_lens, int32_t n, const int32_t* family_start, int32_t families,
+                        void* out, float scale, int Hq, int out_dtype,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* pk_draft_verify -- speculative sampling: which of the drafted tokens of every
+ * request stay, so that they and the token behind them are distributed as if the target
+ * had drawn them one by one.  Requests, their tokens and tree_mask are those of
+ * pk_tree_attn; token 0 of a request is the one that the last step drew (it
+ * stays), the parent of a token t > 0 is the highest token below t in its mask
+ * word (a token without one cannot stay).
+ *   target    device [total_q][vocab] (dtype PK_BF16 or PK_F32, rows target_stride elements
+ *             apart): row t of a request are the logits of the token behind its
+ *             token t; -inf: cannot be drawn; NaN counts as -inf, inf as the
+ *             largest fp32 number.  Logarithms of probabilities are logits too.
+ *   draft     logits of the same form from which the children of token t were
+ *             drawn, independently of one another, at the request's temperature; NULL: the
+ *             drafted tokens were not drawn (they were looked up, or are the
+ *             likeliest)
+ *   tokens    device int32 [total_q]; one outside of [0, vocab) does not stay
+ *   temperature  device float [n]; NULL: 1.  0 and less (and NaN): the first of the
+ *             largest logits has probability 1, and draft is not read
+ *   accept_u, sample_u  device float [total_q], [n]: independent uniform random
+ *             numbers from [0, 1), one for each drafted token, one for the
+ *             token behind
+ * P and Q are softmax(target / temperature) and softmax(draft / temperature) of
+ * the last token that stays so far.  Its children are looked at by rising number.  With
+ * c = 0 and Z = 1 at first, child x stays if P(x) > (c + u Z) Q(x); otherwise
+ * c := c + Z, Z := sum of max(P - c Q, 0).  Without draft x stays if P(x) > u Z;
+ * otherwise Z := Z - P(x), P(x) := 0.  The token behind the last one that stays
+ * is the first x with cumulative weight over sample_u times the whole, of the
+ * weights max(P - c Q, 0) (P where all of them are zero).
+ * Probabilities and sums have 64 bits.
+ *   keep      device int32 [n][max_keep]: the tokens that stay, rising (as
+ *             pk_kv_cache_keep takes them), -1 behind the last one.  Of a branch of more than
+ *             max_keep tokens the first max_keep stay (max_keep >= 1)
+ *   keep_count, next_token  device int32 [n]: how many (0 and -1 for a request without
+ *             tokens); the token behind, -1 where no logit of its row is a number
+ *             above -inf
+ *   workspace device, 256-byte aligned, at least pk_draft_verify_workspace_bytes.
+ *             ZERO-FILLED BEFORE ITS FIRST USE; every call leaves it ready for the
+ *             next.  One workspace serves all calls for which it is large
+ *             enough; the caller orders them.
+ * With one token a request it draws from its logits.  Errors: PK_EINVAL;
+ * PK_EUNSUPPORTED (max_q). */
+size_t pk_draft_verify_workspace_bytes(int32_t n, int64_t total_q, int32_t vocab);
+int pk_draft_verify(const void* target, int64_t target_stride, const void* draft, int64_t draft_stride, int dtype,
+                    int32_t vocab, const int32_t* tokens, const int32_t* q_start, int64_t total_q, int32_t max_q,
+                    const uint64_t* tree_mask, int32_t n, const float* temperature,
+                    const float* accept_u, const float* sample_u,
+                    int32_t* keep, int32_t max_keep, int32_t* keep_count, int32_t* next_token,
+                    void* workspace, size_t workspace_bytes, void* stream);
 
 /* Message of the last error on this thread ("" if none). */
 const char* pk_last_error(void);

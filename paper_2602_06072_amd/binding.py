@@ -96,11 +96,22 @@ def lib():
                         ("pk_qkv_cache_write", [vp] * 8 + [f32, vp, i64, ci, vp]),
                         ("pk_kv_cache_read", [vp, vp, i32, vp, vp, i32, vp, vp, i64, vp]),
                         ("pk_tree_attn", [vp, vp, vp, i64, i32, vp, vp, i32, vp, i32, vp, f32, ci, ci, vp, sz, vp]),
-                        ("pk_kv_cache_keep", [vp, vp, i32, vp, vp, i32, vp, i32, vp, vp, vp])):
+                        ("pk_kv_cache_keep", [vp, vp, i32, vp, vp, i32, vp, i32, vp, vp, vp]),
+                        ("pk_kv_pages_select", [vp, vp, vp, i32, i32, vp, i32, vp, vp, vp, vp, i64, i32, vp]),
+                        ("pk_kv_pages_reserve", [vp, vp, vp, i32, i32, vp, vp, i64, i32, vp, vp, vp, vp, sz, vp]),
+                        ("pk_kv_pages_compact", [vp, vp, i32, i32, vp, i64, vp, vp, vp, vp, i32, vp, sz, vp]),
+                        ("pk_kv_cache_copy", [vp, vp, vp, vp, i32, vp]),
+                        ("pk_shared_tree_attn", [vp, vp, vp, i64, i32, vp, vp, i32, vp, i32, vp, i32, vp, f32, ci, ci, vp, sz, vp]),
+                        ("pk_draft_verify", [vp, i64, vp, i64, ci, i32, vp, vp, i64, i32, vp, i32, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp])):
         getattr(L, name).restype = ci
         getattr(L, name).argtypes = types
     L.pk_tree_attn_workspace_bytes.restype = sz
     L.pk_tree_attn_workspace_bytes.argtypes = [i32, i32, ci, ci, ci]
+    for name, types in (("pk_kv_pages_workspace_bytes", [i64]),
+                        ("pk_shared_tree_attn_workspace_bytes", [i32, i32, i64, ci, ci, ci]),
+                        ("pk_draft_verify_workspace_bytes", [i32, i64, i32])):
+        getattr(L, name).restype = sz
+        getattr(L, name).argtypes = types
     L.pk_last_error.restype = ctypes.c_char_p
     L.pk_last_error.argtypes = []
     _torch = torch
@@ -620,3 +631,127 @@ def kv_cache_keep(cache: KvCache, block_table, kv_lens, q_start, keep, keep_coun
                             _vector(keep_count, "keep_count", _torch.int32, n), _vector(new_lens, "new_lens", _torch.int32, n), _stream(stream))
     _check(rc, "pk_kv_cache_keep")
     return new_lens
+
+
+# --------------------------------------------------------------------------
+# branching and judging: pages that requests share, and which drafted tokens stay
+# --------------------------------------------------------------------------
+
+def _batch(block_table, lens, pages, what=""):
+    """(n, max_blocks, addresses of block table, lengths and pages) of a batch."""
+    if block_table.dim() != 2:
+        raise PackInferError(f"{what}block_table must be [n, max_blocks]")
+    n, most = block_table.shape
+    i32 = _torch.int32
+    return n, most, _vector(block_table, what + "block_table", i32), _vector(lens, what + "lens", i32, n), _vector(pages, what + "pages", i32, n)
+
+
+def kv_pages_select(block_table, lens, pages, rows_from, new_table, new_lens, new_pages, refs, page_size, stream=None):
+    """Request i of the new batch is request rows_from[i] of the old one (outside of it: an empty one): forked, reordered and
+    finished requests.  refs: int32 [num_blocks], how many requests hold a block."""
+    L = lib()
+    n, most, table, ls, ps = _batch(block_table, lens, pages)
+    m, new_most, nt, nl, np_ = _batch(new_table, new_lens, new_pages, "new_")
+    _need(new_most == most, "block_table and new_table differ in their max_blocks")
+    rc = L.pk_kv_pages_select(table, ls, ps, n, most, _vector(rows_from, "rows_from", _torch.int32, m), m, nt, nl, np_,
+                              _vector(refs, "refs", _torch.int32), refs.numel(), int(page_size), _stream(stream))
+    _check(rc, "pk_kv_pages_select")
+    return new_table, new_lens, new_pages
+
+
+def new_pages_workspace(num_blocks, device="cuda"):
+    """Workspace of kv_pages_reserve and kv_pages_compact; zeros, as its first use asks for."""
+    nbytes = max(256, int(lib().pk_kv_pages_workspace_bytes(num_blocks)))
+    return _torch.zeros(nbytes, dtype=_torch.uint8, device=device)
+
+
+def kv_pages_reserve(block_table, lens, pages, grow, refs, page_size, served, copy_src, copy_dst, workspace, stream=None):
+    """Pages for lens[i] + grow[i] tokens of every request, free blocks of the lowest numbers first; where a shared page would be
+    written, copy_src[i] -> copy_dst[i] (-1: none) is to be copied in every layer's cache (kv_cache_copy).  served[i]: 1, or 0
+    where blocks ran out."""
+    L = lib()
+    n, most, table, ls, ps = _batch(block_table, lens, pages)
+    i32 = _torch.int32
+    rc = L.pk_kv_pages_reserve(table, ls, ps, n, most, _vector(grow, "grow", i32, n), _vector(refs, "refs", i32), refs.numel(), int(page_size),
+                               _vector(served, "served", i32, n), _vector(copy_src, "copy_src", i32, n), _vector(copy_dst, "copy_dst", i32, n),
+                               workspace.data_ptr(), workspace.nbytes, _stream(stream))
+    _check(rc, "pk_kv_pages_reserve")
+    return served
+
+
+def kv_pages_compact(block_table, pages, refs, new_table, new_refs, copy_src, copy_dst, workspace, stream=None):
+    """The blocks in use move to the lowest numbers: copy_src[k] -> copy_dst[k] (-1 behind the last one) are to be copied in every
+    layer's cache; no more moves than these have room for.  new_table may be block_table."""
+    L = lib()
+    i32 = _torch.int32
+    n, most, table, _, ps = _batch(block_table, pages, pages)
+    _need(new_table.shape == block_table.shape and copy_src.numel() == copy_dst.numel(), "block_table and new_table, or copy_src and copy_dst: shapes differ")
+    rc = L.pk_kv_pages_compact(table, ps, n, most, _vector(refs, "refs", i32), refs.numel(), _vector(new_table, "new_table", i32),
+                               _vector(new_refs, "new_refs", i32, refs.numel()), _vector(copy_src, "copy_src", i32), _vector(copy_dst, "copy_dst", i32),
+                               copy_src.numel(), workspace.data_ptr(), workspace.nbytes, _stream(stream))
+    _check(rc, "pk_kv_pages_compact")
+    return new_table
+
+
+def kv_cache_copy(cache: KvCache, copy_src, copy_dst, to: Optional[KvCache] = None, stream=None):
+    """Blocks copy_src[i] of the cache to blocks copy_dst[i], of `to` where it is given; numbers outside (-1) are passed over."""
+    L = lib()
+    to = cache if to is None else to
+    rc = L.pk_kv_cache_copy(cache.raw, to.raw, _vector(copy_src, "copy_src", _torch.int32), _vector(copy_dst, "copy_dst", _torch.int32, copy_src.numel()),
+                            copy_src.numel(), _stream(stream))
+    _check(rc, "pk_kv_cache_copy")
+    return to
+
+
+def new_shared_tree_workspace(n, max_q, total_q, Hq, Hkv, d, device="cuda"):
+    """Workspace of shared_tree_attn for up to n requests of up to max_q drafted tokens, total_q in all; zeros, as its first use
+    asks for."""
+    nbytes = max(256, int(lib().pk_shared_tree_attn_workspace_bytes(n, max_q, total_q, Hq, Hkv, d)))
+    return _torch.zeros(nbytes, dtype=_torch.uint8, device=device)
+
+
+def shared_tree_attn(cache: KvCache, q, q_start, max_q, tree_mask, block_table, kv_lens, family_start, out, scale, workspace, stream=None):
+    """tree_attn for requests that have their leading pages in common: family g is requests family_start[g] ..
+    family_start[g + 1] - 1 (int32 [families + 1]), whose shared pages are read once."""
+    L = lib()
+    total, Hq, d = q.shape
+    n, max_blocks = block_table.shape
+    _need(q.dtype == _torch.bfloat16 and q.is_contiguous() and out.is_contiguous() and out.shape == q.shape and d == cache.d,
+          "q must be contiguous bf16 [total, Hq, d], out of the same shape")
+    _need(family_start.numel() > 0, "family_start must be [families + 1]")
+    rc = L.pk_shared_tree_attn(cache.raw, q.data_ptr(), _vector(q_start, "q_start", _torch.int32, n + 1), total, int(max_q),
+                               _vector(tree_mask, "tree_mask", _torch.int64, total), _vector(block_table, "block_table", _torch.int32), max_blocks,
+                               _vector(kv_lens, "kv_lens", _torch.int32, n), n, _vector(family_start, "family_start", _torch.int32),
+                               family_start.numel() - 1, out.data_ptr(), float(scale), Hq, _dtype_code(out), workspace.data_ptr(), workspace.nbytes,
+                               _stream(stream))
+    _check(rc, "pk_shared_tree_attn")
+    return out
+
+
+def new_verify_workspace(n, total_q, vocab, device="cuda"):
+    """Workspace of draft_verify for n requests with total_q tokens; zeros, as its first use asks for."""
+    nbytes = max(256, int(lib().pk_draft_verify_workspace_bytes(n, total_q, vocab)))
+    return _torch.zeros(nbytes, dtype=_torch.uint8, device=device)
+
+
+def draft_verify(target, draft, tokens, q_start, max_q, tree_mask, temperature, accept_u, sample_u, keep, keep_count, next_token, workspace, stream=None):
+    """Which drafted tokens of every request stay (keep [n, max_keep], keep_count [n], as kv_cache_keep takes them) and the token behind
+    them (next_token [n]).  target, draft: logits [total, vocab] (bf16 or fp32, rows any distance apart; draft None: the tokens were not drawn);
+    tokens int32 [total]; q_start, max_q, tree_mask as for tree_attn; temperature fp32 [n] (None: 1; 0: the largest logit); accept_u [total],
+    sample_u [n]: fp32 random numbers from [0, 1)."""
+    L = lib()
+    i32, f32 = _torch.int32, _torch.float32
+    total, vocab = target.shape
+    n = q_start.numel() - 1
+    _need(target.numel() == 0 or vocab == 1 or target.stride(1) == 1, "target must have contiguous rows")
+    _need(draft is None or (draft.shape == target.shape and draft.dtype == target.dtype and (draft.numel() == 0 or vocab == 1 or draft.stride(1) == 1)),
+          "draft must be of target's shape and type, with contiguous rows")
+    _need(keep.dim() == 2 and keep.shape[0] == n, "keep must be [n, max_keep]")
+    rc = L.pk_draft_verify(target.data_ptr(), target.stride(0) if total > 1 else vocab, None if draft is None else draft.data_ptr(),
+                           vocab if draft is None or total < 2 else draft.stride(0), _dtype_code(target), vocab, _vector(tokens, "tokens", i32, total),
+                           _vector(q_start, "q_start", i32), total, int(max_q), _vector(tree_mask, "tree_mask", _torch.int64, total), n,
+                           _vector(temperature, "temperature", f32, n), _vector(accept_u, "accept_u", f32, total), _vector(sample_u, "sample_u", f32, n),
+                           _vector(keep, "keep", i32), keep.shape[1], _vector(keep_count, "keep_count", i32, n),
+                           _vector(next_token, "next_token", i32, n), workspace.data_ptr(), workspace.nbytes, _stream(stream))
+    _check(rc, "pk_draft_verify")
+    return keep, keep_count, next_token

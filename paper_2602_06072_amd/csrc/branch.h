@@ -1,0 +1,87 @@
+// Pages of the paged cache (forking, reserving, compacting, copying) and the judging of drafted tokens: what the launches take.
+// Pointers are device pointers.
+#pragma once
+#include <cstddef>
+#include <cstdint>
+
+#include "cache.h"
+
+namespace pk {
+
+struct PagesSelectArgs {
+    const int32_t* table; const int32_t* lens; const int32_t* pages; int32_t n; int32_t max_blocks;
+    const int32_t* from; int32_t n_new; int32_t* new_table; int32_t* new_lens; int32_t* new_pages;
+    int32_t* refs; int32_t num_blocks; int32_t page;
+};
+int launch_pages_select(const PagesSelectArgs& a, void* stream);
+
+// A workspace of the page calls: kWords arrays of num_blocks words.  Zero between calls: the first two.
+struct PagesWorkspace {
+    static constexpr int kWords = 3;
+    static constexpr int kSegment = 4096;           // blocks that a workgroup looks at
+    static size_t bytes(const int64_t num_blocks) { return static_cast<size_t>((kWords * num_blocks + num_blocks / kSegment + 1) * 4 + 255) / 256 * 256; }
+};
+
+struct PagesReserveArgs {
+    int32_t* table; const int32_t* lens; int32_t* pages; int32_t n; int32_t max_blocks;
+    const int32_t* grow; int32_t* refs; int32_t num_blocks; int32_t page;
+    int32_t* served; int32_t* copy_src; int32_t* copy_dst;
+    int32_t* last_writer; int32_t* writers;         // [num_blocks] each, zero between calls: number + 1 of the last request that would write a shared block; how many would
+    int32_t* free;                                  // [num_blocks] the free blocks that are handed out, by rising number
+};
+int launch_pages_reserve(const PagesReserveArgs& a, void* stream);
+
+struct PagesCompactArgs {
+    const int32_t* table; const int32_t* pages; int32_t n; int32_t max_blocks;
+    const int32_t* refs; int32_t num_blocks; int32_t* new_table; int32_t* new_refs;
+    int32_t* copy_src; int32_t* copy_dst; int32_t max_moves;
+    int32_t* to;                                    // [num_blocks] new number of every block
+    int32_t* used_of;                               // [segments] blocks in use
+};
+int launch_pages_compact(const PagesCompactArgs& a, void* stream);
+
+struct CacheCopyArgs {
+    CacheView from, to; const int32_t* src; const int32_t* dst; int32_t count;
+    int parts;                                      // set by the launch: workgroups that share a block
+};
+int launch_cache_copy(CacheCopyArgs a, void* stream);
+
+// Sum and maximum of a piece of a row of logits, relative to its maximum; where the largest logit stands first
+struct RowPart { double sum; float top; int32_t at; };
+
+// What there is left to draw of a request after its drafted tokens have been looked at
+struct Leftover {
+    int64_t row;                                    // of the last token that stays
+    int32_t kind, pieces;                           // LeftoverKind; pieces of its weights' sums
+    double c, of_target, of_draft;                  // weights max(of_target e^(l - top) - c of_draft e^(l' - top'), 0)
+    float top, draft_top;
+};
+enum LeftoverKind { kNone, kKnown, kUnknown, kResidual, kRemoved, kLargest };
+
+// How a launch cuts rows of logits: `pieces` of a row where all rows are looked at, `last_pieces` where one of each request is
+struct VerifyShape {
+    int pieces, length, last_pieces, last_length;   // lengths in elements, multiples of kStep
+    static constexpr int kStep = 2048;              // elements that a workgroup takes at a time
+    static VerifyShape of(int64_t n, int64_t total_q, int32_t vocab);
+    size_t part_bytes(const int64_t total_q) const { return whole256(total_q * 2 * pieces * static_cast<int64_t>(sizeof(RowPart))); }
+    size_t last_bytes(const int64_t n) const { return whole256(n * last_pieces * static_cast<int64_t>(sizeof(RowPart))); }
+    static size_t left_bytes(const int64_t n) { return whole256(n * static_cast<int64_t>(sizeof(Leftover))); }
+    size_t bytes(const int64_t n, const int64_t total_q) const { return part_bytes(total_q) + last_bytes(n) + left_bytes(n); }
+
+private:
+    static size_t whole256(const int64_t bytes) { return static_cast<size_t>((bytes + 255) / 256 * 256); }
+};
+
+struct VerifyArgs {
+    const void* target; int64_t target_stride; const void* draft; int64_t draft_stride; int f32; int32_t vocab;
+    const int32_t* tokens; const int32_t* q_start; int64_t total_q; int32_t max_q; const uint64_t* mask; int32_t n;
+    const float* temperature; const float* accept_u; const float* sample_u;
+    int32_t* keep; int32_t max_keep; int32_t* keep_count; int32_t* next_token;
+    VerifyShape shape;
+    RowPart* parts;                                 // [total_q][2][pieces]: of the target's rows, of the draft's
+    RowPart* last_parts;                            // [n][last_pieces]
+    Leftover* left;                                 // [n]
+};
+int launch_draft_verify(const VerifyArgs& a, void* stream);
+
+}  // namespace pk

@@ -1,0 +1,337 @@
+// Pages of the paged cache: a new batch out of rows of the old one, pages for the next tokens, compaction, copies of blocks.
+//
+// All but the copies is whole numbers: 4 bytes an entry of a block table and a block of the pool.  Counts of holders change by atomic additions,
+// whose order does not matter; whatever is handed out is found by prefix sums over requests and blocks in their order, so that results repeat.
+#include "branch.h"
+#include "common.hip.h"
+
+namespace pk {
+namespace {
+
+constexpr int kWave = 64;
+
+template <class T>
+__device__ __forceinline__ T wave_prefix_sum(T x) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const T y = __shfl_up(x, o, 64);
+        x += lane >= o ? y : 0;
+    }
+    return x;
+}
+// Sum of x over the threads in front of this one, and over all of them.  `lds`: a word for every wave.
+template <int THREADS, class T>
+__device__ __forceinline__ T sum_in_front(const T x, T* lds, T& all) {
+    const int wave = threadIdx.x >> 6;
+    const T upto = wave_prefix_sum(x);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) lds[wave] = upto;
+    __syncthreads();
+    T before = 0;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+        before += w < wave ? lds[w] : 0;
+        all += lds[w];
+    }
+    return before + upto - x;
+}
+
+__device__ __forceinline__ bool is_block(const int b, const int num_blocks) { return b >= 0 && b < num_blocks; }
+
+// ------------------------------------------------------------------ a new batch out of rows of the old one
+// One wave for every new request, one for every old one.
+__global__ __launch_bounds__(256) void pages_select_kernel(PagesSelectArgs a) {
+    const int lane = threadIdx.x & 63;
+    const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int64_t most = static_cast<int64_t>(a.max_blocks) * a.page;
+    const auto held = [&](const int i) { return min(max(a.pages[i], 0), a.max_blocks); };
+    if (unit < a.n_new) {
+        const int i = static_cast<int>(unit), s = a.from[i];
+        const bool there = s >= 0 && s < a.n;
+        const int len = there ? static_cast<int>(min(static_cast<int64_t>(max(a.lens[s], 0)), most)) : 0;
+        const int pages = there ? min(static_cast<int>((static_cast<int64_t>(len) + a.page - 1) / a.page), held(s)) : 0;
+        const int32_t* row = a.table + static_cast<int64_t>(there ? s : 0) * a.max_blocks;
+        int32_t* to = a.new_table + static_cast<int64_t>(i) * a.max_blocks;
+        for (int j = lane; j < pages; j += kWave) {
+            const int b = row[j];
+            to[j] = b;
+            if (is_block(b, a.num_blocks)) atomicAdd(a.refs + b, 1);
+        }
+        if (lane == 0) { a.new_lens[i] = len; a.new_pages[i] = pages; }
+    } else if (unit - a.n_new < a.n) {
+        const int i = static_cast<int>(unit - a.n_new), pages = held(i);
+        const int32_t* row = a.table + static_cast<int64_t>(i) * a.max_blocks;
+        for (int j = lane; j < pages; j += kWave) {
+            const int b = row[j];
+            if (is_block(b, a.num_blocks)) atomicAdd(a.refs + b, -1);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ pages for the next tokens
+// What a request asks for
+struct Wish {
+    int at, held, end, block;                       // page of its next token, pages it holds, pages it wants; block of that page
+    bool shared;                                    // that page holds tokens and is held by others too: it is not to be written
+};
+__device__ __forceinline__ Wish wish_of(const PagesReserveArgs& a, const int i) {
+    const int64_t most = static_cast<int64_t>(a.max_blocks) * a.page;
+    const int64_t len = min(static_cast<int64_t>(max(a.lens[i], 0)), most);
+    const int grow = max(a.grow[i], 0);
+    Wish w;
+    w.at = static_cast<int>(len / a.page);
+    w.held = min(max(a.pages[i], 0), a.max_blocks);
+    w.end = grow > 0 ? max(w.held, static_cast<int>(min((len + grow + a.page - 1) / a.page, static_cast<int64_t>(a.max_blocks)))) : w.held;
+    w.block = -1;
+    w.shared = false;
+    if (grow > 0 && len % a.page > 0 && w.at < w.held) {
+        w.block = a.table[static_cast<int64_t>(i) * a.max_blocks + w.at];
+        w.shared = is_block(w.block, a.num_blocks) && a.refs[w.block] > 1;
+    }
+    return w;
+}
+__device__ __forceinline__ int device_load(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+enum { kServed = 1, kCopies = 2, kWrites = 4 };     // left in served[i] between the two launches; copy_dst[i]: its first free block's number among those handed out
+
+// One workgroup: who gets what.  (Requests are 4 to 12 bytes, blocks 4: the whole state of a batch is a few hundred KiB.)
+constexpr int kPlanThreads = 1024;
+__global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(PagesReserveArgs a) {
+    __shared__ int64_t lds[kPlanThreads / 64];
+    const int tid = threadIdx.x;
+    for (int i = tid; i < a.n; i += kPlanThreads) {
+        const Wish w = wish_of(a, i);
+        if (!w.shared) continue;
+        atomicMax(a.last_writer + w.block, i + 1);
+        atomicAdd(a.writers + w.block, 1);
+    }
+    __threadfence();
+    __syncthreads();
+    // the blocks that are wanted
+    const auto needs = [&](const int i, const Wish& w, bool& keeps) {
+        // of as many writers as there are holders the last one keeps the page
+        keeps = w.shared && device_load(a.writers + w.block) == a.refs[w.block] && device_load(a.last_writer + w.block) == i + 1;
+        return static_cast<int64_t>(w.end - w.held + (w.shared && !keeps ? 1 : 0));
+    };
+    int64_t wanted = 0;
+    for (int i0 = 0; i0 < a.n; i0 += kPlanThreads) {
+        const int i = i0 + tid;
+        bool keeps;
+        int64_t need = 0, all;
+        if (i < a.n) { const Wish w = wish_of(a, i); need = needs(i, w, keeps); }
+        sum_in_front<kPlanThreads>(need, lds, all);
+        wanted += all;
+        if (wanted >= a.num_blocks) { wanted = a.num_blocks; break; }
+    }
+    // as many free ones, by rising number
+    constexpr int EACH = 16;
+    int64_t found = 0;
+    for (int64_t b0 = 0; b0 < a.num_blocks && found < wanted; b0 += kPlanThreads * EACH) {
+        int refs[EACH];
+        int64_t mine = 0, all;
+        const int64_t b = b0 + tid * EACH;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) refs[e] = b + e < a.num_blocks ? a.refs[b + e] : 1;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) mine += refs[e] == 0 ? 1 : 0;
+        int64_t at = found + sum_in_front<kPlanThreads>(mine, lds, all);
+#pragma unroll
+        for (int e = 0; e < EACH; ++e)
+            if (refs[e] == 0 && at < a.num_blocks) a.free[at++] = static_cast<int32_t>(b + e);
+        found += all;
+    }
+    // in the order of requests
+    int64_t before = 0;
+    for (int i0 = 0; i0 < a.n; i0 += kPlanThreads) {
+        const int i = i0 + tid;
+        bool keeps = false;
+        int64_t need = 0, all;
+        Wish w{};
+        if (i < a.n) { w = wish_of(a, i); need = needs(i, w, keeps); }
+        const int64_t begin = before + sum_in_front<kPlanThreads>(need, lds, all);
+        if (i < a.n) {
+            const bool served = begin + need <= found || (need == 0 && !keeps);
+            a.served[i] = (served ? kServed : 0) | (w.shared && !keeps ? kCopies : 0) | (w.shared ? kWrites : 0);
+            a.copy_dst[i] = served ? static_cast<int32_t>(begin) : -1;
+        }
+        before += all;
+    }
+}
+
+// A wave for every request: its entries
+__global__ __launch_bounds__(256) void pages_apply_kernel(PagesReserveArgs a) {
+    const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (i >= a.n) return;
+    const int flags = a.served[i], begin = a.copy_dst[i];
+    Wish w = wish_of(a, i);
+    w.shared = flags & kWrites;                     // (counts change meanwhile: what was shared stands in the flags)
+    int32_t* row = a.table + static_cast<int64_t>(i) * a.max_blocks;
+    const bool served = flags & kServed, copies = served && (flags & kCopies);
+    if (lane == 0) {
+        int dst = -1;
+        if (copies) {
+            dst = a.free[begin];
+            row[w.at] = dst;
+            a.refs[dst] = 1;
+            atomicAdd(a.refs + w.block, -1);
+        }
+        if (w.shared) { a.last_writer[w.block] = 0; a.writers[w.block] = 0; }
+        a.copy_src[i] = copies ? w.block : -1;
+        a.copy_dst[i] = dst;
+        a.served[i] = served ? 1 : 0;
+        if (served) a.pages[i] = w.end;
+    }
+    if (!served) return;
+    for (int j = w.held + lane; j < w.end; j += kWave) {
+        const int b = a.free[begin + (copies ? 1 : 0) + j - w.held];
+        row[j] = b;
+        a.refs[b] = 1;
+    }
+}
+
+// ------------------------------------------------------------------ compaction
+constexpr int kSegment = PagesWorkspace::kSegment, kOfThread = kSegment / 256;
+
+__device__ __forceinline__ int used_in_segment(const int32_t* refs, const int64_t first, const int64_t end, int* lds) {
+    int mine = 0, all;
+    for (int64_t b = first + threadIdx.x; b < end; b += 256) mine += refs[b] > 0 ? 1 : 0;
+    sum_in_front<256>(mine, lds, all);
+    return all;
+}
+__global__ __launch_bounds__(256) void pages_count_kernel(PagesCompactArgs a) {
+    __shared__ int lds[4];
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * kSegment;
+    const int used = used_in_segment(a.refs, first, min(first + kSegment, static_cast<int64_t>(a.num_blocks)), lds);
+    if (threadIdx.x == 0) a.used_of[blockIdx.x] = used;
+}
+// Every workgroup has its segment's blocks, and finds from all segments' counts how many are in use, in front of it and in front of block U.
+__global__ __launch_bounds__(256) void pages_move_kernel(PagesCompactArgs a) {
+    __shared__ int lds[4];
+    const int segments = gridDim.x, mine = blockIdx.x, tid = threadIdx.x;
+    int of_all = 0, of_front = 0, used, front;
+    for (int s = tid; s < segments; s += 256) {
+        const int x = a.used_of[s];
+        of_all += x;
+        of_front += s < mine ? x : 0;
+    }
+    sum_in_front<256>(of_all, lds, used);
+    sum_in_front<256>(of_front, lds, front);
+    const int cut = used / kSegment;                // segment of block U
+    int of_cut = 0, low;
+    for (int s = tid; s < min(cut, segments); s += 256) of_cut += a.used_of[s];
+    sum_in_front<256>(of_cut, lds, low);
+    low += used_in_segment(a.refs, static_cast<int64_t>(cut) * kSegment, used, lds);           // in use below U
+    const int moves = min(used - low, a.max_moves);
+    for (int64_t k = moves + static_cast<int64_t>(mine) * 256 + tid; k < a.max_moves; k += static_cast<int64_t>(segments) * 256) {
+        a.copy_src[k] = -1;
+        a.copy_dst[k] = -1;
+    }
+    // The lists, block by block.  A block's new number and count are written by whoever moves there: a source's partner is not known here, so
+    // the new numbers of sources, and the counts of both, are set by pages_place_kernel, from the lists.
+    const int64_t first = static_cast<int64_t>(mine) * kSegment + tid * kOfThread;
+    int refs[kOfThread], count = 0, all;
+#pragma unroll
+    for (int e = 0; e < kOfThread; ++e) {
+        refs[e] = first + e < a.num_blocks ? a.refs[first + e] : 0;
+        count += refs[e] > 0 ? 1 : 0;
+    }
+    int before = front + sum_in_front<256>(count, lds, all);       // blocks in use in front of this one
+#pragma unroll
+    for (int e = 0; e < kOfThread; ++e) {
+        const int64_t b = first + e;
+        if (b >= a.num_blocks) break;
+        const bool in_use = refs[e] > 0;
+        if (b >= used && in_use && before - low < moves) a.copy_src[before - low] = static_cast<int32_t>(b);
+        if (b < used && !in_use && b - before < moves) a.copy_dst[b - before] = static_cast<int32_t>(b);
+        a.to[b] = static_cast<int32_t>(b);
+        a.new_refs[b] = refs[e];
+        before += in_use ? 1 : 0;
+    }
+}
+__global__ __launch_bounds__(256) void pages_place_kernel(PagesCompactArgs a) {
+    const int64_t k = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (k >= a.max_moves) return;
+    const int src = a.copy_src[k], dst = a.copy_dst[k];
+    if (src < 0) return;
+    a.to[src] = dst;
+    a.new_refs[dst] = a.refs[src];
+    a.new_refs[src] = 0;
+}
+__global__ __launch_bounds__(256) void pages_rename_kernel(PagesCompactArgs a) {
+    const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (i >= a.n) return;
+    const int pages = min(max(a.pages[i], 0), a.max_blocks);
+    const int64_t row = static_cast<int64_t>(i) * a.max_blocks;
+    for (int j = lane; j < pages; j += kWave) {
+        const int b = a.table[row + j];
+        a.new_table[row + j] = is_block(b, a.num_blocks) ? a.to[b] : b;
+    }
+}
+
+// ------------------------------------------------------------------ copies of blocks
+// bytes [part / parts ..) of an array of a block, 16 at a time
+__device__ __forceinline__ void copy_block(void* to, const void* from, const int64_t dst, const int64_t src, const int64_t bytes, const int part, const int parts) {
+    const u32x4* x = reinterpret_cast<const u32x4*>(static_cast<const char*>(from) + src * bytes);
+    u32x4* y = reinterpret_cast<u32x4*>(static_cast<char*>(to) + dst * bytes);
+    const int words = static_cast<int>(bytes / 16), each = (words + parts - 1) / parts, end = min(words, (part + 1) * each);
+    int w = part * each + threadIdx.x;
+    for (; w + 3 * 256 < end; w += 4 * 256) {
+        u32x4 r[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = x[w + e * 256];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[w + e * 256] = r[e];
+    }
+    for (; w < end; w += 256) y[w] = x[w];
+}
+__global__ __launch_bounds__(256) void cache_copy_kernel(CacheCopyArgs a) {
+    const CacheView &f = a.from, &t = a.to;
+    const int64_t rows = static_cast<int64_t>(f.Hkv) * f.page, units = static_cast<int64_t>(a.count) * a.parts;
+    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+        const int64_t i = u / a.parts;
+        const int part = static_cast<int>(u - i * a.parts), src = a.src[i], dst = a.dst[i];
+        if (src < 0 || src >= f.num_blocks || dst < 0 || dst >= t.num_blocks || (src == dst && f.k == t.k)) continue;
+        const int64_t bytes = rows * f.d * (f.f8 ? 1 : 2);
+        copy_block(t.k, f.k, dst, src, bytes, part, a.parts);
+        copy_block(t.v, f.v, dst, src, bytes, part, a.parts);
+        if (f.f8) copy_block(t.scales, f.scales, dst, src, rows * 2, part, a.parts);
+    }
+}
+
+unsigned groups_of(const int64_t units, const int64_t each) { return static_cast<unsigned>((units + each - 1) / each); }
+
+}  // namespace
+
+int launch_pages_select(const PagesSelectArgs& a, void* stream) {
+    hipLaunchKernelGGL(pages_select_kernel, dim3(groups_of(static_cast<int64_t>(a.n) + a.n_new, 4)), dim3(256), 0, static_cast<hipStream_t>(stream), a);
+    return static_cast<int>(hipGetLastError());
+}
+
+int launch_pages_reserve(const PagesReserveArgs& a, void* stream) {
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    hipLaunchKernelGGL(pages_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return static_cast<int>(e);
+    hipLaunchKernelGGL(pages_apply_kernel, dim3(groups_of(a.n, 4)), dim3(256), 0, st, a);
+    return static_cast<int>(hipGetLastError());
+}
+
+int launch_pages_compact(const PagesCompactArgs& a, void* stream) {
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const unsigned segments = groups_of(a.num_blocks, kSegment);
+    hipLaunchKernelGGL(pages_count_kernel, dim3(segments), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(pages_move_kernel, dim3(segments), dim3(256), 0, st, a);
+    if (a.max_moves > 0) hipLaunchKernelGGL(pages_place_kernel, dim3(groups_of(a.max_moves, 256)), dim3(256), 0, st, a);
+    if (a.n > 0) hipLaunchKernelGGL(pages_rename_kernel, dim3(groups_of(a.n, 4)), dim3(256), 0, st, a);
+    return static_cast<int>(hipGetLastError());
+}
+
+int launch_cache_copy(CacheCopyArgs a, void* stream) {
+    a.parts = a.count <= 512 ? 8 : 1;
+    const int64_t units = static_cast<int64_t>(a.count) * a.parts;
+    hipLaunchKernelGGL(cache_copy_kernel, dim3(static_cast<unsigned>(units < 4096 ? units : 4096)), dim3(256), 0, static_cast<hipStream_t>(stream), a);
+    return static_cast<int>(hipGetLastError());
+}
+
+}  // namespace pk
