@@ -4,6 +4,7 @@
 
 #include "branch.h"
 #include "cache_checks.h"
+#include "shared_attn.h"
 
 using namespace pk;
 
@@ -49,6 +50,11 @@ Refusal check_workspace(const void* workspace, const size_t bytes, const size_t 
 }
 
 constexpr int32_t kMostVocab = 1 << 26;
+
+// Whether shared pages are looked for, or every request is taken alone
+bool shared_pays(const TreeArgs& a, const int32_t families) {
+    return families > 0 && families < a.n && a.total_q * (a.Hq / a.cache.Hkv) < (int64_t{1} << 30);
+}
 
 }  // namespace
 
@@ -153,7 +159,9 @@ extern "C" int pk_kv_cache_copy(const pk_cache* from, const pk_cache* to, const 
 }
 
 extern "C" size_t pk_shared_tree_attn_workspace_bytes(int32_t n, int32_t max_q, int64_t total_q, int Hq, int Hkv, int d) {
-    return total_q < 0 || total_q > kMostTokens ? 0 : pk_tree_attn_workspace_bytes(n, max_q, Hq, Hkv, d);
+    if (!tree_sizes_ok(n, max_q, Hq, Hkv, d) || total_q < 0 || total_q > kMostTokens) return 0;
+    const int cus = compute_units();
+    return SharedWorkspace::of(n, total_q, TreeShape::of(max_q, Hq, Hkv, cus), Hq, Hkv, d, cus).bytes;
 }
 
 extern "C" int pk_shared_tree_attn(const pk_cache* cache, const void* q, const int32_t* q_start, int64_t total_q, int32_t max_q,
@@ -163,10 +171,41 @@ extern "C" int pk_shared_tree_attn(const pk_cache* cache, const void* q, const i
                                    void* workspace, size_t workspace_bytes, void* stream) {
     const char* who = "pk_shared_tree_attn";
     return guarded<int>(PK_ENOMEM, PK_EINVAL, who, [&]() -> int {
-        if (n >= 0 && (families < 0 || families > n)) return refuse(who, {PK_EINVAL, "need 0 <= families <= n"});
+        SharedArgs s{};
+        TreeArgs& a = s.tree;
+        bool empty = false;
+        if (const int rc = tree_args(who, cache, q, q_start, total_q, max_q, tree_mask, block_table, max_blocks, kv_lens, n, out, scale, Hq, out_dtype, workspace, a, empty);
+            rc != PK_OK) return rc;
+        if (families < 0 || families > n) return refuse(who, {PK_EINVAL, "need 0 <= families <= n"});
+        if (empty) return PK_OK;
         if (!family_start) return refuse(who, {PK_EINVAL, "family_start is NULL"});
-        return pk_tree_attn(cache, q, q_start, total_q, max_q, tree_mask, block_table, max_blocks, kv_lens, n, out, scale, Hq, out_dtype, workspace,
-                            workspace_bytes, stream);
+        const int cus = compute_units();
+        const TreeShape shape = TreeShape::of(max_q, Hq, cache->Hkv, cus);
+        const SharedWorkspace w = SharedWorkspace::of(n, total_q, shape, Hq, cache->Hkv, cache->d, cus);
+        if (workspace_bytes < w.bytes) return refuse(who, {PK_EINVAL, "workspace smaller than pk_shared_tree_attn_workspace_bytes"});
+        char* at = static_cast<char*>(workspace);
+        if (!shared_pays(a, families)) {
+            a.arrived = reinterpret_cast<uint32_t*>(at + w.counts);
+            a.part_o = reinterpret_cast<float*>(at + w.plain);
+            a.part_lse = a.part_o + shape.rows_of_slots(cache->Hkv, cus) * cache->d;
+            a.pieces_of = reinterpret_cast<int2*>(at + w.plain + shape.partial_bytes(cache->Hkv, cache->d, cus));
+            return launched(who, launch_tree_attn(a, shape, stream));
+        }
+        s.family_start = family_start; s.families = families;
+        s.arrived = reinterpret_cast<uint32_t*>(at);
+        s.missing = reinterpret_cast<int32_t*>(at + 256);
+        a.pieces_of = reinterpret_cast<int2*>(at + w.arrays);
+        s.pieces_of_family = a.pieces_of + n;
+        s.family_of = reinterpret_cast<int32_t*>(s.pieces_of_family + n);
+        s.shared_of = s.family_of + n;
+        s.first_of = s.shared_of + n;
+        s.len_of = s.first_of + n;
+        s.q_start_of = s.len_of + n;
+        a.part_o = reinterpret_cast<float*>(at + w.own);
+        a.part_lse = a.part_o + w.own_slots * cache->Hkv * shape.rows * cache->d;
+        s.family_o = reinterpret_cast<float*>(at + w.family);
+        s.family_lse = s.family_o + w.family_slots * cache->Hkv * 128 * cache->d;
+        return launched(who, launch_shared_tree_attn(s, shape, stream));
     });
 }
 

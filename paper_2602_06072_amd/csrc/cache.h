@@ -92,6 +92,8 @@ struct TreeArgs {
     float rounds, least_per_share, least_per_many;
     FastDiv by_hkv, by_chunks;
     FastDiv by_r, by_subs;
+    // where requests share pages: tokens that a request shares with its family (a multiple of 64; [n]), and a family's first request ([families])
+    const int32_t* shared_of; const int32_t* first_of;
 };
 int launch_tree_attn(TreeArgs a, const TreeShape& s, void* stream);
 

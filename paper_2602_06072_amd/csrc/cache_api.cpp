@@ -75,10 +75,6 @@ int cache_write_args(const char* who, const pk_cache* cache, const pk_rows* v, c
     return PK_OK;
 }
 
-bool tree_sizes_ok(const int64_t n, const int64_t max_q, const int64_t Hq, const int64_t Hkv, const int64_t d) {
-    return n >= 0 && n <= 65535 && max_q >= 0 && max_q <= PK_MAX_DRAFTS && Hkv > 0 && Hkv <= 65535 && Hq > 0 && Hq <= 16384 && Hq % Hkv == 0 && (d == 64 || d == 128);
-}
-
 }  // namespace
 
 TreeShape TreeShape::of(const int max_q, const int Hq, const int Hkv, const int compute_units) {
@@ -173,27 +169,15 @@ extern "C" int pk_tree_attn(const pk_cache* cache, const void* q, const int32_t*
                             void* workspace, size_t workspace_bytes, void* stream) {
     const char* who = "pk_tree_attn";
     return guarded<int>(PK_ENOMEM, PK_EINVAL, who, [&]() -> int {
-        PK_CHECK(check_cache(cache));
-        PK_CHECK(check_table(block_table, max_blocks, kv_lens, n, *cache));
-        if (Hq <= 0 || Hq % cache->Hkv != 0 || Hq > 16384) return refuse(who, {PK_EINVAL, "need 0 < Hq <= 16384 and Hq % Hkv == 0"});
-        if (total_q < 0 || total_q > kMostTokens || max_q < 0) return refuse(who, {PK_EINVAL, "need 0 <= total_q < 2^31 and max_q >= 0"});
-        if (max_q > PK_MAX_DRAFTS) return refuse(who, {PK_EUNSUPPORTED, "more than 64 drafted tokens of a request (pk_packed_prefill_attn takes chunks)"});
-        if (out_dtype != PK_BF16 && out_dtype != PK_F32) return refuse(who, {PK_EINVAL, "out_dtype must be PK_BF16 or PK_F32"});
-        if (!(std::isfinite(scale) && scale > 0.f)) return refuse(who, {PK_EINVAL, "scale must be finite and positive"});
-        if (n == 0 || total_q == 0 || max_q == 0) return PK_OK;
-        if (!q || !out || !q_start) return refuse(who, {PK_EINVAL, "q, out or q_start is NULL"});
-        if (!aligned(q, 16) || !aligned(out, 16)) return refuse(who, {PK_EINVAL, "q and out must be 16-byte aligned"});
-        if (!workspace || !aligned(workspace, 256)) return refuse(who, {PK_EINVAL, "workspace is NULL or not 256-byte aligned"});
+        TreeArgs a{};
+        bool empty = false;
+        if (const int rc = tree_args(who, cache, q, q_start, total_q, max_q, tree_mask, block_table, max_blocks, kv_lens, n, out, scale, Hq, out_dtype, workspace, a, empty);
+            rc != PK_OK || empty) return rc;
         const int cus = compute_units();
         const TreeShape shape = TreeShape::of(max_q, Hq, cache->Hkv, cus);
         const size_t counts = TreeShape::count_bytes(cache->Hkv, cus), partial = shape.partial_bytes(cache->Hkv, cache->d, cus);
         if (workspace_bytes < counts + partial + TreeShape::pieces_bytes(n))
             return refuse(who, {PK_EINVAL, "workspace smaller than pk_tree_attn_workspace_bytes"});
-        TreeArgs a{};
-        a.cache = view(*cache); a.block_table = block_table; a.max_blocks = max_blocks;
-        a.q = q; a.q_start = q_start; a.total_q = total_q; a.max_q = max_q; a.mask = tree_mask;
-        a.kv_lens = kv_lens; a.n = n;
-        a.out = out; a.out_f32 = out_dtype == PK_F32; a.scale = scale; a.Hq = Hq;
         char* at = static_cast<char*>(workspace);
         a.arrived = reinterpret_cast<uint32_t*>(at);
         a.part_o = reinterpret_cast<float*>(at + counts);

@@ -2,6 +2,7 @@
 #pragma once
 #include <hip/hip_runtime_api.h>
 
+#include <cmath>
 #include <cstdint>
 #include <string>
 
@@ -63,5 +64,32 @@ inline int compute_units() {
 }
 
 #define PK_CHECK(call) do { const Refusal refusal = call; if (refusal.code != PK_OK) return refuse(who, refusal); } while (0)
+
+inline bool tree_sizes_ok(const int64_t n, const int64_t max_q, const int64_t Hq, const int64_t Hkv, const int64_t d) {
+    return n >= 0 && n <= 65535 && max_q >= 0 && max_q <= PK_MAX_DRAFTS && Hkv > 0 && Hkv <= 65535 && Hq > 0 && Hq <= 16384 && Hq % Hkv == 0 && (d == 64 || d == 128);
+}
+
+// Checks of pk_tree_attn, and the part of the arguments that is the caller's; `empty`: nothing to do
+inline int tree_args(const char* who, const pk_cache* cache, const void* q, const int32_t* q_start, const int64_t total_q, const int32_t max_q, const uint64_t* tree_mask,
+                     const int32_t* block_table, const int32_t max_blocks, const int32_t* kv_lens, const int32_t n, void* out, const float scale, const int Hq,
+                     const int out_dtype, void* workspace, TreeArgs& a, bool& empty) {
+    PK_CHECK(check_cache(cache));
+    PK_CHECK(check_table(block_table, max_blocks, kv_lens, n, *cache));
+    if (Hq <= 0 || Hq % cache->Hkv != 0 || Hq > 16384) return refuse(who, {PK_EINVAL, "need 0 < Hq <= 16384 and Hq % Hkv == 0"});
+    if (total_q < 0 || total_q > kMostTokens || max_q < 0) return refuse(who, {PK_EINVAL, "need 0 <= total_q < 2^31 and max_q >= 0"});
+    if (max_q > PK_MAX_DRAFTS) return refuse(who, {PK_EUNSUPPORTED, "more than 64 drafted tokens of a request (pk_packed_prefill_attn takes chunks)"});
+    if (out_dtype != PK_BF16 && out_dtype != PK_F32) return refuse(who, {PK_EINVAL, "out_dtype must be PK_BF16 or PK_F32"});
+    if (!(std::isfinite(scale) && scale > 0.f)) return refuse(who, {PK_EINVAL, "scale must be finite and positive"});
+    empty = n == 0 || total_q == 0 || max_q == 0;
+    if (empty) return PK_OK;
+    if (!q || !out || !q_start) return refuse(who, {PK_EINVAL, "q, out or q_start is NULL"});
+    if (!aligned(q, 16) || !aligned(out, 16)) return refuse(who, {PK_EINVAL, "q and out must be 16-byte aligned"});
+    if (!workspace || !aligned(workspace, 256)) return refuse(who, {PK_EINVAL, "workspace is NULL or not 256-byte aligned"});
+    a.cache = view(*cache); a.block_table = block_table; a.max_blocks = max_blocks;
+    a.q = q; a.q_start = q_start; a.total_q = total_q; a.max_q = max_q; a.mask = tree_mask;
+    a.kv_lens = kv_lens; a.n = n;
+    a.out = out; a.out_f32 = out_dtype == PK_F32; a.scale = scale; a.Hq = Hq;
+    return PK_OK;
+}
 
 }  // namespace pk

@@ -1,0 +1,192 @@
+// Attention of drafted tokens over the paged cache where requests have their leading pages in common.
+//
+// softmax(q K^T) V over the keys of a request is put together from two parts: the keys that its family shares, for the rows of all members at once, and its own ones behind
+// them.  With o = sum p v / sum p and lse = log sum p of each part, the whole is sum exp(lse) o over sum exp(lse).
+//
+// Four launches.  The first finds what a family shares: the pages in which the members' rows of the block table are the same from the front on, less what is not wholly in
+// front of every member's drafted tokens, in whole tiles of 64 keys.  So the result does not depend on what the families are, nothing is masked in the shared part, and
+// there are no lengths to be handed over.  The second and third are the kernels of pk_tree_attn, for a family's rows as one request's and for each request's keys from
+// there on; the fourth joins their partial results.
+#include "shared_attn.h"
+#include "tree_body.hip.h"
+
+namespace pk {
+namespace {
+
+constexpr int kSharedTile = 64;                     // keys
+
+__device__ __forceinline__ int load_there(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void store_there(int32_t* p, const int x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// A wave for each request finds its family and how many tokens it has in common with the family's first request; the last workgroup makes the families' arrays.
+// Families are [M[g], M[g + 1]) with M the largest of family_start up to g, within [0, n]: disjoint whatever the array holds.
+__global__ __launch_bounds__(256) void shared_find_kernel(SharedArgs s) {
+    __shared__ int last, lds[4];
+    const TreeArgs& a = s.tree;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = blockIdx.x * 4 + wave;
+    if (i < a.n) {
+        int first = 0, end = 0, family = -1, before = 0;
+        for (int g0 = 0; g0 <= s.families; g0 += 64) {
+            const int start = g0 + lane <= s.families ? s.family_start[g0 + lane] : -1;
+            const uint64_t behind = __ballot(start > i);
+            const int upto = behind ? __builtin_ctzll(behind) : 64;
+            int most = lane < upto ? start : 0;
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o, 64));
+            before = max(before, most);
+            if (behind) {
+                family = g0 + upto - 1;
+                first = before;
+                end = min(__shfl(start, upto, 64), a.n);
+                break;
+            }
+        }
+        const int asked = a.q_start[i + 1] - a.q_start[i], len = min(max(a.kv_lens[i], 0), a.most_keys);
+        const bool member = family >= 0 && end - first > 1;
+        if (member && min(asked, a.max_q) > 0) {
+            const int context = max(min(a.kv_lens[i] - asked, len), 0), pages = (context + a.cache.page - 1) / a.cache.page;
+            const int32_t* mine = a.block_table + static_cast<int64_t>(i) * a.max_blocks;
+            const int32_t* firsts = a.block_table + static_cast<int64_t>(first) * a.max_blocks;
+            int same = i == first ? pages : 0;
+            while (same < pages) {                  // 256 pages at a time
+                uint64_t differs[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int p = same + 64 * u + lane;
+                    differs[u] = __ballot(p < pages && mine[min(p, pages - 1)] != firsts[min(p, pages - 1)]);
+                }
+                int more = 256;
+#pragma unroll
+                for (int u = 3; u >= 0; --u) more = differs[u] ? 64 * u + __builtin_ctzll(differs[u]) : more;
+                same += more;
+                if (more < 256) break;
+            }
+            const int common = min(context, static_cast<int>(min(static_cast<int64_t>(same) * a.cache.page, static_cast<int64_t>(a.most_keys))));
+            if (lane == 0) atomicMax(s.missing + family, a.most_keys - common + 1);
+        }
+        if (lane == 0) store_there(s.family_of + i, member ? family : -1);
+    }
+    __builtin_amdgcn_s_waitcnt(0x0F70);            // vmcnt(0): what this wave has found is in memory (decode_body.hip.h)
+    __syncthreads();
+    if (tid == 0) last = arrives_last(TreeCount{s.arrived}, gridDim.x);
+    __syncthreads();
+    if (last == 0) return;
+    int carried = 0, carried_q = 0;                 // M, and the largest row of q, so far
+    for (int g0 = 0; g0 <= s.families; g0 += 256) {
+        const int g = g0 + tid;
+        const auto prefix_max = [&](int x, const int carried) {
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int y = __shfl_up(x, o, 64);
+                x = lane >= o ? max(x, y) : x;
+            }
+            __syncthreads();
+            if (lane == 63) lds[wave] = x;
+            __syncthreads();
+            x = max(x, carried);
+            for (int w = 0; w < wave; ++w) x = max(x, lds[w]);
+            return x;
+        };
+        const int first = prefix_max(g <= s.families ? min(s.family_start[g], a.n) : 0, carried);
+        carried = max(max(max(lds[0], lds[1]), max(lds[2], lds[3])), carried);
+        const int q0 = prefix_max(g <= s.families ? static_cast<int>(min(static_cast<int64_t>(a.q_start[first]), a.total_q)) : 0, carried_q);
+        carried_q = max(max(max(lds[0], lds[1]), max(lds[2], lds[3])), carried_q);
+        if (g <= s.families) s.q_start_of[g] = q0;
+        if (g < s.families) {
+            const int missing = load_there(s.missing + g);
+            s.first_of[g] = min(first, a.n - 1);
+            store_there(s.len_of + g, missing == 0 ? 0 : (a.most_keys + 1 - missing) / kSharedTile * kSharedTile);
+            if (missing != 0) store_there(s.missing + g, 0);
+        }
+    }
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+    __syncthreads();
+    for (int r = tid; r < a.n; r += 256) {
+        const int g = load_there(s.family_of + r);
+        s.shared_of[r] = g < 0 ? 0 : load_there(s.len_of + g);
+    }
+}
+
+// Puts the parts together: a workgroup for (request, chunk of its rows, slice of that, KV head).  KV heads go round-robin over the XCDs, as they do in the launches that
+// write the parts.
+template <int D>
+__global__ __launch_bounds__(256) void shared_merge_kernel(SharedArgs s) {
+    const TreeArgs& a = s.tree;
+    int rest = blockIdx.x;
+    const auto take = [&](const int of) { const int x = rest % of; rest /= of; return x; };
+    const int kvh = take(a.cache.Hkv), slice = take(a.slices), chunk = take(a.chunks), i = rest;
+    const int asked = a.q_start[i + 1] - a.q_start[i];
+    const int64_t q0 = min(max(static_cast<int64_t>(a.q_start[i]), int64_t{0}), a.total_q);
+    const int rows = static_cast<int>(min(static_cast<int64_t>(min(asked, a.max_q)), a.total_q - q0)) * a.heads_per_kv;
+    const int chunk_rows = 1 << a.chunk_shift, here = min(rows - chunk * chunk_rows, chunk_rows);
+    if (here <= 0) return;
+    const int2 p = a.pieces_of[i];
+    const bool shares = a.shared_of[i] > 0;
+    if (!shares && p.x == 1) return;
+    const int chunks = (rows + chunk_rows - 1) / chunk_rows, family = max(s.family_of[i], 0);
+    const int2 f = shares ? s.pieces_of_family[family] : int2{0, 0};
+    const int64_t family_q0 = shares ? s.q_start_of[family] : 0;
+    const int family_rows = shares ? (s.q_start_of[family + 1] - static_cast<int>(family_q0)) * a.heads_per_kv : 1;
+    const int family_chunks = (family_rows + kWideRows - 1) / kWideRows;
+    for (int x = slice * 256 + threadIdx.x; x < here * (D / 4); x += a.slices * 256) {
+        const int local = x / (D / 4), col = 4 * (x % (D / 4)), row = chunk * chunk_rows + local, t = a.by_r(row);
+        const int of_family = static_cast<int>(min(max((q0 - family_q0) * a.heads_per_kv + row, int64_t{0}), static_cast<int64_t>(family_rows - 1)));
+        store4(a, ((q0 + t) * a.Hq + kvh * a.heads_per_kv + row - t * a.heads_per_kv) * D + col, merged(p.x + f.x, [&](const int piece, float& lse, floatx4& o) {
+            const bool own = piece < p.x;
+            const int64_t at_own = (static_cast<int64_t>(p.y + piece * chunks + chunk) * a.cache.Hkv + kvh) * chunk_rows + local;
+            const int64_t at_shared = (static_cast<int64_t>(f.y + (piece - p.x) * family_chunks + of_family / kWideRows) * a.cache.Hkv + kvh) * kWideRows + of_family % kWideRows;
+            lse = own ? a.part_lse[at_own] : s.family_lse[at_shared];
+            o = *reinterpret_cast<const floatx4*>(own ? a.part_o + at_own * D + col : s.family_o + at_shared * D + col);
+        }));
+    }
+}
+
+template <int D, bool F8>
+int launch(SharedArgs s, const TreeShape& shape, hipStream_t st) {
+    TreeArgs& a = s.tree;
+    const dim3 block(64 * kWaves);
+    hipLaunchKernelGGL(shared_find_kernel, dim3(static_cast<unsigned>((a.n + 3) / 4)), dim3(256), 0, st, s);
+
+    TreeArgs f = a;                                 // families as requests
+    f.q_start = s.q_start_of; f.kv_lens = s.len_of; f.first_of = s.first_of; f.n = s.families;
+    f.max_q = static_cast<int32_t>(a.total_q); f.mask = nullptr;
+    f.chunk_shift = 7;
+    f.rounds = 5 / 4.f;
+    f.least_per_share = 64.f / kLeastKeys; f.least_per_many = f.least_per_share / 4;
+    f.pieces_of = s.pieces_of_family; f.part_o = s.family_o; f.part_lse = s.family_lse;
+    const int64_t family_loads = a.total_q * a.heads_per_kv / kWideRows + s.families;
+    const int64_t family_groups = (family_loads <= a.items / 2 ? a.items : family_loads + a.items / 2) * a.cache.Hkv;
+    if (family_groups > 0x7FFFFFFF) return static_cast<int>(hipErrorInvalidConfiguration);
+    hipLaunchKernelGGL((tree_attn_wide_kernel<D, F8, kShared>), dim3(static_cast<unsigned>(family_groups)), block, 0, st, f);
+
+    const int row_blocks = shape.rows / 16, keys = 16 * (row_blocks == 1 ? kSubTiles1<D, F8> : row_blocks == 2 ? kSubTiles2<D, F8> : 4);
+    a.least_per_share = static_cast<float>(keys) / kLeastKeys;
+    a.least_per_many = a.least_per_share / (shape.rows == 128 ? 4 : 1);
+    a.shared_of = s.shared_of;
+    const int64_t loads = static_cast<int64_t>(a.n) * a.chunks;
+    const int64_t groups = (loads <= a.items / 2 ? a.items : loads + a.items / 2) * a.cache.Hkv;
+    if (groups > 0x7FFFFFFF) return static_cast<int>(hipErrorInvalidConfiguration);
+    const dim3 grid(static_cast<unsigned>(groups));
+    if (row_blocks == 1) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 1, kSubTiles1<D, F8>, 2, false, kOwn>), grid, block, 0, st, a);
+    else if (row_blocks == 2) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 2, kSubTiles2<D, F8>, kWavesOf2<D, F8>, false, kOwn>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((tree_attn_wide_kernel<D, F8, kOwn>), grid, block, 0, st, a);
+
+    // the merge: up to 2048 workgroups, of 8 rows and more each
+    const int64_t merges = loads * a.cache.Hkv, slices = 2048 / (merges < 2048 ? merges : 2048);
+    a.slices = static_cast<int>(slices < shape.rows / 8 ? slices : shape.rows / 8);
+    if (merges * a.slices > 0x7FFFFFFF) return static_cast<int>(hipErrorInvalidConfiguration);
+    hipLaunchKernelGGL((shared_merge_kernel<D>), dim3(static_cast<unsigned>(merges * a.slices)), dim3(256), 0, st, s);
+    return static_cast<int>(hipGetLastError());
+}
+
+}  // namespace
+
+int launch_shared_tree_attn(SharedArgs s, const TreeShape& shape, void* stream) {
+    set_tree_sizes(s.tree, shape);
+    s.tree.whole = 0;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (s.tree.cache.d == 128) return s.tree.cache.f8 ? launch<128, true>(s, shape, st) : launch<128, false>(s, shape, st);
+    return s.tree.cache.f8 ? launch<64, true>(s, shape, st) : launch<64, false>(s, shape, st);
+}
+
+}  // namespace pk
