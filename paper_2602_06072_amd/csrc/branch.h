@@ -46,27 +46,26 @@ struct CacheCopyArgs {
 };
 int launch_cache_copy(CacheCopyArgs a, void* stream);
 
-// Sum and maximum of a piece of a row of logits, relative to its maximum; where the largest logit stands first
+// Sum of the weights of a piece of a row of logits, relative to that of the logit `top`; or the largest logit and where it stands first
 struct RowPart { double sum; float top; int32_t at; };
 
-// What there is left to draw of a request after its drafted tokens have been looked at
-struct Leftover {
-    int64_t row;                                    // of the last token that stays
-    int32_t kind, pieces;                           // LeftoverKind; pieces of its weights' sums
-    double c, of_target, of_draft;                  // weights max(of_target e^(l - top) - c of_draft e^(l' - top'), 0)
+// What a token with children decides: which of them stays (-1: none), c, and 1 / the sums of its rows with what they are relative to
+struct VerifyChoice {
+    int32_t token;
+    double c, of_target, of_draft;
     float top, draft_top;
 };
-enum LeftoverKind { kNone, kKnown, kUnknown, kResidual, kRemoved, kLargest };
 
-// How a launch cuts rows of logits: `pieces` of a row where all rows are looked at, `last_pieces` where one of each request is
+// How a launch cuts rows of logits: `pieces` of a row where all rows with children are looked at, `last_pieces` where one of each request is
 struct VerifyShape {
     int pieces, length, last_pieces, last_length;   // lengths in elements, multiples of kStep
     static constexpr int kStep = 2048;              // elements that a workgroup takes at a time
+    static constexpr size_t kCountBytes = 65536 * 4;               // arrivals of a request's pieces, zero between calls: in front of everything, as many for every call
     static VerifyShape of(int64_t n, int64_t total_q, int32_t vocab);
     size_t part_bytes(const int64_t total_q) const { return whole256(total_q * 2 * pieces * static_cast<int64_t>(sizeof(RowPart))); }
     size_t last_bytes(const int64_t n) const { return whole256(n * last_pieces * static_cast<int64_t>(sizeof(RowPart))); }
-    static size_t left_bytes(const int64_t n) { return whole256(n * static_cast<int64_t>(sizeof(Leftover))); }
-    size_t bytes(const int64_t n, const int64_t total_q) const { return part_bytes(total_q) + last_bytes(n) + left_bytes(n); }
+    static size_t choice_bytes(const int64_t total_q) { return whole256(total_q * static_cast<int64_t>(sizeof(VerifyChoice))); }
+    size_t bytes(const int64_t n, const int64_t total_q) const { return kCountBytes + part_bytes(total_q) + last_bytes(n) + choice_bytes(total_q); }
 
 private:
     static size_t whole256(const int64_t bytes) { return static_cast<size_t>((bytes + 255) / 256 * 256); }
@@ -78,9 +77,10 @@ struct VerifyArgs {
     const float* temperature; const float* accept_u; const float* sample_u;
     int32_t* keep; int32_t max_keep; int32_t* keep_count; int32_t* next_token;
     VerifyShape shape;
+    uint32_t* arrived;                              // [n], zero between calls
     RowPart* parts;                                 // [total_q][2][pieces]: of the target's rows, of the draft's
     RowPart* last_parts;                            // [n][last_pieces]
-    Leftover* left;                                 // [n]
+    VerifyChoice* choices;                          // [total_q]
 };
 int launch_draft_verify(const VerifyArgs& a, void* stream);
 
