@@ -59,7 +59,7 @@ struct VerifyChoice {
 // How a launch cuts rows of logits: `pieces` of a row where all rows with children are looked at, `last_pieces` where one of each request is
 struct VerifyShape {
     int pieces, length, last_pieces, last_length;   // lengths in elements, multiples of kStep
-    static constexpr int kStep = 2048;              // elements that a workgroup takes at a time
+    static constexpr int kStep = 4096;              // elements that a workgroup takes at a time
     static constexpr size_t kCountBytes = 65536 * 4;               // arrivals of a request's pieces, zero between calls: in front of everything, as many for every call
     static VerifyShape of(int64_t n, int64_t total_q, int32_t vocab);
     size_t part_bytes(const int64_t total_q) const { return whole256(total_q * 2 * pieces * static_cast<int64_t>(sizeof(RowPart))); }

@@ -18,59 +18,76 @@
 namespace pk {
 namespace {
 
-constexpr int kThreads = 256, kVector = 8, kStep = VerifyShape::kStep;
+constexpr int kThreads = 256, kVector = 16, kStep = VerifyShape::kStep;
 static_assert(kStep == kThreads * kVector, "a step is a vector of every thread");
 constexpr float kMostLogit = 3.402823466e38f;
 
 // NaN becomes -inf, inf the largest number
 __device__ __forceinline__ float plain_logit(const float x) { return fminf(fmaxf(x, -INFINITY), kMostLogit); }
 
-// Eight logits from number `at` on; those behind the row's end are -inf.  Rows of odd length begin anywhere: the loads are 16 bytes long at addresses of any alignment.
+// Sixteen logits from number `at` on, and the largest of them; those behind the row's end are -inf, inf is the largest number.  NaN stays: it is no largest one, and has no
+// weight.  Rows of odd length begin anywhere: the loads are 16 bytes long at addresses of any alignment.
+// (as they are in memory, so that what is asked for ahead is not waited for)
+template <bool F32> struct Raw { uint32_t w[F32 ? kVector : kVector / 2]; };
+template <bool F32>
+__device__ __forceinline__ Raw<F32> load_raw(const void* base, const int64_t at) {
+    Raw<F32> r;
+    __builtin_memcpy(r.w, static_cast<const char*>(base) + at * (F32 ? 4 : 2), sizeof r.w);
+    return r;
+}
+template <bool F32>
+__device__ __forceinline__ void unpack(const Raw<F32>& r, float (&x)[kVector]) {
+#pragma unroll
+    for (int e = 0; e < kVector; ++e) x[e] = __uint_as_float(F32 ? r.w[F32 ? e : 0] : e % 2 == 0 ? r.w[e / 2] << 16 : r.w[e / 2] & 0xFFFF0000u);
+}
+template <bool F32>
+__device__ __forceinline__ void load_last(const void* base, const int64_t row_at, const int at, const int vocab, float (&x)[kVector]) {
+#pragma unroll
+    for (int e = 0; e < kVector; ++e) {
+        x[e] = -INFINITY;
+        if (at + e < vocab) x[e] = F32 ? static_cast<const float*>(base)[row_at + at + e] : bf16_bits_to_float(static_cast<const uint16_t*>(base)[row_at + at + e]);
+    }
+}
 template <bool F32>
 __device__ __forceinline__ void load_logits(const void* base, const int64_t row_at, const int at, const int vocab, float (&x)[kVector]) {
-    if (at + kVector <= vocab) {
-        if constexpr (F32) {
-            __builtin_memcpy(x, static_cast<const float*>(base) + row_at + at, 32);
-        } else {
-            uint32_t w[4];
-            __builtin_memcpy(w, static_cast<const uint16_t*>(base) + row_at + at, 16);
+    if (at + kVector <= vocab) unpack<F32>(load_raw<F32>(base, row_at + at), x);
+    else load_last<F32>(base, row_at, at, vocab, x);
+}
+__device__ __forceinline__ float largest_of(float (&x)[kVector]) {
+    // (three at a time, which fmaxf, with its care for signalling NaN, is not compiled to: such a NaN becomes the result, and is seen to below)
+    float top = -INFINITY;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[2 * e] = __uint_as_float(w[e] << 16);
-                x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
-            }
-        }
-    } else {
+    for (int e = 0; e < kVector; e += 2) asm("v_max3_f32 %0, %0, %1, %2" : "+v"(top) : "v"(x[e]), "v"(x[e + 1]));
+    if (!(top < INFINITY)) {
+        top = -INFINITY;
 #pragma unroll
         for (int e = 0; e < kVector; ++e) {
-            x[e] = -INFINITY;
-            if (at + e < vocab) x[e] = F32 ? static_cast<const float*>(base)[row_at + at + e] : bf16_bits_to_float(static_cast<const uint16_t*>(base)[row_at + at + e]);
+            x[e] = plain_logit(x[e]);
+            top = fmaxf(top, x[e]);
         }
     }
-#pragma unroll
-    for (int e = 0; e < kVector; ++e) x[e] = plain_logit(x[e]);
+    return top;
 }
 template <bool F32>
 __device__ __forceinline__ float load_logit(const void* base, const int64_t at) {
     return plain_logit(F32 ? static_cast<const float*>(base)[at] : bf16_bits_to_float(static_cast<const uint16_t*>(base)[at]));
 }
 
-// 2^y for y up to 1000; below -1000 (and for a NaN) 2^-1000.  y = n + f with |f| <= 1/2: adding 1.5 2^52 leaves n in the low bits.  The polynomial has the least largest
-// relative error of its degree with p(0) = 1, 1.5e-14 (fitted to 2^f by least squares with weights that follow the error): equal logits of 0 count exactly.
+// 2^y for y up to 1000; 0 below -1074 and for a NaN.  y = n + f with |f| <= 1/2: adding 1.5 2^52 leaves n in the low bits.  The polynomial has the least largest
+// relative error of its degree with p(0) = 1, 8.1e-13 (fitted to 2^f by least squares with weights that follow the error): equal logits of 0 count exactly.
 __device__ __forceinline__ double exp2_of(const double y) {
     constexpr double kRound = 6755399441055744.0;
-    const double in = fmax(y, -1000.0), t = in + kRound, f = in - (t - kRound);
-    double p = 0x1.b3de2e4961671p-24;
-    p = fma(p, f, 0x1.63e696660f4e6p-20);
-    p = fma(p, f, 0x1.ffce2fc41cb18p-17);
-    p = fma(p, f, 0x1.430897f32df6ap-13);
-    p = fma(p, f, 0x1.5d87fd9387457p-10);
-    p = fma(p, f, 0x1.3b2ab72412277p-7);
-    p = fma(p, f, 0x1.c6b08d70c881ap-5);
-    p = fma(p, f, 0x1.ebfbdff81be06p-3);
-    p = fma(p, f, 0x1.62e42fefa37d1p-1);
+    const double in = fmax(y, -1100.0), t = in + kRound, f = in - (t - kRound);
+    double p = 0x1.61c4f0ed5f063p-20;
+    p = fma(p, f, 0x1.00d85341b87d0p-16);
+    p = fma(p, f, 0x1.430aa882ba307p-13);
+    p = fma(p, f, 0x1.5d874d06fe487p-10);
+    p = fma(p, f, 0x1.3b2ab5ed6fb84p-7);
+    p = fma(p, f, 0x1.c6b08dced3566p-5);
+    p = fma(p, f, 0x1.ebfbdff8ede86p-3);
+    p = fma(p, f, 0x1.62e42fef89d1ep-1);
     p = fma(p, f, 1.0);
-    return __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));
+    return __builtin_amdgcn_ldexp(p, __double2loint(t));
 }
 // weight of a logit relative to that of `ref`; per: log2 e / temperature
 __device__ __forceinline__ double weight_of(const float x, const float ref, const double per) { return exp2_of((static_cast<double>(x) - static_cast<double>(ref)) * per); }
@@ -96,6 +113,22 @@ template <bool LARGEST>
 __device__ __forceinline__ RowPart of_wave(RowPart y, const double per) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) y = joined<LARGEST>(y, {__shfl_xor(y.sum, o, 64), __shfl_xor(y.top, o, 64), __shfl_xor(y.at, o, 64)}, per);
+    return y;
+}
+// ... of all threads, in every thread
+struct WaveParts { double sum[kThreads / 64]; float top[kThreads / 64]; int at[kThreads / 64]; };
+template <bool LARGEST>
+__device__ __forceinline__ RowPart of_all(RowPart y, const double per, WaveParts& lds) {
+    y = of_wave<LARGEST>(y, per);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) {
+        const int wave = threadIdx.x >> 6;
+        lds.sum[wave] = y.sum; lds.top[wave] = y.top; lds.at[wave] = y.at;
+    }
+    __syncthreads();
+    y = {lds.sum[0], lds.top[0], lds.at[0]};
+#pragma unroll
+    for (int w = 1; w < kThreads / 64; ++w) y = joined<LARGEST>(y, {lds.sum[w], lds.top[w], lds.at[w]}, per);
     return y;
 }
 constexpr RowPart kNoPart{0.0, -INFINITY, 0x7FFFFFFF};
@@ -128,51 +161,53 @@ __device__ __forceinline__ Tree tree_of(const VerifyArgs& a, const int i) {
 
 // A piece of a row, all threads: elements [first, end).  A thread's reference is 0 unless weights would leave the range of 64 bits.
 template <bool F32, bool LARGEST>
-__device__ __forceinline__ RowPart part_of_row(const void* base, const int64_t row_at, const int first, const int end, const int vocab, const double per, RowPart* lds) {
+__device__ __forceinline__ RowPart part_of_row(const void* base, const int64_t row_at, const int first, const int end, const int vocab, const double per, WaveParts& lds) {
     RowPart y = kNoPart;
-    constexpr int AHEAD = 2;
     constexpr float kFar = 500.f;                   // octaves
     const float octaves = static_cast<float>(per);
-    for (int at0 = first + static_cast<int>(threadIdx.x) * kVector; at0 < end; at0 += AHEAD * kStep) {
-        float x[AHEAD][kVector];
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) load_logits<F32>(base, row_at, at0 + u * kStep, at0 + u * kStep < end ? vocab : 0, x[u]);
-        float top = -INFINITY;
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
-#pragma unroll
-            for (int e = 0; e < kVector; ++e) top = fmaxf(top, x[u][e]);
+    const auto take = [&](float (&x)[kVector], const int at) {
+        const float top = largest_of(x);
         if constexpr (LARGEST) {
-            if (!(top > y.top)) continue;
+            if (!(top > y.top)) return;
             y.top = top;
-            bool found = false;
+            int place = kVector;
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u)
-#pragma unroll
-                for (int e = 0; e < kVector; ++e)
-                    if (!found && x[u][e] == top) { y.at = at0 + u * kStep + e; found = true; }
+            for (int e = kVector - 1; e >= 0; --e) place = x[e] == top ? e : place;
+            y.at = at + place;
         } else {
-            if (top == -INFINITY) continue;
+            if (top == -INFINITY) return;
             if (y.top == -INFINITY) {
                 y.top = fabsf(top) * octaves <= kFar ? 0.f : top;
             } else if ((top - y.top) * octaves > kFar) {
                 y.sum *= weight_of(y.top, top, per);
                 y.top = top;
             }
+            double sums[2] = {};
+            if (__all(y.top == 0.f)) {              // (as nearly always: a subtraction less)
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u)
+                for (int e = 0; e < kVector; ++e) sums[e % 2] += exp2_of(static_cast<double>(x[e]) * per);
+            } else {
 #pragma unroll
-                for (int e = 0; e < kVector; ++e) y.sum += weight_of(x[u][e], y.top, per);
+                for (int e = 0; e < kVector; ++e) sums[e % 2] += weight_of(x[e], y.top, per);
+            }
+            y.sum += sums[0] + sums[1];
         }
+    };
+    int at = first + static_cast<int>(threadIdx.x) * kVector;
+    Raw<F32> ahead;
+    if (at + kVector <= end) ahead = load_raw<F32>(base, row_at + at);
+    for (; at + kVector <= end; at += kStep) {
+        float x[kVector];
+        unpack<F32>(ahead, x);
+        if (at + kStep + kVector <= end) ahead = load_raw<F32>(base, row_at + at + kStep);
+        take(x, at);
     }
-    y = of_wave<LARGEST>(y, per);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = y;
-    __syncthreads();
-    y = lds[0];
-#pragma unroll
-    for (int w = 1; w < kThreads / 64; ++w) y = joined<LARGEST>(y, lds[w], per);
-    return y;
+    if (at < end) {                                 // the end of a row
+        float x[kVector];
+        load_last<F32>(base, row_at, at, vocab, x);
+        take(x, at);
+    }
+    return of_all<LARGEST>(y, per, lds);
 }
 __device__ __forceinline__ double sum_of_all(double x, double* lds) {
 #pragma unroll
@@ -189,7 +224,7 @@ __device__ __forceinline__ double sum_of_all(double x, double* lds) {
 // Sums of the rows of tokens with children: a workgroup for (piece, target or draft; token; request)
 template <bool F32>
 __global__ __launch_bounds__(kThreads) void verify_rows_kernel(VerifyArgs a) {
-    __shared__ RowPart lds[kThreads / 64];
+    __shared__ WaveParts lds;
     const int of_draft = blockIdx.x >= static_cast<unsigned>(a.shape.pieces) ? 1 : 0, piece = blockIdx.x - of_draft * a.shape.pieces, token = blockIdx.y, i = blockIdx.z;
     const Tree t = tree_of(a, i);
     if (!(t.inner >> token & 1)) return;
@@ -199,7 +234,10 @@ __global__ __launch_bounds__(kThreads) void verify_rows_kernel(VerifyArgs a) {
     const int first = piece * a.shape.length, end = min(first + a.shape.length, a.vocab);
     const RowPart y = warm == 0.f ? part_of_row<F32, true>(a.target, row * a.target_stride, first, end, a.vocab, 0.0, lds)
                                   : part_of_row<F32, false>(of_draft ? a.draft : a.target, row * (of_draft ? a.draft_stride : a.target_stride), first, end, a.vocab, kLog2e64 / warm, lds);
-    if (threadIdx.x == 0) a.parts[(row * 2 + of_draft) * a.shape.pieces + piece] = y;
+    if (threadIdx.x == 0) {
+        RowPart& to = a.parts[(row * 2 + of_draft) * a.shape.pieces + piece];
+        to.sum = y.sum; to.top = y.top; to.at = y.at;
+    }
 }
 
 // Weights that are left of a row: max(P - c Q, 0)
@@ -208,10 +246,7 @@ struct LeftWeight {
     float top, draft_top;
     __device__ __forceinline__ double target(const float x) const { return of(x, top, of_target); }
     __device__ __forceinline__ double draft(const float x) const { return of(x, draft_top, of_draft); }
-    __device__ __forceinline__ double of(const float x, const float ref, const double share) const {
-        const double y = (static_cast<double>(x) - static_cast<double>(ref)) * per;
-        return y >= -1000.0 ? share * exp2_of(y) : 0.0;            // (-inf, with per = 0 a NaN: none)
-    }
+    __device__ __forceinline__ double of(const float x, const float ref, const double share) const { return share * weight_of(x, ref, per); }
     __device__ __forceinline__ double operator()(const float x, const float y) const { return fmax(target(x) - c * draft(y), 0.0); }
 };
 
@@ -260,6 +295,8 @@ __global__ __launch_bounds__(kThreads) void verify_choice_kernel(VerifyArgs a) {
             float vp[kVector], vq[kVector];
             load_logits<F32>(a.target, row * a.target_stride, at, a.vocab, vp);
             load_logits<F32>(a.draft, row * a.draft_stride, at, a.vocab, vq);
+            largest_of(vp);
+            largest_of(vq);
 #pragma unroll
             for (int e = 0; e < kVector; ++e) sum += w(vp[e], vq[e]);
         }
@@ -278,9 +315,17 @@ template <bool F32>
 __device__ __forceinline__ void left_weights(const VerifyArgs& a, const int64_t row, const int kind, const LeftWeight& w, const int at, const int* list, const int removed, double (&v)[kVector]) {
     float x[kVector], z[kVector];
     load_logits<F32>(a.target, row * a.target_stride, at, a.vocab, x);
-    if (kind == kResidual) load_logits<F32>(a.draft, row * a.draft_stride, at, a.vocab, z);
+    if (kind == kResidual) {
+        load_logits<F32>(a.draft, row * a.draft_stride, at, a.vocab, z);
+        largest_of(x);
+        largest_of(z);
 #pragma unroll
-    for (int e = 0; e < kVector; ++e) v[e] = kind == kResidual ? w(x[e], z[e]) : w.target(x[e]);
+        for (int e = 0; e < kVector; ++e) v[e] = w(x[e], z[e]);
+        return;
+    }
+    largest_of(x);
+#pragma unroll
+    for (int e = 0; e < kVector; ++e) v[e] = w.target(x[e]);
     if (kind == kRemoved)
         for (int r = 0; r < removed; ++r)
 #pragma unroll
@@ -289,7 +334,7 @@ __device__ __forceinline__ void left_weights(const VerifyArgs& a, const int64_t 
 }
 template <bool F32>
 __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
-    __shared__ RowPart lds[kThreads / 64];
+    __shared__ WaveParts lds;
     __shared__ double sums[kThreads / 64];
     __shared__ int list[kMostDrafts];
     __shared__ int last, found, last_positive, the_piece;
@@ -302,7 +347,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
     // the tokens that stay: from one choice to the next
     int at = 0, count = 1;
     uint64_t kept = 1;
-    const int choice = t.inner >> lane & 1 ? a.choices[t.q0 + lane].token : -1;
+    const int chosen = lane < t.tokens ? a.choices[t.q0 + lane].token : -1, choice = t.inner >> lane & 1 ? chosen : -1;       // (asked for beside the masks)
     for (; count < a.max_keep; ++count) {
         const int next = __builtin_amdgcn_readlane(choice, at);
         if (next < 0) break;
@@ -373,13 +418,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
         mine = kNoPart;
     }
     // a thread has a piece: the whole row
-    RowPart all = greedy ? of_wave<true>(mine, per) : of_wave<false>(mine, per);
-    __syncthreads();
-    if (lane == 0) lds[wave] = all;
-    __syncthreads();
-    all = lds[0];
-#pragma unroll
-    for (int v = 1; v < kThreads / 64; ++v) all = greedy ? joined<true>(all, lds[v], per) : joined<false>(all, lds[v], per);
+    RowPart all = greedy ? of_all<true>(mine, per, lds) : of_all<false>(mine, per, lds);
     if (greedy || (kind == kPlain && all.top == -INFINITY)) {
         if (tid == 0) a.next_token[i] = all.top == -INFINITY ? -1 : all.at;
         return;
@@ -483,9 +522,9 @@ int launch(const VerifyArgs& a, hipStream_t st) {
 }  // namespace
 
 VerifyShape VerifyShape::of(const int64_t n, const int64_t total_q, const int32_t vocab) {
-    const auto cut = [&](const int64_t rows, const int64_t most, int& pieces, int& length) {
+    const auto cut = [&](const int64_t rows, const int64_t groups, const int64_t most, int& pieces, int& length) {
         const int64_t steps = (static_cast<int64_t>(vocab) + kStep - 1) / kStep;
-        int64_t wanted = 2048 / (rows > 0 ? rows : 1) + 1;
+        int64_t wanted = groups / (rows > 0 ? rows : 1) + 1;
         wanted = wanted < most ? wanted : most;
         wanted = wanted < steps ? wanted : steps;
         const int64_t each = (steps + wanted - 1) / wanted;
@@ -493,8 +532,8 @@ VerifyShape VerifyShape::of(const int64_t n, const int64_t total_q, const int32_
         pieces = static_cast<int>((steps + each - 1) / each);
     };
     VerifyShape s;
-    cut(total_q, 64, s.pieces, s.length);           // (a lane for each in verify_choice_kernel,
-    cut(n, kThreads, s.last_pieces, s.last_length); //  a thread for each in verify_draw_kernel)
+    cut(total_q, 2048, 64, s.pieces, s.length);           // (a lane for each in verify_choice_kernel,
+    cut(n, 1024, kThreads, s.last_pieces, s.last_length); //  a thread for each in verify_draw_kernel)
     return s;
 }
 
