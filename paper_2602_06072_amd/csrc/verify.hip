@@ -25,9 +25,8 @@ constexpr float kMostLogit = 3.402823466e38f;
 // NaN becomes -inf, inf the largest number
 __device__ __forceinline__ float plain_logit(const float x) { return fminf(fmaxf(x, -INFINITY), kMostLogit); }
 
-// Sixteen logits from number `at` on, and the largest of them; those behind the row's end are -inf, inf is the largest number.  NaN stays: it is no largest one, and has no
-// weight.  Rows of odd length begin anywhere: the loads are 16 bytes long at addresses of any alignment.
-// (as they are in memory, so that what is asked for ahead is not waited for)
+// Sixteen logits as they are in memory, so that what is asked for ahead is not waited for.  Rows of odd length begin anywhere: the loads are 16 bytes long at addresses
+// of any alignment.
 template <bool F32> struct Raw { uint32_t w[F32 ? kVector : kVector / 2]; };
 template <bool F32>
 __device__ __forceinline__ Raw<F32> load_raw(const void* base, const int64_t at) {
@@ -36,35 +35,65 @@ __device__ __forceinline__ Raw<F32> load_raw(const void* base, const int64_t at)
     return r;
 }
 template <bool F32>
-__device__ __forceinline__ void unpack(const Raw<F32>& r, float (&x)[kVector]) {
-#pragma unroll
-    for (int e = 0; e < kVector; ++e) x[e] = __uint_as_float(F32 ? r.w[F32 ? e : 0] : e % 2 == 0 ? r.w[e / 2] << 16 : r.w[e / 2] & 0xFFFF0000u);
+__device__ __forceinline__ float logit_of(const Raw<F32>& r, const int e) {
+    return __uint_as_float(F32 ? r.w[F32 ? e : 0] : e % 2 == 0 ? r.w[e / 2] << 16 : r.w[e / 2] & 0xFFFF0000u);
 }
+// The last sixteen of a row, those in front of number `at` hidden (-inf), for a vector that begins there and has fewer
 template <bool F32>
-__device__ __forceinline__ void load_last(const void* base, const int64_t row_at, const int at, const int vocab, float (&x)[kVector]) {
+__device__ __forceinline__ Raw<F32> load_last(const void* base, const int64_t row_at, const int at, const int vocab) {
+    Raw<F32> r;
+    if (vocab >= kVector) {
+        r = load_raw<F32>(base, row_at + vocab - kVector);
+    } else {
+#pragma unroll 1
+        for (int e = vocab - kVector; e < vocab; e += F32 ? 1 : 2) {               // (a word at a time, from the front)
+            const auto half = [&](const int n) { return n >= 0 ? static_cast<uint32_t>(static_cast<const uint16_t*>(base)[row_at + n]) : 0xFF80u; };
+            const uint32_t w = F32 ? (e >= 0 ? static_cast<const uint32_t*>(base)[row_at + e] : 0xFF800000u) : half(e) | half(e + 1) << 16;
 #pragma unroll
-    for (int e = 0; e < kVector; ++e) {
-        x[e] = -INFINITY;
-        if (at + e < vocab) x[e] = F32 ? static_cast<const float*>(base)[row_at + at + e] : bf16_bits_to_float(static_cast<const uint16_t*>(base)[row_at + at + e]);
+            for (int n = 0; n + 1 < static_cast<int>(sizeof r.w / 4); ++n) r.w[n] = r.w[n + 1];
+            r.w[sizeof r.w / 4 - 1] = w;
+        }
+    }
+    const int hidden = at - (vocab - kVector);      // 1 .. 15
+#pragma unroll
+    for (int n = 0; n < static_cast<int>(sizeof r.w / 4); ++n) {
+        if constexpr (F32) r.w[n] = n < hidden ? 0xFF800000u : r.w[n];
+        else r.w[n] = (2 * n < hidden ? 0xFF80u : r.w[n] & 0xFFFFu) | (2 * n + 1 < hidden ? 0xFF800000u : r.w[n] & 0xFFFF0000u);
+    }
+    return r;
+}
+// The vector that begins at number `at`; `begin`: number of its first logit (some of those in front of `at` are hidden)
+template <bool F32>
+__device__ __forceinline__ Raw<F32> load_vector(const void* base, const int64_t row_at, const int at, const int vocab, int& begin) {
+    const bool whole = at + kVector <= vocab;
+    begin = whole ? at : vocab - kVector;
+    return whole ? load_raw<F32>(base, row_at + at) : load_last<F32>(base, row_at, at, vocab);
+}
+// each(four logits, number of the first one among the sixteen): for code that is short (a launch of little work waits for its instructions, too), which four logits
+// at a time keep as busy as sixteen.  NaN becomes -inf, inf the largest number.
+template <bool F32, int UNROLL = 1, class Each>
+__device__ __forceinline__ void by_four(Raw<F32> r, Each each) {
+#pragma unroll UNROLL
+    for (int e = 0; e < kVector; e += 4) {
+        float x[4];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) x[n] = plain_logit(logit_of<F32>(r, n));
+        each(x, e);
+#pragma unroll
+        for (int n = 0; n + (F32 ? 4 : 2) < static_cast<int>(sizeof r.w / 4); ++n) r.w[n] = r.w[n + (F32 ? 4 : 2)];
     }
 }
+// The largest of sixteen logits.  NaN is none; inf and NaN have been replaced where `odd` comes back.
 template <bool F32>
-__device__ __forceinline__ void load_logits(const void* base, const int64_t row_at, const int at, const int vocab, float (&x)[kVector]) {
-    if (at + kVector <= vocab) unpack<F32>(load_raw<F32>(base, row_at + at), x);
-    else load_last<F32>(base, row_at, at, vocab, x);
-}
-__device__ __forceinline__ float largest_of(float (&x)[kVector]) {
+__device__ __forceinline__ float largest_of(const Raw<F32>& r, bool& odd) {
     // (three at a time, which fmaxf, with its care for signalling NaN, is not compiled to: such a NaN becomes the result, and is seen to below)
     float top = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < kVector; e += 2) asm("v_max3_f32 %0, %0, %1, %2" : "+v"(top) : "v"(x[e]), "v"(x[e + 1]));
-    if (!(top < INFINITY)) {
+    for (int e = 0; e < kVector; e += 2) asm("v_max3_f32 %0, %0, %1, %2" : "+v"(top) : "v"(logit_of<F32>(r, e)), "v"(logit_of<F32>(r, e + 1)));
+    odd = !(top < INFINITY);
+    if (odd) {
         top = -INFINITY;
-#pragma unroll
-        for (int e = 0; e < kVector; ++e) {
-            x[e] = plain_logit(x[e]);
-            top = fmaxf(top, x[e]);
-        }
+        by_four<F32>(r, [&](const float (&x)[4], int) { top = fmaxf(fmaxf(top, fmaxf(x[0], x[1])), fmaxf(x[2], x[3])); });
     }
     return top;
 }
@@ -159,53 +188,61 @@ __device__ __forceinline__ Tree tree_of(const VerifyArgs& a, const int i) {
     return t;
 }
 
-// A piece of a row, all threads: elements [first, end).  A thread's reference is 0 unless weights would leave the range of 64 bits.
+// Sixteen logits, the first of them number `begin`, to what a thread has of a row.  Its reference is 0 unless weights would leave the range of 64 bits.  FAST: many of them
+template <bool F32, bool FAST>
+__device__ __forceinline__ void add_weights(RowPart& y, const Raw<F32>& r, const double per, const float octaves) {
+    constexpr float kFar = 500.f;
+    bool odd;
+    const float top = largest_of<F32>(r, odd);
+    if (top == -INFINITY) return;
+    if (y.top == -INFINITY) {
+        y.top = fabsf(top) * octaves <= kFar ? 0.f : top;
+    } else if ((top - y.top) * octaves > kFar) {
+        y.sum *= weight_of(y.top, top, per);
+        y.top = top;
+    }
+    double sums[2] = {};
+    if (FAST && __all(y.top == 0.f && !odd)) {      // (as nearly always: a subtraction less)
+#pragma unroll
+        for (int e = 0; e < kVector; ++e) sums[e % 2] += exp2_of(static_cast<double>(logit_of<F32>(r, e)) * per);
+    } else {
+        by_four<F32>(r, [&](const float (&x)[4], int) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sums[e % 2] += weight_of(x[e], y.top, per);
+        });
+    }
+    y.sum += sums[0] + sums[1];
+}
+template <bool F32>
+__device__ __forceinline__ void add_largest(RowPart& y, const Raw<F32>& r, const int begin) {
+    bool odd;
+    const float top = largest_of<F32>(r, odd);
+    if (!(top > y.top)) return;
+    y.top = top;
+    int place = kVector;
+    by_four<F32>(r, [&](const float (&x)[4], const int e) {
+#pragma unroll
+        for (int n = 3; n >= 0; --n) place = x[n] == top ? min(place, e + n) : place;
+    });
+    y.at = begin + place;
+}
+
+// A piece of a row, all threads: elements [first, end)
 template <bool F32, bool LARGEST>
 __device__ __forceinline__ RowPart part_of_row(const void* base, const int64_t row_at, const int first, const int end, const int vocab, const double per, WaveParts& lds) {
     RowPart y = kNoPart;
-    constexpr float kFar = 500.f;                   // octaves
     const float octaves = static_cast<float>(per);
-    const auto take = [&](float (&x)[kVector], const int at) {
-        const float top = largest_of(x);
-        if constexpr (LARGEST) {
-            if (!(top > y.top)) return;
-            y.top = top;
-            int place = kVector;
-#pragma unroll
-            for (int e = kVector - 1; e >= 0; --e) place = x[e] == top ? e : place;
-            y.at = at + place;
-        } else {
-            if (top == -INFINITY) return;
-            if (y.top == -INFINITY) {
-                y.top = fabsf(top) * octaves <= kFar ? 0.f : top;
-            } else if ((top - y.top) * octaves > kFar) {
-                y.sum *= weight_of(y.top, top, per);
-                y.top = top;
-            }
-            double sums[2] = {};
-            if (__all(y.top == 0.f)) {              // (as nearly always: a subtraction less)
-#pragma unroll
-                for (int e = 0; e < kVector; ++e) sums[e % 2] += exp2_of(static_cast<double>(x[e]) * per);
-            } else {
-#pragma unroll
-                for (int e = 0; e < kVector; ++e) sums[e % 2] += weight_of(x[e], y.top, per);
-            }
-            y.sum += sums[0] + sums[1];
-        }
-    };
     int at = first + static_cast<int>(threadIdx.x) * kVector;
     Raw<F32> ahead;
     if (at + kVector <= end) ahead = load_raw<F32>(base, row_at + at);
-    for (; at + kVector <= end; at += kStep) {
-        float x[kVector];
-        unpack<F32>(ahead, x);
-        if (at + kStep + kVector <= end) ahead = load_raw<F32>(base, row_at + at + kStep);
-        take(x, at);
-    }
-    if (at < end) {                                 // the end of a row
-        float x[kVector];
-        load_last<F32>(base, row_at, at, vocab, x);
-        take(x, at);
+#pragma unroll 1
+    for (; at < end; at += kStep) {
+        const bool whole = at + kVector <= end;
+        Raw<F32> r = ahead;
+        if (!whole) r = load_last<F32>(base, row_at, at, vocab);                   // (the end of a row: pieces are multiples of a vector)
+        else if (at + kStep + kVector <= end) ahead = load_raw<F32>(base, row_at + at + kStep);
+        if constexpr (LARGEST) add_largest<F32>(y, r, whole ? at : vocab - kVector);
+        else add_weights<F32, true>(y, r, per, octaves);
     }
     return of_all<LARGEST>(y, per, lds);
 }
@@ -223,7 +260,7 @@ __device__ __forceinline__ double sum_of_all(double x, double* lds) {
 
 // Sums of the rows of tokens with children: a workgroup for (piece, target or draft; token; request)
 template <bool F32>
-__global__ __launch_bounds__(kThreads) void verify_rows_kernel(VerifyArgs a) {
+__global__ __launch_bounds__(kThreads, F32 ? 5 : 6) void verify_rows_kernel(VerifyArgs a) {
     __shared__ WaveParts lds;
     const int of_draft = blockIdx.x >= static_cast<unsigned>(a.shape.pieces) ? 1 : 0, piece = blockIdx.x - of_draft * a.shape.pieces, token = blockIdx.y, i = blockIdx.z;
     const Tree t = tree_of(a, i);
@@ -249,6 +286,29 @@ struct LeftWeight {
     __device__ __forceinline__ double of(const float x, const float ref, const double share) const { return share * weight_of(x, ref, per); }
     __device__ __forceinline__ double operator()(const float x, const float y) const { return fmax(target(x) - c * draft(y), 0.0); }
 };
+
+// Sum of what is left of sixteen tokens, the first of them number `begin`
+template <bool F32, int UNROLL = 1>
+__device__ __forceinline__ double left_of(const Raw<F32>& p, Raw<F32> q, const bool of_two, const LeftWeight& w, const int begin, const int* list, const int removed) {
+    double sum = 0;
+    by_four<F32, UNROLL>(p, [&](const float (&x)[4], const int e) {
+        double v[4];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) v[n] = w.target(x[n]);
+        if (of_two) {
+#pragma unroll
+            for (int n = 0; n < 4; ++n) v[n] = fmax(v[n] - w.c * w.draft(plain_logit(logit_of<F32>(q, n))), 0.0);
+#pragma unroll
+            for (int n = 0; n + (F32 ? 4 : 2) < static_cast<int>(sizeof q.w / 4); ++n) q.w[n] = q.w[n + (F32 ? 4 : 2)];
+        }
+        for (int r = 0; r < removed; ++r)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) v[n] = list[r] == begin + e + n ? 0.0 : v[n];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) sum += v[n];
+    });
+    return sum;
+}
 
 // What a token with children decides: a workgroup for (token, request), every wave the same (a lane has a token)
 template <bool F32>
@@ -291,55 +351,41 @@ __global__ __launch_bounds__(kThreads) void verify_choice_kernel(VerifyArgs a) {
         w.c += Z;
         if (left == 0) break;                       // (what is left is summed up only for a sibling's sake)
         double sum = 0;
+#pragma unroll 1
         for (int at = static_cast<int>(threadIdx.x) * kVector; at < a.vocab; at += kStep) {
-            float vp[kVector], vq[kVector];
-            load_logits<F32>(a.target, row * a.target_stride, at, a.vocab, vp);
-            load_logits<F32>(a.draft, row * a.draft_stride, at, a.vocab, vq);
-            largest_of(vp);
-            largest_of(vq);
-#pragma unroll
-            for (int e = 0; e < kVector; ++e) sum += w(vp[e], vq[e]);
+            int begin;
+            const Raw<F32> vp = load_vector<F32>(a.target, row * a.target_stride, at, a.vocab, begin), vq = load_vector<F32>(a.draft, row * a.draft_stride, at, a.vocab, begin);
+            sum += left_of<F32, 4>(vp, vq, true, w, begin, nullptr, 0);
         }
         Z = sum_of_all(sum, lds);
     }
     if (threadIdx.x == 0) a.choices[row] = {choice, drawn && gone != 0 ? w.c : 0.0, w.of_target, w.of_draft, w.top, w.draft_top};
 }
 
-// Sums of pieces of the row that a request's next token is drawn from, and the draw: a workgroup for (piece, request), the last of a request to finish goes on
+__device__ __forceinline__ double sum_to_here(double x) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const double z = __shfl_up(x, o, 64);
+        x += lane >= o ? z : 0.0;
+    }
+    return x;
+}
+
+// The draw: sums of the row that a request's next token is drawn from, a wave for a span of it (up to 256 spans, of 1024 tokens where V is up to 2^18), a workgroup for some
+// of them; the last workgroup of a request to finish finds the span, one wave of it the vector in the span and the token in the vector.
 enum { kPlain, kResidual, kRemoved };               // weights: P; max(P - c Q, 0); P without the tokens that were refused
 struct LastCount {
     uint32_t* x;
     __device__ __forceinline__ uint32_t next(const uint32_t limit) const { return __builtin_amdgcn_atomic_inc32(x, limit, __ATOMIC_RELAXED, "agent"); }
 };
 template <bool F32>
-__device__ __forceinline__ void left_weights(const VerifyArgs& a, const int64_t row, const int kind, const LeftWeight& w, const int at, const int* list, const int removed, double (&v)[kVector]) {
-    float x[kVector], z[kVector];
-    load_logits<F32>(a.target, row * a.target_stride, at, a.vocab, x);
-    if (kind == kResidual) {
-        load_logits<F32>(a.draft, row * a.draft_stride, at, a.vocab, z);
-        largest_of(x);
-        largest_of(z);
-#pragma unroll
-        for (int e = 0; e < kVector; ++e) v[e] = w(x[e], z[e]);
-        return;
-    }
-    largest_of(x);
-#pragma unroll
-    for (int e = 0; e < kVector; ++e) v[e] = w.target(x[e]);
-    if (kind == kRemoved)
-        for (int r = 0; r < removed; ++r)
-#pragma unroll
-            for (int e = 0; e < kVector; ++e)
-                if (list[r] == at + e) v[e] = 0;
-}
-template <bool F32>
 __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
     __shared__ WaveParts lds;
-    __shared__ double sums[kThreads / 64];
+    __shared__ double wave_sums[kThreads / 64], begin_of_span;
     __shared__ int list[kMostDrafts];
-    __shared__ int last, found, last_positive, the_piece;
-    __shared__ double the_begin;
-    const int pieces = a.shape.last_pieces, piece = blockIdx.x, i = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ int last, over_span, positive_span;
+    const int i = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const Tree t = tree_of(a, i);
     const float warm = temperature_of(a, i);
     const bool greedy = warm == 0.f;
@@ -347,7 +393,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
     // the tokens that stay: from one choice to the next
     int at = 0, count = 1;
     uint64_t kept = 1;
-    const int chosen = lane < t.tokens ? a.choices[t.q0 + lane].token : -1, choice = t.inner >> lane & 1 ? chosen : -1;       // (asked for beside the masks)
+    const int chosen = lane < t.tokens && a.max_q > 1 ? a.choices[t.q0 + lane].token : -1, choice = t.inner >> lane & 1 ? chosen : -1;       // (asked for beside the masks)
     for (; count < a.max_keep; ++count) {
         const int next = __builtin_amdgcn_readlane(choice, at);
         if (next < 0) break;
@@ -355,7 +401,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
         kept |= uint64_t{1} << at;
     }
     if (t.tokens == 0) count = 0, kept = 0;
-    if (piece == 0 && wave == 0) {
+    if (blockIdx.x == 0 && wave == 0) {
         int32_t* keep = a.keep + static_cast<int64_t>(i) * a.max_keep;
         for (int k = count + lane; k < a.max_keep; k += 64) keep[k] = -1;
         if (kept >> lane & 1) keep[__popcll(kept & ((uint64_t{1} << lane) - 1))] = lane;
@@ -364,7 +410,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
     }
     if (t.tokens == 0) return;
     // what is left of the last one's row
-    const int64_t row = t.q0 + at;
+    const int64_t row = t.q0 + at, target_at = row * a.target_stride, draft_at = row * a.draft_stride;
     const bool judged = !greedy && (t.inner >> at & 1) && __builtin_amdgcn_readlane(choice, at) < 0;         // all of its children were refused
     LeftWeight w{per, 0.0, 1.0, 0.0, 0.f, 0.f};
     int kind = kPlain, removed = 0;
@@ -381,130 +427,122 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
         }
         w = {per, c.c, kind == kRemoved ? 1.0 : c.of_target, c.of_draft, c.top, c.draft_top};
     }
-    const int first = piece * a.shape.last_length, end = min(first + a.shape.last_length, a.vocab);
-    RowPart mine{0.0, 0.f, 0};
-    if (kind == kPlain) {
-        mine = greedy ? part_of_row<F32, true>(a.target, row * a.target_stride, first, end, a.vocab, per, lds)
-                      : part_of_row<F32, false>(a.target, row * a.target_stride, first, end, a.vocab, per, lds);
-    } else {
-        double sum = 0;
-        for (int n = first + tid * kVector; n < end; n += kStep) {
-            double v[kVector];
-            left_weights<F32>(a, row, kind, w, n, list, removed, v);
-#pragma unroll
-            for (int e = 0; e < kVector; ++e) sum += v[e];
+
+    const int spans = a.shape.spans, rounds = a.shape.span_rounds;                 // rounds: times 1024 tokens of a span
+    const auto first_of = [&](const int span, const int round) { return (span * rounds + round) * (64 * kVector) + lane * kVector; };
+    uint64_t* parts = reinterpret_cast<uint64_t*>(a.last_parts + static_cast<int64_t>(i) * spans);
+    RowPart mine, all;
+    for (int turn = 0;; ++turn) {
+        // (a second turn: nothing is left, and the last workgroup has all of P)
+        const int end = turn > 0 ? spans : min((static_cast<int>(blockIdx.x) + 1) * a.shape.group_spans, spans);
+        int span = (turn > 0 ? 0 : static_cast<int>(blockIdx.x) * a.shape.group_spans) + wave, round = 0, begin;
+        const bool of_two = kind == kResidual;
+        Raw<F32> p, q;
+        const auto ask = [&](const int n) {
+            if (n >= a.vocab) return;
+            p = load_vector<F32>(a.target, target_at, n, a.vocab, begin);
+            q = p;
+            if (of_two) q = load_vector<F32>(a.draft, draft_at, n, a.vocab, begin);
+        };
+        mine = kind == kPlain ? kNoPart : RowPart{0.0, 0.f, 0};
+        if (span < end) ask(first_of(span, 0));
+#pragma unroll 1
+        while (span < end) {
+            const int n = first_of(span, round), this_begin = begin;
+            const Raw<F32> r = p, s = q;
+            const bool ends = round + 1 == rounds;
+            const int next_span = ends ? span + kThreads / 64 : span, next_round = ends ? 0 : round + 1;
+            if (next_span < end) ask(first_of(next_span, next_round));
+            if (n < a.vocab) {
+                if (kind != kPlain) mine.sum += left_of<F32>(r, s, of_two, w, this_begin, list, removed);
+                else if (greedy) add_largest<F32>(mine, r, this_begin);
+                else add_weights<F32, false>(mine, r, per, static_cast<float>(per));
+            }
+            if (ends) {
+                const RowPart y = greedy ? of_wave<true>(mine, per) : of_wave<false>(mine, per);
+                if (lane == 0) {                    // (decode_body.hip.h on the order of such stores and the count)
+                    __hip_atomic_store(parts + 2 * span, static_cast<uint64_t>(__double_as_longlong(y.sum)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    __hip_atomic_store(parts + 2 * span + 1, static_cast<uint64_t>(__float_as_uint(y.top)) | static_cast<uint64_t>(static_cast<uint32_t>(y.at)) << 32,
+                                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                }
+                mine = kind == kPlain ? kNoPart : RowPart{0.0, 0.f, 0};
+            }
+            span = next_span; round = next_round;
         }
-        mine.sum = sum_of_all(sum, sums);
-    }
-    if (pieces > 1) {
-        // (decode_body.hip.h on the order of such stores and the count)
-        uint64_t* to = reinterpret_cast<uint64_t*>(a.last_parts + static_cast<int64_t>(i) * pieces);
-        if (tid == 0) {
-            __hip_atomic_store(to + 2 * piece, static_cast<uint64_t>(__double_as_longlong(mine.sum)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            __hip_atomic_store(to + 2 * piece + 1, static_cast<uint64_t>(__float_as_uint(mine.top)) | static_cast<uint64_t>(static_cast<uint32_t>(mine.at)) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            __builtin_amdgcn_s_waitcnt(0x0F70);    // vmcnt(0)
-            last = arrives_last(LastCount{a.arrived + i}, static_cast<uint32_t>(pieces));
-        }
+        __builtin_amdgcn_s_waitcnt(0x0F70);        // vmcnt(0)
         __syncthreads();
-        if (last == 0) return;
+        if (turn == 0 && gridDim.x > 1) {
+            if (tid == 0) last = arrives_last(LastCount{a.arrived + i}, gridDim.x);
+            __syncthreads();
+            if (last == 0) return;
+        }
         mine = kNoPart;
-        if (tid < pieces) {
-            mine.sum = __longlong_as_double(static_cast<long long>(__hip_atomic_load(to + 2 * tid, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)));
-            const uint64_t more = __hip_atomic_load(to + 2 * tid + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (tid < spans) {
+            mine.sum = __longlong_as_double(static_cast<long long>(__hip_atomic_load(parts + 2 * tid, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)));
+            const uint64_t more = __hip_atomic_load(parts + 2 * tid + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             mine.top = __uint_as_float(static_cast<uint32_t>(more));
             mine.at = static_cast<int>(more >> 32);
         }
-    } else if (tid > 0) {
-        mine = kNoPart;
+        all = greedy ? of_all<true>(mine, per, lds) : of_all<false>(mine, per, lds);
+        if (kind == kPlain || all.sum > 0) break;
+        kind = kPlain;
     }
-    // a thread has a piece: the whole row
-    RowPart all = greedy ? of_all<true>(mine, per, lds) : of_all<false>(mine, per, lds);
-    if (greedy || (kind == kPlain && all.top == -INFINITY)) {
+    if (greedy || all.top == -INFINITY) {
         if (tid == 0) a.next_token[i] = all.top == -INFINITY ? -1 : all.at;
         return;
     }
-    int from = 0, to = a.vocab;
-    double before = 0, goal = fmin(fmax(static_cast<double>(a.sample_u[i]), 0.0), 1.0);            // (NaN: 0)
-    if (kind != kPlain && !(all.sum > 0)) {
-        // nothing is left: from P, all of it anew
-        kind = kPlain;
-        all = part_of_row<F32, false>(a.target, row * a.target_stride, 0, a.vocab, a.vocab, per, lds);
-        w.of_target = 1.0; w.top = all.top;
-        if (all.top == -INFINITY) {
-            if (tid == 0) a.next_token[i] = -1;
-            return;
-        }
-        goal *= all.sum;
-    } else {
-        if (kind == kPlain) { w.top = all.top; w.of_target = 1.0; }
-        goal *= all.sum;
-        // the first piece whose cumulative sum is over the goal; the last one that has any weight where rounding leaves none
-        const double weight = mine.top == -INFINITY ? 0.0 : kind == kPlain && mine.top != all.top ? mine.sum * weight_of(mine.top, all.top, per) : mine.sum;
-        double upto = weight;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const double z = __shfl_up(upto, o, 64);
-            upto += lane >= o ? z : 0.0;
-        }
-        if (tid == 0) { found = 0x7FFFFFFF; last_positive = -1; }
+    if (kind == kPlain) { w.top = all.top; w.of_target = 1.0; }
+    const double goal = fmin(fmax(static_cast<double>(a.sample_u[i]), 0.0), 1.0) * all.sum;        // (NaN: 0)
+    // The first span with a cumulative sum over the goal; the last one with a weight where rounding leaves none.  The same then for vectors and tokens.
+    {
+        const double weight = mine.top == -INFINITY ? 0.0 : mine.top != all.top ? mine.sum * weight_of(mine.top, all.top, per) : mine.sum;
+        double upto = sum_to_here(weight);
+        if (lane == 63) wave_sums[wave] = upto;
+        if (tid == 0) { over_span = kThreads; positive_span = 0; }
         __syncthreads();
-        if (lane == 63) sums[wave] = upto;
+        for (int v = 0; v < wave; ++v) upto += wave_sums[v];
+        const uint64_t positive = __ballot(weight > 0), over = __ballot(weight > 0 && upto > goal);
+        if (lane == 0 && positive) atomicMax(&positive_span, wave * 64 + 63 - __builtin_clzll(positive));
+        if (lane == 0 && over) atomicMin(&over_span, wave * 64 + __builtin_ctzll(over));
         __syncthreads();
-        for (int v = 0; v < wave; ++v) upto += sums[v];
-        if (weight > 0) {
-            atomicMax(&last_positive, tid);
-            if (upto > goal) atomicMin(&found, tid);
-        }
+        if (tid == (over_span < kThreads ? over_span : positive_span)) begin_of_span = upto - weight;
         __syncthreads();
-        if (tid == (found != 0x7FFFFFFF ? found : last_positive)) { the_piece = tid; the_begin = upto - weight; }
-        __syncthreads();
-        from = the_piece * a.shape.last_length;
-        to = min(from + a.shape.last_length, a.vocab);
-        before = the_begin;
     }
-    __syncthreads();
-    if (tid == 0) { found = 0x7FFFFFFF; last_positive = -1; }
-    for (int n0 = from; n0 < to; n0 += kStep) {
-        const int n = n0 + tid * kVector;
-        double v[kVector], here = 0;
-        if (n < to) left_weights<F32>(a, row, kind, w, n, list, removed, v);
-#pragma unroll
-        for (int e = 0; e < kVector; ++e) {
-            if (n >= to) v[e] = 0;
-            here += v[e];
+    if (wave != 0) return;
+    bool over_goal = over_span < kThreads;
+    const int span = over_goal ? over_span : positive_span;
+    double before = begin_of_span;
+    int vector = -1;
+    bool found = false;
+#pragma unroll 1
+    for (int round = 0; round < rounds && !found; ++round) {
+        const int n = first_of(span, round);
+        double weight = 0;
+        if (n < a.vocab) {
+            int begin;
+            const Raw<F32> p = load_vector<F32>(a.target, target_at, n, a.vocab, begin);
+            Raw<F32> q = p;
+            if (kind == kResidual) q = load_vector<F32>(a.draft, draft_at, n, a.vocab, begin);
+            weight = left_of<F32>(p, q, kind == kResidual, w, begin, list, removed);
         }
-        double upto = here;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const double z = __shfl_up(upto, o, 64);
-            upto += lane >= o ? z : 0.0;
-        }
-        __syncthreads();
-        if (lane == 63) sums[wave] = upto;
-        __syncthreads();
-        double step = 0, in_front = before;
-#pragma unroll
-        for (int z = 0; z < kThreads / 64; ++z) {
-            in_front += z < wave ? sums[z] : 0.0;
-            step += sums[z];
-        }
-        double x = in_front + (upto - here);
-        int hit = 0x7FFFFFFF, positive = -1;
-#pragma unroll
-        for (int e = 0; e < kVector; ++e) {
-            x += v[e];
-            if (v[e] > 0) {
-                positive = n + e;
-                if (x > goal && hit == 0x7FFFFFFF) hit = n + e;
-            }
-        }
-        if (hit != 0x7FFFFFFF) atomicMin(&found, hit);
-        if (positive >= 0) atomicMax(&last_positive, positive);
-        before += step;
-        __syncthreads();
-        if (found != 0x7FFFFFFF) break;
+        const double upto = before + sum_to_here(weight);
+        const uint64_t positive = __ballot(weight > 0), over = __ballot(over_goal && weight > 0 && upto > goal);
+        const int of = over ? __builtin_ctzll(over) : positive ? 63 - __builtin_clzll(positive) : -1;
+        if (of >= 0) vector = __shfl(n, of, 64);
+        found = over != 0;
+        before = found ? __shfl(upto - weight, of, 64) : __shfl(upto, 63, 64);
     }
-    if (tid == 0) a.next_token[i] = found != 0x7FFFFFFF ? found : last_positive;
+    over_goal = over_goal && found;
+    const int n = vector + lane;
+    double weight = 0;
+    if (lane < kVector && vector >= 0 && n < a.vocab) {
+        weight = w.target(load_logit<F32>(a.target, target_at + n));
+        if (kind == kResidual) weight = fmax(weight - w.c * w.draft(load_logit<F32>(a.draft, draft_at + n)), 0.0);
+        for (int r = 0; r < removed; ++r) weight = list[r] == n ? 0.0 : weight;
+    }
+    const double upto = before + sum_to_here(weight);
+    const uint64_t positive = __ballot(weight > 0), over = __ballot(over_goal && weight > 0 && upto > goal);
+    if (lane == 0) a.next_token[i] = over ? vector + __builtin_ctzll(over) : positive ? vector + 63 - __builtin_clzll(positive) : -1;
 }
 
 template <bool F32>
@@ -515,25 +553,26 @@ int launch(const VerifyArgs& a, hipStream_t st) {
         hipLaunchKernelGGL((verify_rows_kernel<F32>), dim3(static_cast<unsigned>(a.shape.pieces * (a.draft ? 2 : 1)), tokens, n), block, 0, st, a);
         hipLaunchKernelGGL((verify_choice_kernel<F32>), dim3(tokens, n), block, 0, st, a);
     }
-    hipLaunchKernelGGL((verify_draw_kernel<F32>), dim3(static_cast<unsigned>(a.shape.last_pieces), n), block, 0, st, a);
+    hipLaunchKernelGGL((verify_draw_kernel<F32>), dim3(static_cast<unsigned>(a.shape.groups), n), block, 0, st, a);
     return static_cast<int>(hipGetLastError());
 }
 
 }  // namespace
 
 VerifyShape VerifyShape::of(const int64_t n, const int64_t total_q, const int32_t vocab) {
-    const auto cut = [&](const int64_t rows, const int64_t groups, const int64_t most, int& pieces, int& length) {
-        const int64_t steps = (static_cast<int64_t>(vocab) + kStep - 1) / kStep;
-        int64_t wanted = groups / (rows > 0 ? rows : 1) + 1;
-        wanted = wanted < most ? wanted : most;
-        wanted = wanted < steps ? wanted : steps;
-        const int64_t each = (steps + wanted - 1) / wanted;
-        length = static_cast<int>(each * kStep);
-        pieces = static_cast<int>((steps + each - 1) / each);
-    };
+    const auto up = [](const int64_t x, const int64_t by) { return (x + by - 1) / by; };
+    const auto least = [](const int64_t x, const int64_t y) { return x < y ? x : y; };
     VerifyShape s;
-    cut(total_q, 2048, 64, s.pieces, s.length);           // (a lane for each in verify_choice_kernel,
-    cut(n, 1024, kThreads, s.last_pieces, s.last_length); //  a thread for each in verify_draw_kernel)
+    // rows: workgroups for 2048 of them together, and no more than the lanes that put the pieces together
+    const int64_t steps = up(vocab, kStep), each = up(steps, least(least(2048 / (total_q > 0 ? total_q : 1) + 1, 64), steps));
+    s.length = static_cast<int>(each * kStep);
+    s.pieces = static_cast<int>(up(steps, each));
+    // the draw: spans for the threads of a workgroup, workgroups of 4 spans and more, 1024 of them together
+    const int64_t thousands = up(vocab, 64 * kVector);
+    s.span_rounds = static_cast<int>(up(thousands, kThreads));
+    s.spans = static_cast<int>(up(thousands, s.span_rounds));
+    s.group_spans = static_cast<int>(up(up(s.spans, least(1024 / (n > 0 ? n : 1) + 1, up(s.spans, 4))), 4) * 4);
+    s.groups = static_cast<int>(up(s.spans, s.group_spans));
     return s;
 }
 
