@@ -18,7 +18,7 @@ int launch_pages_select(const PagesSelectArgs& a, void* stream);
 // A workspace of the page calls: kWords arrays of num_blocks words.  Zero between calls: the first two.
 struct PagesWorkspace {
     static constexpr int kWords = 3;
-    static constexpr int kSegment = 4096;           // blocks that a workgroup looks at
+    static constexpr int kSegment = 1024;           // blocks that a workgroup looks at
     static size_t bytes(const int64_t num_blocks) { return static_cast<size_t>((kWords * num_blocks + num_blocks / kSegment + 1) * 4 + 255) / 256 * 256; }
 };
 
@@ -35,7 +35,7 @@ struct PagesCompactArgs {
     const int32_t* table; const int32_t* pages; int32_t n; int32_t max_blocks;
     const int32_t* refs; int32_t num_blocks; int32_t* new_table; int32_t* new_refs;
     int32_t* copy_src; int32_t* copy_dst; int32_t max_moves;
-    int32_t* to;                                    // [num_blocks] new number of every block
+    int32_t* to;                                    // [num_blocks] new number of every block; -1 - k: that of move k
     int32_t* used_of;                               // [segments] blocks in use
 };
 int launch_pages_compact(const PagesCompactArgs& a, void* stream);

@@ -40,6 +40,16 @@ __device__ __forceinline__ T sum_in_front(const T x, T* lds, T& all) {
 
 __device__ __forceinline__ bool is_block(const int b, const int num_blocks) { return b >= 0 && b < num_blocks; }
 
+// Counts of four blocks; `none` for those that the pool does not have
+__device__ __forceinline__ void load_refs(const int32_t* refs, const int64_t b, const int64_t num_blocks, const int none, int (&x)[4]) {
+    if (b + 4 <= num_blocks) {
+        __builtin_memcpy(x, refs + b, 16);          // (at any alignment)
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = b + e < num_blocks ? refs[b + e] : none;
+    }
+}
+
 // ------------------------------------------------------------------ a new batch out of rows of the old one
 // One wave for every new request, one for every old one.
 __global__ __launch_bounds__(256) void pages_select_kernel(PagesSelectArgs a) {
@@ -73,7 +83,7 @@ __global__ __launch_bounds__(256) void pages_select_kernel(PagesSelectArgs a) {
 // ------------------------------------------------------------------ pages for the next tokens
 // What a request asks for
 struct Wish {
-    int at, held, end, block;                       // page of its next token, pages it holds, pages it wants; block of that page
+    int at, held, end, block, holders;              // page of its next token, pages it holds, pages it wants; block of that page, how many hold it
     bool shared;                                    // that page holds tokens and is held by others too: it is not to be written
 };
 __device__ __forceinline__ Wish wish_of(const PagesReserveArgs& a, const int i) {
@@ -85,72 +95,124 @@ __device__ __forceinline__ Wish wish_of(const PagesReserveArgs& a, const int i) 
     w.held = min(max(a.pages[i], 0), a.max_blocks);
     w.end = grow > 0 ? max(w.held, static_cast<int>(min((len + grow + a.page - 1) / a.page, static_cast<int64_t>(a.max_blocks)))) : w.held;
     w.block = -1;
+    w.holders = 0;
     w.shared = false;
     if (grow > 0 && len % a.page > 0 && w.at < w.held) {
         w.block = a.table[static_cast<int64_t>(i) * a.max_blocks + w.at];
-        w.shared = is_block(w.block, a.num_blocks) && a.refs[w.block] > 1;
+        w.holders = is_block(w.block, a.num_blocks) ? a.refs[w.block] : 0;
+        w.shared = w.holders > 1;
     }
     return w;
 }
 __device__ __forceinline__ int device_load(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-enum { kServed = 1, kCopies = 2, kWrites = 4 };     // left in served[i] between the two launches; copy_dst[i]: its first free block's number among those handed out
+enum { kServed = 1, kCopies = 2, kWrites = 4 };     // left in served[i] between two launches; copy_dst[i]: its first free block's number among those handed out
 
-// One workgroup: who gets what.  (Requests are 4 to 12 bytes, blocks 4: the whole state of a batch is a few hundred KiB.)
+// One workgroup: who gets what.  (Requests are 4 to 12 bytes, blocks 4: the whole state of a batch is a few hundred KiB, and what takes time is the chain of loads, 12 to 20 us
+// when what is known of a request was read in each of the three passes over them.)  HERE: the requests fit its threads, and it writes their entries too: a thread for each block
+// that is handed out, which finds its request among the prefix sums.
 constexpr int kPlanThreads = 1024;
+template <bool HERE>
 __global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(PagesReserveArgs a) {
     __shared__ int64_t lds[kPlanThreads / 64];
+    __shared__ int begins[HERE ? kPlanThreads : 1];
+    __shared__ int2 rows[HERE ? kPlanThreads : 1];  // page that the first block goes to (negative: -1 - the page that is copied), page of the others less their number
     const int tid = threadIdx.x;
+    // four times four blocks of a thread, those of all threads side by side; counts of the four in 16 bits each
+    constexpr int GROUPS = 4, OF_GROUP = 4 * kPlanThreads;
+    int refs[GROUPS][4];
+    const auto ask = [&](const int64_t b0) {
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) load_refs(a.refs, b0 + g * OF_GROUP + 4 * tid, a.num_blocks, 1, refs[g]);
+    };
+    ask(0);                                         // (beside the requests)
+    Wish kept{};                                    // of request tid
     for (int i = tid; i < a.n; i += kPlanThreads) {
         const Wish w = wish_of(a, i);
+        if (i == tid) kept = w;
         if (!w.shared) continue;
         atomicMax(a.last_writer + w.block, i + 1);
         atomicAdd(a.writers + w.block, 1);
     }
-    __threadfence();
+    __builtin_amdgcn_s_waitcnt(0x0F70);            // vmcnt(0): the sums are in the L2, where they are read
     __syncthreads();
-    // the blocks that are wanted
+    const auto wish = [&](const int i) { return i == tid ? kept : wish_of(a, i); };
     const auto needs = [&](const int i, const Wish& w, bool& keeps) {
         // of as many writers as there are holders the last one keeps the page
-        keeps = w.shared && device_load(a.writers + w.block) == a.refs[w.block] && device_load(a.last_writer + w.block) == i + 1;
+        keeps = w.shared && device_load(a.writers + w.block) == w.holders && device_load(a.last_writer + w.block) == i + 1;
         return static_cast<int64_t>(w.end - w.held + (w.shared && !keeps ? 1 : 0));
     };
-    int64_t wanted = 0;
+    // the blocks that are wanted
+    int64_t wanted = 0, begin = 0, need = 0;
+    bool keeps = false;
     for (int i0 = 0; i0 < a.n; i0 += kPlanThreads) {
         const int i = i0 + tid;
-        bool keeps;
-        int64_t need = 0, all;
-        if (i < a.n) { const Wish w = wish_of(a, i); need = needs(i, w, keeps); }
-        sum_in_front<kPlanThreads>(need, lds, all);
+        int64_t all;
+        need = 0;
+        keeps = false;
+        if (i < a.n) need = needs(i, wish(i), keeps);
+        begin = sum_in_front<kPlanThreads>(need, lds, all);
         wanted += all;
-        if (wanted >= a.num_blocks) { wanted = a.num_blocks; break; }
     }
     // as many free ones, by rising number
-    constexpr int EACH = 16;
     int64_t found = 0;
-    for (int64_t b0 = 0; b0 < a.num_blocks && found < wanted; b0 += kPlanThreads * EACH) {
-        int refs[EACH];
+    for (int64_t b0 = 0; b0 < a.num_blocks && found < wanted; b0 += GROUPS * OF_GROUP) {
+        if (b0 > 0) ask(b0);
         int64_t mine = 0, all;
-        const int64_t b = b0 + tid * EACH;
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) refs[e] = b + e < a.num_blocks ? a.refs[b + e] : 1;
+        for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) mine += refs[e] == 0 ? 1 : 0;
-        int64_t at = found + sum_in_front<kPlanThreads>(mine, lds, all);
+            for (int e = 0; e < 4; ++e) mine += static_cast<int64_t>(refs[g][e] == 0) << 16 * g;
+        const int64_t front = sum_in_front<kPlanThreads>(mine, lds, all);
 #pragma unroll
-        for (int e = 0; e < EACH; ++e)
-            if (refs[e] == 0 && at < a.num_blocks) a.free[at++] = static_cast<int32_t>(b + e);
-        found += all;
+        for (int g = 0; g < GROUPS; ++g) {
+            int64_t at = found + (front >> 16 * g & 0xFFFF);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (refs[g][e] == 0 && at < a.num_blocks) a.free[at++] = static_cast<int32_t>(b0 + g * OF_GROUP + 4 * tid + e);
+            found += all >> 16 * g & 0xFFFF;
+        }
+    }
+    if constexpr (HERE) {
+        const int i = tid;
+        const bool there = i < a.n, served = there && (begin + need <= found || (need == 0 && !keeps)), copies = served && kept.shared && !keeps;
+        // (where blocks run out, requests that are not served want none, and no later one is)
+        begins[tid] = static_cast<int>(begin < found ? begin : found);
+        rows[tid] = {copies ? -1 - kept.at : kept.held, kept.held - (copies ? 1 : 0)};
+        int64_t handed = served ? need : 0, all;
+        sum_in_front<kPlanThreads>(handed, lds, all);
+        if (there) {
+            a.served[i] = served ? 1 : 0;
+            a.copy_src[i] = copies ? kept.block : -1;
+            if (!copies) a.copy_dst[i] = -1;
+            if (served) a.pages[i] = kept.end;
+            if (copies) atomicAdd(a.refs + kept.block, -1);
+            if (kept.shared) { a.last_writer[kept.block] = 0; a.writers[kept.block] = 0; }
+        }
+        __builtin_amdgcn_s_waitcnt(0x0F70);        // (the free blocks: of this workgroup, through the L2)
+        __syncthreads();
+        for (int64_t k = tid; k < all; k += kPlanThreads) {
+            int r = 0;                              // the last request that begins at k or in front of it (those behind it with no blocks begin there too, and are none of k's)
+            for (int step = kPlanThreads / 2; step > 0; step >>= 1) r += r + step < a.n && begins[r + step] <= k ? step : 0;
+            const int b = device_load(a.free + k), number = static_cast<int>(k) - begins[r];
+            const int2 at = rows[r];
+            const bool copy = number == 0 && at.x < 0;
+            a.table[static_cast<int64_t>(r) * a.max_blocks + (copy ? -1 - at.x : at.y + number)] = b;
+            a.refs[b] = 1;
+            if (copy) a.copy_dst[r] = b;
+        }
+        return;
     }
     // in the order of requests
     int64_t before = 0;
     for (int i0 = 0; i0 < a.n; i0 += kPlanThreads) {
         const int i = i0 + tid;
-        bool keeps = false;
-        int64_t need = 0, all;
+        int64_t all;
+        need = 0;
+        keeps = false;
         Wish w{};
-        if (i < a.n) { w = wish_of(a, i); need = needs(i, w, keeps); }
-        const int64_t begin = before + sum_in_front<kPlanThreads>(need, lds, all);
+        if (i < a.n) { w = wish(i); need = needs(i, w, keeps); }
+        begin = before + sum_in_front<kPlanThreads>(need, lds, all);
         if (i < a.n) {
             const bool served = begin + need <= found || (need == 0 && !keeps);
             a.served[i] = (served ? kServed : 0) | (w.shared && !keeps ? kCopies : 0) | (w.shared ? kWrites : 0);
@@ -193,6 +255,7 @@ __global__ __launch_bounds__(256) void pages_apply_kernel(PagesReserveArgs a) {
 
 // ------------------------------------------------------------------ compaction
 constexpr int kSegment = PagesWorkspace::kSegment, kOfThread = kSegment / 256;
+static_assert(kOfThread == 4, "load_refs");
 
 __device__ __forceinline__ int used_in_segment(const int32_t* refs, const int64_t first, const int64_t end, int* lds) {
     int mine = 0, all;
@@ -228,45 +291,40 @@ __global__ __launch_bounds__(256) void pages_move_kernel(PagesCompactArgs a) {
         a.copy_src[k] = -1;
         a.copy_dst[k] = -1;
     }
-    // The lists, block by block.  A block's new number and count are written by whoever moves there: a source's partner is not known here, so
-    // the new numbers of sources, and the counts of both, are set by pages_place_kernel, from the lists.
+    // The lists, block by block.  A block that moves does not know yet where to: its number in the list stands for the new number.
     const int64_t first = static_cast<int64_t>(mine) * kSegment + tid * kOfThread;
     int refs[kOfThread], count = 0, all;
+    load_refs(a.refs, first, a.num_blocks, 0, refs);
 #pragma unroll
-    for (int e = 0; e < kOfThread; ++e) {
-        refs[e] = first + e < a.num_blocks ? a.refs[first + e] : 0;
-        count += refs[e] > 0 ? 1 : 0;
-    }
+    for (int e = 0; e < kOfThread; ++e) count += refs[e] > 0 ? 1 : 0;
     int before = front + sum_in_front<256>(count, lds, all);       // blocks in use in front of this one
 #pragma unroll
     for (int e = 0; e < kOfThread; ++e) {
         const int64_t b = first + e;
         if (b >= a.num_blocks) break;
         const bool in_use = refs[e] > 0;
-        if (b >= used && in_use && before - low < moves) a.copy_src[before - low] = static_cast<int32_t>(b);
+        const bool goes = b >= used && in_use && before - low < moves;
+        if (goes) a.copy_src[before - low] = static_cast<int32_t>(b);
         if (b < used && !in_use && b - before < moves) a.copy_dst[b - before] = static_cast<int32_t>(b);
-        a.to[b] = static_cast<int32_t>(b);
-        a.new_refs[b] = refs[e];
+        a.to[b] = goes ? -1 - (before - low) : static_cast<int32_t>(b);
+        a.new_refs[b] = goes ? 0 : refs[e];
         before += in_use ? 1 : 0;
     }
 }
-__global__ __launch_bounds__(256) void pages_place_kernel(PagesCompactArgs a) {
-    const int64_t k = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (k >= a.max_moves) return;
-    const int src = a.copy_src[k], dst = a.copy_dst[k];
-    if (src < 0) return;
-    a.to[src] = dst;
-    a.new_refs[dst] = a.refs[src];
-    a.new_refs[src] = 0;
-}
+// A wave for the entries of a request, or for the counts of 64 blocks that moved
 __global__ __launch_bounds__(256) void pages_rename_kernel(PagesCompactArgs a) {
-    const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (i >= a.n) return;
-    const int pages = min(max(a.pages[i], 0), a.max_blocks);
-    const int64_t row = static_cast<int64_t>(i) * a.max_blocks;
+    const int lane = threadIdx.x & 63;
+    const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (unit >= a.n) {
+        const int64_t k = (unit - a.n) * kWave + lane;
+        if (k < a.max_moves && a.copy_src[k] >= 0) a.new_refs[a.copy_dst[k]] = a.refs[a.copy_src[k]];
+        return;
+    }
+    const int pages = min(max(a.pages[unit], 0), a.max_blocks);
+    const int64_t row = unit * a.max_blocks;
     for (int j = lane; j < pages; j += kWave) {
-        const int b = a.table[row + j];
-        a.new_table[row + j] = is_block(b, a.num_blocks) ? a.to[b] : b;
+        const int b = a.table[row + j], to = is_block(b, a.num_blocks) ? a.to[b] : b;
+        a.new_table[row + j] = is_block(b, a.num_blocks) && to < 0 ? a.copy_dst[-1 - to] : to;
     }
 }
 
@@ -311,7 +369,11 @@ int launch_pages_select(const PagesSelectArgs& a, void* stream) {
 
 int launch_pages_reserve(const PagesReserveArgs& a, void* stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(pages_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a);
+    if (a.n <= kPlanThreads) {
+        hipLaunchKernelGGL((pages_plan_kernel<true>), dim3(1), dim3(kPlanThreads), 0, st, a);
+        return static_cast<int>(hipGetLastError());
+    }
+    hipLaunchKernelGGL((pages_plan_kernel<false>), dim3(1), dim3(kPlanThreads), 0, st, a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return static_cast<int>(e);
     hipLaunchKernelGGL(pages_apply_kernel, dim3(groups_of(a.n, 4)), dim3(256), 0, st, a);
     return static_cast<int>(hipGetLastError());
@@ -322,8 +384,8 @@ int launch_pages_compact(const PagesCompactArgs& a, void* stream) {
     const unsigned segments = groups_of(a.num_blocks, kSegment);
     hipLaunchKernelGGL(pages_count_kernel, dim3(segments), dim3(256), 0, st, a);
     hipLaunchKernelGGL(pages_move_kernel, dim3(segments), dim3(256), 0, st, a);
-    if (a.max_moves > 0) hipLaunchKernelGGL(pages_place_kernel, dim3(groups_of(a.max_moves, 256)), dim3(256), 0, st, a);
-    if (a.n > 0) hipLaunchKernelGGL(pages_rename_kernel, dim3(groups_of(a.n, 4)), dim3(256), 0, st, a);
+    const int64_t waves = a.n + (static_cast<int64_t>(a.max_moves) + kWave - 1) / kWave;
+    if (waves > 0) hipLaunchKernelGGL(pages_rename_kernel, dim3(groups_of(waves, 4)), dim3(256), 0, st, a);
     return static_cast<int>(hipGetLastError());
 }
 
