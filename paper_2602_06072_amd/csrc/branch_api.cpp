@@ -201,6 +201,7 @@ extern "C" int pk_shared_tree_attn(const pk_cache* cache, const void* q, const i
         s.first_of = s.shared_of + n;
         s.len_of = s.first_of + n;
         s.q_start_of = s.len_of + n;
+        s.places = s.q_start_of + n + 1;
         a.part_o = reinterpret_cast<float*>(at + w.own);
         a.part_lse = a.part_o + w.own_slots * cache->Hkv * shape.rows * cache->d;
         s.family_o = reinterpret_cast<float*>(at + w.family);

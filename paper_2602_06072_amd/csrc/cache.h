@@ -94,6 +94,7 @@ struct TreeArgs {
     FastDiv by_r, by_subs;
     // where requests share pages: tokens that a request shares with its family (a multiple of 64; [n]), and a family's first request ([families])
     const int32_t* shared_of; const int32_t* first_of;
+    const int32_t* places;                          // instead of `items`, for shared keys
 };
 int launch_tree_attn(TreeArgs a, const TreeShape& s, void* stream);
 

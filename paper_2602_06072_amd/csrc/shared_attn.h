@@ -10,6 +10,7 @@ struct SharedArgs {
     uint32_t* arrived; int32_t* missing;            // zero between calls: workgroups that are done; [families] 1 + the keys of a table that a family does not share, 0: it has no rows
     int32_t* family_of; int32_t* shared_of;         // [n]
     int32_t* first_of; int32_t* q_start_of; int32_t* len_of;       // [families (+ 1)]: first request, rows of q, shared tokens
+    int32_t* places; int few_rows;                  // [1] workgroups of a KV head that the shared keys are cut for; set by the launch: up to 32 rows a request
     int2* pieces_of_family; float* family_lse; float* family_o;    // partial results of the shared keys
 };
 int launch_shared_tree_attn(SharedArgs s, const TreeShape& shape, void* stream);
@@ -29,7 +30,7 @@ struct SharedWorkspace {
         w.counts = 256 + kMostFamilies * 4;
         w.plain = w.counts + TreeShape::count_bytes(Hkv, compute_units);
         w.arrays = w.plain;
-        w.own = w.arrays + whole256(4 * (5 * n + 8) + 16 * n);
+        w.own = w.arrays + whole256(4 * (5 * n + 16) + 16 * n);
         w.family = w.own + whole256(w.own_slots * Hkv * s.rows * row);
         const size_t here = w.family + whole256(w.family_slots * Hkv * 128 * row);
         const size_t there = w.plain + s.partial_bytes(Hkv, d, compute_units) + TreeShape::pieces_bytes(n);

@@ -91,7 +91,7 @@ __global__ __launch_bounds__(256) void shared_find_kernel(SharedArgs s) {
         carried = max(max(max(lds[0], lds[1]), max(lds[2], lds[3])), carried);
         const int q0 = prefix_max(g <= s.families ? static_cast<int>(min(static_cast<int64_t>(a.q_start[first]), a.total_q)) : 0, carried_q);
         carried_q = max(max(max(lds[0], lds[1]), max(lds[2], lds[3])), carried_q);
-        if (g <= s.families) s.q_start_of[g] = q0;
+        if (g <= s.families) store_there(s.q_start_of + g, q0);
         if (g < s.families) {
             const int missing = load_there(s.missing + g);
             s.first_of[g] = min(first, a.n - 1);
@@ -101,10 +101,44 @@ __global__ __launch_bounds__(256) void shared_find_kernel(SharedArgs s) {
     }
     __builtin_amdgcn_s_waitcnt(0x0F70);
     __syncthreads();
+    float own = 0.f, shared = 0.f;                  // tiles of 64 keys, for every 128 rows of the shared ones
     for (int r = tid; r < a.n; r += 256) {
-        const int g = load_there(s.family_of + r);
-        s.shared_of[r] = g < 0 ? 0 : load_there(s.len_of + g);
+        const int g = load_there(s.family_of + r), of_family = g < 0 ? 0 : load_there(s.len_of + g), len = min(max(a.kv_lens[r], 0), a.most_keys);
+        s.shared_of[r] = of_family;
+        own += static_cast<float>(len - min(of_family, len)) / kSharedTile;
     }
+    for (int g = tid; g < s.families; g += 256) {
+        const int rows = (load_there(s.q_start_of + g + 1) - load_there(s.q_start_of + g)) * a.heads_per_kv;
+        shared += static_cast<float>(load_there(s.len_of + g) / kSharedTile) * static_cast<float>((rows + kWideRows - 1) / kWideRows);
+    }
+    const auto sum = [&](const float x) {
+        const float y = last_lane(wave_prefix(x));
+        __syncthreads();
+        if (lane == 0) lds[wave] = __float_as_int(y);
+        __syncthreads();
+        return __int_as_float(lds[0]) + __int_as_float(lds[1]) + __int_as_float(lds[2]) + __int_as_float(lds[3]);
+    };
+    own = sum(own);
+    shared = sum(shared);
+    // Where there is much to be done for own keys, by workgroups that wait for memory, the shared ones are cut for half of the workgroups that run at once: both kinds
+    // are on every unit then, and there are half as many partial results to be put together.
+    if (tid == 0) *s.places = s.few_rows && own > 0.7f * shared ? max(a.items / 2, 1) : a.items;
+}
+
+// Shared keys and own ones in one launch, the shared ones, which take longer, first.  (A unit of the one kind and one of the other in turns: 429 us instead of 313 for
+// families of drafted trees.)
+struct BothArgs { TreeArgs own, shared; int own_units, shared_units; };
+template <int D, bool F8, int ROW_BLOCKS>
+__global__ __launch_bounds__(64 * kWaves, 2) void shared_both_kernel(BothArgs b) {
+    __shared__ __align__(16) unsigned char lds[kWideBytes<D>];
+    __shared__ int last;
+    const int Hkv = b.own.cache.Hkv, unit = b.own.by_hkv(blockIdx.x), head = static_cast<int>(blockIdx.x) - unit * Hkv;
+    const bool of_shared = unit < b.shared_units;
+    const int number = (of_shared ? unit : unit - b.shared_units) * Hkv + head;
+    if (of_shared) many_rows<D, F8, kShared, 1>(lds, last, number, b.shared_units * Hkv);
+    else if constexpr (ROW_BLOCKS == 1) few_rows<D, F8, 1, kSubTiles1<D, F8>, false, kOwn, 0>(lds, last, number, b.own_units * Hkv);
+    else if constexpr (ROW_BLOCKS == 2) few_rows<D, F8, 2, kSubTiles2<D, F8>, false, kOwn, 0>(lds, last, number, b.own_units * Hkv);
+    else many_rows<D, F8, kOwn, 0>(lds, last, number, b.own_units * Hkv);
 }
 
 // Puts the parts together: a workgroup for (request, chunk of its rows, slice of that, KV head).  KV heads go round-robin over the XCDs, as they do in the launches that
@@ -145,31 +179,38 @@ template <int D, bool F8>
 int launch(SharedArgs s, const TreeShape& shape, hipStream_t st) {
     TreeArgs& a = s.tree;
     const dim3 block(64 * kWaves);
+    s.few_rows = shape.rows <= 32;
     hipLaunchKernelGGL(shared_find_kernel, dim3(static_cast<unsigned>((a.n + 3) / 4)), dim3(256), 0, st, s);
 
     TreeArgs f = a;                                 // families as requests
     f.q_start = s.q_start_of; f.kv_lens = s.len_of; f.first_of = s.first_of; f.n = s.families;
-    f.max_q = static_cast<int32_t>(a.total_q); f.mask = nullptr;
+    f.max_q = static_cast<int32_t>(a.total_q); f.mask = nullptr; f.places = s.places;
     f.chunk_shift = 7;
     f.rounds = 5 / 4.f;
     f.least_per_share = 64.f / kLeastKeys; f.least_per_many = f.least_per_share / 4;
     f.pieces_of = s.pieces_of_family; f.part_o = s.family_o; f.part_lse = s.family_lse;
     const int64_t family_loads = a.total_q * a.heads_per_kv / kWideRows + s.families;
-    const int64_t family_groups = (family_loads <= a.items / 2 ? a.items : family_loads + a.items / 2) * a.cache.Hkv;
-    if (family_groups > 0x7FFFFFFF) return static_cast<int>(hipErrorInvalidConfiguration);
-    hipLaunchKernelGGL((tree_attn_wide_kernel<D, F8, kShared>), dim3(static_cast<unsigned>(family_groups)), block, 0, st, f);
-
     const int row_blocks = shape.rows / 16, keys = 16 * (row_blocks == 1 ? kSubTiles1<D, F8> : row_blocks == 2 ? kSubTiles2<D, F8> : 4);
     a.least_per_share = static_cast<float>(keys) / kLeastKeys;
     a.least_per_many = a.least_per_share / (shape.rows == 128 ? 4 : 1);
     a.shared_of = s.shared_of;
     const int64_t loads = static_cast<int64_t>(a.n) * a.chunks;
-    const int64_t groups = (loads <= a.items / 2 ? a.items : loads + a.items / 2) * a.cache.Hkv;
-    if (groups > 0x7FFFFFFF) return static_cast<int>(hipErrorInvalidConfiguration);
-    const dim3 grid(static_cast<unsigned>(groups));
-    if (row_blocks == 1) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 1, kSubTiles1<D, F8>, 2, false, kOwn>), grid, block, 0, st, a);
-    else if (row_blocks == 2) hipLaunchKernelGGL((tree_attn_kernel<D, F8, 2, kSubTiles2<D, F8>, kWavesOf2<D, F8>, false, kOwn>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((tree_attn_wide_kernel<D, F8, kOwn>), grid, block, 0, st, a);
+    const auto units_of = [&](const int64_t loads) { return loads <= a.items / 2 ? static_cast<int64_t>(a.items) : loads + a.items / 2; };
+    const int64_t own_units = units_of(loads), shared_units = units_of(family_loads);
+    if ((own_units + shared_units) * a.cache.Hkv > 0x7FFFFFFF) return static_cast<int>(hipErrorInvalidConfiguration);
+    const auto workgroups = [&](const int64_t units) { return dim3(static_cast<unsigned>(units * a.cache.Hkv)); };
+    const BothArgs both{a, f, static_cast<int>(own_units), static_cast<int>(shared_units)};
+    const dim3 grid = workgroups(own_units + shared_units);
+    if (row_blocks == 1) {
+        hipLaunchKernelGGL((shared_both_kernel<D, F8, 1>), grid, block, 0, st, both);
+    } else if (row_blocks > 2) {
+        hipLaunchKernelGGL((shared_both_kernel<D, F8, 3>), grid, block, 0, st, both);
+    } else if constexpr (kWavesOf2<D, F8> == 2) {
+        hipLaunchKernelGGL((shared_both_kernel<D, F8, 2>), grid, block, 0, st, both);
+    } else {                                        // (32 rows of 128 columns in bf16 have twice the registers to a wave)
+        hipLaunchKernelGGL((tree_attn_wide_kernel<D, F8, kShared>), workgroups(shared_units), block, 0, st, f);
+        hipLaunchKernelGGL((tree_attn_kernel<D, F8, 2, kSubTiles2<D, F8>, kWavesOf2<D, F8>, false, kOwn>), workgroups(own_units), block, 0, st, a);
+    }
 
     // the merge: up to 2048 workgroups, of 8 rows and more each
     const int64_t merges = loads * a.cache.Hkv, slices = 2048 / (merges < 2048 ? merges : 2048);

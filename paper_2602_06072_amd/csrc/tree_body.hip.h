@@ -125,7 +125,8 @@ __device__ __forceinline__ Shares share_of(const TreeArgs& a, const Loads<KEPT, 
     });
     tiles = fmaxf(last_lane(wave_prefix(tiles)), 1.f);
     loads = last_lane(wave_prefix(loads));
-    const float least = a.least_per_share, places = static_cast<float>(a.items), taken = static_cast<float>(loads);
+    const int at_once = KEYS == kShared ? *a.places : a.items;
+    const float least = a.least_per_share, places = static_cast<float>(at_once), taken = static_cast<float>(loads);
     Shares s{0.f, -1, 0};
     const bool one_round = taken <= 0.75f * places;
     // the two shares to be looked at, or how many pieces are long and half as long
@@ -141,7 +142,7 @@ __device__ __forceinline__ Shares share_of(const TreeArgs& a, const Loads<KEPT, 
     first = last_lane(wave_prefix(first));
     second = last_lane(wave_prefix(second));
     if (one_round) {
-        if (first > a.items) s.per_share = second <= a.items ? more : min(least, (places - taken) / tiles);
+        if (first > at_once) s.per_share = second <= at_once ? more : min(least, (places - taken) / tiles);
     } else {
         s.middle = first;
         s.last = first + second;
@@ -180,25 +181,28 @@ __device__ __forceinline__ bool find_piece(const TreeArgs& a, const Loads<KEPT, 
 
 // The kernel's arguments, to be read anew: kept in registers over the loop of pieces they would leave too few scalar ones for the loop of tiles inside (trees of 64
 // requests 674 -> 756 us)
+// AT: which of several (a launch with the arguments of two kinds of work, each with workgroups of its own).
+template <int AT = 0>
 __device__ __forceinline__ const TreeArgs& kernel_args() {
-    auto p = (const __attribute__((address_space(4))) TreeArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+    auto p = (const __attribute__((address_space(4))) TreeArgs*)__builtin_amdgcn_kernarg_segment_ptr() + AT;
     asm volatile("" : "+s"(p));
     return *(const TreeArgs*)p;
 }
 
 // Runs `work(arguments, piece, KV head)` for the workgroup's pieces: the one of its number and, where there are more pieces than workgroups, those as many numbers on.
 // Workgroups go round-robin over the XCDs: with eight KV heads an XCD keeps to one, and the chunks of its rows find its keys in the L2.
-template <int TOKENS, int KEPT, Keys KEYS, class Work>
-__device__ __forceinline__ void run_pieces(Work work) {
-    if (const TreeArgs& a = kernel_args(); KEYS == kAll && a.whole) {              // no request can have two pieces
+// (`first`, `step`: the workgroup's first number and the distance to the next one)
+template <int TOKENS, int KEPT, Keys KEYS, int AT = 0, class Work>
+__device__ __forceinline__ void run_pieces(Work work, const int first, const int step) {
+    if (const TreeArgs& a = kernel_args<AT>(); KEYS == kAll && a.whole) {              // no request can have two pieces
         const int rest = a.by_hkv(blockIdx.x), i = a.by_chunks(rest);
         work(a, Piece{i, 0, 1, rest - i * a.chunks, 0, a.chunks}, static_cast<int>(blockIdx.x) - rest * a.cache.Hkv);
         return;
     }
-    const Loads<KEPT, KEYS> loads = read_loads<TOKENS, KEPT, KEYS>(kernel_args());
-    const Shares shares = share_of<TOKENS>(kernel_args(), loads);
-    for (int item = blockIdx.x;; item += gridDim.x) {
-        const TreeArgs& a = kernel_args();
+    const Loads<KEPT, KEYS> loads = read_loads<TOKENS, KEPT, KEYS>(kernel_args<AT>());
+    const Shares shares = share_of<TOKENS>(kernel_args<AT>(), loads);
+    for (int item = first;; item += step) {
+        const TreeArgs& a = kernel_args<AT>();
         Piece w;
         const int rest = a.by_hkv(item), kvh = item - rest * a.cache.Hkv;
         if (!find_piece<TOKENS>(a, loads, rest, shares, w)) return;
@@ -603,13 +607,10 @@ __device__ __forceinline__ void finish(const TreeArgs& a, const Piece& w, const 
 // Up to 16 NB rows: bound by memory, in short launches by latency (four single tokens behind 300 .. 3000 tokens 11 us: the pieces found 2 to 3, first tile 1 to 3,
 // tiles 2, last one 2, results and merge 2 to 4).  The four waves of a workgroup take tiles of N sub-tiles in turns, SETS tiles in flight in each, from memory into
 // registers and from there into the products.  ALONE: every wave has a request (and rows) of its own, all of whose tiles it takes.
-template <int D, bool F8, int NB, int N, int WAVES_PER_SIMD, bool ALONE = false, Keys KEYS = kAll>
-__global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(TreeArgs) {
+template <int D, bool F8, int NB, int N, bool ALONE, Keys KEYS, int AT>
+__device__ __forceinline__ void few_rows(unsigned char* lds, int& last, const int first, const int step_of_items) {
     using Regs = TileRegs<D, F8, N>;
     constexpr int SETS = 2, CH = Regs::CH, TOKENS = 16 * N, KS = D / 32, VT = D / 16, SIZE = F8 ? 1 : 2, STRIDE = ALONE ? 1 : kWaves;
-    __shared__ __align__(16) unsigned char lds[kJoinBytes<D>];
-    __shared__ int last;
-
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6)), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const auto work = [&](const TreeArgs& a, const Piece& w, const int kvh) {
         const Bounds bounds = bounds_of<TOKENS, KEYS>(a, w);
@@ -743,8 +744,14 @@ __global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(
         const int item = blockIdx.x * kWaves + wave, rest = a.by_hkv(item), i = a.by_chunks(rest);
         if (i < a.n) work(a, Piece{i, 0, 1, rest - i * a.chunks, 0, a.chunks}, item - rest * a.cache.Hkv);
     } else {
-        run_pieces<TOKENS, 4, KEYS>(work);
+        run_pieces<TOKENS, 4, KEYS, AT>(work, first, step_of_items);
     }
+}
+template <int D, bool F8, int NB, int N, int WAVES_PER_SIMD, bool ALONE = false, Keys KEYS = kAll>
+__global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(TreeArgs) {
+    __shared__ __align__(16) unsigned char lds[kJoinBytes<D>];
+    __shared__ int last;
+    few_rows<D, F8, NB, N, ALONE, KEYS, 0>(lds, last, blockIdx.x, gridDim.x);
 }
 
 // More rows, 128 in a workgroup: bound by the matrix pipe and what surrounds it (for 32 keys and 32 rows 34 MFMAs of 16 cycles, 16 exponentials of 16, some 60 other
@@ -753,14 +760,14 @@ __global__ __launch_bounds__(64 * kWaves, WAVES_PER_SIMD) void tree_attn_kernel(
 // quarter each, as bf16 operands (the conversion is done once, not by every wave), two tiles at a time; every wave reads it for its 32 rows.  With 64 rows
 // and fewer two waves share 32 rows, half of a tile's keys each.
 constexpr int kWideRows = 128;
-template <int D, bool F8, Keys KEYS = kAll>
-__global__ __launch_bounds__(64 * kWaves, D == 64 && F8 ? 3 : 2) void tree_attn_wide_kernel(TreeArgs) {
+template <int D> constexpr int kWideStage = 2 * 4 * (D / 32) * 1024;           // K and V of 64 keys as operands
+template <int D> constexpr int kWideBytes = 2 * kWideStage<D> > kJoinBytes<D> ? 2 * kWideStage<D> : kJoinBytes<D>;
+template <int D, bool F8, Keys KEYS, int AT>
+__device__ __forceinline__ void many_rows(unsigned char* lds, int& last, const int first_item, const int step_of_items) {
     constexpr int NB = 2, N = 4, TOKENS = 64, KS = D / 32, VT = D / 16, CH = F8 ? D / 64 : D / 32, SIZE = F8 ? 1 : 2;
-    constexpr int K_BYTES = N * KS * 1024, STAGE = 2 * K_BYTES;
-    __shared__ __align__(16) unsigned char lds[2 * STAGE > kJoinBytes<D> ? 2 * STAGE : kJoinBytes<D>];
-    __shared__ int last;
+    constexpr int K_BYTES = N * KS * 1024, STAGE = kWideStage<D>;
 
-    run_pieces<TOKENS, 2, KEYS>([&](const TreeArgs& a, const Piece& w, const int kvh) {
+    run_pieces<TOKENS, 2, KEYS, AT>([&](const TreeArgs& a, const Piece& w, const int kvh) {
         const Bounds bounds = bounds_of<TOKENS, KEYS>(a, w);
         if (bounds.rows_here <= 0) return;
         const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6)), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
@@ -916,7 +923,13 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 && F8 ? 3 : 2) void tree_attn_
             }
         }
         finish<D, F8, NB, false, false, KEYS>(a, w, bounds, kvh, kWaves / sharers, sharers, y, lds, &last);
-    });
+    }, first_item, step_of_items);
+}
+template <int D, bool F8, Keys KEYS = kAll>
+__global__ __launch_bounds__(64 * kWaves, D == 64 && F8 ? 3 : 2) void tree_attn_wide_kernel(TreeArgs) {
+    __shared__ __align__(16) unsigned char lds[kWideBytes<D>];
+    __shared__ int last;
+    many_rows<D, F8, KEYS, 0>(lds, last, blockIdx.x, gridDim.x);
 }
 
 // sub-tiles in a tile: two tiles in flight, and with the accumulators of 16 or 32 rows within 256 registers (512 for 32 rows and d = 128 in bf16)
