@@ -18,9 +18,10 @@ def dev(x):
     return torch.from_numpy(np.ascontiguousarray(x)).to(DEV)
 
 
-def make(seed, families, Hq, Hkv, d, page, cache, front=(), back=(), hostile=True):
+def make(seed, families, Hq, Hkv, d, page, cache, front=(), back=(), hostile=True, roomy=True):
     """families: [(prefix, [(own tokens, drafted tokens), ...]), ...]; front, back: requests that are in none.  The whole pages of a prefix are
-    shared; places where no token of a request is hold NaN."""
+    shared; places where no token of a request is hold NaN.  roomy: a block table with room for 300 MB of keys and values, as shared pages are
+    looked for from 256 MB on; below, every request is taken alone."""
     g, rng = gen(seed), np.random.default_rng(seed)
     requests = [(0, o, t) for o, t in front] + [(p, o, t) for p, m in families for o, t in m] + [(0, o, t) for o, t in back]
     start = np.concatenate([[0], np.cumsum([len(m) for _, m in families])]).astype(np.int32) + len(front)
@@ -34,6 +35,9 @@ def make(seed, families, Hq, Hkv, d, page, cache, front=(), back=(), hostile=Tru
         for i in range(at + 1, at + len(m)):
             host[i, :p // page] = host[at, :p // page]
         at += len(m)
+    if roomy:
+        columns = int(300e6 / (len(lens) * page * 2 * Hkv * (d + 1 if cache == pk.PK_F8 else 2 * d))) + 1
+        host = np.concatenate([host, rng.integers(-(1 << 30), 1 << 30, (len(lens), max(0, columns - host.shape[1])), dtype=np.int32)], 1)
     slots = [host[i, np.arange(x) // page].astype(np.int64) * page + np.arange(x) % page for i, x in enumerate(lens)]
     if hostile:
         used = np.zeros(blocks * page, bool)
@@ -84,6 +88,15 @@ def test_shared_attention(Hq, Hkv, d, batch, kind, cache, page):
         s = make(batch + Hq, b["families"], Hq // Hkv, 1, d, page, cache, b.get("front", ()), b.get("back", ()))           # (the oracle's time)
     mask = masks(s, kind)
     check(s, mask, call(s, mask, torch.float32 if kind == "bits" else torch.bfloat16))
+
+
+def test_tables_of_little_room():
+    for batch in BATCHES[:3]:
+        s = make(11, batch["families"], 8, 2, 128, 16, pk.PK_F8, batch.get("front", ()), batch.get("back", ()), roomy=False)
+        mask = masks(s, "tree")
+        got = call(s, mask, torch.float32)
+        check(s, mask, got)
+        assert torch.equal(got, as_alone(s, mask))
 
 
 def as_alone(s, mask, out_dtype=torch.float32):
@@ -156,7 +169,7 @@ def test_numbers_that_are_not_finite_in_shared_and_in_hidden_places():
 
 
 def test_tables_without_numbers_behind_the_pages_and_lengths_beyond_the_table():
-    s = make(5, [(320, [(20, 1), (50, 1)])], 8, 2, 128, 16, pk.PK_F8)
+    s = make(5, [(320, [(20, 1), (50, 1)] * 210)], 8, 8, 128, 16, pk.PK_F8, hostile=False, roomy=False)
     cut = s["table"][:, :22].contiguous()                          # 352 tokens
     lens = [min(x, 352) for x in s["lens"]]
     s["table"] = cut
@@ -227,9 +240,10 @@ def test_places_behind_four_gib():
     c = pk.new_kv_cache(blocks, page, Hkv, d, pk.PK_BF16)
     rng = np.random.default_rng(9)
     lens, prefix = [700, 645, 900], 640
-    table = np.zeros((3, 15), np.int32)
+    table = np.zeros((3, 500), np.int32)
     table[:, :10] = blocks - 10 + np.arange(10)
-    table[:, 10:] = blocks - 40 + np.arange(15).reshape(3, 5)
+    table[:, 10:15] = blocks - 40 + np.arange(15).reshape(3, 5)
+    table[:, 15:] = blocks - 1
     g = gen(9)
     used = torch.from_numpy(np.unique(table)).long().to(DEV)
     slots = (used[:, None] * page + torch.arange(page, device=DEV)).reshape(-1)
