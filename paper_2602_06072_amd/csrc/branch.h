@@ -60,12 +60,12 @@ struct VerifyChoice {
 // for `groups` workgroups, group_spans for each
 struct VerifyShape {
     int pieces, length;                             // length in elements, a multiple of kStep
-    int spans, span_rounds, groups, group_spans;
+    int spans, span_rounds, groups, group_spans, last_stride;
     static constexpr int kStep = 4096;              // elements that a workgroup takes at a time
     static constexpr size_t kCountBytes = 65536 * 4;               // arrivals of a request's pieces, zero between calls: in front of everything, as many for every call
     static VerifyShape of(int64_t n, int64_t total_q, int32_t vocab);
     size_t part_bytes(const int64_t total_q) const { return whole256(total_q * 2 * pieces * static_cast<int64_t>(sizeof(RowPart))); }
-    size_t last_bytes(const int64_t n) const { return whole256(n * spans * static_cast<int64_t>(sizeof(RowPart))); }
+    size_t last_bytes(const int64_t n) const { return whole256(n * last_stride * static_cast<int64_t>(sizeof(RowPart))); }
     static size_t choice_bytes(const int64_t total_q) { return whole256(total_q * static_cast<int64_t>(sizeof(VerifyChoice))); }
     size_t bytes(const int64_t n, const int64_t total_q) const { return kCountBytes + part_bytes(total_q) + last_bytes(n) + choice_bytes(total_q); }
 
@@ -81,7 +81,7 @@ struct VerifyArgs {
     VerifyShape shape;
     uint32_t* arrived;                              // [n], zero between calls
     RowPart* parts;                                 // [total_q][2][pieces]: of the target's rows, of the draft's
-    RowPart* last_parts;                            // [n][spans]
+    RowPart* last_parts;                            // [n][last_stride]
     VerifyChoice* choices;                          // [total_q]
 };
 int launch_draft_verify(const VerifyArgs& a, void* stream);

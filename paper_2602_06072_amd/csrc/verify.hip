@@ -8,6 +8,10 @@
 // Three launches.  Sums of the rows of tokens with children, target and draft (V logits each, in pieces); the choices of these tokens; then, of every request, the row that the
 // next token is drawn from, in pieces again, the last of which to finish finds the place.  One token a request: the last launch alone.
 //
+// Where a choice takes no sums of what is left (one child each, or no draft), the first sums have terms of 32 bits, which are near enough for nearly every choice (kCoarse), and
+// what the draw needs in 64 bits, the sums of one row of each request, is found in a launch in front of it (chains of 64 requests, 640 rows of 128256 logits: 73 us in
+// 64 bits, and 97 for the call).
+//
 // Probabilities and their sums have 64 bits: a draw is the place of a number between V borders, and with sums of 32 bits every tenth draw of a flat row of 100000
 // would fall on the other side of one.  Vector instructions of 64 bits run at the rate of those of 32 here; a weight takes about 20 of them, 80 cycles for 64 logits, and
 // at 2 10^12 logits a second that, not memory (3 10^12 of bf16), bounds the launches over rows.
@@ -188,8 +192,12 @@ __device__ __forceinline__ Tree tree_of(const VerifyArgs& a, const int i) {
     return t;
 }
 
-// Sixteen logits, the first of them number `begin`, to what a thread has of a row.  Its reference is 0 unless weights would leave the range of 64 bits.  FAST: many of them
-template <bool F32, bool FAST>
+// Sixteen logits, the first of them number `begin`, to what a thread has of a row.  Its reference is 0 unless weights would leave the range of 64 bits.  kFast: many of them.
+// kCoarse: terms of 32 bits where none is over 2^60 or, of the largest, under 2^-60.  With exponents y of two: y has two roundings of 2^-24 (of the factor and the product), which
+// are 60 ln 2 2^-23 = 5e-6 of a term; the exponential has 2^-23, sums of sixteen 16 2^-24: together 6.1e-6 of the sum.  (Terms further below weigh nothing.)
+enum Sums64 { kExact, kFast, kCoarse };
+constexpr double kCoarseError = 6.1e-6;
+template <bool F32, Sums64 HOW>
 __device__ __forceinline__ void add_weights(RowPart& y, const Raw<F32>& r, const double per, const float octaves) {
     constexpr float kFar = 500.f;
     bool odd;
@@ -201,8 +209,18 @@ __device__ __forceinline__ void add_weights(RowPart& y, const Raw<F32>& r, const
         y.sum *= weight_of(y.top, top, per);
         y.top = top;
     }
+    if (HOW == kCoarse && __all(y.top == 0.f && !odd && fabsf(top) * octaves <= 60.f)) {
+        float coarse[2] = {};
+#pragma unroll
+        for (int e = 0; e < kVector; ++e) coarse[e % 2] += __builtin_amdgcn_exp2f(logit_of<F32>(r, e) * octaves);
+        const float sum = coarse[0] + coarse[1];
+        if (sum == sum) {                           // (no NaN among them)
+            y.sum += static_cast<double>(sum);
+            return;
+        }
+    }
     double sums[2] = {};
-    if (FAST && __all(y.top == 0.f && !odd)) {      // (as nearly always: a subtraction less)
+    if (HOW == kFast && __all(y.top == 0.f && !odd)) {             // (as nearly always: a subtraction less)
 #pragma unroll
         for (int e = 0; e < kVector; ++e) sums[e % 2] += exp2_of(static_cast<double>(logit_of<F32>(r, e)) * per);
     } else {
@@ -228,7 +246,7 @@ __device__ __forceinline__ void add_largest(RowPart& y, const Raw<F32>& r, const
 }
 
 // A piece of a row, all threads: elements [first, end)
-template <bool F32, bool LARGEST>
+template <bool F32, bool LARGEST, Sums64 HOW = kFast>
 __device__ __forceinline__ RowPart part_of_row(const void* base, const int64_t row_at, const int first, const int end, const int vocab, const double per, WaveParts& lds) {
     RowPart y = kNoPart;
     const float octaves = static_cast<float>(per);
@@ -242,7 +260,7 @@ __device__ __forceinline__ RowPart part_of_row(const void* base, const int64_t r
         if (!whole) r = load_last<F32>(base, row_at, at, vocab);                   // (the end of a row: pieces are multiples of a vector)
         else if (at + kStep + kVector <= end) ahead = load_raw<F32>(base, row_at + at + kStep);
         if constexpr (LARGEST) add_largest<F32>(y, r, whole ? at : vocab - kVector);
-        else add_weights<F32, true>(y, r, per, octaves);
+        else add_weights<F32, HOW>(y, r, per, octaves);
     }
     return of_all<LARGEST>(y, per, lds);
 }
@@ -259,7 +277,7 @@ __device__ __forceinline__ double sum_of_all(double x, double* lds) {
 }
 
 // Sums of the rows of tokens with children: a workgroup for (piece, target or draft; token; request)
-template <bool F32>
+template <bool F32, Sums64 HOW>
 __global__ __launch_bounds__(kThreads, F32 ? 5 : 6) void verify_rows_kernel(VerifyArgs a) {
     __shared__ WaveParts lds;
     const int of_draft = blockIdx.x >= static_cast<unsigned>(a.shape.pieces) ? 1 : 0, piece = blockIdx.x - of_draft * a.shape.pieces, token = blockIdx.y, i = blockIdx.z;
@@ -270,7 +288,7 @@ __global__ __launch_bounds__(kThreads, F32 ? 5 : 6) void verify_rows_kernel(Veri
     const int64_t row = t.q0 + token;
     const int first = piece * a.shape.length, end = min(first + a.shape.length, a.vocab);
     const RowPart y = warm == 0.f ? part_of_row<F32, true>(a.target, row * a.target_stride, first, end, a.vocab, 0.0, lds)
-                                  : part_of_row<F32, false>(of_draft ? a.draft : a.target, row * (of_draft ? a.draft_stride : a.target_stride), first, end, a.vocab, kLog2e64 / warm, lds);
+                                  : part_of_row<F32, false, HOW>(of_draft ? a.draft : a.target, row * (of_draft ? a.draft_stride : a.target_stride), first, end, a.vocab, kLog2e64 / warm, lds);
     if (threadIdx.x == 0) {
         RowPart& to = a.parts[(row * 2 + of_draft) * a.shape.pieces + piece];
         to.sum = y.sum; to.top = y.top; to.at = y.at;
@@ -311,9 +329,10 @@ __device__ __forceinline__ double left_of(const Raw<F32>& p, Raw<F32> q, const b
 }
 
 // What a token with children decides: a workgroup for (token, request), every wave the same (a lane has a token)
-template <bool F32>
+template <bool F32, Sums64 HOW>
 __global__ __launch_bounds__(kThreads) void verify_choice_kernel(VerifyArgs a) {
     __shared__ double lds[kThreads / 64];
+    __shared__ WaveParts parts_lds;
     const int token = blockIdx.x, i = blockIdx.y, lane = threadIdx.x & 63;
     const Tree t = tree_of(a, i);
     if (!(t.inner >> token & 1)) return;
@@ -333,23 +352,41 @@ __global__ __launch_bounds__(kThreads) void verify_choice_kernel(VerifyArgs a) {
     if (there && drawn) q = a.parts[(row * 2 + 1) * a.shape.pieces + lane];
     p = greedy ? of_wave<true>(p, per) : of_wave<false>(p, per);
     q = of_wave<false>(q, per);
-    LeftWeight w{per, 0.0, p.sum > 0 ? 1 / p.sum : 0.0, q.sum > 0 ? 1 / q.sum : 0.0, p.top, q.top};
-    const double mine_p = able ? w.target(xp) : 0.0, mine_q = able && drawn ? w.draft(xq) : 0.0;
-    uint64_t left = __ballot(able), gone = 0;       // children to be looked at; those that were refused
+    LeftWeight w{per};
+    double mine_p = 0, mine_q = 0, Z = 1;
+    uint64_t left = 0, gone = 0;                    // children to be looked at; those that were refused
     int choice = -1;
-    double Z = 1;
+    bool exact = HOW != kCoarse;
+    const auto begin_with = [&] {
+        w = {per, 0.0, p.sum > 0 ? 1 / p.sum : 0.0, q.sum > 0 ? 1 / q.sum : 0.0, p.top, q.top};
+        mine_p = able ? w.target(xp) : 0.0;
+        mine_q = able && drawn ? w.draft(xq) : 0.0;
+        left = __ballot(able);
+        gone = 0;
+        Z = 1;
+    };
+    begin_with();
     while (left != 0) {
         const int s = __builtin_ctzll(left);
         left &= left - 1;
         const int of = __builtin_amdgcn_readlane(x, s);
         const double px = __shfl(mine_p, s, 64), qx = __shfl(mine_q, s, 64), us = __shfl(u, s, 64);
         const bool before = __ballot((gone >> lane & 1) && x == of) != 0;          // (the same token again)
-        if (greedy ? p.top > -INFINITY && p.at == of : drawn ? px > (w.c + us * Z) * qx : !before && px > us * Z) { choice = s; break; }
+        const double least = drawn ? (w.c + us * Z) * qx : us * Z;
+        // Sums of 32 bits that do not decide it: of P(x) and of Q(x), or of what has left P, each is off by kCoarseError at most.  The row anew, in 64 bits.
+        if (!exact && !greedy && fabs(px - least) <= 4 * kCoarseError * (px + (drawn ? least : us))) {
+            p = part_of_row<F32, false>(a.target, row * a.target_stride, 0, a.vocab, a.vocab, per, parts_lds);
+            if (drawn) q = part_of_row<F32, false>(a.draft, row * a.draft_stride, 0, a.vocab, a.vocab, per, parts_lds);
+            exact = true;
+            begin_with();
+            continue;
+        }
+        if (greedy ? p.top > -INFINITY && p.at == of : drawn ? px > least : !before && px > least) { choice = s; break; }
         if (greedy) continue;
         gone |= uint64_t{1} << s;
         if (!drawn) { Z -= before ? 0.0 : px; continue; }
         w.c += Z;
-        if (left == 0) break;                       // (what is left is summed up only for a sibling's sake)
+        if (HOW == kCoarse || left == 0) break;     // (what is left is summed up only for a sibling's sake)
         double sum = 0;
 #pragma unroll 1
         for (int at = static_cast<int>(threadIdx.x) * kVector; at < a.vocab; at += kStep) {
@@ -372,13 +409,79 @@ __device__ __forceinline__ double sum_to_here(double x) {
     return x;
 }
 
-// The draw: sums of the row that a request's next token is drawn from, a wave for a span of it (up to 256 spans, of 1024 tokens where V is up to 2^18), a workgroup for some
-// of them; the last workgroup of a request to finish finds the span, one wave of it the vector in the span and the token in the vector.
-enum { kPlain, kResidual, kRemoved };               // weights: P; max(P - c Q, 0); P without the tokens that were refused
+// The tokens that stay: from one choice to the next
+struct Walk { int at, count; uint64_t kept; };      // the last one, how many, which
+__device__ __forceinline__ Walk walk_of(const VerifyArgs& a, const Tree& t) {
+    const int lane = threadIdx.x & 63;
+    const int chosen = lane < t.tokens && a.max_q > 1 ? a.choices[t.q0 + lane].token : -1;         // (asked for beside the masks)
+    const int choice = t.inner >> lane & 1 ? chosen : -1;
+    Walk w{0, 1, 1};
+    for (; w.count < a.max_keep; ++w.count) {
+        const int next = __builtin_amdgcn_readlane(choice, w.at);
+        if (next < 0) break;
+        w.at = next;
+        w.kept |= uint64_t{1} << next;
+    }
+    if (t.tokens == 0) { w.count = 0; w.kept = 0; }
+    return w;
+}
+
 struct LastCount {
     uint32_t* x;
     __device__ __forceinline__ uint32_t next(const uint32_t limit) const { return __builtin_amdgcn_atomic_inc32(x, limit, __ATOMIC_RELAXED, "agent"); }
 };
+// Parts of a row for another workgroup of the launch (decode_body.hip.h on the order of such stores and the count)
+__device__ __forceinline__ void store_part(uint64_t* to, const RowPart& y) {
+    __hip_atomic_store(to, static_cast<uint64_t>(__double_as_longlong(y.sum)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(to + 1, static_cast<uint64_t>(__float_as_uint(y.top)) | static_cast<uint64_t>(static_cast<uint32_t>(y.at)) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ RowPart load_part(const uint64_t* from) {
+    const uint64_t sum = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), more = __hip_atomic_load(from + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return {__longlong_as_double(static_cast<long long>(sum)), __uint_as_float(static_cast<uint32_t>(more)), static_cast<int>(more >> 32)};
+}
+
+// In 64 bits, the sums of the rows that are drawn from as max(P - c Q, 0), where the choices had them in 32: workgroups as for the draw
+template <bool F32>
+__global__ __launch_bounds__(kThreads) void verify_sums_kernel(VerifyArgs a) {
+    __shared__ WaveParts lds;
+    __shared__ int last;
+    const int i = blockIdx.y, tid = threadIdx.x;
+    const Tree t = tree_of(a, i);
+    const float warm = temperature_of(a, i);
+    const Walk k = walk_of(a, t);
+    if (t.tokens == 0 || warm == 0.f || k.count >= a.max_keep || !(t.inner >> k.at & 1)) return;
+    const int64_t row = t.q0 + k.at;
+    if (!(a.choices[row].c > 0)) return;
+    const double per = kLog2e64 / warm;
+    const int length = a.shape.group_spans * a.shape.span_rounds * 64 * kVector, first = blockIdx.x * length, end = min(first + length, a.vocab);
+    RowPart p = part_of_row<F32, false>(a.target, row * a.target_stride, first, end, a.vocab, per, lds);
+    RowPart q = part_of_row<F32, false>(a.draft, row * a.draft_stride, first, end, a.vocab, per, lds);
+    if (gridDim.x > 1) {
+        uint64_t* parts = reinterpret_cast<uint64_t*>(a.last_parts + static_cast<int64_t>(i) * a.shape.last_stride);
+        if (tid == 0) {
+            store_part(parts + 4 * blockIdx.x, p);
+            store_part(parts + 4 * blockIdx.x + 2, q);
+            __builtin_amdgcn_s_waitcnt(0x0F70);    // vmcnt(0)
+            last = arrives_last(LastCount{a.arrived + i}, gridDim.x);
+        }
+        __syncthreads();
+        if (last == 0) return;
+        const bool there = tid < static_cast<int>(gridDim.x);
+        p = there ? load_part(parts + 4 * tid) : kNoPart;
+        q = there ? load_part(parts + 4 * tid + 2) : kNoPart;
+        p = of_all<false>(p, per, lds);
+        q = of_all<false>(q, per, lds);
+    }
+    if (tid == 0) {
+        VerifyChoice& c = a.choices[row];
+        c.of_target = p.sum > 0 ? 1 / p.sum : 0.0; c.top = p.top;
+        c.of_draft = q.sum > 0 ? 1 / q.sum : 0.0; c.draft_top = q.top;
+    }
+}
+
+// The draw: sums of the row that a request's next token is drawn from, a wave for a span of it (up to 256 spans, of 1024 tokens where V is up to 2^18), a workgroup for some
+// of them; the last workgroup of a request to finish finds the span, one wave of it the vector in the span and the token in the vector.
+enum { kPlain, kResidual, kRemoved };               // weights: P; max(P - c Q, 0); P without the tokens that were refused
 template <bool F32>
 __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
     __shared__ WaveParts lds;
@@ -390,17 +493,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
     const float warm = temperature_of(a, i);
     const bool greedy = warm == 0.f;
     const double per = greedy ? 0.0 : kLog2e64 / warm;
-    // the tokens that stay: from one choice to the next
-    int at = 0, count = 1;
-    uint64_t kept = 1;
-    const int chosen = lane < t.tokens && a.max_q > 1 ? a.choices[t.q0 + lane].token : -1, choice = t.inner >> lane & 1 ? chosen : -1;       // (asked for beside the masks)
-    for (; count < a.max_keep; ++count) {
-        const int next = __builtin_amdgcn_readlane(choice, at);
-        if (next < 0) break;
-        at = next;
-        kept |= uint64_t{1} << at;
-    }
-    if (t.tokens == 0) count = 0, kept = 0;
+    const auto [at, count, kept] = walk_of(a, t);
     if (blockIdx.x == 0 && wave == 0) {
         int32_t* keep = a.keep + static_cast<int64_t>(i) * a.max_keep;
         for (int k = count + lane; k < a.max_keep; k += 64) keep[k] = -1;
@@ -411,7 +504,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
     if (t.tokens == 0) return;
     // what is left of the last one's row
     const int64_t row = t.q0 + at, target_at = row * a.target_stride, draft_at = row * a.draft_stride;
-    const bool judged = !greedy && (t.inner >> at & 1) && __builtin_amdgcn_readlane(choice, at) < 0;         // all of its children were refused
+    const bool judged = !greedy && count < a.max_keep && (t.inner >> at & 1);      // (and none of its children has stayed)
     LeftWeight w{per, 0.0, 1.0, 0.0, 0.f, 0.f};
     int kind = kPlain, removed = 0;
     if (judged) {
@@ -430,7 +523,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
 
     const int spans = a.shape.spans, rounds = a.shape.span_rounds;                 // rounds: times 1024 tokens of a span
     const auto first_of = [&](const int span, const int round) { return (span * rounds + round) * (64 * kVector) + lane * kVector; };
-    uint64_t* parts = reinterpret_cast<uint64_t*>(a.last_parts + static_cast<int64_t>(i) * spans);
+    uint64_t* parts = reinterpret_cast<uint64_t*>(a.last_parts + static_cast<int64_t>(i) * a.shape.last_stride);
     RowPart mine, all;
     for (int turn = 0;; ++turn) {
         // (a second turn: nothing is left, and the last workgroup has all of P)
@@ -456,15 +549,11 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
             if (n < a.vocab) {
                 if (kind != kPlain) mine.sum += left_of<F32>(r, s, of_two, w, this_begin, list, removed);
                 else if (greedy) add_largest<F32>(mine, r, this_begin);
-                else add_weights<F32, false>(mine, r, per, static_cast<float>(per));
+                else add_weights<F32, kExact>(mine, r, per, static_cast<float>(per));
             }
             if (ends) {
                 const RowPart y = greedy ? of_wave<true>(mine, per) : of_wave<false>(mine, per);
-                if (lane == 0) {                    // (decode_body.hip.h on the order of such stores and the count)
-                    __hip_atomic_store(parts + 2 * span, static_cast<uint64_t>(__double_as_longlong(y.sum)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                    __hip_atomic_store(parts + 2 * span + 1, static_cast<uint64_t>(__float_as_uint(y.top)) | static_cast<uint64_t>(static_cast<uint32_t>(y.at)) << 32,
-                                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                }
+                if (lane == 0) store_part(parts + 2 * span, y);
                 mine = kind == kPlain ? kNoPart : RowPart{0.0, 0.f, 0};
             }
             span = next_span; round = next_round;
@@ -477,12 +566,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
             if (last == 0) return;
         }
         mine = kNoPart;
-        if (tid < spans) {
-            mine.sum = __longlong_as_double(static_cast<long long>(__hip_atomic_load(parts + 2 * tid, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)));
-            const uint64_t more = __hip_atomic_load(parts + 2 * tid + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            mine.top = __uint_as_float(static_cast<uint32_t>(more));
-            mine.at = static_cast<int>(more >> 32);
-        }
+        if (tid < spans) mine = load_part(parts + 2 * tid);
         all = greedy ? of_all<true>(mine, per, lds) : of_all<false>(mine, per, lds);
         if (kind == kPlain || all.sum > 0) break;
         kind = kPlain;
@@ -545,13 +629,22 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
     if (lane == 0) a.next_token[i] = over ? vector + __builtin_ctzll(over) : positive ? vector + 63 - __builtin_clzll(positive) : -1;
 }
 
+constexpr int64_t kCoarseLogits = int64_t{1} << 23;
 template <bool F32>
 int launch(const VerifyArgs& a, hipStream_t st) {
     const dim3 block(kThreads);
     const unsigned n = static_cast<unsigned>(a.n), tokens = static_cast<unsigned>(a.max_q);
     if (a.max_q > 1) {
-        hipLaunchKernelGGL((verify_rows_kernel<F32>), dim3(static_cast<unsigned>(a.shape.pieces * (a.draft ? 2 : 1)), tokens, n), block, 0, st, a);
-        hipLaunchKernelGGL((verify_choice_kernel<F32>), dim3(tokens, n), block, 0, st, a);
+        const dim3 rows(static_cast<unsigned>(a.shape.pieces * (a.draft ? 2 : 1)), tokens, n), groups(static_cast<unsigned>(a.shape.groups), n);
+        // (chains with a draft: what the further launch takes, 6 us and more, has to be saved)
+        if (!a.draft || (!a.mask && a.total_q * a.vocab >= kCoarseLogits)) {
+            hipLaunchKernelGGL((verify_rows_kernel<F32, kCoarse>), rows, block, 0, st, a);
+            hipLaunchKernelGGL((verify_choice_kernel<F32, kCoarse>), dim3(tokens, n), block, 0, st, a);
+            if (a.draft) hipLaunchKernelGGL((verify_sums_kernel<F32>), groups, block, 0, st, a);
+        } else {
+            hipLaunchKernelGGL((verify_rows_kernel<F32, kFast>), rows, block, 0, st, a);
+            hipLaunchKernelGGL((verify_choice_kernel<F32, kFast>), dim3(tokens, n), block, 0, st, a);
+        }
     }
     hipLaunchKernelGGL((verify_draw_kernel<F32>), dim3(static_cast<unsigned>(a.shape.groups), n), block, 0, st, a);
     return static_cast<int>(hipGetLastError());
@@ -573,6 +666,7 @@ VerifyShape VerifyShape::of(const int64_t n, const int64_t total_q, const int32_
     s.spans = static_cast<int>(up(thousands, s.span_rounds));
     s.group_spans = static_cast<int>(up(up(s.spans, least(1024 / (n > 0 ? n : 1) + 1, up(s.spans, 4))), 4) * 4);
     s.groups = static_cast<int>(up(s.spans, s.group_spans));
+    s.last_stride = s.spans < 2 ? 2 : s.spans;      // (two for a workgroup of verify_sums_kernel, which has four spans and more where there are several)
     return s;
 }
 

@@ -71,6 +71,34 @@ def check(s, got, max_keep=None, max_q=64):
 def test_judging(vocab, dtype, drawn, tree):
     s = make(vocab, [1, 5, 0, 64, 17, 2, 33, 1], vocab, dtype, drawn, tree)
     check(s, call(s))
+    check(s, call(s, 2), 2)
+
+
+@pytest.mark.parametrize("dtype, spread", [("bf16", 2.0), ("f32", 2.0), ("bf16", 0.0), ("f32", 40.0)])
+def test_chains_of_many_logits(dtype, spread):
+    s = make(1, [64, 5, 1, 40, 64, 2, 0, 30], 50001, dtype, True, False, spread=spread)            # 206 rows: more than 2^23 logits, whose first sums have 32 bits
+    s["target"][3, ::7], s["draft"][5, 1::9] = float("nan"), -float("inf")
+    check(s, call(s))
+    s["temperature"][:4] = 0.0, 0.01, 5.0, 1e-20
+    check(s, call(s))
+    check(s, call(s, 3), 3)
+
+
+@pytest.mark.parametrize("case", ["chain", "many", "lookup", "tree"])
+def test_choices_next_to_a_border(case):
+    """u is the fp32 number next to the border, off it by 3e-8 or less (and by 1e-11 hardly ever): 64 bits decide."""
+    drawn, tree, vocab = case in ("chain", "many"), case == "tree", 45007 if case == "many" else 3001
+    s = make(2, [2] * (100 if case == "many" else 60), vocab, "f32", drawn, tree)
+    for i in range(len(s["sizes"])):
+        a = s["q_start"][i]
+        x, t = s["tokens"][a + 1], float(s["temperature"][i])
+        border = ob.probabilities(s["target"][a].double().numpy(), t)[x]
+        if drawn:
+            border /= ob.probabilities(s["draft"][a].double().numpy(), t)[x]
+        s["accept"][a + 1] = np.float32(border)
+    got = call(s)
+    check(s, got)
+    assert 0.2 < (got[1] == 2).mean() < 0.95
 
 
 @pytest.mark.parametrize("sizes", [[1], [0], [], [2], [64] * 3, [1] * 300, [3, 0, 9] * 30])
