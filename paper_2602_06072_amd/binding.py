@@ -130,6 +130,8 @@ EXPORTS = [
     "pk_pack_plan_tree", "pk_trie_tree", "pk_plan_tune", "pk_packed_decode_attn_static",
     "pk_packed_mixed_step", "pk_qk_norm_rope", "pk_kv_cache_write", "pk_qkv_cache_write",
     "pk_kv_cache_read", "pk_tree_attn", "pk_tree_attn_workspace_bytes", "pk_kv_cache_keep",
+    "pk_kv_pages_select", "pk_kv_pages_reserve", "pk_kv_pages_compact", "pk_kv_pages_workspace_bytes", "pk_kv_cache_copy",
+    "pk_shared_tree_attn", "pk_shared_tree_attn_workspace_bytes", "pk_draft_verify", "pk_draft_verify_workspace_bytes",
 ]
 STATIC_SCRATCH_BYTES = 16 << 20
 TUNE_DECODE_SPLIT = 0
