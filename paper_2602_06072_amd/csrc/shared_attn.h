@@ -25,7 +25,7 @@ struct SharedWorkspace {
         SharedWorkspace w;
         const int64_t row = 4 * (d + 1);
         // (share_of in tree_body.hip.h: no more pieces than chunks and twice what runs at once, and some for the rounding of its sums)
-        w.own_slots = n * s.chunks + 2 * s.items + 64;
+        w.own_slots = n * s.chunks + 4 * 2 * s.items + 64;            // (four waves of a workgroup with pieces of their own)
         w.family_slots = total_q * (Hq / Hkv) / 128 + n / 2 + 1 + 2 * s.items + 64;
         w.counts = 256 + kMostFamilies * 4;
         w.plain = w.counts + TreeShape::count_bytes(Hkv, compute_units);

@@ -128,7 +128,9 @@ __global__ __launch_bounds__(256) void shared_find_kernel(SharedArgs s) {
 // Shared keys and own ones in one launch, the shared ones, which take longer, first.  (A unit of the one kind and one of the other in turns: 429 us instead of 313 for
 // families of drafted trees.)
 struct BothArgs { TreeArgs own, shared; int own_units, shared_units; };
-template <int D, bool F8, int ROW_BLOCKS>
+// WAVES: own keys by single waves, each with pieces of its own, for batches of many short requests: what a workgroup takes to find its piece, to begin and to put its four waves'
+// results together is half of its time there (128 requests of 16 .. 1024 own tokens: 43 us by workgroups).
+template <int D, bool F8, int ROW_BLOCKS, bool WAVES = false>
 __global__ __launch_bounds__(64 * kWaves, 2) void shared_both_kernel(BothArgs b) {
     __shared__ __align__(16) unsigned char lds[kWideBytes<D>];
     __shared__ int last;
@@ -136,8 +138,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void shared_both_kernel(BothArgs b)
     const bool of_shared = unit < b.shared_units;
     const int number = (of_shared ? unit : unit - b.shared_units) * Hkv + head;
     if (of_shared) many_rows<D, F8, kShared, 1>(lds, last, number, b.shared_units * Hkv);
-    else if constexpr (ROW_BLOCKS == 1) few_rows<D, F8, 1, kSubTiles1<D, F8>, false, kOwn, 0>(lds, last, number, b.own_units * Hkv);
-    else if constexpr (ROW_BLOCKS == 2) few_rows<D, F8, 2, kSubTiles2<D, F8>, false, kOwn, 0>(lds, last, number, b.own_units * Hkv);
+    else if constexpr (ROW_BLOCKS == 1) few_rows<D, F8, 1, kSubTiles1<D, F8>, WAVES, kOwn, 0>(lds, last, number, b.own_units * Hkv);
+    else if constexpr (ROW_BLOCKS == 2) few_rows<D, F8, 2, kSubTiles2<D, F8>, WAVES, kOwn, 0>(lds, last, number, b.own_units * Hkv);
     else many_rows<D, F8, kOwn, 0>(lds, last, number, b.own_units * Hkv);
 }
 
@@ -195,18 +197,23 @@ int launch(SharedArgs s, const TreeShape& shape, hipStream_t st) {
     a.least_per_many = a.least_per_share / (shape.rows == 128 ? 4 : 1);
     a.shared_of = s.shared_of;
     const int64_t loads = static_cast<int64_t>(a.n) * a.chunks;
-    const auto units_of = [&](const int64_t loads) { return loads <= a.items / 2 ? static_cast<int64_t>(a.items) : loads + a.items / 2; };
-    const int64_t own_units = units_of(loads), shared_units = units_of(family_loads);
+    const auto units_of = [](const int64_t loads, const int64_t items) { return loads <= items / 2 ? items : loads + items / 2; };
+    const bool waves = row_blocks < 3 && kWavesOf2<D, F8> == 2 && loads > a.items * 3 / 4;         // (more requests than one round of workgroups holds)
+    const int64_t shared_units = units_of(family_loads, a.items);
+    if (waves) a.items *= kWaves;
+    const int64_t own_units = waves ? (units_of(loads, a.items) + kWaves - 1) / kWaves : units_of(loads, a.items);
     if ((own_units + shared_units) * a.cache.Hkv > 0x7FFFFFFF) return static_cast<int>(hipErrorInvalidConfiguration);
     const auto workgroups = [&](const int64_t units) { return dim3(static_cast<unsigned>(units * a.cache.Hkv)); };
     const BothArgs both{a, f, static_cast<int>(own_units), static_cast<int>(shared_units)};
     const dim3 grid = workgroups(own_units + shared_units);
     if (row_blocks == 1) {
-        hipLaunchKernelGGL((shared_both_kernel<D, F8, 1>), grid, block, 0, st, both);
+        if (waves) hipLaunchKernelGGL((shared_both_kernel<D, F8, 1, true>), grid, block, 0, st, both);
+        else hipLaunchKernelGGL((shared_both_kernel<D, F8, 1>), grid, block, 0, st, both);
     } else if (row_blocks > 2) {
         hipLaunchKernelGGL((shared_both_kernel<D, F8, 3>), grid, block, 0, st, both);
     } else if constexpr (kWavesOf2<D, F8> == 2) {
-        hipLaunchKernelGGL((shared_both_kernel<D, F8, 2>), grid, block, 0, st, both);
+        if (waves) hipLaunchKernelGGL((shared_both_kernel<D, F8, 2, true>), grid, block, 0, st, both);
+        else hipLaunchKernelGGL((shared_both_kernel<D, F8, 2>), grid, block, 0, st, both);
     } else {                                        // (32 rows of 128 columns in bf16 have twice the registers to a wave)
         hipLaunchKernelGGL((tree_attn_wide_kernel<D, F8, kShared>), workgroups(shared_units), block, 0, st, f);
         hipLaunchKernelGGL((tree_attn_kernel<D, F8, 2, kSubTiles2<D, F8>, kWavesOf2<D, F8>, false, kOwn>), workgroups(own_units), block, 0, st, a);

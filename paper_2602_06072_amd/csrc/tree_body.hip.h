@@ -192,7 +192,8 @@ __device__ __forceinline__ const TreeArgs& kernel_args() {
 // Runs `work(arguments, piece, KV head)` for the workgroup's pieces: the one of its number and, where there are more pieces than workgroups, those as many numbers on.
 // Workgroups go round-robin over the XCDs: with eight KV heads an XCD keeps to one, and the chunks of its rows find its keys in the L2.
 // (`first`, `step`: the workgroup's first number and the distance to the next one)
-template <int TOKENS, int KEPT, Keys KEYS, int AT = 0, class Work>
+// OF_WAVE: they are a wave's.
+template <int TOKENS, int KEPT, Keys KEYS, int AT = 0, bool OF_WAVE = false, class Work>
 __device__ __forceinline__ void run_pieces(Work work, const int first, const int step) {
     if (const TreeArgs& a = kernel_args<AT>(); KEYS == kAll && a.whole) {              // no request can have two pieces
         const int rest = a.by_hkv(blockIdx.x), i = a.by_chunks(rest);
@@ -208,7 +209,8 @@ __device__ __forceinline__ void run_pieces(Work work, const int first, const int
         if (!find_piece<TOKENS>(a, loads, rest, shares, w)) return;
         work(a, w, kvh);
         if (shares.middle < 0) return;
-        __syncthreads();
+        if constexpr (OF_WAVE) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        else __syncthreads();
     }
 }
 
@@ -576,9 +578,9 @@ __device__ __forceinline__ void finish(const TreeArgs& a, const Piece& w, const 
             }
         }
     }
-    if constexpr (ALONE) return;
+    if constexpr (ALONE && KEYS == kAll) return;
     if constexpr (!HERE) {
-        if (w.piece == 0 && w.chunk == 0 && kvh == 0 && threadIdx.x == 0) a.pieces_of[w.request] = make_int2(w.pieces, w.slot);
+        if (w.piece == 0 && w.chunk == 0 && kvh == 0 && thread == 0) a.pieces_of[w.request] = make_int2(w.pieces, w.slot);
         return;
     }
     if (w.pieces == 1) return;
@@ -739,7 +741,9 @@ __device__ __forceinline__ void few_rows(unsigned char* lds, int& last, const in
         }
         finish<D, F8, NB, NB == 1 && KEYS == kAll, ALONE, KEYS>(a, w, bounds, kvh, 1, ALONE ? 1 : kWaves, y, lds, &last);
     };
-    if constexpr (ALONE) {
+    if constexpr (ALONE && KEYS != kAll) {
+        run_pieces<TOKENS, 4, KEYS, AT, true>(work, first * kWaves + wave, step_of_items * kWaves);
+    } else if constexpr (ALONE) {
         const TreeArgs& a = kernel_args();
         const int item = blockIdx.x * kWaves + wave, rest = a.by_hkv(item), i = a.by_chunks(rest);
         if (i < a.n) work(a, Piece{i, 0, 1, rest - i * a.chunks, 0, a.chunks}, item - rest * a.cache.Hkv);
