@@ -10,7 +10,8 @@ struct SharedArgs {
     uint32_t* arrived; int32_t* missing;            // zero between calls: workgroups that are done; [families] 1 + the keys of a table that a family does not share, 0: it has no rows
     int32_t* family_of; int32_t* shared_of;         // [n]
     int32_t* first_of; int32_t* q_start_of; int32_t* len_of;       // [families (+ 1)]: first request, rows of q, shared tokens
-    int32_t* places; int few_rows;                  // [1] workgroups of a KV head that the shared keys are cut for; set by the launch: up to 32 rows a request
+    int32_t* places;                                // [1] workgroups of a KV head that the shared keys are cut for
+    int few_rows, at_once;                          // set by the launch: up to 32 rows a request; workgroups of a KV head that run at once
     int2* pieces_of_family; float* family_lse; float* family_o;    // partial results of the shared keys
 };
 int launch_shared_tree_attn(SharedArgs s, const TreeShape& shape, void* stream);
@@ -26,7 +27,7 @@ struct SharedWorkspace {
         const int64_t row = 4 * (d + 1);
         // (share_of in tree_body.hip.h: no more pieces than chunks and twice what runs at once, and some for the rounding of its sums)
         w.own_slots = n * s.chunks + 4 * 2 * s.items + 64;            // (four waves of a workgroup with pieces of their own)
-        w.family_slots = total_q * (Hq / Hkv) / 128 + n / 2 + 1 + 2 * s.items + 64;
+        w.family_slots = total_q * (Hq / Hkv) / 128 + n / 2 + 1 + 3 * s.items + 64;
         w.counts = 256 + kMostFamilies * 4;
         w.plain = w.counts + TreeShape::count_bytes(Hkv, compute_units);
         w.arrays = w.plain;

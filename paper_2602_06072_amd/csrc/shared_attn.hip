@@ -122,7 +122,7 @@ __global__ __launch_bounds__(256) void shared_find_kernel(SharedArgs s) {
     shared = sum(shared);
     // Where there is much to be done for own keys, by workgroups that wait for memory, the shared ones are cut for half of the workgroups that run at once: both kinds
     // are on every unit then, and there are half as many partial results to be put together.
-    if (tid == 0) *s.places = s.few_rows && own > 0.7f * shared ? max(a.items / 2, 1) : a.items;
+    if (tid == 0) *s.places = s.few_rows && own > 0.7f * shared ? max(s.at_once / 2, 1) : s.at_once;
 }
 
 // Shared keys and own ones in one launch, the shared ones, which take longer, first.  (A unit of the one kind and one of the other in turns: 429 us instead of 313 for
@@ -131,7 +131,7 @@ struct BothArgs { TreeArgs own, shared; int own_units, shared_units; };
 // WAVES: own keys by single waves, each with pieces of its own, for batches of many short requests: what a workgroup takes to find its piece, to begin and to put its four waves'
 // results together is half of its time there (128 requests of 16 .. 1024 own tokens: 43 us by workgroups).
 template <int D, bool F8, int ROW_BLOCKS, bool WAVES = false>
-__global__ __launch_bounds__(64 * kWaves, 2) void shared_both_kernel(BothArgs b) {
+__global__ __launch_bounds__(64 * kWaves, D == 64 && ROW_BLOCKS == 3 ? 3 : 2) void shared_both_kernel(BothArgs b) {
     __shared__ __align__(16) unsigned char lds[kWideBytes<D>];
     __shared__ int last;
     const int Hkv = b.own.cache.Hkv, unit = b.own.by_hkv(blockIdx.x), head = static_cast<int>(blockIdx.x) - unit * Hkv;
@@ -182,6 +182,7 @@ int launch(SharedArgs s, const TreeShape& shape, hipStream_t st) {
     TreeArgs& a = s.tree;
     const dim3 block(64 * kWaves);
     s.few_rows = shape.rows <= 32;
+    s.at_once = D == 64 && shape.rows > 32 ? a.items * 3 / 2 : a.items;            // (three workgroups on a unit)
     hipLaunchKernelGGL(shared_find_kernel, dim3(static_cast<unsigned>((a.n + 3) / 4)), dim3(256), 0, st, s);
 
     TreeArgs f = a;                                 // families as requests
@@ -199,7 +200,7 @@ int launch(SharedArgs s, const TreeShape& shape, hipStream_t st) {
     const int64_t loads = static_cast<int64_t>(a.n) * a.chunks;
     const auto units_of = [](const int64_t loads, const int64_t items) { return loads <= items / 2 ? items : loads + items / 2; };
     const bool waves = row_blocks < 3 && kWavesOf2<D, F8> == 2 && loads > a.items * 3 / 4;         // (more requests than one round of workgroups holds)
-    const int64_t shared_units = units_of(family_loads, a.items);
+    const int64_t shared_units = units_of(family_loads, s.at_once);
     if (waves) a.items *= kWaves;
     const int64_t own_units = waves ? (units_of(loads, a.items) + kWaves - 1) / kWaves : units_of(loads, a.items);
     if ((own_units + shared_units) * a.cache.Hkv > 0x7FFFFFFF) return static_cast<int>(hipErrorInvalidConfiguration);
