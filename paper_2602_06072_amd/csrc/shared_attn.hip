@@ -48,18 +48,23 @@ __global__ __launch_bounds__(256) void shared_find_kernel(SharedArgs s) {
             const int32_t* mine = a.block_table + static_cast<int64_t>(i) * a.max_blocks;
             const int32_t* firsts = a.block_table + static_cast<int64_t>(first) * a.max_blocks;
             int same = i == first ? pages : 0;
-            while (same < pages) {                  // 256 pages at a time
-                uint64_t differs[4];
+            constexpr int AT_ONCE = 8;              // times 64 pages
+            while (same < pages) {
+                int32_t a_page[AT_ONCE], b_page[AT_ONCE];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int p = same + 64 * u + lane;
-                    differs[u] = __ballot(p < pages && mine[min(p, pages - 1)] != firsts[min(p, pages - 1)]);
+                for (int u = 0; u < AT_ONCE; ++u) {
+                    const int p = min(same + 64 * u + lane, pages - 1);
+                    a_page[u] = mine[p];
+                    b_page[u] = firsts[p];
                 }
-                int more = 256;
+                int more = 64 * AT_ONCE;
 #pragma unroll
-                for (int u = 3; u >= 0; --u) more = differs[u] ? 64 * u + __builtin_ctzll(differs[u]) : more;
+                for (int u = AT_ONCE - 1; u >= 0; --u) {
+                    const uint64_t differs = __ballot(same + 64 * u + lane < pages && a_page[u] != b_page[u]);
+                    more = differs ? 64 * u + __builtin_ctzll(differs) : more;
+                }
                 same += more;
-                if (more < 256) break;
+                if (more < 64 * AT_ONCE) break;
             }
             const int common = min(context, static_cast<int>(min(static_cast<int64_t>(same) * a.cache.page, static_cast<int64_t>(a.most_keys))));
             if (lane == 0) atomicMax(s.missing + family, a.most_keys - common + 1);
