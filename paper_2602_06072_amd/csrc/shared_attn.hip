@@ -172,13 +172,16 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedArgs s) {
     for (int x = slice * 256 + threadIdx.x; x < here * (D / 4); x += a.slices * 256) {
         const int local = x / (D / 4), col = 4 * (x % (D / 4)), row = chunk * chunk_rows + local, t = a.by_r(row);
         const int of_family = static_cast<int>(min(max((q0 - family_q0) * a.heads_per_kv + row, int64_t{0}), static_cast<int64_t>(family_rows - 1)));
-        store4(a, ((q0 + t) * a.Hq + kvh * a.heads_per_kv + row - t * a.heads_per_kv) * D + col, merged(p.x + f.x, [&](const int piece, float& lse, floatx4& o) {
+        const auto part = [&](const int piece, float& lse, floatx4& o) {
             const bool own = piece < p.x;
             const int64_t at_own = (static_cast<int64_t>(p.y + piece * chunks + chunk) * a.cache.Hkv + kvh) * chunk_rows + local;
             const int64_t at_shared = (static_cast<int64_t>(f.y + (piece - p.x) * family_chunks + of_family / kWideRows) * a.cache.Hkv + kvh) * kWideRows + of_family % kWideRows;
             lse = own ? a.part_lse[at_own] : s.family_lse[at_shared];
             o = *reinterpret_cast<const floatx4*>(own ? a.part_o + at_own * D + col : s.family_o + at_shared * D + col);
-        }));
+        };
+        const int pieces = p.x + f.x;               // (nearly always few, where there are many rows)
+        store4(a, ((q0 + t) * a.Hq + kvh * a.heads_per_kv + row - t * a.heads_per_kv) * D + col,
+               pieces <= 2 ? merged<2>(pieces, part) : pieces <= 4 ? merged<4>(pieces, part) : merged<8>(pieces, part));
     }
 }
 

@@ -480,10 +480,9 @@ __device__ __forceinline__ void product_with_hidden(const bf16x8 v, const uint32
     }
 }
 
-// Four columns of a row from the partial results of its pieces: sum of exp(lse) o over sum of exp(lse), eight pieces on their way at a time
-template <class Read>
+// Four columns of a row from the partial results of its pieces: sum of exp(lse) o over sum of exp(lse), eight pieces (BATCH) on their way at a time
+template <int BATCH = 8, class Read>
 __device__ __forceinline__ floatx4 merged(const int pieces, Read read) {
-    constexpr int BATCH = 8;
     float top = -INFINITY, sum = 0.f;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
     for (int p = 0; p < pieces; p += BATCH) {
