@@ -264,6 +264,7 @@ __device__ __forceinline__ RowPart part_of_row(const void* base, const int64_t r
     }
     return of_all<LARGEST>(y, per, lds);
 }
+template <int THREADS>
 __device__ __forceinline__ double sum_of_all(double x, double* lds) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
@@ -272,7 +273,7 @@ __device__ __forceinline__ double sum_of_all(double x, double* lds) {
     __syncthreads();
     double y = lds[0];
 #pragma unroll
-    for (int w = 1; w < kThreads / 64; ++w) y += lds[w];
+    for (int w = 1; w < THREADS / 64; ++w) y += lds[w];
     return y;
 }
 
@@ -329,9 +330,11 @@ __device__ __forceinline__ double left_of(const Raw<F32>& p, Raw<F32> q, const b
 }
 
 // What a token with children decides: a workgroup for (token, request), every wave the same (a lane has a token)
-template <bool F32, Sums64 HOW>
-__global__ __launch_bounds__(kThreads) void verify_choice_kernel(VerifyArgs a) {
-    __shared__ double lds[kThreads / 64];
+// THREADS: where sums of what is left are to be expected (a mask and a draft), 512, as the one workgroup of a token waits for its loads: 16 trees of 24 tokens, 128256
+// logits, 40 us (256: 48, 1024: 41).  Without them 256, which begin sooner.
+template <bool F32, Sums64 HOW, int THREADS>
+__global__ __launch_bounds__(THREADS) void verify_choice_kernel(VerifyArgs a) {
+    __shared__ double lds[THREADS / 64];
     __shared__ WaveParts parts_lds;
     const int token = blockIdx.x, i = blockIdx.y, lane = threadIdx.x & 63;
     const Tree t = tree_of(a, i);
@@ -374,7 +377,7 @@ __global__ __launch_bounds__(kThreads) void verify_choice_kernel(VerifyArgs a) {
         const bool before = __ballot((gone >> lane & 1) && x == of) != 0;          // (the same token again)
         const double least = drawn ? (w.c + us * Z) * qx : us * Z;
         // Sums of 32 bits that do not decide it: of P(x) and of Q(x), or of what has left P, each is off by kCoarseError at most.  The row anew, in 64 bits.
-        if (!exact && !greedy && fabs(px - least) <= 4 * kCoarseError * (px + (drawn ? least : us))) {
+        if (HOW == kCoarse && !exact && !greedy && fabs(px - least) <= 4 * kCoarseError * (px + (drawn ? least : us))) {
             p = part_of_row<F32, false>(a.target, row * a.target_stride, 0, a.vocab, a.vocab, per, parts_lds);
             if (drawn) q = part_of_row<F32, false>(a.draft, row * a.draft_stride, 0, a.vocab, a.vocab, per, parts_lds);
             exact = true;
@@ -389,12 +392,12 @@ __global__ __launch_bounds__(kThreads) void verify_choice_kernel(VerifyArgs a) {
         if (HOW == kCoarse || left == 0) break;     // (what is left is summed up only for a sibling's sake)
         double sum = 0;
 #pragma unroll 1
-        for (int at = static_cast<int>(threadIdx.x) * kVector; at < a.vocab; at += kStep) {
+        for (int at = static_cast<int>(threadIdx.x) * kVector; at < a.vocab; at += THREADS * kVector) {
             int begin;
             const Raw<F32> vp = load_vector<F32>(a.target, row * a.target_stride, at, a.vocab, begin), vq = load_vector<F32>(a.draft, row * a.draft_stride, at, a.vocab, begin);
             sum += left_of<F32, 4>(vp, vq, true, w, begin, nullptr, 0);
         }
-        Z = sum_of_all(sum, lds);
+        Z = sum_of_all<THREADS>(sum, lds);
     }
     if (threadIdx.x == 0) a.choices[row] = {choice, drawn && gone != 0 ? w.c : 0.0, w.of_target, w.of_draft, w.top, w.draft_top};
 }
@@ -639,11 +642,12 @@ int launch(const VerifyArgs& a, hipStream_t st) {
         // (chains with a draft: what the further launch takes, 6 us and more, has to be saved)
         if (!a.draft || (!a.mask && a.total_q * a.vocab >= kCoarseLogits)) {
             hipLaunchKernelGGL((verify_rows_kernel<F32, kCoarse>), rows, block, 0, st, a);
-            hipLaunchKernelGGL((verify_choice_kernel<F32, kCoarse>), dim3(tokens, n), block, 0, st, a);
+            hipLaunchKernelGGL((verify_choice_kernel<F32, kCoarse, kThreads>), dim3(tokens, n), block, 0, st, a);
             if (a.draft) hipLaunchKernelGGL((verify_sums_kernel<F32>), groups, block, 0, st, a);
         } else {
             hipLaunchKernelGGL((verify_rows_kernel<F32, kFast>), rows, block, 0, st, a);
-            hipLaunchKernelGGL((verify_choice_kernel<F32, kFast>), dim3(tokens, n), block, 0, st, a);
+            if (a.mask) hipLaunchKernelGGL((verify_choice_kernel<F32, kFast, 512>), dim3(tokens, n), dim3(512), 0, st, a);
+            else hipLaunchKernelGGL((verify_choice_kernel<F32, kFast, kThreads>), dim3(tokens, n), block, 0, st, a);
         }
     }
     hipLaunchKernelGGL((verify_draw_kernel<F32>), dim3(static_cast<unsigned>(a.shape.groups), n), block, 0, st, a);
