@@ -330,8 +330,8 @@ __device__ __forceinline__ double left_of(const Raw<F32>& p, Raw<F32> q, const b
 }
 
 // What a token with children decides: a workgroup for (token, request), every wave the same (a lane has a token)
-// THREADS: where sums of what is left are to be expected (a mask and a draft), 512, as the one workgroup of a token waits for its loads: 16 trees of 24 tokens, 128256
-// logits, 40 us (256: 48, 1024: 41).  Without them 256, which begin sooner.
+// THREADS: where sums of what is left are to be expected (a mask and a draft), 512, as the one workgroup of a token waits for its loads: 16 trees of 16 to 48 tokens, 32000
+// logits of 32 bits, 40 us (256: 48, 1024: 41).  Without such sums 256, which begin sooner.
 template <bool F32, Sums64 HOW, int THREADS>
 __global__ __launch_bounds__(THREADS) void verify_choice_kernel(VerifyArgs a) {
     __shared__ double lds[THREADS / 64];
