@@ -679,7 +679,8 @@ int pk_kv_pages_select(const int32_t* block_table, const int32_t* lens, const in
  *   grow      device int32 [n], at least 0 (less counts as 0)
  *   workspace device, 256-byte aligned, at least pk_kv_pages_workspace_bytes.
  *             ZERO-FILLED BEFORE ITS FIRST USE; every call leaves it ready for the
- *             next, also of another of these calls; the caller orders them.
+ *             next.  One workspace serves both calls and all pools for which it
+ *             is large enough; the caller orders them.
  * A row must not name a block twice.  Errors: PK_EINVAL. */
 size_t pk_kv_pages_workspace_bytes(int64_t num_blocks);
 int pk_kv_pages_reserve(int32_t* block_table, const int32_t* lens, int32_t* pages, int32_t n, int32_t max_blocks,

@@ -15,19 +15,23 @@ struct PagesSelectArgs {
 };
 int launch_pages_select(const PagesSelectArgs& a, void* stream);
 
-// A workspace of the page calls: kWords arrays of num_blocks words.  Zero between calls: the first two.
+// A workspace of the page calls: for every 1024 blocks three times 1024 words and one more.  The first two thousand are zero between calls, and which words these are
+// does not depend on num_blocks: no call has its zeros where one for a smaller pool has written something else.
 struct PagesWorkspace {
-    static constexpr int kWords = 3;
     static constexpr int kSegment = 1024;           // blocks that a workgroup looks at
-    static size_t bytes(const int64_t num_blocks) { return static_cast<size_t>((kWords * num_blocks + num_blocks / kSegment + 1) * 4 + 255) / 256 * 256; }
+    static constexpr int kWriters = kSegment, kNumbers = 2 * kSegment, kUsed = 3 * kSegment, kWords = kUsed + 64;     // (whole cache lines)
+    static size_t bytes(const int64_t num_blocks) { return static_cast<size_t>((num_blocks + kSegment - 1) / kSegment) * kWords * 4; }
+    // of block b's words the first
+    static constexpr int64_t at(const uint32_t b) { return static_cast<int64_t>(b / kSegment) * kWords + b % kSegment; }
 };
 
 struct PagesReserveArgs {
     int32_t* table; const int32_t* lens; int32_t* pages; int32_t n; int32_t max_blocks;
     const int32_t* grow; int32_t* refs; int32_t num_blocks; int32_t page;
     int32_t* served; int32_t* copy_src; int32_t* copy_dst;
-    int32_t* last_writer; int32_t* writers;         // [num_blocks] each, zero between calls: number + 1 of the last request that would write a shared block; how many would
-    int32_t* free;                                  // [num_blocks] the free blocks that are handed out, by rising number
+    // at PagesWorkspace::at of a block; zero between calls: number + 1 of the last request that would write it though it is shared; how many would
+    int32_t* last_writer; int32_t* writers;
+    int32_t* free;                                  // (the same) the free blocks that are handed out, by rising number
 };
 int launch_pages_reserve(const PagesReserveArgs& a, void* stream);
 
@@ -35,8 +39,8 @@ struct PagesCompactArgs {
     const int32_t* table; const int32_t* pages; int32_t n; int32_t max_blocks;
     const int32_t* refs; int32_t num_blocks; int32_t* new_table; int32_t* new_refs;
     int32_t* copy_src; int32_t* copy_dst; int32_t max_moves;
-    int32_t* to;                                    // [num_blocks] new number of every block; -1 - k: that of move k
-    int32_t* used_of;                               // [segments] blocks in use
+    int32_t* to;                                    // at PagesWorkspace::at: new number of every block; -1 - k: that of move k
+    int32_t* used_of;                               // blocks in use of every segment, kWords apart
 };
 int launch_pages_compact(const PagesCompactArgs& a, void* stream);
 

@@ -102,7 +102,7 @@ extern "C" int pk_kv_pages_reserve(int32_t* block_table, const int32_t* lens, in
         PK_CHECK(check_apart({table, ps, rf, sv, cs, cd, ws}, {ls, gr}));
         int32_t* at = static_cast<int32_t*>(workspace);
         PagesReserveArgs a{block_table, lens, pages, n, max_blocks, grow, refs, static_cast<int32_t>(num_blocks), page_size,
-                           served, copy_src, copy_dst, at, at + num_blocks, at + 2 * num_blocks};
+                           served, copy_src, copy_dst, at, at + PagesWorkspace::kWriters, at + PagesWorkspace::kNumbers};
         return launched(who, launch_pages_reserve(a, stream));
     });
 }
@@ -126,7 +126,7 @@ extern "C" int pk_kv_pages_compact(const int32_t* block_table, const int32_t* pa
         if (new_table != block_table) PK_CHECK(check_apart({nt}, {table}));
         int32_t* at = static_cast<int32_t*>(workspace);
         PagesCompactArgs a{block_table, pages, n, max_blocks, refs, static_cast<int32_t>(num_blocks), new_table, new_refs, copy_src, copy_dst, max_moves,
-                           at + 2 * num_blocks, at + 3 * num_blocks};
+                           at + PagesWorkspace::kNumbers, at + PagesWorkspace::kUsed};
         return launched(who, launch_pages_compact(a, stream));
     });
 }

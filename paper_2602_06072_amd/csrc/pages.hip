@@ -38,6 +38,7 @@ __device__ __forceinline__ T sum_in_front(const T x, T* lds, T& all) {
     return before + upto - x;
 }
 
+__device__ __forceinline__ int64_t place_of(const int64_t b) { return PagesWorkspace::at(static_cast<uint32_t>(b)); }
 __device__ __forceinline__ bool is_block(const int b, const int num_blocks) { return b >= 0 && b < num_blocks; }
 
 // Counts of four blocks; `none` for those that the pool does not have
@@ -131,15 +132,15 @@ __global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(PagesReserveAr
         const Wish w = wish_of(a, i);
         if (i == tid) kept = w;
         if (!w.shared) continue;
-        atomicMax(a.last_writer + w.block, i + 1);
-        atomicAdd(a.writers + w.block, 1);
+        atomicMax(a.last_writer + place_of(w.block), i + 1);
+        atomicAdd(a.writers + place_of(w.block), 1);
     }
     __builtin_amdgcn_s_waitcnt(0x0F70);            // vmcnt(0): the sums are in the L2, where they are read
     __syncthreads();
     const auto wish = [&](const int i) { return i == tid ? kept : wish_of(a, i); };
     const auto needs = [&](const int i, const Wish& w, bool& keeps) {
         // of as many writers as there are holders the last one keeps the page
-        keeps = w.shared && device_load(a.writers + w.block) == w.holders && device_load(a.last_writer + w.block) == i + 1;
+        keeps = w.shared && device_load(a.writers + place_of(w.block)) == w.holders && device_load(a.last_writer + place_of(w.block)) == i + 1;
         return static_cast<int64_t>(w.end - w.held + (w.shared && !keeps ? 1 : 0));
     };
     // the blocks that are wanted
@@ -169,7 +170,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(PagesReserveAr
             int64_t at = found + (front >> 16 * g & 0xFFFF);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (refs[g][e] == 0 && at < a.num_blocks) a.free[at++] = static_cast<int32_t>(b0 + g * OF_GROUP + 4 * tid + e);
+                if (refs[g][e] == 0 && at < a.num_blocks) a.free[place_of(at++)] = static_cast<int32_t>(b0 + g * OF_GROUP + 4 * tid + e);
             found += all >> 16 * g & 0xFFFF;
         }
     }
@@ -187,14 +188,14 @@ __global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(PagesReserveAr
             if (!copies) a.copy_dst[i] = -1;
             if (served) a.pages[i] = kept.end;
             if (copies) atomicAdd(a.refs + kept.block, -1);
-            if (kept.shared) { a.last_writer[kept.block] = 0; a.writers[kept.block] = 0; }
+            if (kept.shared) { a.last_writer[place_of(kept.block)] = 0; a.writers[place_of(kept.block)] = 0; }
         }
         __builtin_amdgcn_s_waitcnt(0x0F70);        // (the free blocks: of this workgroup, through the L2)
         __syncthreads();
         for (int64_t k = tid; k < all; k += kPlanThreads) {
             int r = 0;                              // the last request that begins at k or in front of it (those behind it with no blocks begin there too, and are none of k's)
             for (int step = kPlanThreads / 2; step > 0; step >>= 1) r += r + step < a.n && begins[r + step] <= k ? step : 0;
-            const int b = device_load(a.free + k), number = static_cast<int>(k) - begins[r];
+            const int b = device_load(a.free + place_of(k)), number = static_cast<int>(k) - begins[r];
             const int2 at = rows[r];
             const bool copy = number == 0 && at.x < 0;
             a.table[static_cast<int64_t>(r) * a.max_blocks + (copy ? -1 - at.x : at.y + number)] = b;
@@ -234,12 +235,12 @@ __global__ __launch_bounds__(256) void pages_apply_kernel(PagesReserveArgs a) {
     if (lane == 0) {
         int dst = -1;
         if (copies) {
-            dst = a.free[begin];
+            dst = a.free[place_of(begin)];
             row[w.at] = dst;
             a.refs[dst] = 1;
             atomicAdd(a.refs + w.block, -1);
         }
-        if (w.shared) { a.last_writer[w.block] = 0; a.writers[w.block] = 0; }
+        if (w.shared) { a.last_writer[place_of(w.block)] = 0; a.writers[place_of(w.block)] = 0; }
         a.copy_src[i] = copies ? w.block : -1;
         a.copy_dst[i] = dst;
         a.served[i] = served ? 1 : 0;
@@ -247,7 +248,7 @@ __global__ __launch_bounds__(256) void pages_apply_kernel(PagesReserveArgs a) {
     }
     if (!served) return;
     for (int j = w.held + lane; j < w.end; j += kWave) {
-        const int b = a.free[begin + (copies ? 1 : 0) + j - w.held];
+        const int b = a.free[place_of(begin + (copies ? 1 : 0) + j - w.held)];
         row[j] = b;
         a.refs[b] = 1;
     }
@@ -267,7 +268,7 @@ __global__ __launch_bounds__(256) void pages_count_kernel(PagesCompactArgs a) {
     __shared__ int lds[4];
     const int64_t first = static_cast<int64_t>(blockIdx.x) * kSegment;
     const int used = used_in_segment(a.refs, first, min(first + kSegment, static_cast<int64_t>(a.num_blocks)), lds);
-    if (threadIdx.x == 0) a.used_of[blockIdx.x] = used;
+    if (threadIdx.x == 0) a.used_of[static_cast<int64_t>(blockIdx.x) * PagesWorkspace::kWords] = used;
 }
 // Every workgroup has its segment's blocks, and finds from all segments' counts how many are in use, in front of it and in front of block U.
 __global__ __launch_bounds__(256) void pages_move_kernel(PagesCompactArgs a) {
@@ -275,7 +276,7 @@ __global__ __launch_bounds__(256) void pages_move_kernel(PagesCompactArgs a) {
     const int segments = gridDim.x, mine = blockIdx.x, tid = threadIdx.x;
     int of_all = 0, of_front = 0, used, front;
     for (int s = tid; s < segments; s += 256) {
-        const int x = a.used_of[s];
+        const int x = a.used_of[static_cast<int64_t>(s) * PagesWorkspace::kWords];
         of_all += x;
         of_front += s < mine ? x : 0;
     }
@@ -283,7 +284,7 @@ __global__ __launch_bounds__(256) void pages_move_kernel(PagesCompactArgs a) {
     sum_in_front<256>(of_front, lds, front);
     const int cut = used / kSegment;                // segment of block U
     int of_cut = 0, low;
-    for (int s = tid; s < min(cut, segments); s += 256) of_cut += a.used_of[s];
+    for (int s = tid; s < min(cut, segments); s += 256) of_cut += a.used_of[static_cast<int64_t>(s) * PagesWorkspace::kWords];
     sum_in_front<256>(of_cut, lds, low);
     low += used_in_segment(a.refs, static_cast<int64_t>(cut) * kSegment, used, lds);           // in use below U
     const int moves = min(used - low, a.max_moves);
@@ -306,7 +307,7 @@ __global__ __launch_bounds__(256) void pages_move_kernel(PagesCompactArgs a) {
         const bool goes = b >= used && in_use && before - low < moves;
         if (goes) a.copy_src[before - low] = static_cast<int32_t>(b);
         if (b < used && !in_use && b - before < moves) a.copy_dst[b - before] = static_cast<int32_t>(b);
-        a.to[b] = goes ? -1 - (before - low) : static_cast<int32_t>(b);
+        a.to[place_of(b)] = goes ? -1 - (before - low) : static_cast<int32_t>(b);
         a.new_refs[b] = goes ? 0 : refs[e];
         before += in_use ? 1 : 0;
     }
@@ -323,7 +324,7 @@ __global__ __launch_bounds__(256) void pages_rename_kernel(PagesCompactArgs a) {
     const int pages = min(max(a.pages[unit], 0), a.max_blocks);
     const int64_t row = unit * a.max_blocks;
     for (int j = lane; j < pages; j += kWave) {
-        const int b = a.table[row + j], to = is_block(b, a.num_blocks) ? a.to[b] : b;
+        const int b = a.table[row + j], to = is_block(b, a.num_blocks) ? a.to[place_of(b)] : b;
         a.new_table[row + j] = is_block(b, a.num_blocks) && to < 0 ? a.copy_dst[-1 - to] : to;
     }
 }

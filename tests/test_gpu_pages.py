@@ -57,7 +57,7 @@ class Batch:
         want = ob.pages_reserve(self.table, self.lens, self.pages, grow, self.refs, self.page)
         for g, w in zip(host(t, ps, refs, served, src, dst), (self.table, self.pages, self.refs) + want):
             assert np.array_equal(g, w)
-        assert not ws[:8 * len(self.refs)].any()                   # ready for the next call
+        assert not ws.view(torch.int32).view(-1, 3136)[:, :2048].any()                 # ready for the next call, of whatever size
         return want
 
     def compact(self, moves, ws, in_place=False):
@@ -128,6 +128,19 @@ def test_pages_run_out_in_the_order_of_requests():
     b.select([0, 0])
     served, src, _ = b.reserve(np.array([1, 1], np.int32), pk.new_pages_workspace(3))
     assert served.tolist() == [0, 0] and src.tolist() == [-1, -1]  # the second one must not write what the first still reads
+
+
+@pytest.mark.parametrize("large, small", [(700, 300), (5000, 1300), (5000, 40)])
+def test_one_workspace_for_pools_of_several_sizes(large, small):
+    rng, ws = np.random.default_rng(large), pk.new_pages_workspace(large)
+    for turn in range(3):
+        for blocks in (small, large, large):
+            n = blocks // 20
+            b = Batch(rng, n, 8, blocks, 16, 90)
+            b.select(np.repeat(np.arange(n), 2)[rng.permutation(2 * n)])
+            b.reserve(rng.integers(0, 30, 2 * n).astype(np.int32), ws)
+            b.compact(blocks, ws)
+            b.reserve(rng.integers(0, 30, 2 * n).astype(np.int32), ws)
 
 
 def test_blocks_that_a_caller_holds_and_numbers_outside_of_the_pool():
