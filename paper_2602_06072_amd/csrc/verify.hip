@@ -144,6 +144,14 @@ __device__ __forceinline__ RowPart joined(const RowPart& x, const RowPart& y, co
 }
 template <bool LARGEST>
 __device__ __forceinline__ RowPart of_wave(RowPart y, const double per) {
+    if constexpr (!LARGEST) {
+        if (__all(y.top == 0.f || y.top == -INFINITY)) {           // (as nearly always)
+            y.top = __any(y.top == 0.f) ? 0.f : -INFINITY;
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) y.sum += __shfl_xor(y.sum, o, 64);
+            return y;
+        }
+    }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) y = joined<LARGEST>(y, {__shfl_xor(y.sum, o, 64), __shfl_xor(y.top, o, 64), __shfl_xor(y.at, o, 64)}, per);
     return y;
