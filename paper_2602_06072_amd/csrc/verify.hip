@@ -13,8 +13,8 @@
 // 64 bits, and 97 for the call).
 //
 // Probabilities and their sums have 64 bits: a draw is the place of a number between V borders, and with sums of 32 bits every tenth draw of a flat row of 100000
-// would fall on the other side of one.  Vector instructions of 64 bits run at the rate of those of 32 here; a weight takes about 20 of them, 80 cycles for 64 logits, and
-// at 2 10^12 logits a second that, not memory (3 10^12 of bf16), bounds the launches over rows.
+// would fall on the other side of one.  Vector instructions of 64 bits run at the rate of those of 32 here; a weight takes about 20 of them, 90 cycles for 64 logits, and
+// at 1.7 10^12 logits a second at most that, not memory (3 10^12 of bf16), bounds the launches over rows in 64 bits; terms of 32 bits reach 2.3 10^12, 4.7 TB/s.
 #include "arrival.h"
 #include "branch.h"
 #include "common.hip.h"
@@ -285,7 +285,8 @@ __device__ __forceinline__ double sum_of_all(double x, double* lds) {
     return y;
 }
 
-// Sums of the rows of tokens with children: a workgroup for (piece, target or draft; token; request)
+// Sums of the rows of tokens with children: a workgroup for (piece, target or draft; token; request).  Chains of 64 requests (640 rows of 128256 logits) 35 us with terms of
+// 32 bits, 4.7 TB/s; 581 rows of 50257 logits that begin at any address 17, 3.5 TB/s; trees (612 rows of 32000 in fp32) in 64 bits 26.
 template <bool F32, Sums64 HOW>
 __global__ __launch_bounds__(kThreads, F32 ? 5 : 6) void verify_rows_kernel(VerifyArgs a) {
     __shared__ WaveParts lds;
@@ -337,7 +338,8 @@ __device__ __forceinline__ double left_of(const Raw<F32>& p, Raw<F32> q, const b
     return sum;
 }
 
-// What a token with children decides: a workgroup for (token, request), every wave the same (a lane has a token)
+// What a token with children decides: a workgroup for (token, request), every wave the same (a lane has a token).  Without sums of what is left 6 us, loads one behind the
+// other; each of them is a pass over two rows by one unit, 64000 weights in 10 us, and a token's siblings need them one after the other, which bounds the launch for trees.
 // THREADS: where sums of what is left are to be expected (a mask and a draft), 512, as the one workgroup of a token waits for its loads: 16 trees of 16 to 48 tokens, 32000
 // logits of 32 bits, 40 us (256: 48, 1024: 41).  Without such sums 256, which begin sooner.
 template <bool F32, Sums64 HOW, int THREADS>
@@ -451,7 +453,8 @@ __device__ __forceinline__ RowPart load_part(const uint64_t* from) {
     return {__longlong_as_double(static_cast<long long>(sum)), __uint_as_float(static_cast<uint32_t>(more)), static_cast<int>(more >> 32)};
 }
 
-// In 64 bits, the sums of the rows that are drawn from as max(P - c Q, 0), where the choices had them in 32: workgroups as for the draw
+// In 64 bits, the sums of the rows that are drawn from as max(P - c Q, 0), where the choices had them in 32: workgroups as for the draw.  Up to 64 pairs of rows of
+// 128256 logits 19 us, 0.9 10^12 logits a second: half of it the way there and the end.
 template <bool F32>
 __global__ __launch_bounds__(kThreads) void verify_sums_kernel(VerifyArgs a) {
     __shared__ WaveParts lds;
@@ -491,7 +494,8 @@ __global__ __launch_bounds__(kThreads) void verify_sums_kernel(VerifyArgs a) {
 }
 
 // The draw: sums of the row that a request's next token is drawn from, a wave for a span of it (up to 256 spans, of 1024 tokens where V is up to 2^18), a workgroup for some
-// of them; the last workgroup of a request to finish finds the span, one wave of it the vector in the span and the token in the vector.
+// of them; the last workgroup of a request to finish finds the span, one wave of it the vector in the span and the token in the vector.  Four rows of 32000 logits 9.2 us,
+// the chain of loads and the end; 200 rows of 50257 and 64 pairs of rows of 128256 25, of them 9 to 12 for the weights.
 enum { kPlain, kResidual, kRemoved };               // weights: P; max(P - c Q, 0); P without the tokens that were refused
 template <bool F32>
 __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
