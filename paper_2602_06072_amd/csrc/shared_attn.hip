@@ -23,13 +23,41 @@ constexpr int kSharedTile = 64;                     // keys
 __device__ __forceinline__ int load_there(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ void store_there(int32_t* p, const int x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-// A wave for each request finds its family and how many tokens it has in common with the family's first request; the last workgroup makes the families' arrays.
-// Families are [M[g], M[g + 1]) with M the largest of family_start up to g, within [0, n]: disjoint whatever the array holds.
+// A wave for each request finds its family and how many tokens it has in common with the family's first request; one more workgroup finds where families begin, and the last
+// one to finish what each of them shares.  Families are [M[g], M[g + 1]) with M the largest of family_start up to g, within [0, n]: disjoint whatever the array holds.
+// Bound by loads one behind the other, of 0.6 us and more each: those that need not wait for others are asked for in front of them (128 requests 8.1 us when the last workgroup
+// found where families begin, too).
 __global__ __launch_bounds__(256) void shared_find_kernel(SharedArgs s) {
-    __shared__ int last, lds[4];
+    constexpr int kNear = 1024;                     // families whose lengths the last workgroup has in LDS
+    __shared__ int last, lds[4], len_near[kNear];
     const TreeArgs& a = s.tree;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = blockIdx.x * 4 + wave;
-    if (i < a.n) {
+    if (blockIdx.x == gridDim.x - 1) {
+        int carried = 0, carried_q = 0;             // M, and the largest row of q, so far
+        for (int g0 = 0; g0 <= s.families; g0 += 256) {
+            const int g = g0 + tid;
+            const auto prefix_max = [&](int x, const int carried) {
+#pragma unroll
+                for (int o = 1; o < 64; o <<= 1) {
+                    const int y = __shfl_up(x, o, 64);
+                    x = lane >= o ? max(x, y) : x;
+                }
+                __syncthreads();
+                if (lane == 63) lds[wave] = x;
+                __syncthreads();
+                x = max(x, carried);
+                for (int w = 0; w < wave; ++w) x = max(x, lds[w]);
+                return x;
+            };
+            const int first = prefix_max(g <= s.families ? min(s.family_start[g], a.n) : 0, carried);
+            carried = max(max(max(lds[0], lds[1]), max(lds[2], lds[3])), carried);
+            const int q0 = prefix_max(g <= s.families ? static_cast<int>(min(static_cast<int64_t>(a.q_start[first]), a.total_q)) : 0, carried_q);
+            carried_q = max(max(max(lds[0], lds[1]), max(lds[2], lds[3])), carried_q);
+            if (g <= s.families) store_there(s.q_start_of + g, q0);
+            if (g < s.families) s.first_of[g] = min(first, a.n - 1);
+        }
+    } else if (i < a.n) {
+        const int asked = a.q_start[i + 1] - a.q_start[i], kv_len = a.kv_lens[i], len = min(max(kv_len, 0), a.most_keys);
         int first = 0, end = 0, family = -1, before = 0;
         for (int g0 = 0; g0 <= s.families; g0 += 64) {
             const int start = g0 + lane <= s.families ? s.family_start[g0 + lane] : -1;
@@ -46,10 +74,9 @@ __global__ __launch_bounds__(256) void shared_find_kernel(SharedArgs s) {
                 break;
             }
         }
-        const int asked = a.q_start[i + 1] - a.q_start[i], len = min(max(a.kv_lens[i], 0), a.most_keys);
         const bool member = family >= 0 && end - first > 1;
         if (member && min(asked, a.max_q) > 0) {
-            const int context = max(min(a.kv_lens[i] - asked, len), 0), pages = (context + a.cache.page - 1) / a.cache.page;
+            const int context = max(min(kv_len - asked, len), 0), pages = a.by_subs((context + 15) / 16 + a.subs - 1);
             const int32_t* mine = a.block_table + static_cast<int64_t>(i) * a.max_blocks;
             const int32_t* firsts = a.block_table + static_cast<int64_t>(first) * a.max_blocks;
             int same = i == first ? pages : 0;
@@ -81,45 +108,23 @@ __global__ __launch_bounds__(256) void shared_find_kernel(SharedArgs s) {
     if (tid == 0) last = arrives_last(TreeCount{s.arrived}, gridDim.x);
     __syncthreads();
     if (last == 0) return;
-    int carried = 0, carried_q = 0;                 // M, and the largest row of q, so far
-    for (int g0 = 0; g0 <= s.families; g0 += 256) {
-        const int g = g0 + tid;
-        const auto prefix_max = [&](int x, const int carried) {
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int y = __shfl_up(x, o, 64);
-                x = lane >= o ? max(x, y) : x;
-            }
-            __syncthreads();
-            if (lane == 63) lds[wave] = x;
-            __syncthreads();
-            x = max(x, carried);
-            for (int w = 0; w < wave; ++w) x = max(x, lds[w]);
-            return x;
-        };
-        const int first = prefix_max(g <= s.families ? min(s.family_start[g], a.n) : 0, carried);
-        carried = max(max(max(lds[0], lds[1]), max(lds[2], lds[3])), carried);
-        const int q0 = prefix_max(g <= s.families ? static_cast<int>(min(static_cast<int64_t>(a.q_start[first]), a.total_q)) : 0, carried_q);
-        carried_q = max(max(max(lds[0], lds[1]), max(lds[2], lds[3])), carried_q);
-        if (g <= s.families) store_there(s.q_start_of + g, q0);
-        if (g < s.families) {
-            const int missing = load_there(s.missing + g);
-            s.first_of[g] = min(first, a.n - 1);
-            store_there(s.len_of + g, missing == 0 ? 0 : (a.most_keys + 1 - missing) / kSharedTile * kSharedTile);
-            if (missing != 0) store_there(s.missing + g, 0);
-        }
-    }
-    __builtin_amdgcn_s_waitcnt(0x0F70);
-    __syncthreads();
+    const int near_family = tid < a.n ? load_there(s.family_of + tid) : -1, near_len = tid < a.n ? a.kv_lens[tid] : 0;            // (asked for beside the families)
     float own = 0.f, shared = 0.f;                  // tiles of 64 keys, for every 128 rows of the shared ones
+    for (int g = tid; g < s.families; g += 256) {
+        const int missing = load_there(s.missing + g), rows = (load_there(s.q_start_of + g + 1) - load_there(s.q_start_of + g)) * a.heads_per_kv;
+        const int tiles = missing == 0 ? 0 : (a.most_keys + 1 - missing) / kSharedTile;
+        if (g < kNear) len_near[g] = tiles * kSharedTile;
+        store_there(s.len_of + g, tiles * kSharedTile);
+        if (missing != 0) store_there(s.missing + g, 0);
+        shared += static_cast<float>(tiles) * static_cast<float>((rows + kWideRows - 1) / kWideRows);
+    }
+    if (s.families > kNear) __builtin_amdgcn_s_waitcnt(0x0F70);
+    __syncthreads();
     for (int r = tid; r < a.n; r += 256) {
-        const int g = load_there(s.family_of + r), of_family = g < 0 ? 0 : load_there(s.len_of + g), len = min(max(a.kv_lens[r], 0), a.most_keys);
+        const int g = r < 256 ? near_family : load_there(s.family_of + r), len = min(max(r < 256 ? near_len : a.kv_lens[r], 0), a.most_keys);
+        const int of_family = g < 0 ? 0 : g < kNear ? len_near[g] : load_there(s.len_of + g);
         s.shared_of[r] = of_family;
         own += static_cast<float>(len - min(of_family, len)) / kSharedTile;
-    }
-    for (int g = tid; g < s.families; g += 256) {
-        const int rows = (load_there(s.q_start_of + g + 1) - load_there(s.q_start_of + g)) * a.heads_per_kv;
-        shared += static_cast<float>(load_there(s.len_of + g) / kSharedTile) * static_cast<float>((rows + kWideRows - 1) / kWideRows);
     }
     const auto sum = [&](const float x) {
         const float y = last_lane(wave_prefix(x));
@@ -196,7 +201,7 @@ int launch(SharedArgs s, const TreeShape& shape, hipStream_t st) {
     const dim3 block(64 * kWaves);
     s.few_rows = shape.rows <= 32;
     s.at_once = D == 64 && shape.rows > 32 ? a.items * 3 / 2 : a.items;            // (three workgroups on a unit)
-    hipLaunchKernelGGL(shared_find_kernel, dim3(static_cast<unsigned>((a.n + 3) / 4)), dim3(256), 0, st, s);
+    hipLaunchKernelGGL(shared_find_kernel, dim3(static_cast<unsigned>((a.n + 3) / 4 + 1)), dim3(256), 0, st, s);
 
     TreeArgs f = a;                                 // families as requests
     f.q_start = s.q_start_of; f.kv_lens = s.len_of; f.first_of = s.first_of; f.n = s.families;
