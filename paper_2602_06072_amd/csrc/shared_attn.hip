@@ -166,26 +166,29 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedArgs s) {
     int rest = blockIdx.x;
     const auto take = [&](const int of) { const int x = rest % of; rest /= of; return x; };
     const int kvh = take(a.cache.Hkv), slice = take(a.slices), chunk = take(a.chunks), i = rest;
-    const int asked = a.q_start[i + 1] - a.q_start[i];
-    const int64_t q0 = min(max(static_cast<int64_t>(a.q_start[i]), int64_t{0}), a.total_q);
+    // (asked for at once, also what is not needed)
+    const int start = a.q_start[i], asked = a.q_start[i + 1] - start, of_family = a.shared_of[i], family = max(s.family_of[i], 0);
+    const int2 p = a.pieces_of[i];
+    const int2 pieces_of_family = s.pieces_of_family[family];
+    const int family_start = s.q_start_of[family], family_end = s.q_start_of[family + 1];
+    const int64_t q0 = min(max(static_cast<int64_t>(start), int64_t{0}), a.total_q);
     const int rows = static_cast<int>(min(static_cast<int64_t>(min(asked, a.max_q)), a.total_q - q0)) * a.heads_per_kv;
     const int chunk_rows = 1 << a.chunk_shift, here = min(rows - chunk * chunk_rows, chunk_rows);
     if (here <= 0) return;
-    const int2 p = a.pieces_of[i];
-    const bool shares = a.shared_of[i] > 0;
+    const bool shares = of_family > 0;
     if (!shares && p.x == 1) return;
-    const int chunks = (rows + chunk_rows - 1) / chunk_rows, family = max(s.family_of[i], 0);
-    const int2 f = shares ? s.pieces_of_family[family] : int2{0, 0};
-    const int64_t family_q0 = shares ? s.q_start_of[family] : 0;
-    const int family_rows = shares ? (s.q_start_of[family + 1] - static_cast<int>(family_q0)) * a.heads_per_kv : 1;
+    const int chunks = (rows + chunk_rows - 1) / chunk_rows;
+    const int2 f = shares ? pieces_of_family : int2{0, 0};
+    const int64_t family_q0 = shares ? family_start : 0;
+    const int family_rows = shares ? (family_end - family_start) * a.heads_per_kv : 1;
     const int family_chunks = (family_rows + kWideRows - 1) / kWideRows;
     for (int x = slice * 256 + threadIdx.x; x < here * (D / 4); x += a.slices * 256) {
         const int local = x / (D / 4), col = 4 * (x % (D / 4)), row = chunk * chunk_rows + local, t = a.by_r(row);
-        const int of_family = static_cast<int>(min(max((q0 - family_q0) * a.heads_per_kv + row, int64_t{0}), static_cast<int64_t>(family_rows - 1)));
+        const int row_of_family = static_cast<int>(min(max((q0 - family_q0) * a.heads_per_kv + row, int64_t{0}), static_cast<int64_t>(family_rows - 1)));
         const auto part = [&](const int piece, float& lse, floatx4& o) {
             const bool own = piece < p.x;
             const int64_t at_own = (static_cast<int64_t>(p.y + piece * chunks + chunk) * a.cache.Hkv + kvh) * chunk_rows + local;
-            const int64_t at_shared = (static_cast<int64_t>(f.y + (piece - p.x) * family_chunks + of_family / kWideRows) * a.cache.Hkv + kvh) * kWideRows + of_family % kWideRows;
+            const int64_t at_shared = (static_cast<int64_t>(f.y + (piece - p.x) * family_chunks + row_of_family / kWideRows) * a.cache.Hkv + kvh) * kWideRows + row_of_family % kWideRows;
             lse = own ? a.part_lse[at_own] : s.family_lse[at_shared];
             o = *reinterpret_cast<const floatx4*>(own ? a.part_o + at_own * D + col : s.family_o + at_shared * D + col);
         };
