@@ -52,8 +52,19 @@ __device__ __forceinline__ void load_refs(const int32_t* refs, const int64_t b, 
 }
 
 // ------------------------------------------------------------------ a new batch out of rows of the old one
-// One wave for every new request, one for every old one.  Bound by the way there, three loads one behind the other and the additions: 2 to 8 forks of
-// each of 64 requests of 200 to 6000 tokens 7.2 us, four requests forked twice 2.6.
+// One wave for kOfRow entries of every new request (and as many again, gridDim.y times that further on), one for those of every old one.  Bound by the way there, three loads
+// one behind the other and the additions: 2 to 8 forks of each of 64 requests of 200 to 6000 tokens 6.5 us, four requests forked twice 2.5 (a wave for a whole row 7.5 and 2.6, and 6 requests of 1000 pages renamed 20 us instead of 5).
+constexpr int kAtOnce = 4, kOfRow = kAtOnce * kWave;
+template <class Each>
+__device__ __forceinline__ void for_entries(const int32_t* row, const int pages, Each each) {       // each(entry's number, block)
+    for (int64_t j0 = static_cast<int64_t>(blockIdx.y) * kOfRow + (threadIdx.x & 63); j0 < pages; j0 += static_cast<int64_t>(gridDim.y) * kOfRow) {
+        int b[kAtOnce];
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e) b[e] = row[min(j0 + e * kWave, static_cast<int64_t>(pages) - 1)];
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e) if (j0 + e * kWave < pages) each(j0 + e * kWave, b[e]);
+    }
+}
 __global__ __launch_bounds__(256) void pages_select_kernel(PagesSelectArgs a) {
     const int lane = threadIdx.x & 63;
     const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
@@ -64,21 +75,17 @@ __global__ __launch_bounds__(256) void pages_select_kernel(PagesSelectArgs a) {
         const bool there = s >= 0 && s < a.n;
         const int len = there ? static_cast<int>(min(static_cast<int64_t>(max(a.lens[s], 0)), most)) : 0;
         const int pages = there ? min(static_cast<int>((static_cast<int64_t>(len) + a.page - 1) / a.page), held(s)) : 0;
-        const int32_t* row = a.table + static_cast<int64_t>(there ? s : 0) * a.max_blocks;
         int32_t* to = a.new_table + static_cast<int64_t>(i) * a.max_blocks;
-        for (int j = lane; j < pages; j += kWave) {
-            const int b = row[j];
+        for_entries(a.table + static_cast<int64_t>(there ? s : 0) * a.max_blocks, pages, [&](const int64_t j, const int b) {
             to[j] = b;
             if (is_block(b, a.num_blocks)) atomicAdd(a.refs + b, 1);
-        }
-        if (lane == 0) { a.new_lens[i] = len; a.new_pages[i] = pages; }
+        });
+        if (lane == 0 && blockIdx.y == 0) { a.new_lens[i] = len; a.new_pages[i] = pages; }
     } else if (unit - a.n_new < a.n) {
-        const int i = static_cast<int>(unit - a.n_new), pages = held(i);
-        const int32_t* row = a.table + static_cast<int64_t>(i) * a.max_blocks;
-        for (int j = lane; j < pages; j += kWave) {
-            const int b = row[j];
+        const int i = static_cast<int>(unit - a.n_new);
+        for_entries(a.table + static_cast<int64_t>(i) * a.max_blocks, held(i), [&](int64_t, const int b) {
             if (is_block(b, a.num_blocks)) atomicAdd(a.refs + b, -1);
-        }
+        });
     }
 }
 
@@ -271,8 +278,8 @@ __global__ __launch_bounds__(256) void pages_count_kernel(PagesCompactArgs a) {
     const int used = used_in_segment(a.refs, first, min(first + kSegment, static_cast<int64_t>(a.num_blocks)), lds);
     if (threadIdx.x == 0) a.used_of[static_cast<int64_t>(blockIdx.x) * PagesWorkspace::kWords] = used;
 }
-// Three launches, bound by the ways to what the one in front has written: 300 requests on a pool of which 24000 blocks move 4.5, 5.0 and 7.5 us (the tables' 4 bytes an
-// entry, one load behind the other, in the last), 6 requests 2.2, 4.0 and 2.5.
+// Three launches, bound by the ways to what the one in front has written: 300 requests on a pool of which 24000 blocks move 4.6, 5.1 and 5.4 us (the tables' 4 bytes an
+// entry, one load behind the other, in the last), 6 requests 2.5, 3.9 and 2.8.
 //
 // Every workgroup has its segment's blocks, and finds from all segments' counts how many are in use, in front of it and in front of block U.
 __global__ __launch_bounds__(256) void pages_move_kernel(PagesCompactArgs a) {
@@ -316,60 +323,77 @@ __global__ __launch_bounds__(256) void pages_move_kernel(PagesCompactArgs a) {
         before += in_use ? 1 : 0;
     }
 }
-// A wave for the entries of a request, or for the counts of 64 blocks that moved
+// A wave for kOfRow entries of a request (as above), or for the counts of 64 blocks that moved
 __global__ __launch_bounds__(256) void pages_rename_kernel(PagesCompactArgs a) {
     const int lane = threadIdx.x & 63;
     const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
     if (unit >= a.n) {
+        if (blockIdx.y > 0) return;
         const int64_t k = (unit - a.n) * kWave + lane;
         if (k < a.max_moves && a.copy_src[k] >= 0) a.new_refs[a.copy_dst[k]] = a.refs[a.copy_src[k]];
         return;
     }
     const int pages = min(max(a.pages[unit], 0), a.max_blocks);
     const int64_t row = unit * a.max_blocks;
-    for (int j = lane; j < pages; j += kWave) {
-        const int b = a.table[row + j], to = is_block(b, a.num_blocks) ? a.to[place_of(b)] : b;
-        a.new_table[row + j] = is_block(b, a.num_blocks) && to < 0 ? a.copy_dst[-1 - to] : to;
+    for (int64_t j0 = static_cast<int64_t>(blockIdx.y) * kOfRow + lane; j0 < pages; j0 += static_cast<int64_t>(gridDim.y) * kOfRow) {
+        int b[kAtOnce], to[kAtOnce];
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e) b[e] = a.table[row + min(j0 + e * kWave, static_cast<int64_t>(pages) - 1)];
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e) to[e] = is_block(b[e], a.num_blocks) ? a.to[place_of(b[e])] : 0;
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e) to[e] = !is_block(b[e], a.num_blocks) ? b[e] : to[e] < 0 ? a.copy_dst[-1 - to[e]] : to[e];
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e) if (j0 + e * kWave < pages) a.new_table[row + j0 + e * kWave] = to[e];
     }
 }
 
 // ------------------------------------------------------------------ copies of blocks
-// bytes [part / parts ..) of an array of a block, 16 at a time
-__device__ __forceinline__ void copy_block(void* to, const void* from, const int64_t dst, const int64_t src, const int64_t bytes, const int part, const int parts) {
-    const u32x4* x = reinterpret_cast<const u32x4*>(static_cast<const char*>(from) + src * bytes);
-    u32x4* y = reinterpret_cast<u32x4*>(static_cast<char*>(to) + dst * bytes);
-    const int64_t words = bytes / 16, each = (words + parts - 1) / parts, end = min(words, (part + 1) * each);
-    int64_t w = part * each + threadIdx.x;
-    for (; w + 3 * 256 < end; w += 4 * 256) {
-        u32x4 r[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) r[e] = x[w + e * 256];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[w + e * 256] = r[e];
-    }
-    for (; w < end; w += 256) y[w] = x[w];
-}
-// Bound by memory: 24000 blocks of 33 KB 302 to 317 us, 5.0 to 5.3 TB/s read and written together (a copy of 2 GiB: 4.9).
+// A wave for (block, keys or values, part of them); the scales go with the first part of the values.  Bound by memory: 24000 blocks of 33 KB (16 tokens of 8 heads of 128 columns in 8 bits)
+// 300 to 320 us, 5.0 to 5.3 TB/s read and written together (a copy of 2 GiB: 4.9).  By workgroups, a block or a part of it each: the same there, but 24000 blocks of 4 KB 37 us instead of 26
+// and of 2 KB 34 instead of 17.5, 32 blocks of 1 MB 19 instead of 13.  With parts for 1024 waves 32 of these 15; for 16384 1024 blocks of 33 KB 14.6 instead of 13.9.
 __global__ __launch_bounds__(256) void cache_copy_kernel(CacheCopyArgs a) {
     const CacheView &f = a.from, &t = a.to;
-    const int64_t rows = static_cast<int64_t>(f.Hkv) * f.page, units = static_cast<int64_t>(a.count) * a.parts;
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int64_t i = u / a.parts;
-        const int part = static_cast<int>(u - i * a.parts), src = a.src[i], dst = a.dst[i];
+    const int lane = threadIdx.x & 63;
+    const int64_t rows = static_cast<int64_t>(f.Hkv) * f.page, units = 2 * static_cast<int64_t>(a.count) * a.parts;
+    const int64_t words = rows * f.d * (f.f8 ? 1 : 2) / 16, each = (words + a.parts - 1) / a.parts, scales = f.f8 ? rows * 2 / 16 : 0;
+    for (int64_t u = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6); u < units; u += 4 * static_cast<int64_t>(gridDim.x)) {
+        const int64_t pair = u / a.parts, i = pair >> 1, part = u - pair * a.parts;
+        const bool values = pair & 1;
+        const int src = a.src[i], dst = a.dst[i];
         if (src < 0 || src >= f.num_blocks || dst < 0 || dst >= t.num_blocks || (src == dst && f.k == t.k)) continue;
-        const int64_t bytes = rows * f.d * (f.f8 ? 1 : 2);
-        copy_block(t.k, f.k, dst, src, bytes, part, a.parts);
-        copy_block(t.v, f.v, dst, src, bytes, part, a.parts);
-        if (f.f8) copy_block(t.scales, f.scales, dst, src, rows * 2, part, a.parts);
+        const u32x4* x = static_cast<const u32x4*>(values ? f.v : f.k) + src * words;
+        u32x4* y = static_cast<u32x4*>(values ? t.v : t.k) + dst * words;
+        if (values && part == 0) {
+            const u32x4* xs = reinterpret_cast<const u32x4*>(f.scales) + src * scales;
+            u32x4* ys = reinterpret_cast<u32x4*>(t.scales) + dst * scales;
+            for (int64_t w = lane; w < scales; w += 64) ys[w] = xs[w];
+        }
+        const int64_t end = min(words, (part + 1) * each);
+        int64_t w = part * each + lane;
+        constexpr int AT_ONCE = 4;
+        for (; w + (AT_ONCE - 1) * 64 < end; w += AT_ONCE * 64) {
+            u32x4 r[AT_ONCE];
+#pragma unroll
+            for (int e = 0; e < AT_ONCE; ++e) r[e] = x[w + e * 64];
+#pragma unroll
+            for (int e = 0; e < AT_ONCE; ++e) y[w + e * 64] = r[e];
+        }
+        u32x4 r[AT_ONCE - 1];
+#pragma unroll
+        for (int e = 0; e < AT_ONCE - 1; ++e) if (w + e * 64 < end) r[e] = x[w + e * 64];
+#pragma unroll
+        for (int e = 0; e < AT_ONCE - 1; ++e) if (w + e * 64 < end) y[w + e * 64] = r[e];
     }
 }
 
 unsigned groups_of(const int64_t units, const int64_t each) { return static_cast<unsigned>((units + each - 1) / each); }
+unsigned parts_of_row(const int max_blocks) { return groups_of(max_blocks < 64 * kOfRow ? max_blocks : 64 * kOfRow, kOfRow); }
 
 }  // namespace
 
 int launch_pages_select(const PagesSelectArgs& a, void* stream) {
-    hipLaunchKernelGGL(pages_select_kernel, dim3(groups_of(static_cast<int64_t>(a.n) + a.n_new, 4)), dim3(256), 0, static_cast<hipStream_t>(stream), a);
+    hipLaunchKernelGGL(pages_select_kernel, dim3(groups_of(static_cast<int64_t>(a.n) + a.n_new, 4), parts_of_row(a.max_blocks)), dim3(256), 0, static_cast<hipStream_t>(stream), a);
     return static_cast<int>(hipGetLastError());
 }
 
@@ -391,16 +415,17 @@ int launch_pages_compact(const PagesCompactArgs& a, void* stream) {
     hipLaunchKernelGGL(pages_count_kernel, dim3(segments), dim3(256), 0, st, a);
     hipLaunchKernelGGL(pages_move_kernel, dim3(segments), dim3(256), 0, st, a);
     const int64_t waves = a.n + (static_cast<int64_t>(a.max_moves) + kWave - 1) / kWave;
-    if (waves > 0) hipLaunchKernelGGL(pages_rename_kernel, dim3(groups_of(waves, 4)), dim3(256), 0, st, a);
+    if (waves > 0) hipLaunchKernelGGL(pages_rename_kernel, dim3(groups_of(waves, 4), a.max_blocks > 0 ? parts_of_row(a.max_blocks) : 1), dim3(256), 0, st, a);
     return static_cast<int>(hipGetLastError());
 }
 
 int launch_cache_copy(CacheCopyArgs a, void* stream) {
-    // (us a call with 1, 4 and 8 parts: 32 blocks of 33 KB, 16 tokens of 8 heads of 128 columns in 8 bits, 3.4, 3.2 and 3.2; 512 of them 11.6, 10.9 and 12.7; 1024 14.1, 14.4 and
-    // 19.5; 4096 42, 48 and 66; in bf16 4.9, 4.4 and 3.8; 17.5, 17.4 and 17.2; 24, 24 and 24; 112, 93 and 110)
-    a.parts = a.count <= 512 ? 4 : 1;
-    const int64_t units = static_cast<int64_t>(a.count) * a.parts;
-    hipLaunchKernelGGL(cache_copy_kernel, dim3(static_cast<unsigned>(units < 4096 ? units : 4096)), dim3(256), 0, static_cast<hipStream_t>(stream), a);
+    const int64_t words = static_cast<int64_t>(a.from.Hkv) * a.from.page * a.from.d * (a.from.f8 ? 1 : 2) / 16;
+    // parts: waves for the machine, of 256 words and more each
+    const int64_t pairs = 2 * static_cast<int64_t>(a.count), parts = (4096 + pairs - 1) / pairs, most = (words + 255) / 256;
+    a.parts = static_cast<int>(parts < most ? parts : most);
+    const int64_t groups = (pairs * a.parts + 3) / 4;
+    hipLaunchKernelGGL(cache_copy_kernel, dim3(static_cast<unsigned>(groups < 65536 ? groups : 65536)), dim3(256), 0, static_cast<hipStream_t>(stream), a);
     return static_cast<int>(hipGetLastError());
 }
 

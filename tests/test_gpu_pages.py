@@ -95,6 +95,20 @@ def test_steps_of_forking_and_growing(n, most, blocks, page, longest, extra, tig
     assert (b.refs[:used] > 0).all() and not b.refs[used:].any()
 
 
+def test_rows_of_many_entries():
+    rng = np.random.default_rng(6)
+    b = Batch(rng, 3, 33001, 70000, 16, 16 * 33001)
+    b.lens[:], b.pages[:] = np.minimum(b.lens, [16 * 33001, 16 * 20000 - 5, 16 * 255]), np.minimum(b.pages, [33001, 20000, 255])
+    b.refs[:] = 0
+    for i in range(3):
+        np.add.at(b.refs, b.table[i, :b.pages[i]], 1)
+    ws = pk.new_pages_workspace(70000)
+    b.select([1, 0, 1, 2])
+    b.reserve(np.array([40, 0, 700, 3], np.int32), ws)
+    b.select([3, 0, 2])
+    b.compact(50000, ws, in_place=True)
+
+
 def test_a_page_stays_with_the_last_of_its_holders():
     page, ws = 16, pk.new_pages_workspace(64)
     for n, writers in ((5, [0, 1, 2, 3, 4]), (5, [1, 2]), (5, [4]), (2000, list(range(2000)))):
