@@ -74,14 +74,14 @@ __device__ __forceinline__ Raw<F32> load_vector(const void* base, const int64_t 
     return whole ? load_raw<F32>(base, row_at + at) : load_last<F32>(base, row_at, at, vocab);
 }
 // each(four logits, number of the first one among the sixteen): for code that is short (a launch of little work waits for its instructions, too), which four logits
-// at a time keep as busy as sixteen.  NaN becomes -inf, inf the largest number.
-template <bool F32, int UNROLL = 1, class Each>
+// at a time keep as busy as sixteen.  NaN becomes -inf, inf the largest number, but with AS_IS.
+template <bool F32, int UNROLL = 1, bool AS_IS = false, class Each>
 __device__ __forceinline__ void by_four(Raw<F32> r, Each each) {
 #pragma unroll UNROLL
     for (int e = 0; e < kVector; e += 4) {
         float x[4];
 #pragma unroll
-        for (int n = 0; n < 4; ++n) x[n] = plain_logit(logit_of<F32>(r, n));
+        for (int n = 0; n < 4; ++n) x[n] = AS_IS ? logit_of<F32>(r, n) : plain_logit(logit_of<F32>(r, n));
         each(x, e);
 #pragma unroll
         for (int n = 0; n + (F32 ? 4 : 2) < static_cast<int>(sizeof r.w / 4); ++n) r.w[n] = r.w[n + (F32 ? 4 : 2)];
@@ -122,8 +122,9 @@ __device__ __forceinline__ double exp2_of(const double y) {
     p = fma(p, f, 1.0);
     return __builtin_amdgcn_ldexp(p, __double2loint(t));
 }
-// weight of a logit relative to that of `ref`; per: log2 e / temperature
+// weight of a logit relative to that of `ref`; that of a logit of 0 and less than inf, the same to the last bit where ref is 0
 __device__ __forceinline__ double weight_of(const float x, const float ref, const double per) { return exp2_of((static_cast<double>(x) - static_cast<double>(ref)) * per); }
+__device__ __forceinline__ double weight_of(const float x, const double per) { return exp2_of(static_cast<double>(x) * per); }
 constexpr double kLog2e64 = 1.4426950408889634074;
 
 // Temperature of a request; 0: the largest logit is taken
@@ -228,9 +229,10 @@ __device__ __forceinline__ void add_weights(RowPart& y, const Raw<F32>& r, const
         }
     }
     double sums[2] = {};
-    if (HOW == kFast && __all(y.top == 0.f && !odd)) {             // (as nearly always: a subtraction less)
+    const bool near = __all(y.top == 0.f && !odd);  // (as nearly always: a subtraction less)
+    if (HOW == kFast && near) {
 #pragma unroll
-        for (int e = 0; e < kVector; ++e) sums[e % 2] += exp2_of(static_cast<double>(logit_of<F32>(r, e)) * per);
+        for (int e = 0; e < kVector; ++e) sums[e % 2] += weight_of(logit_of<F32>(r, e), per);
     } else {
         by_four<F32>(r, [&](const float (&x)[4], int) {
 #pragma unroll
@@ -305,35 +307,63 @@ __global__ __launch_bounds__(kThreads, F32 ? 5 : 6) void verify_rows_kernel(Veri
     }
 }
 
-// Weights that are left of a row: max(P - c Q, 0)
+// Weights that are left of a row: max(P - c Q, 0).  `near`: both rows' sums are relative to logits of 0, and neither row has an inf (weights of less than 2^500 with such a
+// scale); then a weight is max(e^x - ratio e^y, 0) times 1 / sum.
 struct LeftWeight {
     double per, c, of_target, of_draft;             // 1 / sums of the rows, relative to
     float top, draft_top;
-    __device__ __forceinline__ double target(const float x) const { return of(x, top, of_target); }
-    __device__ __forceinline__ double draft(const float x) const { return of(x, draft_top, of_draft); }
-    __device__ __forceinline__ double of(const float x, const float ref, const double share) const { return share * weight_of(x, ref, per); }
-    __device__ __forceinline__ double operator()(const float x, const float y) const { return fmax(target(x) - c * draft(y), 0.0); }
+    double ratio;
+    bool near;
+    __device__ __forceinline__ void set() {         // (behind any change)
+        near = top == 0.f && (c == 0 || draft_top == 0.f) && of_target > 0 && per >= 1e-30;
+        ratio = c == 0 ? 0.0 : c * of_draft / of_target;
+    }
+    __device__ __forceinline__ double target(const float x) const { return of_target * weight_of(x, top, per); }
+    __device__ __forceinline__ double draft(const float x) const { return of_draft * weight_of(x, draft_top, per); }
+    __device__ __forceinline__ double left(const float x, const float y) const {
+        return near ? of_target * fmax(fma(-ratio, weight_of(y, per), weight_of(x, per)), 0.0) : fmax(target(x) - c * draft(y), 0.0);
+    }
 };
 
 // Sum of what is left of sixteen tokens, the first of them number `begin`
 template <bool F32, int UNROLL = 1>
 __device__ __forceinline__ double left_of(const Raw<F32>& p, Raw<F32> q, const bool of_two, const LeftWeight& w, const int begin, const int* list, const int removed) {
     double sum = 0;
-    by_four<F32, UNROLL>(p, [&](const float (&x)[4], const int e) {
+    const auto add = [&](double (&v)[4], const int e) {
+        for (int r = 0; r < removed; ++r)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) v[n] = list[r] == begin + e + n ? 0.0 : v[n];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) sum += v[n];
+    };
+    const auto next_of_q = [&] {
+#pragma unroll
+        for (int n = 0; n + (F32 ? 4 : 2) < static_cast<int>(sizeof q.w / 4); ++n) q.w[n] = q.w[n + (F32 ? 4 : 2)];
+    };
+    if (w.near) {
+        by_four<F32, UNROLL, true>(p, [&](const float (&x)[4], const int e) {
+            double v[4];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) v[n] = weight_of(x[n], w.per);
+            if (of_two) {
+#pragma unroll
+                for (int n = 0; n < 4; ++n) v[n] = fmax(fma(-w.ratio, weight_of(logit_of<F32>(q, n), w.per), v[n]), 0.0);
+                next_of_q();
+            }
+            add(v, e);
+        });
+        return w.of_target * sum;
+    }
+    by_four<F32>(p, [&](const float (&x)[4], const int e) {
         double v[4];
 #pragma unroll
         for (int n = 0; n < 4; ++n) v[n] = w.target(x[n]);
         if (of_two) {
 #pragma unroll
             for (int n = 0; n < 4; ++n) v[n] = fmax(v[n] - w.c * w.draft(plain_logit(logit_of<F32>(q, n))), 0.0);
-#pragma unroll
-            for (int n = 0; n + (F32 ? 4 : 2) < static_cast<int>(sizeof q.w / 4); ++n) q.w[n] = q.w[n + (F32 ? 4 : 2)];
+            next_of_q();
         }
-        for (int r = 0; r < removed; ++r)
-#pragma unroll
-            for (int n = 0; n < 4; ++n) v[n] = list[r] == begin + e + n ? 0.0 : v[n];
-#pragma unroll
-        for (int n = 0; n < 4; ++n) sum += v[n];
+        add(v, e);
     });
     return sum;
 }
@@ -399,6 +429,7 @@ __global__ __launch_bounds__(THREADS) void verify_choice_kernel(VerifyArgs a) {
         gone |= uint64_t{1} << s;
         if (!drawn) { Z -= before ? 0.0 : px; continue; }
         w.c += Z;
+        w.set();
         if (HOW == kCoarse || left == 0) break;     // (what is left is summed up only for a sibling's sake)
         double sum = 0;
 #pragma unroll 1
@@ -533,7 +564,8 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
             if (wave == 0 && (gone >> lane & 1)) list[__popcll(gone & ((uint64_t{1} << lane) - 1))] = a.tokens[t.q0 + lane];
             __syncthreads();
         }
-        w = {per, c.c, kind == kRemoved ? 1.0 : c.of_target, c.of_draft, c.top, c.draft_top};
+        w = {per, kind == kResidual ? c.c : 0.0, kind == kRemoved ? 1.0 : c.of_target, c.of_draft, c.top, c.draft_top};
+        w.set();
     }
 
     const int spans = a.shape.spans, rounds = a.shape.span_rounds;                 // rounds: times 1024 tokens of a span
@@ -590,7 +622,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
         if (tid == 0) a.next_token[i] = all.top == -INFINITY ? -1 : all.at;
         return;
     }
-    if (kind == kPlain) { w.top = all.top; w.of_target = 1.0; }
+    if (kind == kPlain) { w.top = all.top; w.of_target = 1.0; w.c = 0; w.set(); }
     const double goal = fmin(fmax(static_cast<double>(a.sample_u[i]), 0.0), 1.0) * all.sum;        // (NaN: 0)
     // The first span with a cumulative sum over the goal; the last one with a weight where rounding leaves none.  The same then for vectors and tokens.
     {
@@ -635,8 +667,8 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
     const int n = vector + lane;
     double weight = 0;
     if (lane < kVector && vector >= 0 && n < a.vocab) {
-        weight = w.target(load_logit<F32>(a.target, target_at + n));
-        if (kind == kResidual) weight = fmax(weight - w.c * w.draft(load_logit<F32>(a.draft, draft_at + n)), 0.0);
+        const float x = load_logit<F32>(a.target, target_at + n);
+        weight = kind == kResidual ? w.left(x, load_logit<F32>(a.draft, draft_at + n)) : w.target(x);
         for (int r = 0; r < removed; ++r) weight = list[r] == n ? 0.0 : weight;
     }
     const double upto = before + sum_to_here(weight);
