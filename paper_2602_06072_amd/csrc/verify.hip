@@ -369,9 +369,9 @@ __device__ __forceinline__ double left_of(const Raw<F32>& p, Raw<F32> q, const b
 }
 
 // What a token with children decides: a workgroup for (token, request), every wave the same (a lane has a token).  Without sums of what is left 6 us, loads one behind the
-// other; each of them is a pass over two rows by one unit, 64000 weights in 10 us, and a token's siblings need them one after the other, which bounds the launch for trees.
+// other; each of them is a pass over two rows by one unit, 64000 weights in 8 us, and a token's siblings need them one after the other, which bounds the launch for trees.
 // THREADS: where sums of what is left are to be expected (a mask and a draft), 512, as the one workgroup of a token waits for its loads: 16 trees of 16 to 48 tokens, 32000
-// logits of 32 bits, 40 us (256: 48, 1024: 41).  Without such sums 256, which begin sooner.
+// logits of 32 bits, 40 us (256: 48, 1024: 41; 36 since a weight takes fewer instructions).  Without such sums 256, which begin sooner.
 template <bool F32, Sums64 HOW, int THREADS>
 __global__ __launch_bounds__(THREADS) void verify_choice_kernel(VerifyArgs a) {
     __shared__ double lds[THREADS / 64];
@@ -526,7 +526,7 @@ __global__ __launch_bounds__(kThreads) void verify_sums_kernel(VerifyArgs a) {
 
 // The draw: sums of the row that a request's next token is drawn from, a wave for a span of it (up to 256 spans, of 1024 tokens where V is up to 2^18), a workgroup for some
 // of them; the last workgroup of a request to finish finds the span, one wave of it the vector in the span and the token in the vector.  Four rows of 32000 logits 9.2 us,
-// the chain of loads and the end; 200 rows of 50257 and 64 pairs of rows of 128256 25, of them 9 to 12 for the weights.
+// the chain of loads and the end; 200 rows of 50257 and 64 pairs of rows of 128256 24, of them 9 to 12 for the weights.
 enum { kPlain, kResidual, kRemoved };               // weights: P; max(P - c Q, 0); P without the tokens that were refused
 template <bool F32>
 __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
