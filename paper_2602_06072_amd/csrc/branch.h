@@ -53,11 +53,15 @@ int launch_cache_copy(CacheCopyArgs a, void* stream);
 // Sum of the weights of a piece of a row of logits, relative to that of the logit `top`; or the largest logit and where it stands first
 struct RowPart { double sum; float top; int32_t at; };
 
-// What a token with children decides: which of them stays (-1: none), c, and 1 / the sums of its rows with what they are relative to
+// What a token with children decides: which of them stays (-1: none), c, and 1 / the sums of its rows with what they are relative to.  Until then: workgroups that are done
+// (zero from the launch in front), and what each of them has of the first sum of what is left.
 struct VerifyChoice {
+    static constexpr int kMostParts = 8;
     int32_t token;
     double c, of_target, of_draft;
     float top, draft_top;
+    uint32_t arrived;
+    double left[kMostParts];
 };
 
 // How a launch cuts rows of logits: `pieces` of a row where all rows with children are looked at; where one of each request is, `spans`, each of span_rounds times 1024 elements,
@@ -87,6 +91,7 @@ struct VerifyArgs {
     RowPart* parts;                                 // [total_q][2][pieces]: of the target's rows, of the draft's
     RowPart* last_parts;                            // [n][last_stride]
     VerifyChoice* choices;                          // [total_q]
+    int choice_parts;                               // set by the launch: workgroups that share the first sum of what is left
 };
 int launch_draft_verify(const VerifyArgs& a, void* stream);
 

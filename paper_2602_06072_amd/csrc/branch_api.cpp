@@ -253,7 +253,7 @@ extern "C" int pk_draft_verify(const void* target, int64_t target_stride, const 
         const Words tm{"temperature", temperature, temperature ? n : 0}, mk{"tree_mask", tree_mask, tree_mask ? 2 * total_q : 0};
         PK_CHECK(check_apart({kp, kc, nt, ws}, {tk, qs, au, su, tm, mk}));
         VerifyArgs a{target, target_stride, draft, draft_stride, dtype == PK_F32, vocab, tokens, q_start, total_q, max_q > 0 ? max_q : 1, tree_mask, n, temperature,
-                     accept_u, sample_u, keep, max_keep, keep_count, next_token, shape, nullptr, nullptr, nullptr, nullptr};
+                     accept_u, sample_u, keep, max_keep, keep_count, next_token, shape, nullptr, nullptr, nullptr, nullptr, 1};
         if (max_q == 0) a.total_q = 0;              // no tokens: the outputs say so
         char* at = static_cast<char*>(workspace);
         a.arrived = reinterpret_cast<uint32_t*>(at);

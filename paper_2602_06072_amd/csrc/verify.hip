@@ -15,6 +15,8 @@
 // Probabilities and their sums have 64 bits: a draw is the place of a number between V borders, and with sums of 32 bits every tenth draw of a flat row of 100000
 // would fall on the other side of one.  Vector instructions of 64 bits run at the rate of those of 32 here; a weight takes about 20 of them, 90 cycles for 64 logits, and
 // at 1.7 10^12 logits a second at most that, not memory (3 10^12 of bf16), bounds the launches over rows in 64 bits; terms of 32 bits reach 2.3 10^12, 4.7 TB/s.
+#include <algorithm>
+
 #include "arrival.h"
 #include "branch.h"
 #include "common.hip.h"
@@ -304,6 +306,7 @@ __global__ __launch_bounds__(kThreads, F32 ? 5 : 6) void verify_rows_kernel(Veri
     if (threadIdx.x == 0) {
         RowPart& to = a.parts[(row * 2 + of_draft) * a.shape.pieces + piece];
         to.sum = y.sum; to.top = y.top; to.at = y.at;
+        if (HOW == kFast && !of_draft && piece == 0) a.choices[row].arrived = 0;
     }
 }
 
@@ -368,15 +371,23 @@ __device__ __forceinline__ double left_of(const Raw<F32>& p, Raw<F32> q, const b
     return sum;
 }
 
+struct LastCount {
+    uint32_t* x;
+    __device__ __forceinline__ uint32_t next(const uint32_t limit) const { return __builtin_amdgcn_atomic_inc32(x, limit, __ATOMIC_RELAXED, "agent"); }
+};
+
 // What a token with children decides: a workgroup for (token, request), every wave the same (a lane has a token).  Without sums of what is left 6 us, loads one behind the
 // other; each of them is a pass over two rows by one unit, 64000 weights in 8 us, and a token's siblings need them one after the other, which bounds the launch for trees.
 // THREADS: where sums of what is left are to be expected (a mask and a draft), 512, as the one workgroup of a token waits for its loads: 16 trees of 16 to 48 tokens, 32000
 // logits of 32 bits, 40 us (256: 48, 1024: 41; 36 since a weight takes fewer instructions).  Without such sums 256, which begin sooner.
-template <bool F32, Sums64 HOW, int THREADS>
-__global__ __launch_bounds__(THREADS) void verify_choice_kernel(VerifyArgs a) {
+// MORE: workgroups share the first of those sums, and the last one to finish goes on, where tokens are too few for the machine: 4 trees of 16 tokens, 128256 logits, 80 -> 53 us
+// for the whole call, one of 64 tokens 100 -> 69, 16 of 32 215 -> 199; 16 of 24 with 32000 logits 63 either way; with four parts for every token 16 trees of 16 to 48 73 -> 76.
+template <bool F32, Sums64 HOW, int THREADS, bool MORE = false>
+__global__ __launch_bounds__(THREADS, MORE ? 4 : 1) void verify_choice_kernel(VerifyArgs a) {
     __shared__ double lds[THREADS / 64];
     __shared__ WaveParts parts_lds;
-    const int token = blockIdx.x, i = blockIdx.y, lane = threadIdx.x & 63;
+    __shared__ int last;
+    const int token = blockIdx.x, i = blockIdx.y, part = MORE ? blockIdx.z : 0, lane = threadIdx.x & 63;
     const Tree t = tree_of(a, i);
     if (!(t.inner >> token & 1)) return;
     const float warm = temperature_of(a, i);
@@ -409,6 +420,8 @@ __global__ __launch_bounds__(THREADS) void verify_choice_kernel(VerifyArgs a) {
         Z = 1;
     };
     begin_with();
+    bool together = MORE && drawn && __popcll(left) > 1;           // (none of the sums has been begun)
+    if (part > 0 && !together) return;
     while (left != 0) {
         const int s = __builtin_ctzll(left);
         left &= left - 1;
@@ -432,15 +445,37 @@ __global__ __launch_bounds__(THREADS) void verify_choice_kernel(VerifyArgs a) {
         w.set();
         if (HOW == kCoarse || left == 0) break;     // (what is left is summed up only for a sibling's sake)
         double sum = 0;
+        constexpr int STEP = THREADS * kVector;
 #pragma unroll 1
-        for (int at = static_cast<int>(threadIdx.x) * kVector; at < a.vocab; at += THREADS * kVector) {
+        for (int at = (together ? part * STEP : 0) + static_cast<int>(threadIdx.x) * kVector; at < a.vocab; at += together ? a.choice_parts * STEP : STEP) {
             int begin;
             const Raw<F32> vp = load_vector<F32>(a.target, row * a.target_stride, at, a.vocab, begin), vq = load_vector<F32>(a.draft, row * a.draft_stride, at, a.vocab, begin);
             sum += left_of<F32, 4>(vp, vq, true, w, begin, nullptr, 0);
         }
         Z = sum_of_all<THREADS>(sum, lds);
+        if (MORE && together) {
+            VerifyChoice& c = a.choices[row];
+            if (threadIdx.x == 0) {                // (decode_body.hip.h on the order of such stores and the count)
+                __hip_atomic_store(reinterpret_cast<uint64_t*>(c.left + part), static_cast<uint64_t>(__double_as_longlong(Z)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                __builtin_amdgcn_s_waitcnt(0x0F70);    // vmcnt(0)
+                last = arrives_last(LastCount{&c.arrived}, a.choice_parts);
+            }
+            __syncthreads();
+            if (last == 0) return;
+            together = false;
+            Z = 0;
+            for (int n = 0; n < a.choice_parts; ++n)
+                Z += __longlong_as_double(static_cast<long long>(__hip_atomic_load(reinterpret_cast<uint64_t*>(c.left + n), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)));
+        }
     }
-    if (threadIdx.x == 0) a.choices[row] = {choice, drawn && gone != 0 ? w.c : 0.0, w.of_target, w.of_draft, w.top, w.draft_top};
+    if (part > 0 && together) return;              // (a child stays, and no sum was needed)
+    if (threadIdx.x == 0) {
+        VerifyChoice& c = a.choices[row];
+        c.token = choice;
+        c.c = drawn && gone != 0 ? w.c : 0.0;
+        c.of_target = w.of_target; c.of_draft = w.of_draft;
+        c.top = w.top; c.draft_top = w.draft_top;
+    }
 }
 
 __device__ __forceinline__ double sum_to_here(double x) {
@@ -470,10 +505,6 @@ __device__ __forceinline__ Walk walk_of(const VerifyArgs& a, const Tree& t) {
     return w;
 }
 
-struct LastCount {
-    uint32_t* x;
-    __device__ __forceinline__ uint32_t next(const uint32_t limit) const { return __builtin_amdgcn_atomic_inc32(x, limit, __ATOMIC_RELAXED, "agent"); }
-};
 // Parts of a row for another workgroup of the launch (decode_body.hip.h on the order of such stores and the count)
 __device__ __forceinline__ void store_part(uint64_t* to, const RowPart& y) {
     __hip_atomic_store(to, static_cast<uint64_t>(__double_as_longlong(y.sum)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -677,6 +708,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
 }
 
 constexpr int64_t kCoarseLogits = int64_t{1} << 23;
+constexpr int64_t kChoices = 1024;                  // workgroups to be had for the choices of trees
 template <bool F32>
 int launch(const VerifyArgs& a, hipStream_t st) {
     const dim3 block(kThreads);
@@ -690,7 +722,12 @@ int launch(const VerifyArgs& a, hipStream_t st) {
             if (a.draft) hipLaunchKernelGGL((verify_sums_kernel<F32>), groups, block, 0, st, a);
         } else {
             hipLaunchKernelGGL((verify_rows_kernel<F32, kFast>), rows, block, 0, st, a);
-            if (a.mask) hipLaunchKernelGGL((verify_choice_kernel<F32, kFast, 512>), dim3(tokens, n), dim3(512), 0, st, a);
+            VerifyArgs b = a;
+            const int64_t steps = (a.vocab + 512 * kVector - 1) / (512 * kVector), each = kChoices / (a.total_q > 0 ? a.total_q : 1);
+            // (two or three parts of a row of few steps save what they cost: 16 trees of 16 to 48 tokens, 32000 logits, 73.1 us, with two 74.4)
+            b.choice_parts = each < 4 && steps < 8 ? 1 : static_cast<int>(std::min({steps, each, int64_t{VerifyChoice::kMostParts}}));
+            if (a.mask && b.choice_parts > 1) hipLaunchKernelGGL((verify_choice_kernel<F32, kFast, 512, true>), dim3(tokens, n, b.choice_parts), dim3(512), 0, st, b);
+            else if (a.mask) hipLaunchKernelGGL((verify_choice_kernel<F32, kFast, 512>), dim3(tokens, n), dim3(512), 0, st, a);
             else hipLaunchKernelGGL((verify_choice_kernel<F32, kFast, kThreads>), dim3(tokens, n), block, 0, st, a);
         }
     }

@@ -84,6 +84,17 @@ def test_chains_of_many_logits(dtype, spread):
     check(s, call(s, 3), 3)
 
 
+@pytest.mark.parametrize("dtype, sizes, vocab", [("bf16", [64], 130001), ("f32", [12, 3, 0, 20, 1], 70001), ("bf16", [2, 1, 9], 16385), ("bf16", [40] * 6, 66003), ("f32", [7], 8193)])
+def test_few_trees_with_long_rows(dtype, sizes, vocab):
+    """Tokens with siblings whose rows several workgroups share."""
+    s = make(vocab, sizes, vocab, dtype, True, True, spread=0.7)
+    for turn in range(3):
+        got = call(s)
+        check(s, got)
+        s["temperature"][turn % len(sizes)] = (0.0, 0.3, 1e-25)[turn]
+        s["accept"][1::2] = 0.9999                                 # (most are refused)
+
+
 @pytest.mark.parametrize("case", ["chain", "many", "lookup", "tree"])
 def test_choices_next_to_a_border(case):
     """u is the fp32 number next to the border, off it by 3e-8 or less (and by 1e-11 hardly ever): 64 bits decide."""
