@@ -648,6 +648,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
         all = greedy ? of_all<true>(mine, per, lds) : of_all<false>(mine, per, lds);
         if (kind == kPlain || all.sum > 0) break;
         kind = kPlain;
+        removed = 0;                                // (tokens that were refused have their weights again)
     }
     if (greedy || all.top == -INFINITY) {
         if (tid == 0) a.next_token[i] = all.top == -INFINITY ? -1 : all.at;

@@ -1,0 +1,48 @@
+"""Judging of drafted tokens where nothing is left of a row.  Whole numbers, which have to equal oracle/branch.py's."""
+import numpy as np
+import pytest
+import torch
+
+from tests.test_gpu_verify import call, check, make
+
+pytestmark = pytest.mark.gpu
+
+
+def with_few_tokens(seed, sizes, vocab, dtype, drawn, finite):
+    """Every row has logits of 0 at the places `finite`, of which every drafted token is one (in turns), and none elsewhere."""
+    s = make(seed, sizes, vocab, dtype, drawn, True)
+    s["target"][:] = -float("inf")
+    s["target"][:, finite] = 0.0
+    if drawn:
+        s["draft"] = s["target"].clone()
+    words = [1 | 2 << t for t in range(max(sizes) - 1)]            # all of them are children of the first
+    s["mask"] = np.concatenate([np.array(([1] + words)[:T], np.uint64) for T in sizes])
+    for a, T in zip(s["q_start"], sizes):
+        s["tokens"][a + 1:a + T] = [finite[t % len(finite)] for t in range(T - 1)]
+    return s
+
+
+@pytest.mark.parametrize("u", [1.0, float("nan")])
+@pytest.mark.parametrize("finite", [[17], [3, 250]])
+@pytest.mark.parametrize("vocab", [301, 50001])
+@pytest.mark.parametrize("dtype, drawn", [("bf16", False), ("f32", False), ("f32", True)])
+def test_refused_tokens_that_held_all_of_the_row(u, finite, vocab, dtype, drawn):
+    """1 > 1 * 1 and 1/2 > 1 * 1/2 are false, as anything over a NaN is: both are refused, nothing is left, and the token behind is drawn from the whole row.
+    (Logits of 0 have weights of 1 on both sides, so that these probabilities are exact.)"""
+    s = with_few_tokens(vocab, [3, 2, 5, 3, 1], vocab, dtype, drawn, finite)
+    s["accept"][:] = u
+    s["sample"][:] = [0.1, 0.9, 0.6, 0.4, 0.5]
+    got = call(s)
+    check(s, got)
+    assert set(got[2].tolist()) <= set(finite)
+    if len(finite) == 1 or u != u:
+        assert (got[1] == 1).all()
+
+
+def test_a_row_of_which_no_number_is_left_and_none_was():
+    s = with_few_tokens(1, [3, 1], 400, "bf16", False, [9])
+    s["target"][:] = -float("inf")
+    s["accept"][:] = 1.0
+    got = call(s)
+    check(s, got)
+    assert (got[2] == -1).all()
