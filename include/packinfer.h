@@ -768,8 +768,9 @@ int pk_shared_tree_attn(const pk_cache* cache, const void* q, const int32_t* q_s
  *             above -inf
  *   workspace device, 256-byte aligned, at least pk_draft_verify_workspace_bytes.
  *             ZERO-FILLED BEFORE ITS FIRST USE; every call leaves it ready for the
- *             next.  One workspace serves all calls for which it is large
- *             enough; the caller orders them.
+ *             next.  The size does not fall with n, total_q or vocab: one
+ *             workspace serves all calls of up to the sizes that it was made
+ *             for; the caller orders them.
  * With one token a request it draws from its logits.  Errors: PK_EINVAL;
  * PK_EUNSUPPORTED (max_q). */
 size_t pk_draft_verify_workspace_bytes(int32_t n, int64_t total_q, int32_t vocab);

@@ -731,7 +731,7 @@ def shared_tree_attn(cache: KvCache, q, q_start, max_q, tree_mask, block_table, 
 
 
 def new_verify_workspace(n, total_q, vocab, device="cuda"):
-    """Workspace of draft_verify for n requests with total_q tokens; zeros, as its first use asks for."""
+    """Workspace of draft_verify for up to n requests with up to total_q tokens and vocab logits; zeros, as its first use asks for."""
     nbytes = max(256, int(lib().pk_draft_verify_workspace_bytes(n, total_q, vocab)))
     return _torch.zeros(nbytes, dtype=_torch.uint8, device=device)
 

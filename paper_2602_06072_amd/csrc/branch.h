@@ -70,12 +70,25 @@ struct VerifyShape {
     int pieces, length;                             // length in elements, a multiple of kStep
     int spans, span_rounds, groups, group_spans, last_stride;
     static constexpr int kStep = 4096;              // elements that a workgroup takes at a time
+    static constexpr int kRows = 2048, kMostPieces = 64;           // pieces of all rows together, about; of a row (the lanes that put them together)
+    static constexpr int kSpan = 1024, kMostSpans = 256;           // elements of a round of a span; spans (the threads that put them together)
     static constexpr size_t kCountBytes = 65536 * 4;               // arrivals of a request's pieces, zero between calls: in front of everything, as many for every call
     static VerifyShape of(int64_t n, int64_t total_q, int32_t vocab);
-    size_t part_bytes(const int64_t total_q) const { return whole256(total_q * 2 * pieces * static_cast<int64_t>(sizeof(RowPart))); }
-    size_t last_bytes(const int64_t n) const { return whole256(n * last_stride * static_cast<int64_t>(sizeof(RowPart))); }
+    // Room for as much as any call of up to so many tokens, requests and logits takes, so that a workspace of the largest batch serves all smaller ones: `pieces` and
+    // `last_stride` fall where a row is cut into fewer, longer parts.  Rows have up to 2048 / total_q + 1 pieces, of a step and more, and up to 64; last_stride is up to 256
+    // spans of 1024 logits.
+    static size_t part_bytes(const int64_t total_q, const int32_t vocab) {
+        const int64_t steps = (vocab + kStep - 1) / kStep, each = total_q * (steps < kMostPieces ? steps : kMostPieces), all = kRows + total_q;
+        return whole256(2 * (each < all ? each : all) * static_cast<int64_t>(sizeof(RowPart)));
+    }
+    static size_t last_bytes(const int64_t n, const int32_t vocab) {
+        const int64_t spans = (vocab + kSpan - 1) / kSpan;
+        return whole256(n * (spans < 2 ? 2 : spans < kMostSpans ? spans : kMostSpans) * static_cast<int64_t>(sizeof(RowPart)));
+    }
     static size_t choice_bytes(const int64_t total_q) { return whole256(total_q * static_cast<int64_t>(sizeof(VerifyChoice))); }
-    size_t bytes(const int64_t n, const int64_t total_q) const { return kCountBytes + part_bytes(total_q) + last_bytes(n) + choice_bytes(total_q); }
+    static size_t bytes(const int64_t n, const int64_t total_q, const int32_t vocab) {
+        return kCountBytes + part_bytes(total_q, vocab) + last_bytes(n, vocab) + choice_bytes(total_q);
+    }
 
 private:
     static size_t whole256(const int64_t bytes) { return static_cast<size_t>((bytes + 255) / 256 * 256); }

@@ -217,7 +217,7 @@ extern "C" int pk_shared_tree_attn(const pk_cache* cache, const void* q, const i
 
 extern "C" size_t pk_draft_verify_workspace_bytes(int32_t n, int64_t total_q, int32_t vocab) {
     if (n < 0 || n > 65535 || total_q < 0 || total_q > kMostTokens || vocab <= 0 || vocab > kMostVocab) return 0;
-    return VerifyShape::of(n, total_q, vocab).bytes(n, total_q);
+    return VerifyShape::bytes(n, total_q, vocab);
 }
 
 extern "C" int pk_draft_verify(const void* target, int64_t target_stride, const void* draft, int64_t draft_stride, int dtype,
@@ -248,8 +248,9 @@ extern "C" int pk_draft_verify(const void* target, int64_t target_stride, const 
         const Words tk{"tokens", tokens, total_q}, qs{"q_start", q_start, n + 1}, au{"accept_u", accept_u, total_q}, su{"sample_u", sample_u, n};
         PK_CHECK(check_words({kp, kc, nt, tk, qs, au, su}));
         const VerifyShape shape = VerifyShape::of(n, total_q, vocab);
-        PK_CHECK(check_workspace(workspace, workspace_bytes, shape.bytes(n, total_q), "pk_draft_verify_workspace_bytes"));
-        const Words ws{"workspace", workspace, static_cast<int64_t>(shape.bytes(n, total_q) / 4)};
+        const size_t needed = VerifyShape::bytes(n, total_q, vocab);
+        PK_CHECK(check_workspace(workspace, workspace_bytes, needed, "pk_draft_verify_workspace_bytes"));
+        const Words ws{"workspace", workspace, static_cast<int64_t>(needed / 4)};
         const Words tm{"temperature", temperature, temperature ? n : 0}, mk{"tree_mask", tree_mask, tree_mask ? 2 * total_q : 0};
         PK_CHECK(check_apart({kp, kc, nt, ws}, {tk, qs, au, su, tm, mk}));
         VerifyArgs a{target, target_stride, draft, draft_stride, dtype == PK_F32, vocab, tokens, q_start, total_q, max_q > 0 ? max_q : 1, tree_mask, n, temperature,
@@ -259,8 +260,8 @@ extern "C" int pk_draft_verify(const void* target, int64_t target_stride, const 
         a.arrived = reinterpret_cast<uint32_t*>(at);
         at += VerifyShape::kCountBytes;
         a.parts = reinterpret_cast<RowPart*>(at);
-        a.last_parts = reinterpret_cast<RowPart*>(at + shape.part_bytes(total_q));
-        a.choices = reinterpret_cast<VerifyChoice*>(at + shape.part_bytes(total_q) + shape.last_bytes(n));
+        a.last_parts = reinterpret_cast<RowPart*>(at + VerifyShape::part_bytes(total_q, vocab));
+        a.choices = reinterpret_cast<VerifyChoice*>(at + VerifyShape::part_bytes(total_q, vocab) + VerifyShape::last_bytes(n, vocab));
         return launched(who, launch_draft_verify(a, stream));
     });
 }

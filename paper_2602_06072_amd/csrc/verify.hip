@@ -26,6 +26,7 @@ namespace {
 
 constexpr int kThreads = 256, kVector = 16, kStep = VerifyShape::kStep;
 static_assert(kStep == kThreads * kVector, "a step is a vector of every thread");
+static_assert(VerifyShape::kSpan == 64 * kVector && VerifyShape::kMostSpans == kThreads && VerifyShape::kMostPieces == 64, "lanes and threads that put parts together");
 constexpr float kMostLogit = 3.402823466e38f;
 
 // NaN becomes -inf, inf the largest number
@@ -742,13 +743,13 @@ VerifyShape VerifyShape::of(const int64_t n, const int64_t total_q, const int32_
     const auto up = [](const int64_t x, const int64_t by) { return (x + by - 1) / by; };
     const auto least = [](const int64_t x, const int64_t y) { return x < y ? x : y; };
     VerifyShape s;
-    // rows: workgroups for 2048 of them together, and no more than the lanes that put the pieces together
-    const int64_t steps = up(vocab, kStep), each = up(steps, least(least(2048 / (total_q > 0 ? total_q : 1) + 1, 64), steps));
+    // rows: workgroups for kRows of them together
+    const int64_t steps = up(vocab, kStep), each = up(steps, least(least(kRows / (total_q > 0 ? total_q : 1) + 1, kMostPieces), steps));
     s.length = static_cast<int>(each * kStep);
     s.pieces = static_cast<int>(up(steps, each));
-    // the draw: spans for the threads of a workgroup, workgroups of 4 spans and more, 1024 of them together
-    const int64_t thousands = up(vocab, 64 * kVector);
-    s.span_rounds = static_cast<int>(up(thousands, kThreads));
+    // the draw: workgroups of 4 spans and more, 1024 of them together
+    const int64_t thousands = up(vocab, kSpan);
+    s.span_rounds = static_cast<int>(up(thousands, kMostSpans));
     s.spans = static_cast<int>(up(thousands, s.span_rounds));
     s.group_spans = static_cast<int>(up(up(s.spans, least(1024 / (n > 0 ? n : 1) + 1, up(s.spans, 4))), 4) * 4);
     s.groups = static_cast<int>(up(s.spans, s.group_spans));

@@ -1,8 +1,9 @@
-"""Judging of drafted tokens where nothing is left of a row.  Whole numbers, which have to equal oracle/branch.py's."""
+"""Judging of drafted tokens where nothing is left of a row, and in a workspace of a larger batch.  Whole numbers, which have to equal oracle/branch.py's."""
 import numpy as np
 import pytest
 import torch
 
+from paper_2602_06072_amd import binding as pk
 from tests.test_gpu_verify import call, check, make
 
 pytestmark = pytest.mark.gpu
@@ -39,6 +40,18 @@ def test_refused_tokens_that_held_all_of_the_row(u, finite, vocab, dtype, drawn)
         assert (got[1] == 1).all()
 
 
+def quick(seed, sizes, vocab):
+    """A chain for each request, whose drafted tokens are the likeliest of the target's row in front of them, or any."""
+    rng = np.random.default_rng(seed)
+    total = sum(sizes)
+    target = torch.from_numpy(rng.normal(size=(total, vocab)).astype(np.float32) * 4).bfloat16()
+    tokens = rng.integers(0, vocab, total).astype(np.int32)
+    tokens[1:] = np.where(rng.random(total - 1) < 0.8, target.float().argmax(1)[:-1].numpy(), tokens[1:])
+    return dict(target=target, draft=None, vocab=vocab, tokens=tokens, q_start=np.concatenate([[0], np.cumsum(sizes)]).astype(np.int32), sizes=sizes, mask=None,
+                temperature=np.full(len(sizes), 0.4, np.float32), accept=rng.random(total).astype(np.float32), sample=rng.random(len(sizes)).astype(np.float32),
+                max_q=max(sizes))
+
+
 def test_a_row_of_which_no_number_is_left_and_none_was():
     s = with_few_tokens(1, [3, 1], 400, "bf16", False, [9])
     s["target"][:] = -float("inf")
@@ -46,3 +59,13 @@ def test_a_row_of_which_no_number_is_left_and_none_was():
     got = call(s)
     check(s, got)
     assert (got[2] == -1).all()
+
+
+@pytest.mark.parametrize("vocab, sizes, smaller", [(128256, [1] * 35 + [32], [[1] * 34 + [32], [2] * 3]), (32000, [8] * 257, [[8] * 256, [64] * 12]),
+                                                   (128256, [9] * 11 + [1], [[8] * 8, [1]]), (262145, [2, 3], [[1], [2, 2]])])
+def test_a_workspace_of_the_largest_batch_serves_smaller_ones(vocab, sizes, smaller):
+    ws = pk.new_verify_workspace(len(sizes), sum(sizes), vocab)
+    for x in [sizes] + smaller:
+        s = quick(vocab, x, vocab)
+        check(s, call(s, ws=ws))
+    assert not ws[:65536 * 4].any()                                # counts of arrivals: ready for the next call
