@@ -10,11 +10,11 @@
 //
 // Where a choice takes no sums of what is left (one child each, or no draft), the first sums have terms of 32 bits, which are near enough for nearly every choice (kCoarse), and
 // what the draw needs in 64 bits, the sums of one row of each request, is found in a launch in front of it (chains of 64 requests, 640 rows of 128256 logits: 73 us in
-// 64 bits, and 97 for the call).
+// 64 bits and 97 for the call, when a weight took 20 instructions).
 //
 // Probabilities and their sums have 64 bits: a draw is the place of a number between V borders, and with sums of 32 bits every tenth draw of a flat row of 100000
-// would fall on the other side of one.  Vector instructions of 64 bits run at the rate of those of 32 here; a weight takes about 20 of them, 90 cycles for 64 logits, and
-// at 1.7 10^12 logits a second at most that, not memory (3 10^12 of bf16), bounds the launches over rows in 64 bits; terms of 32 bits reach 2.3 10^12, 4.7 TB/s.
+// would fall on the other side of one.  Vector instructions of 64 bits run at the rate of those of 32 here; a weight takes about 22 of them, 100 cycles for 64 logits, and
+// at 1.6 10^12 logits a second at most that, not memory (3 10^12 of bf16), bounds the launches over rows in 64 bits; terms of 32 bits reach 2.4 10^12, 4.8 TB/s.
 #include <algorithm>
 
 #include "arrival.h"
@@ -109,19 +109,29 @@ __device__ __forceinline__ float load_logit(const void* base, const int64_t at) 
     return plain_logit(F32 ? static_cast<const float*>(base)[at] : bf16_bits_to_float(static_cast<const uint16_t*>(base)[at]));
 }
 
+// A constant in scalar registers.  Left alone, the compiler holds those of a single weight in vector registers over the loop that it stands in: twenty more, with which the
+// first sums in terms of 32 bits spill (chains of 64 requests 87.5 us instead of 84.5).
+__device__ __forceinline__ double scalar(double x) {
+    asm("" : "+s"(x));
+    return x;
+}
 // 2^y for y up to 1000; 0 below -1074 and for a NaN.  y = n + f with |f| <= 1/2: adding 1.5 2^52 leaves n in the low bits.  The polynomial has the least largest
-// relative error of its degree with p(0) = 1, 8.1e-13 (fitted to 2^f by least squares with weights that follow the error): equal logits of 0 count exactly.
+// relative error of its degree with p(0) = 1, 2.2e-16 (exchange of extremal points, 60 digits), so that what is left are roundings of 64 bits; equal logits of 0 count exactly.
+// (Degree 8, 8.1e-13, saves two instructions of 22: 81 us instead of 82.5 for chains of 64 requests, 74 instead of 79 for trees, 44.3 instead of 45.5 for looked-up tokens.  But a
+// number within 1e-13 of a border then falls to its other side.)
 __device__ __forceinline__ double exp2_of(const double y) {
     constexpr double kRound = 6755399441055744.0;
     const double in = fmax(y, -1100.0), t = in + kRound, f = in - (t - kRound);
-    double p = 0x1.61c4f0ed5f063p-20;
-    p = fma(p, f, 0x1.00d85341b87d0p-16);
-    p = fma(p, f, 0x1.430aa882ba307p-13);
-    p = fma(p, f, 0x1.5d874d06fe487p-10);
-    p = fma(p, f, 0x1.3b2ab5ed6fb84p-7);
-    p = fma(p, f, 0x1.c6b08dced3566p-5);
-    p = fma(p, f, 0x1.ebfbdff8ede86p-3);
-    p = fma(p, f, 0x1.62e42fef89d1ep-1);
+    double p = 0x1.e3a9046bc2ff4p-28;
+    p = fma(p, f, scalar(0x1.b671b2f14537ap-24));
+    p = fma(p, f, scalar(0x1.62c147a4afdfcp-20));
+    p = fma(p, f, scalar(0x1.ffcb58ca31191p-17));
+    p = fma(p, f, scalar(0x1.4309126c00bdfp-13));
+    p = fma(p, f, scalar(0x1.5d87fe9b8efd1p-10));
+    p = fma(p, f, scalar(0x1.3b2ab6fbd6d05p-7));
+    p = fma(p, f, scalar(0x1.c6b08d703e17ap-5));
+    p = fma(p, f, scalar(0x1.ebfbdff82c431p-3));
+    p = fma(p, f, scalar(0x1.62e42fefa3a12p-1));
     p = fma(p, f, 1.0);
     return __builtin_amdgcn_ldexp(p, __double2loint(t));
 }
@@ -290,8 +300,8 @@ __device__ __forceinline__ double sum_of_all(double x, double* lds) {
     return y;
 }
 
-// Sums of the rows of tokens with children: a workgroup for (piece, target or draft; token; request).  Chains of 64 requests (640 rows of 128256 logits) 35 us with terms of
-// 32 bits, 4.7 TB/s; 581 rows of 50257 logits that begin at any address 17, 3.5 TB/s; trees (612 rows of 32000 in fp32) in 64 bits 26.
+// Sums of the rows of tokens with children: a workgroup for (piece, target or draft; token; request).  Chains of 64 requests (640 rows of 128256 logits) 34 us with terms of
+// 32 bits, 4.8 TB/s; 581 rows of 50257 logits that begin at any address 16, 3.6 TB/s; trees (612 rows of 32000 in fp32) in 64 bits 27.
 template <bool F32, Sums64 HOW>
 __global__ __launch_bounds__(kThreads, F32 ? 5 : 6) void verify_rows_kernel(VerifyArgs a) {
     __shared__ WaveParts lds;
@@ -380,11 +390,12 @@ struct LastCount {
 // What a token with children decides: a workgroup for (token, request), every wave the same (a lane has a token).  Without sums of what is left 6 us, loads one behind the
 // other; each of them is a pass over two rows by one unit, 64000 weights in 8 us, and a token's siblings need them one after the other, which bounds the launch for trees.
 // THREADS: where sums of what is left are to be expected (a mask and a draft), 512, as the one workgroup of a token waits for its loads: 16 trees of 16 to 48 tokens, 32000
-// logits of 32 bits, 40 us (256: 48, 1024: 41; 36 since a weight takes fewer instructions).  Without such sums 256, which begin sooner.
+// logits of 32 bits, 40 us (256: 48, 1024: 41).  Without such sums 256, which begin sooner.
 // MORE: workgroups share the first of those sums, and the last one to finish goes on, where tokens are too few for the machine: 4 trees of 16 tokens, 128256 logits, 80 -> 53 us
 // for the whole call, one of 64 tokens 100 -> 69, 16 of 32 215 -> 199; 16 of 24 with 32000 logits 63 either way; with four parts for every token 16 trees of 16 to 48 73 -> 76.
+// (Both sides with weights of 20 instructions.)  Terms of 32 bits: registers for four workgroups a unit, looked-up tokens 46.9 -> 45.5.
 template <bool F32, Sums64 HOW, int THREADS, bool MORE = false>
-__global__ __launch_bounds__(THREADS, MORE ? 4 : 1) void verify_choice_kernel(VerifyArgs a) {
+__global__ __launch_bounds__(THREADS, MORE || HOW == kCoarse ? 4 : 1) void verify_choice_kernel(VerifyArgs a) {
     __shared__ double lds[THREADS / 64];
     __shared__ WaveParts parts_lds;
     __shared__ int last;
@@ -517,7 +528,7 @@ __device__ __forceinline__ RowPart load_part(const uint64_t* from) {
 }
 
 // In 64 bits, the sums of the rows that are drawn from as max(P - c Q, 0), where the choices had them in 32: workgroups as for the draw.  Up to 64 pairs of rows of
-// 128256 logits 19 us, 0.9 10^12 logits a second: half of it the way there and the end.
+// 128256 logits 20 us, 0.8 10^12 logits a second: half of it the way there and the end.
 template <bool F32>
 __global__ __launch_bounds__(kThreads) void verify_sums_kernel(VerifyArgs a) {
     __shared__ WaveParts lds;
@@ -557,11 +568,12 @@ __global__ __launch_bounds__(kThreads) void verify_sums_kernel(VerifyArgs a) {
 }
 
 // The draw: sums of the row that a request's next token is drawn from, a wave for a span of it (up to 256 spans, of 1024 tokens where V is up to 2^18), a workgroup for some
-// of them; the last workgroup of a request to finish finds the span, one wave of it the vector in the span and the token in the vector.  Four rows of 32000 logits 9.2 us,
-// the chain of loads and the end; 200 rows of 50257 and 64 pairs of rows of 128256 24, of them 9 to 12 for the weights.
+// of them; the last workgroup of a request to finish finds the span, one wave of it the vector in the span and the token in the vector.  Four rows of 32000 logits 9.7 us,
+// the chain of loads and the end; 200 rows of 50257 and 64 pairs of rows of 128256 25, of them 10 to 13 for the weights.  bf16: registers for four workgroups a unit (131
+// otherwise, three: chains of 64 requests 84.5 us instead of 82, looked-up tokens 49.5 instead of 47).
 enum { kPlain, kResidual, kRemoved };               // weights: P; max(P - c Q, 0); P without the tokens that were refused
 template <bool F32>
-__global__ __launch_bounds__(kThreads) void verify_draw_kernel(VerifyArgs a) {
+__global__ __launch_bounds__(kThreads, F32 ? 3 : 4) void verify_draw_kernel(VerifyArgs a) {
     __shared__ WaveParts lds;
     __shared__ double wave_sums[kThreads / 64], begin_of_span;
     __shared__ int list[kMostDrafts];
