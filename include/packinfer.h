@@ -771,6 +771,8 @@ int pk_shared_tree_attn(const pk_cache* cache, const void* q, const int32_t* q_s
  *             next.  The size does not fall with n, total_q or vocab: one
  *             workspace serves all calls of up to the sizes that it was made
  *             for; the caller orders them.
+ * No output overlaps an input, the workspace or another output (what lies between
+ * two rows of logits is none of them).
  * With one token a request it draws from its logits.  Errors: PK_EINVAL;
  * PK_EUNSUPPORTED (max_q). */
 size_t pk_draft_verify_workspace_bytes(int32_t n, int64_t total_q, int32_t vocab);

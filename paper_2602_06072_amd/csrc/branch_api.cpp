@@ -35,6 +35,18 @@ Refusal check_apart(const std::initializer_list<Words>& outputs, const std::init
     return {PK_OK, ""};
 }
 
+// Rows of logits, in bytes: what is between them is not theirs
+struct Rows { const char* name; const void* at; int64_t count, stride, length; };
+
+bool overlap(const Words& x, const Rows& r) {
+    if (x.count <= 0 || r.count <= 0) return false;
+    const uintptr_t first = reinterpret_cast<uintptr_t>(r.at), begin = reinterpret_cast<uintptr_t>(x.at), end = begin + static_cast<uintptr_t>(x.count) * 4;
+    if (end <= first) return false;
+    const int64_t from = begin > first ? static_cast<int64_t>(begin - first) : 0, to = static_cast<int64_t>(end - first);
+    const int64_t in = r.count > 1 ? from / r.stride : 0, row = in < r.count ? in : r.count - 1;      // the last row that begins at `from` or in front of it
+    return from < row * r.stride + r.length || (row + 1 < r.count && to > (row + 1) * r.stride);
+}
+
 Refusal check_pages(const int32_t n, const int32_t max_blocks, const int64_t num_blocks, const int32_t page_size) {
     if (n < 0 || n > 65535) return {PK_EINVAL, "need 0 <= n < 65536"};
     if (num_blocks <= 0 || num_blocks > kMostTokens) return {PK_EINVAL, "need 0 < num_blocks < 2^31"};
@@ -253,6 +265,10 @@ extern "C" int pk_draft_verify(const void* target, int64_t target_stride, const 
         const Words ws{"workspace", workspace, static_cast<int64_t>(needed / 4)};
         const Words tm{"temperature", temperature, temperature ? n : 0}, mk{"tree_mask", tree_mask, tree_mask ? 2 * total_q : 0};
         PK_CHECK(check_apart({kp, kc, nt, ws}, {tk, qs, au, su, tm, mk}));
+        const int64_t bytes = static_cast<int64_t>(size);
+        for (const Words& x : {kp, kc, nt, ws})
+            for (const Rows& r : {Rows{"target", target, total_q, target_stride * bytes, vocab * bytes}, Rows{"draft", draft, draft ? total_q : 0, draft_stride * bytes, vocab * bytes}})
+                if (overlap(x, r)) return refuse(who, {PK_EINVAL, std::string(x.name) + " overlaps " + r.name});
         VerifyArgs a{target, target_stride, draft, draft_stride, dtype == PK_F32, vocab, tokens, q_start, total_q, max_q > 0 ? max_q : 1, tree_mask, n, temperature,
                      accept_u, sample_u, keep, max_keep, keep_count, next_token, shape, nullptr, nullptr, nullptr, nullptr, 1};
         if (max_q == 0) a.total_q = 0;              // no tokens: the outputs say so

@@ -69,3 +69,22 @@ def test_a_workspace_of_the_largest_batch_serves_smaller_ones(vocab, sizes, smal
         s = quick(vocab, x, vocab)
         check(s, call(s, ws=ws))
     assert not ws[:65536 * 4].any()                                # counts of arrivals: ready for the next call
+
+
+def test_outputs_between_the_rows():
+    """Rows apart from one another leave room that is nobody's: outputs may be there."""
+    s = quick(3, [3, 1, 4, 2], 500)
+    room = torch.full((10, 540), float("nan"), device="cuda")
+    room[:, :500] = s["target"].float()
+    words = room.view(torch.int32)
+    flat = lambda row, n: words[row, 500:500 + n]  # noqa: E731
+    keep, count, after = flat(2, 16).view(4, 4), flat(0, 4), flat(9, 4)
+    dev = lambda x: torch.from_numpy(x).cuda()  # noqa: E731
+    pk.draft_verify(room[:, :500], None, dev(s["tokens"]), dev(s["q_start"]), 4, None, dev(s["temperature"]), dev(s["accept"]), dev(s["sample"]), keep, count, after,
+                    pk.new_verify_workspace(4, 10, 500))
+    torch.cuda.synchronize()
+    check(s, (keep.cpu().numpy(), count.cpu().numpy(), after.cpu().numpy()))
+    with pytest.raises(pk.PackInferError, match="keep_count overlaps target"):
+        pk.draft_verify(room[:, :500], None, dev(s["tokens"]), dev(s["q_start"]), 4, None, dev(s["temperature"]), dev(s["accept"]), dev(s["sample"]), keep,
+                        words[4, 497:501], after, pk.new_verify_workspace(4, 10, 500))
+    assert torch.equal(room[:, :500].cpu(), s["target"].float())
