@@ -646,7 +646,10 @@ int pk_kv_cache_keep(const pk_cache* cache, const int32_t* block_table, int32_t 
  *   block_table  device int32 [n][max_blocks]: the blocks of a request's pages
  *   lens         device int32 [n]: its tokens
  *   pages        device int32 [n]: entries of its row that it holds (at least
- *                those of its tokens; more where room was reserved)
+ *                those of its tokens; more where room was reserved, which is
+ *                its alone).  A request that is cut to fewer tokens behind a
+ *                fork still shares pages behind them: pk_kv_pages_select
+ *                gives them up, and has to before pk_kv_pages_reserve
  *   refs         device int32 [num_blocks]: how many requests hold a block;
  *                0: it is free.  A caller may count itself in for blocks that are
  *                to outlive the requests (a prefix that is kept).
@@ -668,8 +671,8 @@ int pk_kv_pages_select(const int32_t* block_table, const int32_t* lens, const in
 
 /* pk_kv_pages_reserve -- every request gets pages for lens[i] + grow[i] tokens (no
  * more than max_blocks of them), in the order of requests the free blocks of
- * the lowest numbers.  Where its next token goes to a page that holds tokens
- * and that others hold too, the page is replaced by a free block and noted for
+ * the lowest numbers.  Where its next token goes to a page that holds tokens of
+ * its own and that others hold too, the page is replaced by a free block and noted for
  * copying: copy_src[i] -> copy_dst[i] (-1: nothing to copy), its block before its
  * other new ones.  If all holders of such a page grow in this call, the one of
  * the highest number keeps it.

@@ -15,7 +15,7 @@ struct PagesSelectArgs {
 };
 int launch_pages_select(const PagesSelectArgs& a, void* stream);
 
-// A workspace of the page calls: for every 1024 blocks three times 1024 words and one more.  The first two thousand are zero between calls, and which words these are
+// A workspace of the page calls: for every 1024 blocks three times 1024 words and a cache line's worth for one more.  The first two thousand are zero between calls, and which words these are
 // does not depend on num_blocks: no call has its zeros where one for a smaller pool has written something else.
 struct PagesWorkspace {
     static constexpr int kSegment = 1024;           // blocks that a workgroup looks at
@@ -46,7 +46,7 @@ int launch_pages_compact(const PagesCompactArgs& a, void* stream);
 
 struct CacheCopyArgs {
     CacheView from, to; const int32_t* src; const int32_t* dst; int32_t count;
-    int parts;                                      // set by the launch: workgroups that share a block
+    int parts;                                      // set by the launch: waves that share a block's keys, and its values
 };
 int launch_cache_copy(CacheCopyArgs a, void* stream);
 
