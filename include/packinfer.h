@@ -646,10 +646,8 @@ int pk_kv_cache_keep(const pk_cache* cache, const int32_t* block_table, int32_t 
  *   block_table  device int32 [n][max_blocks]: the blocks of a request's pages
  *   lens         device int32 [n]: its tokens
  *   pages        device int32 [n]: entries of its row that it holds (at least
- *                those of its tokens; more where room was reserved, which is
- *                its alone).  A request that is cut to fewer tokens behind a
- *                fork still shares pages behind them: pk_kv_pages_select
- *                gives them up, and has to before pk_kv_pages_reserve
+ *                those of its tokens; more where room was reserved, or where it
+ *                was cut to fewer tokens)
  *   refs         device int32 [num_blocks]: how many requests hold a block;
  *                0: it is free.  A caller may count itself in for blocks that are
  *                to outlive the requests (a prefix that is kept).
@@ -674,7 +672,9 @@ int pk_kv_pages_select(const int32_t* block_table, const int32_t* lens, const in
  * the lowest numbers.  Where its next token goes to a page that holds tokens of
  * its own and that others hold too, the page is replaced by a free block and noted for
  * copying: copy_src[i] -> copy_dst[i] (-1: nothing to copy), its block before its
- * other new ones.  If all holders of such a page grow in this call, the one of
+ * other new ones.  Where tokens would go to a page behind its own ones that others hold too
+ * (it was cut to fewer tokens behind a fork), it gives that page and all behind it
+ * up and gets free blocks instead; what nobody holds any more is free from the next call on.  If all holders of such a page grow in this call, the one of
  * the highest number keeps it.
  *   served    device int32 [n]: 1, or 0 where blocks run out: from the first request on for
  *             which they do, none that needs one (or keeps a page that others

@@ -34,11 +34,16 @@ def pages_reserve(table, lens, pages, grow, refs, page):
     served, src, dst = np.zeros(n, np.int32), np.full(n, -1, np.int32), np.full(n, -1, np.int32)
 
     def wants(i):
-        """(page of the next token, pages held, pages wanted, whether a shared page would be written)"""
+        """(page of the next token, pages held (less those that are given up), pages wanted, whether a shared page would be written)"""
         length, g = min(max(int(lens[i]), 0), most * page), max(int(grow[i]), 0)
         has = min(max(int(pages[i]), 0), most)
         at = length // page
-        end = max(has, min(-(-(length + g) // page), most)) if g else has
+        wanted = min(-(-(length + g) // page), most) if g else 0
+        for j in range(-(-length // page), min(has, wanted)):      # a shared page without a token of the request, where tokens are to go: it is given up, with what is behind it
+            if 0 <= table[i, j] < len(refs) and held[table[i, j]] > 1:
+                has = j
+                break
+        end = max(has, wanted)
         b = table[i, at] if g and length % page and at < has else -1
         return at, has, end, 0 <= b < len(refs) and held[b] > 1
 
@@ -58,6 +63,9 @@ def pages_reserve(table, lens, pages, grow, refs, page):
         if short and (need or i in keepers):
             continue
         served[i] = 1
+        for b in table[i, has:min(max(int(pages[i]), 0), most)]:
+            if 0 <= b < len(refs):
+                refs[b] -= 1
         if copies:
             src[i], dst[i] = table[i, at], free.pop(0)
             refs[src[i]] -= 1

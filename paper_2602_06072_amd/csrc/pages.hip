@@ -90,32 +90,44 @@ __global__ __launch_bounds__(256) void pages_select_kernel(PagesSelectArgs a) {
 }
 
 // ------------------------------------------------------------------ pages for the next tokens
-// What a request asks for
+// What a request asks for.  A page wholly behind its tokens that others hold too (it was cut to fewer tokens behind a fork) is not to be written either: the request gives it
+// up, with the entries behind it, and takes free blocks instead.
 struct Wish {
-    int at, held, end, block, holders;              // page of its next token, pages it holds, pages it wants; block of that page, how many hold it
-    bool shared;                                    // that page holds tokens and is held by others too: it is not to be written
+    int at, had, held, wanted, end;                 // page of its next token, pages it holds, those that it goes on holding, pages of all its tokens then, pages it holds then
+    int block, holders;                             // block of the next token's page, how many hold it
+    bool shared;                                    // that page holds tokens of its own and is held by others too: it is not to be written
 };
 __device__ __forceinline__ Wish wish_of(const PagesReserveArgs& a, const int i) {
     const int64_t most = static_cast<int64_t>(a.max_blocks) * a.page;
     const int64_t len = min(static_cast<int64_t>(max(a.lens[i], 0)), most);
+    const int32_t* row = a.table + static_cast<int64_t>(i) * a.max_blocks;
     const int grow = max(a.grow[i], 0);
     Wish w;
     w.at = static_cast<int>(len / a.page);
-    w.held = min(max(a.pages[i], 0), a.max_blocks);
-    w.end = grow > 0 ? max(w.held, static_cast<int>(min((len + grow + a.page - 1) / a.page, static_cast<int64_t>(a.max_blocks)))) : w.held;
-    w.block = -1;
-    w.holders = 0;
-    w.shared = false;
-    if (grow > 0 && len % a.page > 0 && w.at < w.held) {
-        w.block = a.table[static_cast<int64_t>(i) * a.max_blocks + w.at];
-        w.holders = is_block(w.block, a.num_blocks) ? a.refs[w.block] : 0;
-        w.shared = w.holders > 1;
+    w.had = w.held = min(max(a.pages[i], 0), a.max_blocks);
+    const bool part = len % a.page > 0;
+    w.wanted = grow > 0 ? static_cast<int>(min((len + grow + a.page - 1) / a.page, static_cast<int64_t>(a.max_blocks))) : 0;
+    const int behind = w.at + (part ? 1 : 0), upto = min(w.held, w.wanted);
+    // (the next token's page and the one behind are asked for together, also where they are not needed; further ones hardly ever are)
+    const int block = row[min(w.at, a.max_blocks - 1)], next = row[min(behind, a.max_blocks - 1)];
+    const auto holders_of = [&](const int b) { const int x = a.refs[is_block(b, a.num_blocks) ? b : 0]; return is_block(b, a.num_blocks) ? x : 0; };
+    const int holders = holders_of(block), holders_of_next = holders_of(next);
+    const bool there = grow > 0 && part && w.at < w.held;
+    w.block = there ? block : -1;
+    w.holders = there ? holders : 0;
+    w.shared = w.holders > 1;
+    if (behind < upto) {
+        int j = behind;
+        if (holders_of_next <= 1) do ++j; while (j < upto && holders_of(row[j]) <= 1);
+        w.held = j < upto ? j : w.held;
     }
+    w.end = max(w.held, w.wanted);
     return w;
 }
 __device__ __forceinline__ int device_load(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-enum { kServed = 1, kCopies = 2, kWrites = 4 };     // left in served[i] between two launches; copy_dst[i]: its first free block's number among those handed out
+// left in served[i] between two launches; copy_dst[i]: its first free block's number among those handed out; copy_src[i]: pages that it goes on holding
+enum { kServed = 1, kCopies = 2, kWrites = 4 };
 
 // One workgroup: who gets what.  (Requests are 4 to 12 bytes, blocks 4: the whole state of a batch is a few hundred KiB, and what takes time is the chain of loads: 8 us for
 // 8 requests, 13 for 320 and 20000 blocks; 20 when what is known of a request was read in each of the three passes over them.)  HERE: the requests fit its threads, and it writes their entries too: a thread for each block
@@ -197,6 +209,8 @@ __global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(PagesReserveAr
             if (served) a.pages[i] = kept.end;
             if (copies) atomicAdd(a.refs + kept.block, -1);
             if (kept.shared) { a.last_writer[place_of(kept.block)] = 0; a.writers[place_of(kept.block)] = 0; }
+            for (int j = kept.held; served && j < kept.had; ++j)
+                if (const int b = a.table[static_cast<int64_t>(i) * a.max_blocks + j]; is_block(b, a.num_blocks)) atomicAdd(a.refs + b, -1);
         }
         __builtin_amdgcn_s_waitcnt(0x0F70);        // (the free blocks: of this workgroup, through the L2)
         __syncthreads();
@@ -226,6 +240,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(PagesReserveAr
             const bool served = begin + need <= found || (need == 0 && !keeps);
             a.served[i] = (served ? kServed : 0) | (w.shared && !keeps ? kCopies : 0) | (w.shared ? kWrites : 0);
             a.copy_dst[i] = served ? static_cast<int32_t>(begin) : -1;
+            a.copy_src[i] = w.held;
         }
         before += all;
     }
@@ -237,7 +252,9 @@ __global__ __launch_bounds__(256) void pages_apply_kernel(PagesReserveArgs a) {
     if (i >= a.n) return;
     const int flags = a.served[i], begin = a.copy_dst[i];
     Wish w = wish_of(a, i);
-    w.shared = flags & kWrites;                     // (counts change meanwhile: what was shared stands in the flags)
+    w.shared = flags & kWrites;                     // (counts change meanwhile: what was shared has been left here)
+    w.held = a.copy_src[i];
+    w.end = max(w.held, w.wanted);
     int32_t* row = a.table + static_cast<int64_t>(i) * a.max_blocks;
     const bool served = flags & kServed, copies = served && (flags & kCopies);
     if (lane == 0) {
@@ -255,7 +272,9 @@ __global__ __launch_bounds__(256) void pages_apply_kernel(PagesReserveArgs a) {
         if (served) a.pages[i] = w.end;
     }
     if (!served) return;
-    for (int j = w.held + lane; j < w.end; j += kWave) {
+    for (int j = w.held + lane; j < max(w.had, w.end); j += kWave) {
+        if (j < w.had && is_block(row[j], a.num_blocks)) atomicAdd(a.refs + row[j], -1);
+        if (j >= w.end) continue;
         const int b = a.free[place_of(begin + (copies ? 1 : 0) + j - w.held)];
         row[j] = b;
         a.refs[b] = 1;
