@@ -720,10 +720,15 @@ int pk_kv_cache_copy(const pk_cache* from, const pk_cache* to, const int32_t* co
  *   family_start  device int32 [families + 1], not decreasing: family g is
  *             requests family_start[g] .. family_start[g + 1] - 1; requests in
  *             none share nothing
- *   families  0 .. n
- * How many pages a family shares is found from its rows of block_table: the
- * result is that of pk_tree_attn whatever the families are, but for the order of
- * the sums.  It repeats bit for bit.
+ *   families  0 .. n; 0: every request is taken alone, in one or two launches instead of
+ *             three, which is faster where the requests have less than 256 MB of keys and
+ *             values or so (lengths are on the device: without this only the
+ *             table's width tells)
+ * How many pages a family shares is found from its rows of block_table: what all of
+ * its requests with drafted tokens have in common (one that has less in common with the
+ * others belongs into a family of its own).  The result is that of
+ * pk_tree_attn whatever the families are, but for the order of the sums.  It
+ * repeats bit for bit.
  *   workspace as for pk_tree_attn, of at least
  *             pk_shared_tree_attn_workspace_bytes; not to be shared with
  *             pk_tree_attn

@@ -714,7 +714,8 @@ def new_shared_tree_workspace(n, max_q, total_q, Hq, Hkv, d, device="cuda"):
 
 def shared_tree_attn(cache: KvCache, q, q_start, max_q, tree_mask, block_table, kv_lens, family_start, out, scale, workspace, stream=None):
     """tree_attn for requests that have their leading pages in common: family g is requests family_start[g] ..
-    family_start[g + 1] - 1 (int32 [families + 1]), whose shared pages are read once."""
+    family_start[g + 1] - 1 (int32 [families + 1]), whose shared pages are read once.  One number: no families, every request alone
+    (faster where they are few or short)."""
     L = lib()
     total, Hq, d = q.shape
     n, max_blocks = block_table.shape

@@ -67,6 +67,8 @@ constexpr int32_t kMostVocab = 1 << 26;
 // reads of what is shared come from the caches: with requests that share nearly all, of 32 / 8 heads of 128 columns in 8 bits, one new token each, 31 us against 31 at 278 MB of keys and
 // values (32 requests of 4100 tokens), 35 against 46 at 403 MB (16 of 12100), 26 against 20 at 139 MB; with six new tokens each 70 against 99 at 556 MB (64 of
 // 4100), 54 against 62 at 226 MB (64 of 1600), 55 against 44 at 278 MB; in bf16 27 against 28 and 50 against 39 around 250 MB.
+// What it costs where tables are wide and requests short: eight requests of one token behind 1200 to 1400, 11 us up to 512 pages of 16 tokens and 22 from 1024 on; eight of 60 to 300 18
+// against 9.  A caller who knows such lengths says so with no families.
 bool shared_pays(const TreeArgs& a, const int32_t families) {
     const CacheView& c = a.cache;
     const int64_t row = 2 * static_cast<int64_t>(c.Hkv) * (c.f8 ? c.d + 1 : 2 * c.d), tokens = static_cast<int64_t>(a.max_blocks) * c.page;       // (below 2^25 and 2^31)

@@ -129,9 +129,10 @@ __device__ __forceinline__ int device_load(const int32_t* p) { return __hip_atom
 // left in served[i] between two launches; copy_dst[i]: its first free block's number among those handed out; copy_src[i]: pages that it goes on holding
 enum { kServed = 1, kCopies = 2, kWrites = 4 };
 
-// One workgroup: who gets what.  (Requests are 4 to 12 bytes, blocks 4: the whole state of a batch is a few hundred KiB, and what takes time is the chain of loads: 8 us for
-// 8 requests, 13 for 320 and 20000 blocks; 20 when what is known of a request was read in each of the three passes over them.)  HERE: the requests fit its threads, and it writes their entries too: a thread for each block
-// that is handed out, which finds its request among the prefix sums.
+// One workgroup: who gets what.  (Requests are 4 to 12 bytes, blocks 4: the whole state of a batch is a few hundred KiB, and what takes time is the chain of loads: 9 us for
+// 8 requests, 14 for 320 and 20000 blocks; 20 when what is known of a request was read in each of the three passes over them.)  HERE: the requests fit its threads, and it writes their entries too: a thread for each block
+// that is handed out, which finds its request among the prefix sums.  (More requests: this workgroup reads each three times, and a second launch writes; 2000 on 140000 blocks 16 to 25 us, by how
+// far the free ones are behind; 65535 on 2000000 blocks 590 to 690.)
 constexpr int kPlanThreads = 1024;
 template <bool HERE>
 __global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(PagesReserveArgs a) {

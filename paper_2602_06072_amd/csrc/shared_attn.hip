@@ -10,8 +10,8 @@
 //
 // Shared keys are bound by the matrix pipe and the exponentials, as prefill is: they are read once for all members, 4 d operations a row and key.  Own keys are bound by
 // memory, (2 d + 2) bytes each.  Measured, cache in 8 bits: 128 requests of one token behind 8200 shared ones, 16 .. 1024 of their own, 32 / 8 heads of 128 columns, 6 + 53 + 8 us
-// (pk_tree_attn 303); 16 families of 4 .. 12 trees, 64 / 8 heads, 290 together, of which 255 shared keys alone and 25 the last launch, where the operations take 143; bf16, two documents of 40000 .. 66000 tokens for 9 .. 16 requests of 64
-// columns 6 + 173 + 9, of 84 (what a score's exponential, maximum and rounding take does not halve with d, as its products do).
+// (pk_tree_attn 303; one request with less in common takes the rest from all: 71 -> 273, and 79 with it in a family of its own); 16 families of 4 .. 12 trees, 64 / 8 heads, 6 + 256 + 26, where the operations
+// take 143; bf16, two documents of 40000 .. 66000 tokens for 9 .. 16 requests of 64 columns 6 + 172 + 9, of 84 (what a score's exponential, maximum and rounding take does not halve with d, as its products do).
 #include "shared_attn.h"
 #include "tree_body.hip.h"
 

@@ -14,7 +14,7 @@
 //
 // Probabilities and their sums have 64 bits: a draw is the place of a number between V borders, and with sums of 32 bits every tenth draw of a flat row of 100000
 // would fall on the other side of one.  Vector instructions of 64 bits run at the rate of those of 32 here; a weight takes about 22 of them, 100 cycles for 64 logits, and
-// at 1.6 10^12 logits a second at most that, not memory (3 10^12 of bf16), bounds the launches over rows in 64 bits; terms of 32 bits reach 2.4 10^12, 4.8 TB/s.
+// at 1.6 10^12 logits a second at most that, not memory (3 10^12 of bf16), bounds the launches over rows in 64 bits; terms of 32 bits reach 2.5 10^12, 5.1 TB/s.
 #include <algorithm>
 
 #include "arrival.h"
@@ -300,8 +300,8 @@ __device__ __forceinline__ double sum_of_all(double x, double* lds) {
     return y;
 }
 
-// Sums of the rows of tokens with children: a workgroup for (piece, target or draft; token; request).  Chains of 64 requests (640 rows of 128256 logits) 34 us with terms of
-// 32 bits, 4.8 TB/s; 581 rows of 50257 logits that begin at any address 16, 3.6 TB/s; trees (612 rows of 32000 in fp32) in 64 bits 27.
+// Sums of the rows of tokens with children: a workgroup for (piece, target or draft; token; request).  Chains of 64 requests (640 rows of 128256 logits) 32 us with terms of
+// 32 bits, 5.1 TB/s; 581 rows of 50257 logits that begin at any address 16, 3.7 TB/s; trees (612 rows of 32000 in fp32) in 64 bits 25.
 template <bool F32, Sums64 HOW>
 __global__ __launch_bounds__(kThreads, F32 ? 5 : 6) void verify_rows_kernel(VerifyArgs a) {
     __shared__ WaveParts lds;
@@ -528,7 +528,7 @@ __device__ __forceinline__ RowPart load_part(const uint64_t* from) {
 }
 
 // In 64 bits, the sums of the rows that are drawn from as max(P - c Q, 0), where the choices had them in 32: workgroups as for the draw.  Up to 64 pairs of rows of
-// 128256 logits 20 us, 0.8 10^12 logits a second: half of it the way there and the end.
+// 128256 logits 19 us, 0.9 10^12 logits a second: half of it the way there and the end.
 template <bool F32>
 __global__ __launch_bounds__(kThreads) void verify_sums_kernel(VerifyArgs a) {
     __shared__ WaveParts lds;
@@ -569,7 +569,8 @@ __global__ __launch_bounds__(kThreads) void verify_sums_kernel(VerifyArgs a) {
 
 // The draw: sums of the row that a request's next token is drawn from, a wave for a span of it (up to 256 spans, of 1024 tokens where V is up to 2^18), a workgroup for some
 // of them; the last workgroup of a request to finish finds the span, one wave of it the vector in the span and the token in the vector.  Four rows of 32000 logits 9.7 us,
-// the chain of loads and the end; 200 rows of 50257 and 64 pairs of rows of 128256 25, of them 10 to 13 for the weights.  bf16: registers for four workgroups a unit (131
+// the chain of loads and the end; 200 rows of 50257 and 64 pairs of rows of 128256 24, of them 10 to 13 for the weights.
+// One token a request of whole batches, 128256 logits of bf16: 64 rows 20 us, 256 rows 53 (10.6 at memory's rate): weights by four, in the form for few rows.  bf16: registers for four workgroups a unit (131
 // otherwise, three: chains of 64 requests 84.5 us instead of 82, looked-up tokens 49.5 instead of 47).
 enum { kPlain, kResidual, kRemoved };               // weights: P; max(P - c Q, 0); P without the tokens that were refused
 template <bool F32>
