@@ -670,12 +670,13 @@ int pk_kv_pages_select(const int32_t* block_table, const int32_t* lens, const in
 /* pk_kv_pages_reserve -- every request gets pages for lens[i] + grow[i] tokens (no
  * more than max_blocks of them), in the order of requests the free blocks of
  * the lowest numbers.  Where its next token goes to a page that holds tokens of
- * its own and that others hold too, the page is replaced by a free block and noted for
- * copying: copy_src[i] -> copy_dst[i] (-1: nothing to copy), its block before its
- * other new ones.  Where tokens would go to a page behind its own ones that others hold too
- * (it was cut to fewer tokens behind a fork), it gives that page and all behind it
- * up and gets free blocks instead; what nobody holds any more is free from the next call on.  If all holders of such a page grow in this call, the one of
- * the highest number keeps it.
+ * its own and that others hold too, the page is replaced by a free block and
+ * noted for copying: copy_src[i] -> copy_dst[i] (-1: nothing to copy), its block
+ * before its other new ones.  If all holders of such a page grow in this call,
+ * the one of the highest number keeps it.  Where tokens would go to a page
+ * behind its own ones that others hold too (it was cut to fewer tokens behind a
+ * fork), it gives that page and all behind it up and gets free blocks instead;
+ * what nobody holds any more is free from the next call on.
  *   served    device int32 [n]: 1, or 0 where blocks run out: from the first request on for
  *             which they do, none that needs one (or keeps a page that others
  *             would have had to leave) gets any, and it is left as it was

@@ -668,9 +668,9 @@ def new_pages_workspace(num_blocks, device="cuda"):
 
 
 def kv_pages_reserve(block_table, lens, pages, grow, refs, page_size, served, copy_src, copy_dst, workspace, stream=None):
-    """Pages for lens[i] + grow[i] tokens of every request, free blocks of the lowest numbers first; where a shared page with tokens of its own would be
-    written, copy_src[i] -> copy_dst[i] (-1: none) is to be copied in every layer's cache (kv_cache_copy).  served[i]: 1, or 0
-    where blocks ran out."""
+    """Pages for lens[i] + grow[i] tokens of every request, free blocks of the lowest numbers first; where a shared page with tokens of
+    its own would be written, copy_src[i] -> copy_dst[i] (-1: none) is to be copied in every layer's cache (kv_cache_copy).
+    served[i]: 1, or 0 where blocks ran out."""
     L = lib()
     n, most, table, ls, ps = _batch(block_table, lens, pages)
     i32 = _torch.int32
